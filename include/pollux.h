@@ -112,7 +112,8 @@ enum {
                                then unspecified, the other jobs' results are unaffected */
     PX_ST_ZERO_FAIR = 2,    /* a job's fair-share goodput is 0: its SPEEDUP is set to 0 */
     PX_ST_BAD_RESTART = 4,  /* T_j - R_j * delta <= 0 for some job (penalty enabled) */
-    PX_ST_NEG_ALLOC = 8     /* a negative entry in population or current_alloc */
+    PX_ST_NEG_ALLOC = 8,    /* a negative entry in population or current_alloc */
+    PX_ST_BAD_TOKEN = 16    /* a token or target that is neither -1 nor an entry of the vocabulary */
 };
 
 /* Bytes of workspace needed by pollux_fitness and pollux_ga_step for `dims`
@@ -458,6 +459,74 @@ int pollux_apply_best(const pollux_dims *dims,           /* host */
                       int32_t *nodes,                    /* [J] out */
                       int32_t *changed,                  /* [J] out */
                       void *hip_stream);
+
+/*
+ * A training iteration of a language-model job
+ * --------------------------------------------
+ * What the scheduler is told of a job, its agent measures: the gradient noise scale phi_t (PX_PHI) on the gradients of the
+ * job's iterations, and the iteration times that pollux_fit_theta takes.  The calls below are such an iteration's operators on
+ * one GPU: rows looked up by token, the loss over the vocabulary and its gradients, the table's gradient, the noise scale and
+ * the mean of the gradients of an iteration's s + 1 micro-batches (Sec. 3.1, Eq. 5), and the orthogonalised update.
+ *
+ * Matrices are row-major with a stride in elements from row to row (0: the row's length); base pointers are aligned to 16
+ * bytes.  Element types are PX_TYPE_*; products and sums are held in fp32 (fp64 where said), results rounded once, to nearest.
+ * A token or target of -1 stands for none: padding, or a prompt that is not trained on.  One that is neither -1 nor an entry of
+ * the vocabulary counts as none too, and is reported by PX_ST_BAD_TOKEN.
+ */
+enum {
+    PX_TYPE_F32 = 0,
+    PX_TYPE_BF16 = 1,
+    PX_TYPE_F16 = 2
+};
+enum {
+    PX_FLAG_TOKENS_I64 = 1,     /* tokens and targets are int64 (without the flag, int32) */
+    PX_FLAG_ACCUMULATE = 2      /* the gradient of the table or of the weights is added to what the buffer holds */
+};
+
+/*
+ * Cross entropy of N tokens over a vocabulary of V entries: with l[n,v] = sum_d hidden[n,d] * weight[v,d],
+ *   lse[n] = log sum_v exp(l[n,v]),  loss[n] = lse[n] - l[n, targets[n]], 0 where there is no target.
+ * The logits are never in memory.  An infinite or NaN logit gives what the formula gives: lse inf for one of +inf, -inf where
+ * all are -inf, NaN with a NaN.
+ *
+ * pollux_token_loss_grad: for row weights g[n] (the gradient of what is minimised by loss[n]; row_weight NULL: all 1) and the
+ * lse of pollux_token_loss,
+ *   q[n,v] = g[n] * (exp(l[n,v] - lse[n]) - [v = targets[n]]),
+ *   hidden_grad[n,:] = sum_v q[n,v] weight[v,:],   weight_grad[v,:] = sum_n q[n,v] hidden[n,:].
+ * A token without a target, or of row weight 0, adds nothing to weight_grad and has a row of zeros in hidden_grad whatever its
+ * hidden row holds.  Either gradient may be NULL.  The logits are formed again, a piece of the vocabulary at a time; q is rounded to
+ * the type of the inputs for the matrix units (fp16: scaled, so that weights g of any size keep their precision).  Sums over
+ * tokens and entries are in fp32 and in a fixed order: the same call gives the same bits.
+ *
+ * Limits: 0 <= N <= 2^20, 1 <= V <= 2^20, 1 <= D <= 2^16, strides below 2^20.  workspace: pollux_loss_workspace_size bytes,
+ * 256-byte aligned; pollux_last_status on it reads the status word (PX_ST_BAD_TOKEN).
+ * Gradients and inputs must not overlap.
+ */
+typedef struct {
+    int64_t N;                  /* tokens                                            */
+    int32_t V, D;               /* vocabulary, width of a row                        */
+    int32_t type;               /* PX_TYPE_* of hidden, weight and both gradients    */
+    int32_t flags;              /* PX_FLAG_TOKENS_I64, PX_FLAG_ACCUMULATE            */
+    int64_t hidden_stride, weight_stride, hidden_grad_stride, weight_grad_stride;
+} pollux_loss_dims;
+
+int pollux_loss_workspace_size(const pollux_loss_dims *dims, int32_t with_grad /* 0: pollux_token_loss, 1: its gradient */,
+                               size_t *bytes /* host, out */);
+int pollux_token_loss(const pollux_loss_dims *dims,      /* host */
+                      const void *hidden,                /* [N,D] */
+                      const void *weight,                /* [V,D] */
+                      const void *targets,               /* [N] */
+                      void *workspace, size_t workspace_bytes,
+                      float *loss, float *lse,           /* [N] out */
+                      void *hip_stream);
+int pollux_token_loss_grad(const pollux_loss_dims *dims, /* host */
+                           const void *hidden, const void *weight, const void *targets,
+                           const float *lse,             /* [N] of pollux_token_loss */
+                           const float *row_weight,      /* [N] or NULL */
+                           void *workspace, size_t workspace_bytes,
+                           void *hidden_grad,            /* [N,D] out, may be NULL */
+                           void *weight_grad,            /* [V,D] out (in/out with PX_FLAG_ACCUMULATE), may be NULL */
+                           void *hip_stream);
 
 /* Copies the status word of the last pollux_fitness (or pollux_fitness_timed) call that used `workspace`
  * to *host_out.  Synchronises `hip_stream`.  pollux_goodput_per_gpu and pollux_sim_tick neither clear nor

@@ -20,12 +20,15 @@ PX_FLAG_SAMPLE_M = 16
 PX_FLAG_PAIR_RESULTS = 32
 PX_GA_IN_PLACE = 1
 PX_GA_INHERIT_ROWS = 2
-PX_ST_BAD_PARAM, PX_ST_ZERO_FAIR, PX_ST_BAD_RESTART, PX_ST_NEG_ALLOC = 1, 2, 4, 8
+PX_ST_BAD_PARAM, PX_ST_ZERO_FAIR, PX_ST_BAD_RESTART, PX_ST_NEG_ALLOC, PX_ST_BAD_TOKEN = 1, 2, 4, 8, 16
+PX_TYPE_F32, PX_TYPE_BF16, PX_TYPE_F16 = 0, 1, 2
+PX_FLAG_TOKENS_I64, PX_FLAG_ACCUMULATE = 1, 2
 
 EXPORTS = ("pollux_version", "pollux_strerror", "pollux_workspace_size", "pollux_fitness", "pollux_fitness_static",
            "pollux_ga_step",
            "pollux_fit_theta", "pollux_goodput_per_gpu", "pollux_autoscale", "pollux_sim_tick", "pollux_last_status",
-           "pollux_fitness_timed", "pollux_apply_best", "pollux_generation")
+           "pollux_fitness_timed", "pollux_apply_best", "pollux_generation",
+           "pollux_loss_workspace_size", "pollux_token_loss", "pollux_token_loss_grad")
 
 
 class PolluxError(RuntimeError):
@@ -41,6 +44,12 @@ class Dims(ctypes.Structure):
 class GaParams(ctypes.Structure):
     _fields_ = [("seed", ctypes.c_uint64), ("generation", ctypes.c_uint32), ("elite_k", ctypes.c_uint32),
                 ("mut_threshold", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("job_gpu_cap", ctypes.c_void_p)]
+
+
+class LossDims(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int32), ("D", ctypes.c_int32), ("type", ctypes.c_int32), ("flags", ctypes.c_int32),
+                ("hidden_stride", ctypes.c_int64), ("weight_stride", ctypes.c_int64), ("hidden_grad_stride", ctypes.c_int64),
+                ("weight_grad_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -83,6 +92,12 @@ def lib() -> ctypes.CDLL:
                                         + [vp] * 6 + [vp])
         L.pollux_apply_best.restype = i
         L.pollux_apply_best.argtypes = [ctypes.POINTER(Dims)] + [vp] * 7 + [vp]
+        L.pollux_loss_workspace_size.restype = i
+        L.pollux_loss_workspace_size.argtypes = [ctypes.POINTER(LossDims), ctypes.c_int32, ctypes.POINTER(sz)]
+        L.pollux_token_loss.restype = i
+        L.pollux_token_loss.argtypes = [ctypes.POINTER(LossDims), vp, vp, vp, vp, sz, vp, vp, vp]
+        L.pollux_token_loss_grad.restype = i
+        L.pollux_token_loss_grad.argtypes = [ctypes.POINTER(LossDims), vp, vp, vp, vp, vp, vp, sz, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -328,3 +343,6 @@ class FitnessCall:
                     best_s=self.best_s.cpu().numpy(), best_goodput=self.best_goodput.cpu().numpy(),
                     speedup=self.speedup.cpu().numpy(), violations=self.violations.cpu().numpy(),
                     status=self.status())
+
+
+from .train import token_loss, token_loss_grad  # noqa: E402,F401  (needs the names above)

@@ -10,6 +10,7 @@
 
 #include "../../include/pollux.h"
 #include "pollux_host.h"
+#include "pollux_train.h"
 
 // ---- scratch memory owned by the library (pollux_fitness_static) -------------------------------------------
 // One array per GPU, part of the code object: every device the library runs on holds its own copy, at its own
@@ -25,7 +26,9 @@ constexpr int kMaxDevices = 64;
 // that find it unknown both query the device and store the same value.
 std::atomic<int> g_arch_ok[kMaxDevices];
 
-int check_device(int *device = nullptr)
+}  // namespace
+
+int px::check_device(int *device)
 {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return PX_E_HIP;
@@ -40,6 +43,10 @@ int check_device(int *device = nullptr)
     }
     return ok == 1 ? PX_OK : PX_E_UNSUPPORTED_ARCH;
 }
+
+namespace {
+
+using px::check_device;
 
 void *g_scratch_ptr[kMaxDevices];     // device address of `scratch` on each device, null until looked up
 std::mutex g_scratch_lock;

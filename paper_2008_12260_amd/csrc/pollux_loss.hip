@@ -1,0 +1,667 @@
+// Cross entropy of tokens over a large vocabulary, from hidden rows and the projection's weights, and its gradients, in pieces
+// of the vocabulary: the logits of all tokens over all entries are never in memory.
+//
+//   l[n,v] = <h_n, w_v>     lse_n = max_v l + log sum_v exp(l - max)     loss_n = lse_n - l[n, y_n]
+//   q[n,v] = g_n (exp(l[n,v] - lse_n) - [v = y_n])      dH = q W      dW = q' H
+//
+// Forward: a tile of logits is reduced, as it leaves the matrix units, to each token's largest logit and sum of exponentials
+// over the tile's entries (loss_tiles); a second launch joins a token's tiles (loss_join).
+// Backward: for each piece of the vocabulary the logits are formed again, q of the piece is written once as [token, entry] and
+// once as [entry, token] (q_tiles), and both gradients are products of it (grad_tiles) with transposed copies of the hidden rows
+// and of the piece's weights: every product then has its k contiguous, and all share one kernel core.  The hidden rows'
+// gradient is summed over pieces in fp32 (and over slices of a piece where few tiles would leave the chip idle), in a
+// fixed order, and rounded once (join_slices).
+//
+// q is rounded to the type of the inputs because the matrix units take it so: half a step of that type per element, as large
+// as the rounding of the result.  fp16 has too few exponents for q (a mean over 10^4 tokens of probabilities of 10^-6): there q is
+// scaled by the power of two that brings the largest row weight to 2^13, and the gradients are scaled back in fp32.
+
+#include "pollux_host.h"
+#include "pollux_tiles.h"
+#include "pollux_train.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+namespace px {
+namespace {
+
+// A token's target, -1 where there is none or it is no entry of the vocabulary (then `bad`).
+__device__ __forceinline__ int target_of(const void *targets, int64_t n, bool i64, int V, bool &bad)
+{
+    const int64_t y = i64 ? ((const int64_t *)targets)[n] : (int64_t)((const int32_t *)targets)[n];
+    bad = y < -1 || y >= V;
+    return y < 0 || y >= V ? -1 : (int)y;
+}
+__device__ __forceinline__ int target_of(const void *targets, int64_t n, bool i64, int V)
+{
+    bool bad;
+    return target_of(targets, n, i64, V, bad);
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// A maximum to subtract: 0 stands in for one that is infinite, so that inf - inf is never formed.
+__device__ __forceinline__ float finite_or_zero(float m) { return fabsf(m) < __builtin_inff() ? m : 0.f; }
+
+struct LogitArgs {
+    Operands o;                 // a: weights of the piece, b: hidden rows
+    int first, V, N;            // the piece's first vocabulary entry
+    int tiles_m, tiles_n, group;
+    const void *targets;
+    bool i64;
+    // forward
+    float2 *parts;              // of the piece's first tile
+    float *picked;
+    int32_t *status;            // cleared by the first workgroup; null in all but the first piece
+    // backward
+    const float *lse, *row_weight, *scale;
+    void *q, *qt;
+    int64_t ld_q, ld_qt;        // elements
+    int rows;                   // entries of the piece
+};
+
+// One tile of logits -> per token (largest logit, sum of exponentials from it) over the tile's entries, and the target's logit
+// where the tile holds it.  A lane has one token and 4 FM entries of it; four lanes share a token in a wavefront, WM wavefronts
+// in the workgroup.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void loss_tiles(const LogitArgs A)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    extern __shared__ __align__(16) char lds[];
+    const Tile t = tile_of(blockIdx.x, A.tiles_m, A.tiles_n, A.group);
+    if (A.status && blockIdx.x == 0 && threadIdx.x < kStatusWords) A.status[threadIdx.x] = 0;
+    f32x4 acc[S::FM][S::FN];
+    tile_product<S>(A.o, t, lds, acc);
+    const Place<S> at(t);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, left = A.o.rows_a;
+    float2 *const shared = (float2 *)lds;        // [WM][BN]
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = at.first_n + j * 16;
+        const int y = n < A.N ? target_of(A.targets, n, A.i64, A.V) - A.first : -1;
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int v = at.first_m + 16 * i + r;
+                if (v >= left) acc[i][j][r] = -__builtin_inff();
+                top = fmaxf(top, acc[i][j][r]);
+                if (v == y && v < left) A.picked[n] = acc[i][j][r];
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float from = finite_or_zero(top);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - from) * kLog2e);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 16) shared[wave / S::WN * S::BN + wave % S::WN * S::TN + j * 16 + lane] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < S::BN; c += S::kThreads) {
+        const int n = t.n * S::BN + c;
+        if (n >= A.N) break;
+        float top = shared[c].x;
+#pragma unroll
+        for (int w = 1; w < S::WM; ++w) top = fmaxf(top, shared[w * S::BN + c].x);
+        const float from = finite_or_zero(top);
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < S::WM; ++w) {
+            const float2 p = shared[w * S::BN + c];
+            sum += p.y == __builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
+        }
+        A.parts[(int64_t)t.m * A.N + n] = make_float2(top, sum);
+    }
+#endif
+}
+
+// Each token's tiles joined: kJoinTokens neighbouring tokens (a line of a tile's values) by kJoinParts parts of the list.
+constexpr int kJoinTokens = 16, kJoinParts = 16;
+__global__ __launch_bounds__(kJoinTokens *kJoinParts) void loss_join(const float2 *parts, int tiles, int N, const float *picked,
+                                                                     const void *targets, bool i64, int V, float *loss, float *lse,
+                                                                     int32_t *status)
+{
+    __shared__ float2 shared[kJoinParts][kJoinTokens];
+    const int c = threadIdx.x % kJoinTokens, k = threadIdx.x / kJoinTokens, n = blockIdx.x * kJoinTokens + c;
+    float top = -__builtin_inff(), sum = 0.f;
+    if (n < N)
+        for (int t = k; t < tiles; t += kJoinParts) {
+            const float2 p = parts[(int64_t)t * N + n];
+            const float most = fmaxf(top, p.x), from = finite_or_zero(most);
+            const float x = sum == __builtin_inff() ? sum : sum * __builtin_amdgcn_exp2f((finite_or_zero(top) - from) * kLog2e);
+            const float y = p.y == __builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
+            // (the sum from a maximum of -inf is 0, or NaN)
+            sum = (top == -__builtin_inff() ? sum : x) + (p.x == -__builtin_inff() ? p.y : y);
+            top = most;
+        }
+    shared[k][c] = make_float2(top, sum);
+    __syncthreads();
+    if (k != 0 || n >= N) return;
+    for (int i = 1; i < kJoinParts; ++i) top = fmaxf(top, shared[i][c].x);
+    const float from = finite_or_zero(top);
+    sum = 0.f;
+    for (int i = 0; i < kJoinParts; ++i) {
+        const float2 p = shared[i][c];
+        sum += p.y == __builtin_inff() || p.x == -__builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
+    }
+    const float whole = from + logf(sum);
+    lse[n] = whole;
+    bool bad;
+    const int y = target_of(targets, n, i64, V, bad);
+    loss[n] = y < 0 ? 0.f : whole - picked[n];
+    if (bad) atomicOr(status, PX_ST_BAD_TOKEN);
+}
+
+// ---- backward ------------------------------------------------------------------------------------------------------
+
+// Clears the status word, reports targets that are no entry, and, for fp16, finds the power of two that q is scaled by:
+// scale[0] that, scale[1] its inverse.
+template <bool SCALED>
+__global__ __launch_bounds__(1024) void grad_begin(const void *targets, bool i64, int V, int N, const float *row_weight, int32_t *status, float *scale)
+{
+    __shared__ int bad_any;
+    __shared__ float tops[16];
+    if (threadIdx.x == 0) bad_any = 0;
+    if (threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
+    __syncthreads();
+    float top = 0.f;
+    for (int n = threadIdx.x; n < N; n += 1024) {
+        bool bad;
+        const int y = target_of(targets, n, i64, V, bad);
+        if (bad) bad_any = 1;
+        if (SCALED && y >= 0) {
+            const float g = row_weight ? fabsf(row_weight[n]) : 1.f;
+            if (g < __builtin_inff()) top = fmaxf(top, g);
+        }
+    }
+    if (SCALED) {
+#pragma unroll
+        for (int w = 1; w < 64; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
+        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    if (bad_any) *status = PX_ST_BAD_TOKEN;
+    if (SCALED) {
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, tops[i]);
+        const int e = top > 0.f ? min(100, max(-100, 13 - ilogbf(top))) : 0;
+        scale[0] = ldexpf(1.f, e);
+        scale[1] = ldexpf(1.f, -e);
+    }
+}
+
+// One tile of q from the logits' tile, written both ways.  A token without a target, or of weight 0, has a row of zeros,
+// whatever its logits are.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void q_tiles(const LogitArgs A)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef typename S::element::type type;
+    extern __shared__ __align__(16) char lds[];
+    const Tile t = tile_of(blockIdx.x, A.tiles_m, A.tiles_n, A.group);
+    f32x4 acc[S::FM][S::FN];
+    tile_product<S>(A.o, t, lds, acc);
+    const Place<S> at(t);
+    const float scale = A.scale ? A.scale[0] : 1.f;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = at.first_n + j * 16;
+        const int y = n < A.N ? target_of(A.targets, n, A.i64, A.V) : -1;
+        const float g = y < 0 ? 0.f : (A.row_weight ? A.row_weight[n] : 1.f) * scale;
+        const float lse = y < 0 ? 0.f : A.lse[n];
+        const int hit = y - A.first;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            const int v = at.first_m + 16 * i;
+            f32x4 q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e) - (v + r == hit ? 1.f : 0.f);
+                q[r] = g != 0.f && v + r < A.rows ? p * g : 0.f;
+            }
+            if (n < A.N && v < A.ld_q) store4<typename S::element>((type *)A.q + (int64_t)n * A.ld_q + v, q);
+            const f32x4 qt = turned(q);
+            const int row = v + (threadIdx.x & 3), col = n & ~3;
+            if (row < A.rows && col < A.ld_qt) store4<typename S::element>((type *)A.qt + (int64_t)row * A.ld_qt + col, qt);
+        }
+    }
+#endif
+}
+
+struct GradArgs {
+    Operands o;
+    int tiles_m, tiles_n, group;
+    int slice_k;                // bytes of k a slice (blockIdx.y) takes
+    int cols, rows;             // m and n
+    void *out;                  // [rows, ld]: the gradient, or fp32 sums [slices, rows, cols]
+    int64_t ld;                 // elements
+    int sums;                   // 0: the gradient itself; 1: sums begin; 2: sums go on
+    bool add;                   // what `out` holds is added to
+    const float *scale;
+    const void *targets;        // rows without a target, or of weight 0, are zeros; null: no such rows
+    const float *row_weight;
+    bool i64;
+    int V;
+};
+
+#ifdef __HIP_DEVICE_COMPILE__
+template <class T>
+__device__ __forceinline__ void put(typename T::type *to, f32x4 v, int left, bool whole, bool add)
+{
+    typedef typename T::type type;
+    typedef type vec __attribute__((ext_vector_type(4)));
+    if (whole && left >= 4) {
+        if (add) v += __builtin_convertvector(*(const vec *)to, f32x4);
+        store4<T>(to, v);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < left) to[r] = (type)(add ? v[r] + (float)to[r] : v[r]);
+    }
+}
+#endif
+
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void grad_tiles(const GradArgs A)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef typename S::element::type type;
+    extern __shared__ __align__(16) char lds[];
+    const Tile t = tile_of(blockIdx.x, A.tiles_m, A.tiles_n, A.group);
+    Operands o = A.o;
+    const int k0 = blockIdx.y * A.slice_k;
+    o.a += k0;
+    o.b += k0;
+    o.k_bytes = max(0, min(A.slice_k, A.o.k_bytes - k0));
+    f32x4 acc[S::FM][S::FN];
+    tile_product<S>(o, t, lds, acc);
+    const Place<S> at(t);
+    const float scale = A.scale ? A.scale[1] : 1.f;
+    const bool whole = A.sums ? (A.cols & 3) == 0 : (A.ld & 3) == 0 && ((uintptr_t)A.out & (4 * sizeof(type) - 1)) == 0;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = at.first_n + j * 16;
+        if (n >= A.rows) continue;
+        bool none = false;
+        if (A.targets && !A.sums) none = target_of(A.targets, n, A.i64, A.V) < 0 || (A.row_weight && A.row_weight[n] == 0.f);
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+            const int m = at.first_m + 16 * i, left = A.cols - m;
+            if (left <= 0) continue;
+            if (A.sums) {
+                put<F32>((float *)A.out + ((int64_t)blockIdx.y * A.rows + n) * A.cols + m, acc[i][j], left, whole, A.sums == 2);
+            } else {
+                f32x4 v = acc[i][j] * scale;
+                if (none) v = f32x4{0.f, 0.f, 0.f, 0.f};
+                put<typename S::element>((type *)A.out + (int64_t)n * A.ld + m, v, left, whole, A.add);
+            }
+        }
+    }
+#endif
+}
+
+// The slices' sums, added in their order and rounded.
+template <class T>
+__global__ __launch_bounds__(256) void join_slices(const float *sums, int slices, int64_t N, int D, const float *scale, const void *targets,
+                                                   const float *row_weight, bool i64, int V, typename T::type *out, int64_t ld)
+{
+    const int64_t total = N * D;
+    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
+        const int64_t n = at / D;
+        float v = sums[at];
+        for (int s = 1; s < slices; ++s) v += sums[s * total + at];
+        const bool none = target_of(targets, n, i64, V) < 0 || (row_weight && row_weight[n] == 0.f);
+        out[n * ld + (at - n * D)] = (typename T::type)(none ? 0.f : v * (scale ? scale[1] : 1.f));
+    }
+}
+
+// Rows copied to aligned ones, `cols` padded with zeros to ld_to.
+template <class E>
+__global__ __launch_bounds__(256) void pack_rows(const E *from, int64_t ld_from, int64_t rows, int cols, E *to, int64_t ld_to)
+{
+    const int64_t total = rows * ld_to;
+    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
+        const int64_t n = at / ld_to;
+        const int c = (int)(at - n * ld_to);
+        to[at] = c < cols ? from[n * ld_from + c] : E(0);
+    }
+}
+
+// to[c, n] = from[n, c], n padded with zeros to ld_to; rows without a target, or of weight 0, count as zeros.
+template <class E>
+__global__ __launch_bounds__(256) void transpose_rows(const E *from, int64_t ld_from, int rows, int cols, E *to, int64_t ld_to,
+                                                      const void *targets, const float *row_weight, bool i64, int V)
+{
+    __shared__ E tile[64][65];
+    const int n0 = blockIdx.x * 64, c0 = blockIdx.y * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    for (int i = y; i < 64; i += 4) {
+        const int n = n0 + i, c = c0 + x;
+        bool there = n < rows && c < cols;
+        if (there && targets) there = target_of(targets, n, i64, V) >= 0 && !(row_weight && row_weight[n] == 0.f);
+        tile[i][x] = there ? from[(int64_t)n * ld_from + c] : E(0);
+    }
+    __syncthreads();
+    for (int i = y; i < 64; i += 4) {
+        const int c = c0 + i, n = n0 + x;
+        if (c < cols && n < ld_to) to[(int64_t)c * ld_to + n] = tile[x][i];
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------
+
+constexpr int kShapes = 4;
+struct ShapeOf {
+    int bm, bn, per_cu;         // tile, workgroups a compute unit holds
+    float rate;                 // of the matrix units' while it runs, relative
+};
+constexpr ShapeOf kShape[kShapes] = {{256, 256, 1, 1.0f}, {128, 128, 2, 0.75f}, {64, 64, 4, 0.45f}, {128, 16, 4, 0.15f}};
+
+// The shape whose rounds over the compute units take least: ceil(tiles / (256 x per_cu)) rounds of per_cu tiles.
+int shape_for(int64_t m, int64_t n, int64_t slices, bool f32)
+{
+    int best = 0;
+    double least = 1e300;
+    for (int s = 0; s < kShapes; ++s) {
+        const ShapeOf &h = kShape[s];
+        const double tiles = (double)((m + h.bm - 1) / h.bm) * ((n + h.bn - 1) / h.bn) * slices;
+        const double cost = ceil(tiles / (256.0 * h.per_cu)) * h.per_cu * h.bm * h.bn / (f32 ? 1.0 : h.rate);
+        if (cost < least) least = cost, best = s;
+    }
+    return best;
+}
+
+template <class T>
+using Shape0 = TileShape<T, 256, 256, 2, 4>;
+template <class T>
+using Shape1 = TileShape<T, 128, 128, 2, 2>;
+template <class T>
+using Shape2 = TileShape<T, 64, 64, 2, 2>;
+template <class T>
+using Shape3 = TileShape<T, 128, 16, 2, 1>;
+
+int status_of(hipError_t e) { return e == hipSuccess ? PX_OK : PX_E_HIP; }
+
+enum LogitKind { kLoss, kQ };
+template <class S>
+void launch_logits(LogitKind kind, LogitArgs a, hipStream_t stream)
+{
+    a.tiles_m = (a.o.rows_a + S::BM - 1) / S::BM;
+    a.tiles_n = (a.N + S::BN - 1) / S::BN;
+    a.group = 8;
+    const dim3 grid((unsigned)(a.tiles_m * a.tiles_n));
+    if (kind == kLoss) hipLaunchKernelGGL(loss_tiles<S>, grid, dim3(S::kThreads), S::kLds, stream, a);
+    else hipLaunchKernelGGL(q_tiles<S>, grid, dim3(S::kThreads), S::kLds, stream, a);
+}
+template <class T>
+void launch_logits(int shape, LogitKind kind, const LogitArgs &a, hipStream_t stream)
+{
+    switch (shape) {
+        case 0: launch_logits<Shape0<T>>(kind, a, stream); break;
+        case 1: launch_logits<Shape1<T>>(kind, a, stream); break;
+        case 2: launch_logits<Shape2<T>>(kind, a, stream); break;
+        default: launch_logits<Shape3<T>>(kind, a, stream); break;
+    }
+}
+template <class S>
+void launch_grad(GradArgs a, int slices, hipStream_t stream)
+{
+    a.tiles_m = (a.cols + S::BM - 1) / S::BM;
+    a.tiles_n = (a.rows + S::BN - 1) / S::BN;
+    a.group = 8;
+    hipLaunchKernelGGL(grad_tiles<S>, dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)slices), dim3(S::kThreads), S::kLds, stream, a);
+}
+template <class T>
+void launch_grad(int shape, const GradArgs &a, int slices, hipStream_t stream)
+{
+    switch (shape) {
+        case 0: launch_grad<Shape0<T>>(a, slices, stream); break;
+        case 1: launch_grad<Shape1<T>>(a, slices, stream); break;
+        case 2: launch_grad<Shape2<T>>(a, slices, stream); break;
+        default: launch_grad<Shape3<T>>(a, slices, stream); break;
+    }
+}
+
+unsigned blocks_for(int64_t elements) { return (unsigned)std::min<int64_t>((elements + 255) / 256, 8192); }
+
+template <class T>
+int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden, const char *weight, const void *targets, char *ws,
+               float *loss, float *lse, hipStream_t stream)
+{
+    typedef typename T::type type;
+    constexpr int e = sizeof(type);
+    const int N = (int)d.N;
+    const int64_t ld_h = p.pack_hidden ? p.d_pad : d.hidden_stride, ld_w = p.pack_weight ? p.d_pad : d.weight_stride;
+    int32_t *status = (int32_t *)(ws + p.status);
+    if (N == 0) {
+        hipLaunchKernelGGL(grad_begin<false>, dim3(1), dim3(1024), 0, stream, targets, false, d.V, 0, (const float *)nullptr, status, (float *)nullptr);
+        return status_of(hipGetLastError());
+    }
+    if (p.pack_hidden) {
+        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * p.d_pad)), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad);
+        hidden = ws + p.hidden;
+    }
+    LogitArgs a = {};
+    a.targets = targets;
+    a.i64 = d.flags & PX_FLAG_TOKENS_I64;
+    a.V = d.V;
+    a.N = N;
+    a.picked = (float *)(ws + p.picked);
+    a.o.b = hidden;
+    a.o.ldb = ld_h * e;
+    a.o.rows_b = N;
+    a.o.lda = ld_w * e;
+    a.o.k_bytes = (int)(p.d_pad * e);      // (where D is padded, both operands are packed)
+    int tiles = 0;
+    for (int k = 0; k < p.pieces; ++k) {
+        a.first = k * p.piece;
+        a.rows = a.o.rows_a = std::min(p.piece, d.V - a.first);
+        const char *from = weight + (int64_t)a.first * d.weight_stride * e;
+        if (p.pack_weight) {
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * p.d_pad)), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad);
+            from = ws + p.weight;
+        }
+        a.o.a = from;
+        a.parts = (float2 *)(ws + p.parts) + (int64_t)tiles * N;
+        a.status = k == 0 ? status : nullptr;
+        launch_logits<T>(p.tiles, kLoss, a, stream);
+        tiles += (a.rows + kShape[p.tiles].bm - 1) / kShape[p.tiles].bm;
+    }
+    hipLaunchKernelGGL(loss_join, dim3((N + kJoinTokens - 1) / kJoinTokens), dim3(kJoinTokens * kJoinParts), 0, stream, (const float2 *)(ws + p.parts),
+                       tiles, N, (const float *)(ws + p.picked), targets, a.i64, d.V, loss, lse, status);
+    return status_of(hipGetLastError());
+}
+
+template <class T>
+int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hidden, const char *weight, const void *targets, const float *lse,
+                    const float *row_weight, char *ws, char *hidden_grad, char *weight_grad, hipStream_t stream)
+{
+    typedef typename T::type type;
+    constexpr int e = sizeof(type);
+    constexpr bool scaled = std::is_same<T, F16>::value;
+    const int N = (int)d.N;
+    const bool i64 = d.flags & PX_FLAG_TOKENS_I64;
+    int32_t *status = (int32_t *)(ws + p.status);
+    float *scale = scaled ? (float *)(ws + p.top) : nullptr;
+    hipLaunchKernelGGL(grad_begin<scaled>, dim3(1), dim3(1024), 0, stream, targets, i64, d.V, N, row_weight, status, scale);
+    if (N == 0) {
+        if (weight_grad && !(d.flags & PX_FLAG_ACCUMULATE)) {      // products over no tokens
+            GradArgs g = {};
+            g.o.rows_a = g.cols = d.D;
+            g.o.rows_b = g.rows = d.V;
+            g.out = weight_grad;
+            g.ld = d.weight_grad_stride;
+            launch_grad<T>(0, g, 1, stream);
+        }
+        return status_of(hipGetLastError());
+    }
+    if (weight_grad)
+        hipLaunchKernelGGL(transpose_rows<type>, dim3((unsigned)((p.n_pad + 63) / 64), (d.D + 63) / 64), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, N, d.D,
+                           (type *)(ws + p.ht), p.n_pad, targets, row_weight, i64, d.V);
+    const char *logit_hidden = hidden;
+    int64_t ld_h = d.hidden_stride;
+    if (p.pack_hidden) {
+        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * p.d_pad)), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad);
+        logit_hidden = ws + p.hidden;
+        ld_h = p.d_pad;
+    }
+    LogitArgs a = {};
+    a.targets = targets;
+    a.i64 = i64;
+    a.V = d.V;
+    a.N = N;
+    a.lse = lse;
+    a.row_weight = row_weight;
+    a.scale = scale;
+    a.q = ws + p.q;
+    a.qt = ws + p.qt;
+    a.ld_q = p.v_pad;
+    a.ld_qt = p.n_pad;
+    a.o.b = logit_hidden;
+    a.o.ldb = ld_h * e;
+    a.o.rows_b = N;
+    a.o.lda = (p.pack_weight ? p.d_pad : d.weight_stride) * e;
+    a.o.k_bytes = (int)(p.d_pad * e);      // (where D is padded, both operands are packed)
+    for (int k = 0; k < p.pieces; ++k) {
+        a.first = k * p.piece;
+        a.rows = a.o.rows_a = std::min(p.piece, d.V - a.first);
+        const char *piece = weight + (int64_t)a.first * d.weight_stride * e, *from = piece;
+        if (p.pack_weight) {
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * p.d_pad)), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad);
+            from = ws + p.weight;
+        }
+        a.o.a = from;
+        const int64_t pad = 16 / e, v_pad = (a.rows + pad - 1) / pad * pad;      // of this piece
+        a.ld_q = v_pad;
+        launch_logits<T>(p.tiles, kQ, a, stream);
+        if (hidden_grad) {
+            hipLaunchKernelGGL(transpose_rows<type>, dim3((unsigned)((v_pad + 63) / 64), (d.D + 63) / 64), dim3(256), 0, stream, (const type *)piece, d.weight_stride, a.rows, d.D,
+                               (type *)(ws + p.wt), v_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
+            GradArgs g = {};
+            g.o = {ws + p.wt, ws + p.q, v_pad * e, v_pad * e, d.D, N, (int)(v_pad * e)};
+            g.cols = d.D;
+            g.rows = N;
+            const int stages = (int)((v_pad * e + kRowBytes - 1) / kRowBytes);
+            g.slice_k = (stages + p.slices - 1) / p.slices * kRowBytes;
+            g.scale = scale;
+            g.targets = targets;
+            g.row_weight = row_weight;
+            g.i64 = i64;
+            g.V = d.V;
+            g.sums = p.slices == 1 && p.pieces == 1 ? 0 : k == 0 ? 1 : 2;
+            g.out = g.sums ? (void *)(ws + p.sums) : (void *)hidden_grad;
+            g.ld = d.hidden_grad_stride;
+            launch_grad<T>(p.grad_tiles, g, p.slices, stream);
+        }
+        if (weight_grad) {
+            GradArgs g = {};
+            g.o = {ws + p.ht, ws + p.qt, p.n_pad * e, p.n_pad * e, d.D, a.rows, (int)(p.n_pad * e)};
+            g.cols = d.D;
+            g.rows = a.rows;
+            g.slice_k = (int)((p.n_pad * e + kRowBytes - 1) / kRowBytes) * kRowBytes;
+            g.scale = scale;
+            g.out = weight_grad + (int64_t)a.first * d.weight_grad_stride * e;
+            g.ld = d.weight_grad_stride;
+            g.add = d.flags & PX_FLAG_ACCUMULATE;
+            launch_grad<T>(shape_for(d.D, a.rows, 1, e == 4), g, 1, stream);
+        }
+    }
+    if (hidden_grad && (p.slices > 1 || p.pieces > 1))
+        hipLaunchKernelGGL(join_slices<T>, dim3(blocks_for((int64_t)N * d.D)), dim3(256), 0, stream, (const float *)(ws + p.sums), p.slices, (int64_t)N, d.D, scale, targets,
+                           row_weight, i64, d.V, (type *)hidden_grad, d.hidden_grad_stride);
+    return status_of(hipGetLastError());
+}
+
+}  // namespace
+
+LossPlan loss_plan(const pollux_loss_dims &d, bool grad)
+{
+    LossPlan p = {};
+    const int64_t e = size_of_type(d.type), pad = 16 / e, N = d.N;
+    const bool f32 = e == 4;
+    auto padded = [&](int64_t x) { return (x + pad - 1) / pad * pad; };
+    p.grad = grad;
+    p.d_pad = padded(d.D);
+    p.n_pad = padded(N);
+    p.pack_hidden = d.hidden_stride % pad != 0 || d.D % pad != 0;
+    p.pack_weight = d.weight_stride % pad != 0 || d.D % pad != 0;
+    // A piece's q and its transpose, and its transposed or packed weights, are held to 512 and 256 MiB: pieces that large keep the
+    // matrix kernels' ends and the sums' passes over memory to a few per cent.
+    int64_t piece = (d.V + 255) / 256 * 256;
+    if (grad) piece = std::min(piece, std::max<int64_t>(256, ((512ll << 20) / (std::max<int64_t>(N, 1) * e)) / 256 * 256));
+    if (grad || p.pack_weight) piece = std::min(piece, std::max<int64_t>(256, ((256ll << 20) / (p.d_pad * e)) / 256 * 256));
+    p.pieces = (int)((d.V + piece - 1) / piece);
+    // (even shares)
+    piece = ((d.V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
+    p.piece = (int)piece;
+    p.pieces = (int)((d.V + piece - 1) / piece);
+    p.v_pad = padded(std::min<int64_t>(piece, d.V));
+    p.tiles = shape_for(std::min<int64_t>(piece, d.V), N, 1, f32);
+    p.slices = 1;
+    if (grad) {
+        // the hidden rows' gradient has few tiles and a long sum: the number of workgroups a tile that takes least
+        double least = 1e300;
+        for (int slices = 1; slices <= 16; slices *= 2) {
+            if (slices > 1 && (p.v_pad * e / kRowBytes < 8 * slices || (int64_t)slices * N * d.D * 4 > (512ll << 20))) break;
+            const int shape = shape_for(d.D, N, slices, f32);
+            const ShapeOf &h = kShape[shape];
+            const double tiles = (double)((d.D + h.bm - 1) / h.bm) * ((N + h.bn - 1) / h.bn) * slices;
+            const double cost = ceil(tiles / (256.0 * h.per_cu)) * h.per_cu * h.bm * h.bn / (f32 ? 1.0 : h.rate) / slices;
+            if (cost < 0.9 * least) least = cost, p.slices = slices, p.grad_tiles = shape;
+        }
+    }
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
+    p.status = take(4 * kStatusWords);
+    p.top = take(256);
+    if (!grad) {
+        const size_t tiles = (size_t)p.pieces * ((piece + kShape[p.tiles].bm - 1) / kShape[p.tiles].bm);
+        p.parts = take(8 * tiles * (size_t)N);
+        p.picked = take(4 * (size_t)N);
+    }
+    if (p.pack_hidden) p.hidden = take((size_t)N * p.d_pad * e);
+    if (p.pack_weight) p.weight = take((size_t)piece * p.d_pad * e);
+    if (grad) {
+        p.q = take((size_t)N * p.v_pad * e);
+        p.qt = take((size_t)p.v_pad * p.n_pad * e);
+        p.ht = take((size_t)d.D * p.n_pad * e);
+        p.wt = take((size_t)d.D * p.v_pad * e);
+        if (p.slices > 1 || p.pieces > 1) p.sums = take((size_t)p.slices * N * d.D * 4);
+    }
+    p.total = o;
+    return p;
+}
+
+int launch_token_loss(const pollux_loss_dims &d, const LossPlan &p, const void *hidden, const void *weight, const void *targets,
+                      void *workspace, float *loss, float *lse, hipStream_t stream)
+{
+    const char *h = (const char *)hidden, *w = (const char *)weight;
+    switch (d.type) {
+        case PX_TYPE_F32: return token_loss<F32>(d, p, h, w, targets, (char *)workspace, loss, lse, stream);
+        case PX_TYPE_BF16: return token_loss<Bf16>(d, p, h, w, targets, (char *)workspace, loss, lse, stream);
+        default: return token_loss<F16>(d, p, h, w, targets, (char *)workspace, loss, lse, stream);
+    }
+}
+
+int launch_token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const void *hidden, const void *weight, const void *targets,
+                           const float *lse, const float *row_weight, void *workspace, void *hidden_grad, void *weight_grad,
+                           hipStream_t stream)
+{
+    const char *h = (const char *)hidden, *w = (const char *)weight;
+    char *hg = (char *)hidden_grad, *wg = (char *)weight_grad, *ws = (char *)workspace;
+    switch (d.type) {
+        case PX_TYPE_F32: return token_loss_grad<F32>(d, p, h, w, targets, lse, row_weight, ws, hg, wg, stream);
+        case PX_TYPE_BF16: return token_loss_grad<Bf16>(d, p, h, w, targets, lse, row_weight, ws, hg, wg, stream);
+        default: return token_loss_grad<F16>(d, p, h, w, targets, lse, row_weight, ws, hg, wg, stream);
+    }
+}
+
+}  // namespace px
