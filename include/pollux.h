@@ -528,6 +528,98 @@ int pollux_token_loss_grad(const pollux_loss_dims *dims, /* host */
                            void *weight_grad,            /* [V,D] out (in/out with PX_FLAG_ACCUMULATE), may be NULL */
                            void *hip_stream);
 
+/*
+ * Rows of a table looked up by token: rows[n,:] = scale * table[tokens[n],:], zeros where there is no token.  No workspace.
+ * status: device pointer to one int32, or NULL; PX_ST_BAD_TOKEN is OR-ed into it (the caller clears it).
+ *
+ * pollux_embed_grad: table_grad[v,:] = scale * (sum of rows_grad[n,:] over the n with tokens[n] = v), zeros for an entry that no
+ * token names; with PX_FLAG_ACCUMULATE that is added to what table_grad holds, and rows that no token names are neither read nor
+ * written.  The tokens are sorted (stably) and each entry's rows summed in fp32 in an order that depends on the tokens
+ * alone: the same call gives the same bits.  pollux_last_status on the workspace reads the status word.
+ *
+ * Limits: 0 <= N <= 2^20, 1 <= V < 2^20, 1 <= D <= 2^16, strides below 2^20, scale finite.  table and its gradient, and rows and
+ * theirs, have the types table_type and rows_type.  Outputs and inputs must not overlap.
+ */
+typedef struct {
+    int64_t N;                  /* tokens                                   */
+    int32_t V, D;               /* entries of the table, width of a row     */
+    int32_t table_type, rows_type;
+    int32_t flags;              /* PX_FLAG_TOKENS_I64, PX_FLAG_ACCUMULATE   */
+    float scale;
+    int64_t table_stride, rows_stride;
+} pollux_embed_dims;
+
+int pollux_embed(const pollux_embed_dims *dims,          /* host */
+                 const void *tokens,                     /* [N] */
+                 const void *table,                      /* [V,D] */
+                 void *rows,                             /* [N,D] out */
+                 int32_t *status,                        /* in/out, may be NULL */
+                 void *hip_stream);
+int pollux_embed_workspace_size(const pollux_embed_dims *dims, size_t *bytes /* host, out */);
+int pollux_embed_grad(const pollux_embed_dims *dims,     /* host */
+                      const void *tokens,                /* [N] */
+                      const void *rows_grad,             /* [N,D] */
+                      void *workspace, size_t workspace_bytes,
+                      void *table_grad,                  /* [V,D] out (in/out with PX_FLAG_ACCUMULATE) */
+                      void *hip_stream);
+
+/*
+ * The gradient noise scale (Eq. 5, and the estimator over several gradients of Sec. 3.1) of B gradients g_i of n elements, each the mean
+ * over `examples` examples: those of an iteration's micro-batches or replicas, or, for one GPU without accumulation, of
+ * two iterations in a row.  P is the optimiser's pre-conditioner, a diagonal (precondition NULL: 1):
+ *   mean     = sum_i g_i / B
+ *   scale[0] = tr(P Sigma P') = examples / (B - 1) * sum_i |P (g_i - mean)|^2      (Sigma: covariance of one example's gradient)
+ *   scale[1] = |P g|^2        = |P mean|^2 - scale[0] / (examples * B)
+ *   scale[2] = phi_t          = scale[0] / scale[1]
+ * scale[0] and scale[1] are unbiased; an agent averages them over iterations before it divides, since scale[1] may come out
+ * small or negative where noise prevails.  mean, of type mean_type, is what the optimiser takes; it may be NULL.
+ * Sums in fp64, in a fixed order.  Gradient i begins `stride` elements (0: n) after gradient i - 1; any alignment of the element.
+ * Limits: 2 <= B <= 65536, 0 <= n < 2^40, examples > 0.
+ */
+typedef struct {
+    int64_t n;                  /* elements of a gradient                */
+    int32_t B;                  /* gradients                             */
+    int32_t type, mean_type;    /* PX_TYPE_*                             */
+    int32_t flags;              /* 0                                     */
+    int64_t stride;
+    double examples;            /* that each gradient is the mean over   */
+} pollux_noise_dims;
+
+int pollux_noise_workspace_size(const pollux_noise_dims *dims, size_t *bytes /* host, out */);
+int pollux_noise_scale(const pollux_noise_dims *dims,    /* host */
+                       const void *grads,                /* [B,n] */
+                       const float *precondition,        /* [n] or NULL */
+                       void *workspace, size_t workspace_bytes,
+                       void *mean,                       /* [n] out, may be NULL */
+                       double *scale,                    /* [3] out */
+                       void *hip_stream);
+
+/*
+ * Orthogonalised update of `batch` gradient matrices G [rows, cols]: X = G / |G|_F (zeros for a gradient of zeros), then `steps` times
+ *   X <- a X + (b X X' + c (X X')^2) X        (rows <= cols; for more rows than columns on the transposes)
+ * which, with the coefficients of a Newton-Schulz iteration (1.5, -0.5, 0) or of one tuned for few steps, moves every singular
+ * value of G towards 1.  update: bfloat16.  The products take X in fp16, scaled to its range, with sums in fp32: the update is
+ * within about 2^-9 of its size (2-norm) of the formula's, which is the rounding of the result.
+ * Limits: batch >= 0, 1 <= rows, cols <= 2^16 with the smaller <= 2^14, batch * rows * cols < 2^40, 0 <= steps <= 64,
+ * coefficients finite.  Matrix k begins grads_batch_stride (update_batch_stride) elements after matrix k - 1; rows are
+ * grads_stride (update_stride) apart; 0 stands for contiguous.
+ */
+typedef struct {
+    int32_t batch, rows, cols;
+    int32_t type;               /* PX_TYPE_* of the gradients            */
+    int32_t steps;
+    int32_t flags;              /* 0                                     */
+    double a, b, c;
+    int64_t grads_stride, update_stride, grads_batch_stride, update_batch_stride;
+} pollux_ortho_dims;
+
+int pollux_ortho_workspace_size(const pollux_ortho_dims *dims, size_t *bytes /* host, out */);
+int pollux_orthogonalize(const pollux_ortho_dims *dims,  /* host */
+                         const void *grads,              /* [batch,rows,cols] */
+                         void *workspace, size_t workspace_bytes,
+                         void *update,                   /* [batch,rows,cols] bfloat16 out */
+                         void *hip_stream);
+
 /* Copies the status word of the last pollux_fitness (or pollux_fitness_timed) call that used `workspace`
  * to *host_out.  Synchronises `hip_stream`.  pollux_goodput_per_gpu and pollux_sim_tick neither clear nor
  * set the word; they leave the workspace as it is. */

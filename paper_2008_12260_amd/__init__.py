@@ -28,7 +28,9 @@ EXPORTS = ("pollux_version", "pollux_strerror", "pollux_workspace_size", "pollux
            "pollux_ga_step",
            "pollux_fit_theta", "pollux_goodput_per_gpu", "pollux_autoscale", "pollux_sim_tick", "pollux_last_status",
            "pollux_fitness_timed", "pollux_apply_best", "pollux_generation",
-           "pollux_loss_workspace_size", "pollux_token_loss", "pollux_token_loss_grad")
+           "pollux_loss_workspace_size", "pollux_token_loss", "pollux_token_loss_grad", "pollux_embed", "pollux_embed_workspace_size",
+           "pollux_embed_grad", "pollux_noise_workspace_size", "pollux_noise_scale", "pollux_ortho_workspace_size",
+           "pollux_orthogonalize")
 
 
 class PolluxError(RuntimeError):
@@ -50,6 +52,21 @@ class LossDims(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int32), ("D", ctypes.c_int32), ("type", ctypes.c_int32), ("flags", ctypes.c_int32),
                 ("hidden_stride", ctypes.c_int64), ("weight_stride", ctypes.c_int64), ("hidden_grad_stride", ctypes.c_int64),
                 ("weight_grad_stride", ctypes.c_int64)]
+
+
+class EmbedDims(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int32), ("D", ctypes.c_int32), ("table_type", ctypes.c_int32), ("rows_type", ctypes.c_int32),
+                ("flags", ctypes.c_int32), ("scale", ctypes.c_float), ("table_stride", ctypes.c_int64), ("rows_stride", ctypes.c_int64)]
+
+
+class NoiseDims(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("B", ctypes.c_int32), ("type", ctypes.c_int32), ("mean_type", ctypes.c_int32), ("flags", ctypes.c_int32),
+                ("stride", ctypes.c_int64), ("examples", ctypes.c_double)]
+
+
+class OrthoDims(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "rows", "cols", "type", "steps", "flags")] + [(n, ctypes.c_double) for n in ("a", "b", "c")]
+                + [(n, ctypes.c_int64) for n in ("grads_stride", "update_stride", "grads_batch_stride", "update_batch_stride")])
 
 
 _lib = None
@@ -98,6 +115,20 @@ def lib() -> ctypes.CDLL:
         L.pollux_token_loss.argtypes = [ctypes.POINTER(LossDims), vp, vp, vp, vp, sz, vp, vp, vp]
         L.pollux_token_loss_grad.restype = i
         L.pollux_token_loss_grad.argtypes = [ctypes.POINTER(LossDims), vp, vp, vp, vp, vp, vp, sz, vp, vp, vp]
+        L.pollux_embed.restype = i
+        L.pollux_embed.argtypes = [ctypes.POINTER(EmbedDims), vp, vp, vp, vp, vp]
+        L.pollux_embed_workspace_size.restype = i
+        L.pollux_embed_workspace_size.argtypes = [ctypes.POINTER(EmbedDims), ctypes.POINTER(sz)]
+        L.pollux_embed_grad.restype = i
+        L.pollux_embed_grad.argtypes = [ctypes.POINTER(EmbedDims), vp, vp, vp, sz, vp, vp]
+        L.pollux_noise_workspace_size.restype = i
+        L.pollux_noise_workspace_size.argtypes = [ctypes.POINTER(NoiseDims), ctypes.POINTER(sz)]
+        L.pollux_noise_scale.restype = i
+        L.pollux_noise_scale.argtypes = [ctypes.POINTER(NoiseDims), vp, vp, vp, sz, vp, vp, vp]
+        L.pollux_ortho_workspace_size.restype = i
+        L.pollux_ortho_workspace_size.argtypes = [ctypes.POINTER(OrthoDims), ctypes.POINTER(sz)]
+        L.pollux_orthogonalize.restype = i
+        L.pollux_orthogonalize.argtypes = [ctypes.POINTER(OrthoDims), vp, vp, sz, vp, vp]
         _lib = L
     return _lib
 
@@ -345,4 +376,4 @@ class FitnessCall:
                     status=self.status())
 
 
-from .train import token_loss, token_loss_grad  # noqa: E402,F401  (needs the names above)
+from .train import embed, embed_grad, noise_scale, orthogonalize, token_loss, token_loss_grad  # noqa: E402,F401  (needs the names above)

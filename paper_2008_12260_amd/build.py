@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpollux_hip.so")
 BUILD_INFO = LIB + ".buildinfo"     # one line: the compiler that built LIB (written beside it, read by bench.py)
 SOURCES = ["pollux_api.hip", "pollux_fitness.hip", "pollux_ga.hip", "pollux_theta.hip", "pollux_train_api.hip",
-           "pollux_loss.hip"]
+           "pollux_loss.hip", "pollux_embed.hip", "pollux_noise.hip", "pollux_ortho.hip"]
 OBJECTS = os.path.join(HERE, "_build")
 
 HIPCC_FLAGS = [

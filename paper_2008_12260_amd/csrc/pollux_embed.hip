@@ -1,0 +1,468 @@
+// Rows of a table looked up by token, and the table's gradient: the rows' gradients summed by token.
+//
+// The lookup moves N rows in and out and nothing else.  The gradient is a sum over the places where a token occurs, as uneven as
+// words are: a few tokens hold thousands of places, most one or none.  So the tokens are sorted first (stably, so that every
+// order below is one), and the sorted places are cut into windows of equal length: each window sums its runs of equal tokens,
+// writes those that lie within it, and leaves the sums of the two that its ends may cut (sum_windows); a second launch adds
+// up the pieces of the runs that were cut, in their order (join_runs).  Work is even whatever the tokens are, no result depends on
+// the order in which atomics arrive, and rows that no token names are zeroed by further workgroups of the first launch.
+
+#include "pollux_host.h"
+#include "pollux_train.h"
+
+#include <algorithm>
+
+namespace px {
+namespace {
+
+template <int TYPE>
+struct ElementOf;
+template <>
+struct ElementOf<PX_TYPE_F32> {
+    typedef float type;
+};
+template <>
+struct ElementOf<PX_TYPE_BF16> {
+    typedef __bf16 type;
+};
+template <>
+struct ElementOf<PX_TYPE_F16> {
+    typedef _Float16 type;
+};
+
+constexpr int kVec = 8;         // columns a lane takes at a time
+
+// Eight neighbouring columns as fp32; `left` of them are the row's.  Rows may begin at any element: whole groups of eight are one
+// load of 16 bytes (two of a row in fp32) at whatever alignment.
+template <class E>
+struct Eight {
+    E v[kVec];
+};
+template <class E>
+__device__ __forceinline__ void load8(const E *from, int left, float (&to)[kVec])
+{
+    if (left >= kVec) {
+        Eight<E> t;
+        __builtin_memcpy(&t, from, sizeof(t));
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) to[i] = (float)t.v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) to[i] = i < left ? (float)from[i] : 0.f;
+    }
+}
+template <class E>
+__device__ __forceinline__ void store8(E *to, int left, const float (&v)[kVec])
+{
+    if (left >= kVec) {
+        Eight<E> t;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) t.v[i] = (E)v[i];
+        __builtin_memcpy(to, &t, sizeof(t));
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i < left) to[i] = (E)v[i];
+    }
+}
+
+// A wavefront a row, or, of wide rows, kRowPart columns of one (blockIdx.y).
+constexpr int kRowPart = 64 * kVec * 8;
+template <class T, class R>
+__global__ __launch_bounds__(256) void embed_rows(const void *tokens, bool i64, int64_t N, int V, int D, const T *table, int64_t ld_table, float scale, R *rows,
+                                                  int64_t ld_rows, int32_t *status)
+{
+    const int64_t n = blockIdx.x * 4ll + (threadIdx.x >> 6);
+    if (n >= N) return;
+    bool bad;
+    const int v = token_at(tokens, n, i64, V, bad);
+    const int first = blockIdx.y * kRowPart, last = min(D, first + kRowPart);
+    if (bad && status && blockIdx.y == 0 && (threadIdx.x & 63) == 0) atomicOr(status, PX_ST_BAD_TOKEN);
+    const T *from = table + (int64_t)max(v, 0) * ld_table;
+    R *to = rows + n * ld_rows;
+#pragma unroll 4
+    for (int c = first + (threadIdx.x & 63) * kVec; c < last; c += 64 * kVec) {
+        float x[kVec];
+        if (v >= 0) load8(from + c, last - c, x);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) x[i] = v >= 0 ? x[i] * scale : 0.f;
+        store8(to + c, last - c, x);
+    }
+}
+
+// ---- sort ----------------------------------------------------------------------------------------------------------
+// Keys are tokens, V for none (sorted last, and dropped).  Up to kFew tokens: one workgroup counts, for every token, those before it.
+// More: two passes, lowest digit first, of ceil(log2(V + 1)) / 2 bits.
+
+constexpr int kFew = 1024, kThreads = 1024, kWaves = kThreads / 64, kMaxBits = 10;
+
+__global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i64, int N, int V, int32_t *status, int *keys, int *places)
+{
+    __shared__ int shared[kFew];
+    __shared__ int bad_any;
+    const int n = threadIdx.x;
+    if (n == 0) bad_any = 0;
+    if (n < kStatusWords) status[n] = 0;
+    bool bad = false;
+    int key = 0x7fffffff;
+    if (n < N) {
+        const int v = token_at(tokens, n, i64, V, bad);
+        key = v < 0 ? V : v;
+    }
+    shared[n] = key;
+    __syncthreads();
+    if (bad) bad_any = 1;
+    int before = 0;
+    for (int i = 0; i < N; ++i) {
+        const int k = shared[i];
+        before += k < key || (k == key && i < n) ? 1 : 0;
+    }
+    if (n < N) {
+        keys[before] = key;
+        places[before] = n;
+    }
+    __syncthreads();
+    if (n == 0 && bad_any) *status = PX_ST_BAD_TOKEN;
+}
+
+// A workgroup's tokens counted by their lowest digit; the second pass's counts and the status word are cleared.
+__global__ __launch_bounds__(kThreads) void count_digits(const void *tokens, bool i64, int N, int V, int per_block, int bits, int *counts, int *counts2, int32_t *status)
+{
+    __shared__ int bins[1 << kMaxBits];
+    const int size = 1 << bits, first = blockIdx.x * per_block, last = min(N, first + per_block);
+    for (int i = threadIdx.x; i < size; i += kThreads) bins[i] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
+    __syncthreads();
+    for (int n = first + threadIdx.x; n < last; n += kThreads) {
+        bool bad;
+        const int v = token_at(tokens, n, i64, V, bad);
+        atomicAdd(&bins[(v < 0 ? V : v) & (size - 1)], 1);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < size; i += kThreads) {
+        counts[blockIdx.x * size + i] = bins[i];
+        counts2[blockIdx.x * size + i] = 0;
+    }
+}
+
+// One pass: every workgroup finds, from all workgroups' counts, where its tokens of each digit go, and puts them there in their
+// order.  The first pass reads the tokens themselves and counts, for the second, the next digits of the places it fills.
+template <bool FIRST>
+__global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, bool i64, const int *keys_in, const int *places_in, int N, int V, int blocks, int per_block,
+                                                         int bits, const int *counts, int *counts2, int *keys, int *places, int32_t *status)
+{
+    __shared__ int base[1 << kMaxBits];
+    __shared__ int in_wave[kWaves][1 << kMaxBits];
+    __shared__ int waves[kWaves];
+    const int size = 1 << bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // digit `tid`: tokens of it in all workgroups and in those before this one
+    int all = 0, before = 0;
+    if (tid < size)
+        for (int b = 0; b < blocks; ++b) {
+            const int c = counts[b * size + tid];
+            all += c;
+            before += b < (int)blockIdx.x ? c : 0;
+        }
+    int sum = all;
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) {
+        const int up = __shfl_up(sum, w);
+        if (lane >= w) sum += up;
+    }
+    if (lane == 63) waves[wave] = sum;
+    __syncthreads();
+    int lower = 0;
+    for (int w = 0; w < wave; ++w) lower += waves[w];
+    if (tid < size) base[tid] = lower + sum - all + before;
+    bool bad_seen = false;
+    const int first = blockIdx.x * per_block, last = min(N, first + per_block);
+    for (int at = first; at < last; at += kThreads) {
+        const int n = at + tid;
+        const bool there = n < last;
+        int key = 0, place = 0;
+        if (there) {
+            if (FIRST) {
+                bool bad;
+                const int v = token_at(tokens, n, i64, V, bad);
+                bad_seen |= bad;
+                key = v < 0 ? V : v;
+                place = n;
+            } else {
+                key = keys_in[n];
+                place = places_in[n];
+            }
+        }
+        const int digit = (FIRST ? key : key >> bits) & (size - 1);
+        for (int i = tid; i < kWaves * size; i += kThreads) in_wave[i >> bits][i & (size - 1)] = 0;
+        __syncthreads();
+        // lanes of this wavefront with the same digit
+        unsigned long long same = __ballot(there);
+        for (int b = 0; b < bits; ++b) {
+            const unsigned long long set = __ballot((digit >> b) & 1);
+            same &= (digit >> b) & 1 ? set : ~set;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        if (there && rank == 0) in_wave[wave][digit] = __popcll(same);
+        __syncthreads();
+        int total = 0;
+        if (tid < size)
+            for (int w = 0; w < kWaves; ++w) {
+                const int c = in_wave[w][tid];
+                in_wave[w][tid] = total;
+                total += c;
+            }
+        __syncthreads();
+        if (there) {
+            const int to = base[digit] + in_wave[wave][digit] + rank;
+            keys[to] = key;
+            places[to] = place;
+            if (FIRST) atomicAdd(&counts2[to / per_block * size + ((key >> bits) & (size - 1))], 1);
+        }
+        __syncthreads();
+        if (tid < size) base[tid] += total;
+        __syncthreads();
+    }
+    if (FIRST && bad_seen) atomicOr(status, PX_ST_BAD_TOKEN);
+}
+
+// ---- sums ----------------------------------------------------------------------------------------------------------
+
+struct SumArgs {
+    const int *keys, *places;
+    int64_t ld_rows, ld_table;
+    float *partial;             // [2][windows][D]: the run cut by a window's first place, by its last
+    int N, V, D, window, windows;
+    int lanes;                  // threads that share a window, kVec columns each: a power of two
+    int groups;                 // 256 / lanes windows a workgroup
+    int window_blocks;          // workgroups after these zero the rows that no token names, kZeroRows each
+    bool add;
+    float scale;
+};
+constexpr int kZeroRows = 32;
+
+template <class R, class T>
+__global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *rows, T *table)
+{
+    if ((int)blockIdx.x >= A.window_blocks) {
+        // the first place of a token not below row v: is it v's?
+        __shared__ unsigned char named[kZeroRows];
+        const int v0 = ((int)blockIdx.x - A.window_blocks) * kZeroRows;
+        if (threadIdx.x < kZeroRows) {
+            const int v = v0 + threadIdx.x;
+            int lo = 0, hi = A.N;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (A.keys[mid] < v) lo = mid + 1;
+                else hi = mid;
+            }
+            named[threadIdx.x] = lo < A.N && A.keys[lo] == v;
+        }
+        __syncthreads();
+        const float zeros[kVec] = {};
+        for (int i = threadIdx.x; i < kZeroRows * A.lanes; i += 256) {
+            const int r = i / A.lanes, c = (blockIdx.y * A.lanes + i % A.lanes) * kVec;
+            if (v0 + r < A.V && c < A.D && !named[r]) store8(table + (int64_t)(v0 + r) * A.ld_table + c, A.D - c, zeros);
+        }
+        return;
+    }
+    const int w = blockIdx.x * A.groups + threadIdx.x / A.lanes;
+    const int c = (blockIdx.y * A.lanes + threadIdx.x % A.lanes) * kVec;
+    if (w >= A.windows || c >= A.D) return;
+    const int first = w * A.window, last = min(A.N, first + A.window), left = A.D - c;
+    float sum[kVec] = {};
+    int run = A.keys[first];
+    bool cut = first > 0 && A.keys[first - 1] == run;         // by the window's first place
+    constexpr int kAhead = 8;
+    for (int at = first; at < last; at += kAhead) {
+        float x[kAhead][kVec];
+        int key[kAhead + 1];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int p = min(at + i, A.N - 1);
+            key[i] = A.keys[p];
+            if (at + i < last && key[i] < A.V) load8(rows + (int64_t)A.places[p] * A.ld_rows + c, left, x[i]);
+        }
+        key[kAhead] = at + kAhead < A.N ? A.keys[at + kAhead] : -1;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (at + i >= last) break;
+            if (key[i] >= A.V) return;                        // from here on no tokens
+            if (key[i] != run) {
+                run = key[i];
+                cut = false;
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) sum[k] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) sum[k] += x[i][k];
+            const bool ends = at + i + 1 >= A.N || key[i + 1] != run, final = at + i + 1 >= last;
+            if (!ends && !final) continue;
+            if (ends && !cut) {
+                T *to = table + (int64_t)run * A.ld_table + c;
+                float out[kVec];
+                if (A.add) {
+                    float held[kVec];
+                    load8(to, left, held);
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k) out[k] = held[k] + sum[k] * A.scale;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k) out[k] = sum[k] * A.scale;
+                }
+                store8(to, left, out);
+            } else {
+                store8(A.partial + ((int64_t)(cut ? 0 : A.windows) + w) * A.D + c, left, sum);
+            }
+        }
+    }
+}
+
+// The runs that windows cut: the window in which one begins adds up the pieces, its own and those of the windows after it.
+template <class T>
+__global__ __launch_bounds__(256) void join_runs(const SumArgs A, T *table)
+{
+    const int w = blockIdx.x * A.groups + threadIdx.x / A.lanes;
+    const int c = (blockIdx.y * A.lanes + threadIdx.x % A.lanes) * kVec;
+    if (w + 1 >= A.windows || c >= A.D) return;
+    const int first = w * A.window, last = first + A.window, run = A.keys[last - 1], left = A.D - c;
+    if (run >= A.V || A.keys[last] != run) return;            // nothing is cut by this window's end
+    if (A.keys[first] == run && first > 0 && A.keys[first - 1] == run) return;      // it began before
+    float sum[kVec];
+    load8(A.partial + ((int64_t)A.windows + w) * A.D + c, left, sum);
+    // windows that the run reaches: up to the one that holds its last place
+    int lo = last, hi = A.N;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (A.keys[mid] <= run) lo = mid + 1;
+        else hi = mid;
+    }
+    const int end = (lo - 1) / A.window;
+#pragma unroll 4
+    for (int u = w + 1; u <= end; ++u) {
+        float x[kVec];
+        load8(A.partial + (int64_t)u * A.D + c, left, x);
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) sum[k] += x[k];
+    }
+    T *to = table + (int64_t)run * A.ld_table + c;
+    if (A.add) {
+        float held[kVec];
+        load8(to, left, held);
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) sum[k] = held[k] + sum[k] * A.scale;
+    } else {
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) sum[k] *= A.scale;
+    }
+    store8(to, left, sum);
+}
+
+template <class R, class T>
+int embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *tokens, const R *rows, char *ws, T *table, hipStream_t stream)
+{
+    const int N = (int)d.N;
+    const bool i64 = d.flags & PX_FLAG_TOKENS_I64;
+    int32_t *status = (int32_t *)(ws + p.status);
+    int *keys[2] = {(int *)(ws + p.keys[0]), (int *)(ws + p.keys[1])}, *places[2] = {(int *)(ws + p.places[0]), (int *)(ws + p.places[1])};
+    if (p.passes == 0) {
+        hipLaunchKernelGGL(rank_few, dim3(1), dim3(kThreads), 0, stream, tokens, i64, N, d.V, status, keys[1], places[1]);
+    } else {
+        int *counts = (int *)(ws + p.counts), *counts2 = counts + ((size_t)p.blocks << p.bits);
+        hipLaunchKernelGGL(count_digits, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, N, d.V, p.per_block, p.bits, counts, counts2, status);
+        hipLaunchKernelGGL(place_digits<true>, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, (const int *)nullptr, (const int *)nullptr, N, d.V, p.blocks,
+                           p.per_block, p.bits, (const int *)counts, counts2, keys[0], places[0], status);
+        hipLaunchKernelGGL(place_digits<false>, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, (const int *)keys[0], (const int *)places[0], N, d.V, p.blocks,
+                           p.per_block, p.bits, (const int *)counts2, (int *)nullptr, keys[1], places[1], status);
+    }
+    SumArgs a = {};
+    a.keys = keys[1];
+    a.places = places[1];
+    a.ld_rows = d.rows_stride;
+    a.ld_table = d.table_stride;
+    a.partial = (float *)(ws + p.partial);
+    a.N = N;
+    a.V = d.V;
+    a.D = d.D;
+    a.window = p.window;
+    a.windows = p.windows;
+    a.lanes = 1;
+    while (a.lanes < 256 && a.lanes * kVec < d.D) a.lanes *= 2;
+    a.groups = 256 / a.lanes;
+    a.window_blocks = (p.windows + a.groups - 1) / a.groups;
+    a.add = d.flags & PX_FLAG_ACCUMULATE;
+    a.scale = d.scale;
+    const unsigned parts = (unsigned)((d.D + 256 * kVec - 1) / (256 * kVec));
+    const int zero_blocks = a.add ? 0 : (d.V + kZeroRows - 1) / kZeroRows;
+    if (a.window_blocks + zero_blocks > 0)
+        hipLaunchKernelGGL((sum_windows<R, T>), dim3((unsigned)(a.window_blocks + zero_blocks), parts), dim3(256), 0, stream, a, rows, table);
+    if (p.windows > 1) hipLaunchKernelGGL(join_runs<T>, dim3((unsigned)a.window_blocks, parts), dim3(256), 0, stream, a, table);
+    return status_of(hipGetLastError());
+}
+
+template <class F>
+int with_type(int type, F f)
+{
+    switch (type) {
+        case PX_TYPE_F32: return f(ElementOf<PX_TYPE_F32>());
+        case PX_TYPE_BF16: return f(ElementOf<PX_TYPE_BF16>());
+        default: return f(ElementOf<PX_TYPE_F16>());
+    }
+}
+
+}  // namespace
+
+EmbedPlan embed_plan(const pollux_embed_dims &d)
+{
+    EmbedPlan p = {};
+    const int N = (int)d.N;
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
+    p.status = take(4 * kStatusWords);
+    if (N > kFew) {
+        int bits = 1;
+        while (((int64_t)1 << (2 * bits)) <= d.V) ++bits;       // keys 0 .. V
+        p.bits = bits;
+        p.passes = 2;
+        // at most 64 workgroups: each reads all of their counts
+        p.per_block = std::max(kThreads, ((N + 63) / 64 + kThreads - 1) / kThreads * kThreads);
+        p.blocks = (N + p.per_block - 1) / p.per_block;
+        p.counts = take((size_t)2 * p.blocks * 4 << bits);
+        p.keys[0] = take(4 * (size_t)N);
+        p.places[0] = take(4 * (size_t)N);
+    }
+    p.keys[1] = take(4 * (size_t)N);
+    p.places[1] = take(4 * (size_t)N);
+    p.window = N <= 1 << 16 ? 32 : 128;
+    p.windows = (N + p.window - 1) / p.window;
+    p.partial = take(2 * (size_t)p.windows * d.D * 4);
+    p.total = o;
+    return p;
+}
+
+int launch_embed(const pollux_embed_dims &d, const void *tokens, const void *table, void *rows, int32_t *status, hipStream_t stream)
+{
+    if (d.N == 0) return PX_OK;
+    return with_type(d.table_type, [&](auto t) {
+        return with_type(d.rows_type, [&](auto r) {
+            typedef typename decltype(t)::type T;
+            typedef typename decltype(r)::type R;
+            hipLaunchKernelGGL((embed_rows<T, R>), dim3((unsigned)((d.N + 3) / 4), (unsigned)((d.D + kRowPart - 1) / kRowPart)), dim3(256), 0, stream, tokens,
+                               (d.flags & PX_FLAG_TOKENS_I64) != 0, d.N, d.V, d.D, (const T *)table, d.table_stride, d.scale, (R *)rows, d.rows_stride, status);
+            return status_of(hipGetLastError());
+        });
+    });
+}
+
+int launch_embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *tokens, const void *rows_grad, void *workspace, void *table_grad,
+                      hipStream_t stream)
+{
+    return with_type(d.table_type, [&](auto t) {
+        return with_type(d.rows_type, [&](auto r) {
+            typedef typename decltype(t)::type T;
+            typedef typename decltype(r)::type R;
+            return embed_grad<R, T>(d, p, tokens, (const R *)rows_grad, (char *)workspace, (T *)table_grad, stream);
+        });
+    });
+}
+
+}  // namespace px

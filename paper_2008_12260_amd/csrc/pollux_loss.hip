@@ -28,17 +28,10 @@
 namespace px {
 namespace {
 
-// A token's target, -1 where there is none or it is no entry of the vocabulary (then `bad`).
-__device__ __forceinline__ int target_of(const void *targets, int64_t n, bool i64, int V, bool &bad)
-{
-    const int64_t y = i64 ? ((const int64_t *)targets)[n] : (int64_t)((const int32_t *)targets)[n];
-    bad = y < -1 || y >= V;
-    return y < 0 || y >= V ? -1 : (int)y;
-}
 __device__ __forceinline__ int target_of(const void *targets, int64_t n, bool i64, int V)
 {
     bool bad;
-    return target_of(targets, n, i64, V, bad);
+    return token_at(targets, n, i64, V, bad);
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -156,7 +149,7 @@ __global__ __launch_bounds__(kJoinTokens *kJoinParts) void loss_join(const float
     const float whole = from + logf(sum);
     lse[n] = whole;
     bool bad;
-    const int y = target_of(targets, n, i64, V, bad);
+    const int y = token_at(targets, n, i64, V, bad);
     loss[n] = y < 0 ? 0.f : whole - picked[n];
     if (bad) atomicOr(status, PX_ST_BAD_TOKEN);
 }
@@ -176,7 +169,7 @@ __global__ __launch_bounds__(1024) void grad_begin(const void *targets, bool i64
     float top = 0.f;
     for (int n = threadIdx.x; n < N; n += 1024) {
         bool bad;
-        const int y = target_of(targets, n, i64, V, bad);
+        const int y = token_at(targets, n, i64, V, bad);
         if (bad) bad_any = 1;
         if (SCALED && y >= 0) {
             const float g = row_weight ? fabsf(row_weight[n]) : 1.f;
@@ -357,38 +350,6 @@ __global__ __launch_bounds__(256) void transpose_rows(const E *from, int64_t ld_
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
-
-constexpr int kShapes = 4;
-struct ShapeOf {
-    int bm, bn, per_cu;         // tile, workgroups a compute unit holds
-    float rate;                 // of the matrix units' while it runs, relative
-};
-constexpr ShapeOf kShape[kShapes] = {{256, 256, 1, 1.0f}, {128, 128, 2, 0.75f}, {64, 64, 4, 0.45f}, {128, 16, 4, 0.15f}};
-
-// The shape whose rounds over the compute units take least: ceil(tiles / (256 x per_cu)) rounds of per_cu tiles.
-int shape_for(int64_t m, int64_t n, int64_t slices, bool f32)
-{
-    int best = 0;
-    double least = 1e300;
-    for (int s = 0; s < kShapes; ++s) {
-        const ShapeOf &h = kShape[s];
-        const double tiles = (double)((m + h.bm - 1) / h.bm) * ((n + h.bn - 1) / h.bn) * slices;
-        const double cost = ceil(tiles / (256.0 * h.per_cu)) * h.per_cu * h.bm * h.bn / (f32 ? 1.0 : h.rate);
-        if (cost < least) least = cost, best = s;
-    }
-    return best;
-}
-
-template <class T>
-using Shape0 = TileShape<T, 256, 256, 2, 4>;
-template <class T>
-using Shape1 = TileShape<T, 128, 128, 2, 2>;
-template <class T>
-using Shape2 = TileShape<T, 64, 64, 2, 2>;
-template <class T>
-using Shape3 = TileShape<T, 128, 16, 2, 1>;
-
-int status_of(hipError_t e) { return e == hipSuccess ? PX_OK : PX_E_HIP; }
 
 enum LogitKind { kLoss, kQ };
 template <class S>

@@ -1,0 +1,151 @@
+// The gradient noise scale of several gradients, and their mean, in one pass over them.
+//
+// Per element, with deviations d_i = g_i - g_0 from the first gradient (exact in fp64 for 16-bit gradients; equal gradients
+// then show no noise at all): sum_i (g_i - mean)^2 = sum d_i^2 - (sum d_i)^2 / B and mean = g_0 + sum d_i / B.  Bound by reading
+// the gradients: about five fp64 operations an element hide behind 2 bytes of it.  Workgroups leave fp64 sums in the workspace
+// and a second launch adds them up in their order, so that the result depends on nothing but the gradients.
+
+#include "pollux_host.h"
+#include "pollux_train.h"
+
+#include <algorithm>
+
+namespace px {
+namespace {
+
+constexpr int kVec = 8, kAhead = 4, kThreads = 256;
+
+template <class E>
+struct Eight {
+    E v[kVec];
+};
+
+template <class E>
+__device__ __forceinline__ void load8(const E *from, int64_t left, Eight<E> &to)
+{
+    if (left >= kVec) __builtin_memcpy(&to, from, sizeof(to));      // one load of 16 bytes (two in fp32) at any alignment of the element
+    else
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) to.v[i] = i < left ? from[i] : E(0.f);
+}
+
+template <class E, class M>
+__global__ __launch_bounds__(kThreads) void noise_sums(const E *grads, int64_t n, int B, int64_t stride, const float *precondition, M *mean, double2 *sums)
+{
+    double trace = 0.0, norm = 0.0;
+    const double over_b = 1.0 / B;
+    for (int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kVec; at < n; at += (int64_t)gridDim.x * kThreads * kVec) {
+        const int64_t left = n - at;
+        Eight<E> g0;
+        load8(grads + at, left, g0);
+        double s1[kVec] = {}, s2[kVec] = {};
+        for (int b = 1; b < B; b += kAhead) {
+            Eight<E> g[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (b + k < B) load8(grads + (b + k) * stride + at, left, g[k]);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (b + k < B) {
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) {
+                        const double d = (double)(float)g[k].v[i] - (double)(float)g0.v[i];
+                        s1[i] += d;
+                        s2[i] = fma(d, d, s2[i]);
+                    }
+                }
+        }
+        Eight<float> p;
+        if (precondition) load8(precondition + at, left, p);
+        Eight<M> out;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const double m = (double)(float)g0.v[i] + s1[i] * over_b;
+            out.v[i] = (M)(float)m;
+            if (i < left) {
+                const double w = precondition ? (double)p.v[i] * (double)p.v[i] : 1.0;
+                const double v = fma(-s1[i] * over_b, s1[i], s2[i]);
+                trace += w * (v < 0.0 ? 0.0 : v);              // (NaN stays)
+                norm += w * (m * m);
+            }
+        }
+        if (mean) {
+            if (left >= kVec) __builtin_memcpy(mean + at, &out, sizeof(out));
+            else
+                for (int i = 0; i < left; ++i) mean[at + i] = out.v[i];
+        }
+    }
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) {
+        trace += __shfl_xor(trace, w);
+        norm += __shfl_xor(norm, w);
+    }
+    __shared__ double2 waves[kThreads / 64];
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = make_double2(trace, norm);
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int i = 1; i < kThreads / 64; ++i) {
+        trace += waves[i].x;
+        norm += waves[i].y;
+    }
+    sums[blockIdx.x] = make_double2(trace, norm);
+}
+
+__global__ __launch_bounds__(kThreads) void noise_join(const double2 *sums, int blocks, int B, double examples, double *scale)
+{
+    __shared__ double2 shared[kThreads];
+    double trace = 0.0, norm = 0.0;
+    for (int i = threadIdx.x; i < blocks; i += kThreads) {
+        trace += sums[i].x;
+        norm += sums[i].y;
+    }
+    shared[threadIdx.x] = make_double2(trace, norm);
+    __syncthreads();
+    for (int w = kThreads / 2; w > 0; w >>= 1) {
+        if (threadIdx.x < w) {
+            shared[threadIdx.x].x += shared[threadIdx.x + w].x;
+            shared[threadIdx.x].y += shared[threadIdx.x + w].y;
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x != 0) return;
+    const double t = shared[0].x * (examples / (B - 1)), e = shared[0].y - t / (examples * B);
+    scale[0] = t;
+    scale[1] = e;
+    scale[2] = t / e;
+}
+
+}  // namespace
+
+// Workgroups of the pass: eight a compute unit at most, so that there are few sums to add up.
+unsigned noise_blocks(int64_t n)
+{
+    return (unsigned)std::max<int64_t>(1, std::min<int64_t>((n + kThreads * kVec - 1) / (kThreads * kVec), 2048));
+}
+
+int launch_noise_scale(const pollux_noise_dims &d, const void *grads, const float *precondition, void *workspace, void *mean, double *scale,
+                       hipStream_t stream)
+{
+    const unsigned blocks = noise_blocks(d.n);
+    auto pass = [&](auto e, auto m) {
+        typedef decltype(e) E;
+        typedef decltype(m) M;
+        hipLaunchKernelGGL((noise_sums<E, M>), dim3(blocks), dim3(kThreads), 0, stream, (const E *)grads, d.n, d.B, d.stride, precondition, (M *)mean, (double2 *)workspace);
+    };
+    auto with_mean = [&](auto e) {
+        switch (d.mean_type) {
+            case PX_TYPE_F32: pass(e, 0.f); break;
+            case PX_TYPE_BF16: pass(e, (__bf16)0.f); break;
+            default: pass(e, (_Float16)0.f); break;
+        }
+    };
+    switch (d.type) {
+        case PX_TYPE_F32: with_mean(0.f); break;
+        case PX_TYPE_BF16: with_mean((__bf16)0.f); break;
+        default: with_mean((_Float16)0.f); break;
+    }
+    hipLaunchKernelGGL(noise_join, dim3(1), dim3(kThreads), 0, stream, (const double2 *)workspace, (int)blocks, d.B, d.examples, scale);
+    return status_of(hipGetLastError());
+}
+
+}  // namespace px

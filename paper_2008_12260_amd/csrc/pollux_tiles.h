@@ -12,6 +12,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 namespace px {
@@ -19,8 +20,7 @@ namespace px {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 // The element types: what a value is stored as, and the product of 16 bytes of k of sixteen rows with those of sixteen others
 // (four lanes share a row).
@@ -69,6 +69,36 @@ struct TileShape {
     static constexpr int kLoadsA = BM * kRowBytes / (kThreads * 16), kLoadsB = BN * kRowBytes / (kThreads * 16);
     static_assert(kLoadsA * kThreads * 16 == BM * kRowBytes && kLoadsB * kThreads * 16 == BN * kRowBytes, "whole loads");
 };
+
+constexpr int kShapes = 4;
+struct ShapeOf {
+    int bm, bn, per_cu;         // tile, workgroups a compute unit holds
+    float rate;                 // of the matrix units' while it runs, relative
+};
+constexpr ShapeOf kShape[kShapes] = {{256, 256, 1, 1.0f}, {128, 128, 2, 0.75f}, {64, 64, 4, 0.45f}, {128, 16, 4, 0.15f}};
+
+// The shape whose rounds over the compute units take least: ceil(tiles / (256 x per_cu)) rounds of per_cu tiles.
+inline int shape_for(int64_t m, int64_t n, int64_t slices, bool f32)
+{
+    int best = 0;
+    double least = 1e300;
+    for (int s = 0; s < kShapes; ++s) {
+        const ShapeOf &h = kShape[s];
+        const double tiles = (double)((m + h.bm - 1) / h.bm) * ((n + h.bn - 1) / h.bn) * slices;
+        const double cost = ceil(tiles / (256.0 * h.per_cu)) * h.per_cu * h.bm * h.bn / (f32 ? 1.0 : h.rate);
+        if (cost < least) least = cost, best = s;
+    }
+    return best;
+}
+
+template <class T>
+using Shape0 = TileShape<T, 256, 256, 2, 4>;
+template <class T>
+using Shape1 = TileShape<T, 128, 128, 2, 2>;
+template <class T>
+using Shape2 = TileShape<T, 64, 64, 2, 2>;
+template <class T>
+using Shape3 = TileShape<T, 128, 16, 2, 1>;
 
 #ifdef __HIP_DEVICE_COMPILE__
 

@@ -158,3 +158,121 @@ def token_loss_grad(hidden, weight, targets, lse, row_weight=None, hidden_grad=N
                                                 _px._ptr(hidden_grad), _px._ptr(weight_grad), _px._stream_handle(stream)),
                "pollux_token_loss_grad")
     return hidden_grad, weight_grad
+
+
+def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=None):
+    """scale * table[tokens]: rows [*tokens.shape, D] in `dtype` (None: the table's), zeros where a token is -1.
+
+    A token that is neither -1 nor an entry of the table counts as -1 and sets PX_ST_BAD_TOKEN in `status`, an int32 tensor
+    of one element that the caller clears."""
+    import torch
+    with _on(stream):
+        _on_device(tokens=tokens, table=table, out=out, status=status)
+        dtype = table.dtype if dtype is None else dtype
+        table_type = _type(table, "table")
+        table, table_stride = _rows(table, "table")
+        count, D = tokens.numel(), table.shape[1]
+        if status is not None and (status.dtype != torch.int32 or status.numel() != 1):
+            raise ValueError("status is one int32")
+        shape = tuple(tokens.shape) + (D,)
+        flat, flag = _tokens(tokens, "tokens", count)
+        rows = torch.empty((count, D), dtype=dtype, device=table.device) if out is None else out.view(count, D)
+        rows_type = _type(rows, "rows")
+        rows, rows_stride = _result(rows, "out", (count, D), dtype)
+        dims = _px.EmbedDims(count, table.shape[0], D, table_type, rows_type, flag, float(scale), table_stride, rows_stride)
+        _check(_px.lib().pollux_embed(ctypes.byref(dims), flat.data_ptr(), table.data_ptr(), rows.data_ptr(), _px._ptr(status),
+                                      _px._stream_handle(stream)), "pollux_embed")
+    return rows.view(shape) if out is None else out
+
+
+def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, accumulate=False, workspace=None, stream=None):
+    """Gradient of a table of V entries from that of its looked-up rows: [V, D] in `dtype` (None: that of rows_grad), row v being
+    scale times the sum of the rows whose token is v.  accumulate: table_grad is given and added to; rows that no token names
+    are then not touched."""
+    import torch
+    with _on(stream):
+        _on_device(tokens=tokens, rows_grad=rows_grad, table_grad=table_grad)
+        count, D = tokens.numel(), rows_grad.shape[-1]
+        if rows_grad.shape[:-1] != tokens.shape and rows_grad.numel() != count * D:
+            raise ValueError(f"rows_grad {tuple(rows_grad.shape)} has not a row for each of the tokens {tuple(tokens.shape)}")
+        if accumulate and table_grad is None:
+            raise ValueError("accumulate needs a table_grad to add to")
+        flat, flag = _tokens(tokens, "tokens", count)
+        rows_type = _type(rows_grad, "rows_grad")
+        rows, rows_stride = _rows(rows_grad if rows_grad.dim() == 2 else rows_grad.reshape(count, D), "rows_grad")
+        if table_grad is None:
+            table_grad = torch.empty((V, D), dtype=rows.dtype if dtype is None else dtype, device=rows.device)
+        table_grad, table_stride = _result(table_grad, "table_grad", (V, D), table_grad.dtype if dtype is None else dtype)
+        dims = _px.EmbedDims(count, V, D, _type(table_grad, "table_grad"), rows_type, flag | (_px.PX_FLAG_ACCUMULATE if accumulate else 0), float(scale),
+                             table_stride, rows_stride)
+        need = ctypes.c_size_t(0)
+        _check(_px.lib().pollux_embed_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_embed_workspace_size")
+        if workspace is None:
+            workspace = _scratch(need.value, rows.device)
+        _check(_px.lib().pollux_embed_grad(ctypes.byref(dims), flat.data_ptr(), rows.data_ptr(), workspace.data_ptr(),
+                                           workspace.numel() * workspace.element_size(), table_grad.data_ptr(), _px._stream_handle(stream)),
+               "pollux_embed_grad")
+    return table_grad
+
+
+def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=True, stream=None):
+    """(mean, scale) of the gradients grads[i], each the mean over `examples` examples: their mean, in `mean_dtype` (None: fp32), and the
+    fp64 tensor [tr(P Sigma P'), |P g|^2, their quotient phi], P the diagonal `precondition` (fp32, one value an element; None: 1).
+    want_mean False: None in the place of the mean."""
+    import torch
+    with _on(stream):
+        _on_device(grads=grads, precondition=precondition)
+        if grads.dim() < 2:
+            raise ValueError("grads holds one gradient a row: [B, ...]")
+        type_, B, shape = _type(grads, "grads"), grads.shape[0], tuple(grads.shape[1:])
+        flat = grads.flatten(1)
+        n = flat.shape[1]
+        if n > 1 and flat.stride(1) != 1 or flat.stride(0) < n or flat.data_ptr() % 16:
+            flat = flat.clone(memory_format=_contiguous())
+        if precondition is not None:
+            if precondition.dtype != torch.float32 or precondition.numel() != n:
+                raise ValueError(f"precondition is {precondition.dtype} of {precondition.numel()} elements: float32 of {n} is wanted")
+            precondition = precondition.contiguous()
+            if precondition.data_ptr() % 16:
+                precondition = precondition.clone()
+        mean = torch.empty(shape, dtype=torch.float32 if mean_dtype is None else mean_dtype, device=flat.device) if want_mean else None
+        scale = torch.empty(3, dtype=torch.float64, device=flat.device)
+        dims = _px.NoiseDims(n, B, type_, _px.PX_TYPE_F32 if mean is None else _type(mean, "mean"), 0, flat.stride(0), float(examples))
+        need = ctypes.c_size_t(0)
+        _check(_px.lib().pollux_noise_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_noise_workspace_size")
+        workspace = _scratch(need.value, flat.device)
+        _check(_px.lib().pollux_noise_scale(ctypes.byref(dims), flat.data_ptr(), _px._ptr(precondition), workspace.data_ptr(), workspace.numel(),
+                                            _px._ptr(mean), scale.data_ptr(), _px._stream_handle(stream)), "pollux_noise_scale")
+    return mean, scale
+
+
+def orthogonalize(grads, steps=5, coefficients=(3.4445, -4.7750, 2.0315), out=None, workspace=None, stream=None):
+    """The update, in bfloat16, of gradient matrices grads [..., rows, cols]: X = G / |G|_F, then `steps` times
+    X <- a X + (b X X' + c (X X')^2) X with (a, b, c) = coefficients, which moves the singular values towards 1 (the default
+    coefficients bring those above 1e-3 of the norm to 0.7 .. 1.2 in five steps; (1.5, -0.5, 0) converges to 1)."""
+    import torch
+    with _on(stream):
+        _on_device(grads=grads, out=out)
+        if grads.dim() < 2:
+            raise ValueError("grads holds matrices: [..., rows, cols]")
+        type_ = _type(grads, "grads")
+        rows, cols = grads.shape[-2:]
+        shape = tuple(grads.shape)
+        flat = grads.reshape(-1, rows, cols)
+        batch = flat.shape[0]
+        if cols > 1 and flat.stride(2) != 1 or rows > 1 and (flat.stride(1) < cols or flat.stride(1) >= 1 << 20) or flat.data_ptr() % 16 \
+                or batch > 1 and flat.stride(0) < (rows - 1) * flat.stride(1) + cols:
+            flat = flat.clone(memory_format=_contiguous())
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=flat.device)
+        elif tuple(out.shape) != shape or out.dtype != torch.bfloat16 or not out.is_contiguous() or out.data_ptr() % 16:
+            raise ValueError(f"out is {out.dtype} {tuple(out.shape)}: contiguous bfloat16 {shape} is wanted")
+        ld = flat.stride(1) if rows > 1 else cols
+        dims = _px.OrthoDims(batch, rows, cols, type_, steps, 0, *(float(c) for c in coefficients), ld, 0, flat.stride(0) if batch > 1 else 0, 0)
+        need = ctypes.c_size_t(0)
+        _check(_px.lib().pollux_ortho_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_ortho_workspace_size")
+        if workspace is None:
+            workspace = _scratch(need.value, flat.device)
+        _check(_px.lib().pollux_orthogonalize(ctypes.byref(dims), flat.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                              out.data_ptr(), _px._stream_handle(stream)), "pollux_orthogonalize")
+    return out

@@ -66,9 +66,72 @@ def test_loss_refusals():
     refused(L.pollux_token_loss_grad, d, backward, [(5, NULL), (5, ODD), (6, 16)], px.PX_E_WORKSPACE)
 
 
+def changed(make, changes):
+    return [(-1, None)] + [(-1, make(**c)) for c in changes]
+
+
+def of(cls, values):
+    def make(**changes):
+        d = cls(*values)
+        for k, v in changes.items():
+            setattr(d, k, v)
+        return d
+    return make
+
+
+embed_dims = of(px.EmbedDims, (64, 1000, 128, px.PX_TYPE_F32, px.PX_TYPE_BF16, 0, 1.0, 0, 0))
+noise_dims = of(px.NoiseDims, (1000, 4, px.PX_TYPE_BF16, px.PX_TYPE_F32, 0, 0, 8.0))
+ortho_dims = of(px.OrthoDims, (2, 100, 60, px.PX_TYPE_F32, 5, 0, 3.0, -4.0, 2.0, 0, 0, 0, 0))
+
+BAD_EMBED = [dict(N=-1), dict(N=(1 << 20) + 1), dict(V=0), dict(V=1 << 20), dict(D=0), dict(D=(1 << 16) + 1), dict(table_type=3), dict(rows_type=-1), dict(flags=4),
+             dict(scale=float("inf")), dict(scale=float("nan")), dict(table_stride=127), dict(rows_stride=1 << 20)]
+BAD_NOISE = [dict(n=-1), dict(n=1 << 40), dict(B=1), dict(B=0), dict(B=65537), dict(type=3), dict(mean_type=-1), dict(flags=1), dict(stride=999), dict(examples=0.0),
+             dict(examples=-1.0), dict(examples=float("nan")), dict(examples=float("inf"))]
+BAD_ORTHO = [dict(batch=-1), dict(batch=65536), dict(rows=0), dict(cols=0), dict(rows=(1 << 16) + 1), dict(rows=20000, cols=20000), dict(type=5), dict(steps=-1), dict(steps=65),
+             dict(flags=1), dict(a=float("nan")), dict(b=float("inf")), dict(c=-float("inf")), dict(grads_stride=59), dict(update_stride=59), dict(grads_batch_stride=5999),
+             dict(update_batch_stride=1)]
+
+
+@pytest.mark.parametrize("size,make,bad", [("pollux_embed_workspace_size", embed_dims, BAD_EMBED), ("pollux_noise_workspace_size", noise_dims, BAD_NOISE),
+                                           ("pollux_ortho_workspace_size", ortho_dims, BAD_ORTHO)])
+def test_workspaces(size, make, bad):
+    call, n = getattr(px.lib(), size), ctypes.c_size_t()
+    assert call(ctypes.byref(make()), ctypes.byref(n)) == px.PX_OK and n.value > 0
+    assert call(ctypes.byref(make()), None) == px.PX_E_INVALID_ARG
+    refused(call, make(), [ctypes.byref(n)], changed(make, bad), px.PX_E_INVALID_ARG)
+
+
+def test_lookup_refusals():
+    L = px.lib()
+    # tokens, table, rows, status, stream
+    refused(L.pollux_embed, embed_dims(), [FAKE, FAKE, FAKE, NULL, NULL], changed(embed_dims, BAD_EMBED) + [(0, NULL), (1, NULL), (2, NULL), (1, ODD), (2, ODD)],
+            px.PX_E_INVALID_ARG)
+    # tokens, rows_grad, workspace, bytes, table_grad, stream
+    backward = [FAKE, FAKE, FAKE, 1 << 40, FAKE, NULL]
+    refused(L.pollux_embed_grad, embed_dims(), backward, changed(embed_dims, BAD_EMBED) + [(0, NULL), (1, NULL), (4, NULL), (1, ODD), (4, ODD)], px.PX_E_INVALID_ARG)
+    refused(L.pollux_embed_grad, embed_dims(), backward, [(2, NULL), (2, ODD), (3, 16)], px.PX_E_WORKSPACE)
+
+
+def test_noise_scale_refusals():
+    # grads, precondition, workspace, bytes, mean, scale, stream
+    args = [FAKE, NULL, FAKE, 1 << 40, FAKE, FAKE, NULL]
+    refused(px.lib().pollux_noise_scale, noise_dims(), args, changed(noise_dims, BAD_NOISE) + [(0, NULL), (5, NULL), (0, ODD), (1, ODD), (4, ODD)], px.PX_E_INVALID_ARG)
+    refused(px.lib().pollux_noise_scale, noise_dims(), args, [(2, NULL), (2, ODD), (3, 0)], px.PX_E_WORKSPACE)
+
+
+def test_orthogonalize_refusals():
+    # grads, workspace, bytes, update, stream
+    args = [FAKE, FAKE, 1 << 40, FAKE, NULL]
+    refused(px.lib().pollux_orthogonalize, ortho_dims(), args, changed(ortho_dims, BAD_ORTHO) + [(0, NULL), (3, NULL), (0, ODD), (3, ODD)], px.PX_E_INVALID_ARG)
+    refused(px.lib().pollux_orthogonalize, ortho_dims(), args, [(1, NULL), (1, ODD), (2, 16)], px.PX_E_WORKSPACE)
+
+
 def test_tensors_that_are_not_on_a_gpu_are_refused():
     torch = pytest.importorskip("torch")
     if torch.cuda.is_available():
         pytest.skip("a GPU is there")
-    with pytest.raises((RuntimeError, ValueError, AssertionError)):
-        px.token_loss(torch.zeros((2, 8)), torch.zeros((4, 8)), torch.zeros(2, dtype=torch.int64))
+    tokens = torch.zeros(2, dtype=torch.int64)
+    for call in (lambda: px.token_loss(torch.zeros((2, 8)), torch.zeros((4, 8)), tokens), lambda: px.embed(tokens, torch.zeros((4, 8))),
+                 lambda: px.embed_grad(tokens, torch.zeros((2, 8)), 4), lambda: px.noise_scale(torch.zeros((2, 8)), 1.0), lambda: px.orthogonalize(torch.zeros((2, 8)))):
+        with pytest.raises((RuntimeError, ValueError, AssertionError)):
+            call()
