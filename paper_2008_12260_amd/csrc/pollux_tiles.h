@@ -131,9 +131,9 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
     typedef typename S::element::piece piece;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rows_a = min(o.rows_a - t.m * S::BM, S::BM), rows_b = min(o.rows_b - t.n * S::BN, S::BN);
-    // (rows - 1) * ld + k_bytes stays below 2^31: the launches check it.  A load beyond it gives zeros.
-    const auto from_a = __builtin_amdgcn_make_buffer_rsrc((void *)(o.a + (int64_t)t.m * S::BM * o.lda), 0, (int)((rows_a - 1) * o.lda) + o.k_bytes, 0x00027000);
-    const auto from_b = __builtin_amdgcn_make_buffer_rsrc((void *)(o.b + (int64_t)t.n * S::BN * o.ldb), 0, (int)((rows_b - 1) * o.ldb) + o.k_bytes, 0x00027000);
+    // (rows - 1) * ld + k_bytes stays below 2^31: the entry points' limits see to it.  A load beyond the buffer gives zeros.
+    const char *const base_a = o.a + (int64_t)t.m * S::BM * o.lda, *const base_b = o.b + (int64_t)t.n * S::BN * o.ldb;
+    const int bytes_a = (int)((rows_a - 1) * o.lda) + o.k_bytes, bytes_b = (int)((rows_b - 1) * o.ldb) + o.k_bytes;
     const int piece_at = ((lane & 7) ^ (lane >> 3)) * 16;
     int at_a[S::kLoadsA], at_b[S::kLoadsB];
 #pragma unroll
@@ -141,47 +141,93 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
 #pragma unroll
     for (int i = 0; i < S::kLoadsB; ++i) at_b[i] = min((i * (S::kThreads / 64) + wave) * 8 + (lane >> 3), rows_b - 1) * (int)o.ldb + piece_at;
 
-    auto load = [&](int stage, int k) {
-        char *to = lds + stage * S::kStage + wave * 1024;
-        // pieces beyond a row's end (in its last stage) are taken from beyond the buffer
-        const int off = k + piece_at < o.k_bytes ? 0 : (int)0x80000000;
+    const int stages = (o.k_bytes + kRowBytes - 1) / kRowBytes, part = o.k_bytes % kRowBytes ? stages - 1 : -1;
+    // Stages past the end are asked for like any other, from a buffer of no bytes: zeros, and no traffic.  Of a last stage that is
+    // not whole, a row's pieces beyond its end are taken from beyond the buffer.
+    auto load = [&](int stage) {
+        const int k = stage * kRowBytes;
+        char *to = lds + (stage & 1) * S::kStage + wave * 1024;
+        if (stage == part) {
+            const int off = k + piece_at < o.k_bytes ? 0 : (int)0x80000000;
+#pragma unroll
+            for (int i = 0; i < S::kLoadsA; ++i) at_a[i] |= off;
+#pragma unroll
+            for (int i = 0; i < S::kLoadsB; ++i) at_b[i] |= off;
+        }
+        const auto from_a = __builtin_amdgcn_make_buffer_rsrc((void *)base_a, 0, stage < stages ? bytes_a : 0, 0x00027000);
+        const auto from_b = __builtin_amdgcn_make_buffer_rsrc((void *)base_b, 0, stage < stages ? bytes_b : 0, 0x00027000);
 #pragma unroll
         for (int i = 0; i < S::kLoadsA; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_a, (lds_void *)(to + i * S::kThreads * 16), 16, at_a[i] | off, k, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_a, (lds_void *)(to + i * S::kThreads * 16), 16, at_a[i], k, 0, 0);
 #pragma unroll
         for (int i = 0; i < S::kLoadsB; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_b, (lds_void *)(to + S::BM * kRowBytes + i * S::kThreads * 16), 16, at_b[i] | off, k, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_b, (lds_void *)(to + S::BM * kRowBytes + i * S::kThreads * 16), 16, at_b[i], k, 0, 0);
+    };
+    const int row_a = (wave / S::WN * S::TM + (lane & 15)) * kRowBytes, row_b = (S::BM + wave % S::WN * S::TN + (lane & 15)) * kRowBytes;
+    const int piece_of = ((lane >> 4) ^ (lane & 7)) * 16;
+    auto read = [&](int stage, int half, piece (&a)[S::FM], piece (&b)[S::FN]) {
+        const char *from = lds + (stage & 1) * S::kStage + (piece_of ^ (half * 64));
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) b[j] = *(const piece *)(from + row_b + j * 16 * kRowBytes);
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) a[i] = *(const piece *)(from + row_a + i * 16 * kRowBytes);
+    };
+    auto multiply_all = [&](const piece (&a)[S::FM], const piece (&b)[S::FN]) {
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) acc[i][j] = multiply(a[i], b[j], acc[i][j]);
+    };
+    auto wait_for_all = [] {
+        // this wavefront's loads have arrived and what it read is in registers; after the barrier, everybody's
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
 
 #pragma unroll
     for (int i = 0; i < S::FM; ++i)
 #pragma unroll
         for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int row_a = (wave / S::WN * S::TM + (lane & 15)) * kRowBytes, row_b = (S::BM + wave % S::WN * S::TN + (lane & 15)) * kRowBytes;
-    const int piece_of = ((lane >> 4) ^ (lane & 7)) * 16;
-    const int stages = (o.k_bytes + kRowBytes - 1) / kRowBytes;
-    if (stages > 0) load(0, 0);
+    if (stages == 0) return;
+    // Half a stage ahead: while one half is multiplied, the other is on its way from LDS to registers; the barrier stands between the
+    // halves, when the whole stage has been read: the loads of the stage after next go where it was.
+    constexpr int kReads = S::FM + S::FN, kLoads = S::kLoadsA + S::kLoadsB, kProducts = S::FM * S::FN * (sizeof(typename S::element::type) == 4 ? 4 : 1);
+    constexpr int kPerRead = kProducts / (kReads + 4) > 0 ? kProducts / (kReads + 4) : 1, kPerLoad = kProducts / (kReads + 4) > 0 ? kProducts / (kReads + 4) : 1;
+    constexpr int kMatrix = 0x008, kVector = 0x010, kLds = 0x100;         // the scheduler's groups of instructions
+    piece a0[S::FM], b0[S::FN], a1[S::FM], b1[S::FN];
+    load(0);
+    wait_for_all();
+    load(1);
+    read(0, 0, a0, b0);
     for (int s = 0; s < stages; ++s) {
-        // this wavefront's loads have arrived and what it read of the stage before is in registers; after the barrier, everybody's
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        const char *from = lds + (s & 1) * S::kStage;
-        if (s + 1 < stages) load((s + 1) & 1, (s + 1) * kRowBytes);
+        read(s, 1, a1, b1);
+        multiply_all(a0, b0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            piece a[S::FM], b[S::FN];
-#pragma unroll
-            for (int j = 0; j < S::FN; ++j) b[j] = *(const piece *)(from + row_b + j * 16 * kRowBytes + (piece_of ^ (h * 64)));
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i) a[i] = *(const piece *)(from + row_a + i * 16 * kRowBytes + (piece_of ^ (h * 64)));
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FN; ++j) acc[i][j] = multiply(a[i], b[j], acc[i][j]);
+        for (int i = 0; i < kReads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kLds, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kMatrix, kPerRead, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(kMatrix, kProducts, 0);
+        wait_for_all();
+        load(s + 2);
+        read(s + 1, 0, a0, b0);
+        multiply_all(a1, b1);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kVector, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(kMatrix, kPerLoad, 1);
+        }
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kLds, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMatrix, kProducts, 1);
     }
+    // the loads of stages past the end write zeros: nobody else's data may be there before they have
+    wait_for_all();
 }
 
 // Four values in the lane's own row n, as stored: contiguous in m.
