@@ -6,9 +6,8 @@
 //
 // Forward: a tile of logits is reduced, as it leaves the matrix units, to each token's largest logit and sum of exponentials
 // over the tile's entries (loss_tiles); a second launch joins a token's tiles (loss_join).
-// Backward: for each piece of the vocabulary the logits are formed again, q of the piece is written once as [token, entry] and
-// once as [entry, token] (q_tiles), and both gradients are products of it (grad_tiles) with transposed copies of the hidden rows
-// and of the piece's weights: every product then has its k contiguous, and all share one kernel core.  The hidden rows'
+// Backward: for each piece of the vocabulary the logits are formed again, q of the piece is written once (q_tiles), and both
+// gradients are products with it (grad_tiles): of the hidden rows' the weights lie as columns, of the weights' both operands.  The hidden rows'
 // gradient is summed over pieces in fp32 (and over slices of a piece where few tiles would leave the chip idle), in a
 // fixed order, and rounded once (join_slices).
 //
@@ -51,8 +50,8 @@ struct LogitArgs {
     int32_t *status;            // cleared by the first workgroup; null in all but the first piece
     // backward
     const float *lse, *row_weight, *scale;
-    void *q, *qt;
-    int64_t ld_q, ld_qt;        // elements
+    void *q;
+    int64_t ld_q;               // elements
     int rows;                   // entries of the piece
 };
 
@@ -69,7 +68,7 @@ __global__ __launch_bounds__(S::kThreads) void loss_tiles(const LogitArgs A)
     f32x4 acc[S::FM][S::FN];
     tile_product<S>(A.o, t, lds, acc);
     const Place<S> at(t);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, left = A.o.rows_a;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, left = A.o.m;
     float2 *const shared = (float2 *)lds;        // [WM][BN]
     __syncthreads();
 #pragma unroll
@@ -192,7 +191,7 @@ __global__ __launch_bounds__(1024) void grad_begin(const void *targets, bool i64
     }
 }
 
-// One tile of q from the logits' tile, written both ways.  A token without a target, or of weight 0, has a row of zeros,
+// One tile of q from the logits' tile.  A token without a target, or of weight 0, has a row of zeros,
 // whatever its logits are.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void q_tiles(const LogitArgs A)
@@ -222,9 +221,6 @@ __global__ __launch_bounds__(S::kThreads) void q_tiles(const LogitArgs A)
                 q[r] = g != 0.f && v + r < A.rows ? p * g : 0.f;
             }
             if (n < A.N && v < A.ld_q) store4<typename S::element>((type *)A.q + (int64_t)n * A.ld_q + v, q);
-            const f32x4 qt = turned(q);
-            const int row = v + (threadIdx.x & 3), col = n & ~3;
-            if (row < A.rows && col < A.ld_qt) store4<typename S::element>((type *)A.qt + (int64_t)row * A.ld_qt + col, qt);
         }
     }
 #endif
@@ -233,7 +229,7 @@ __global__ __launch_bounds__(S::kThreads) void q_tiles(const LogitArgs A)
 struct GradArgs {
     Operands o;
     int tiles_m, tiles_n, group;
-    int slice_k;                // bytes of k a slice (blockIdx.y) takes
+    int slice_k;                // k that a slice (blockIdx.y) takes
     int cols, rows;             // m and n
     void *out;                  // [rows, ld]: the gradient, or fp32 sums [slices, rows, cols]
     int64_t ld;                 // elements
@@ -272,9 +268,9 @@ __global__ __launch_bounds__(S::kThreads) void grad_tiles(const GradArgs A)
     const Tile t = tile_of(blockIdx.x, A.tiles_m, A.tiles_n, A.group);
     Operands o = A.o;
     const int k0 = blockIdx.y * A.slice_k;
-    o.a += k0;
-    o.b += k0;
-    o.k_bytes = max(0, min(A.slice_k, A.o.k_bytes - k0));
+    o.a += S::COLS_A ? k0 * o.lda : k0 * (int64_t)sizeof(type);
+    o.b += S::COLS_B ? k0 * o.ldb : k0 * (int64_t)sizeof(type);
+    o.k = max(0, min(A.slice_k, A.o.k - k0));
     f32x4 acc[S::FM][S::FN];
     tile_product<S>(o, t, lds, acc);
     const Place<S> at(t);
@@ -317,35 +313,28 @@ __global__ __launch_bounds__(256) void join_slices(const float *sums, int slices
     }
 }
 
-// Rows copied to aligned ones, `cols` padded with zeros to ld_to.
+// Rows copied to aligned ones, `cols` padded with zeros to ld_to; rows without a target, or of weight 0, are copied as zeros.  Eight
+// bytes at a time where rows allow it.
 template <class E>
-__global__ __launch_bounds__(256) void pack_rows(const E *from, int64_t ld_from, int64_t rows, int cols, E *to, int64_t ld_to)
+__global__ __launch_bounds__(256) void pack_rows(const E *from, int64_t ld_from, int64_t rows, int cols, E *to, int64_t ld_to, const void *targets, const float *row_weight,
+                                                 bool i64, int V)
 {
-    const int64_t total = rows * ld_to;
+    constexpr int kVec = 16 / sizeof(E);
+    struct Vec {
+        E v[kVec];
+    };
+    const int groups = (int)(ld_to / kVec);
+    const int64_t total = rows * groups;
     for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
-        const int64_t n = at / ld_to;
-        const int c = (int)(at - n * ld_to);
-        to[at] = c < cols ? from[n * ld_from + c] : E(0);
-    }
-}
-
-// to[c, n] = from[n, c], n padded with zeros to ld_to; rows without a target, or of weight 0, count as zeros.
-template <class E>
-__global__ __launch_bounds__(256) void transpose_rows(const E *from, int64_t ld_from, int rows, int cols, E *to, int64_t ld_to,
-                                                      const void *targets, const float *row_weight, bool i64, int V)
-{
-    __shared__ E tile[64][65];
-    const int n0 = blockIdx.x * 64, c0 = blockIdx.y * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    for (int i = y; i < 64; i += 4) {
-        const int n = n0 + i, c = c0 + x;
-        bool there = n < rows && c < cols;
-        if (there && targets) there = target_of(targets, n, i64, V) >= 0 && !(row_weight && row_weight[n] == 0.f);
-        tile[i][x] = there ? from[(int64_t)n * ld_from + c] : E(0);
-    }
-    __syncthreads();
-    for (int i = y; i < 64; i += 4) {
-        const int c = c0 + i, n = n0 + x;
-        if (c < cols && n < ld_to) to[(int64_t)c * ld_to + n] = tile[x][i];
+        const int64_t n = at / groups;
+        const int c = (int)(at - n * groups) * kVec;
+        const bool there = !targets || (target_of(targets, n, i64, V) >= 0 && !(row_weight && row_weight[n] == 0.f));
+        Vec t;
+        if (there && c + kVec <= cols) __builtin_memcpy(&t, from + n * ld_from + c, sizeof(t));
+        else
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) t.v[i] = there && c + i < cols ? from[n * ld_from + c + i] : E(0.f);
+        *(Vec *)(to + n * ld_to + c) = t;
     }
 }
 
@@ -355,7 +344,7 @@ enum LogitKind { kLoss, kQ };
 template <class S>
 void launch_logits(LogitKind kind, LogitArgs a, hipStream_t stream)
 {
-    a.tiles_m = (a.o.rows_a + S::BM - 1) / S::BM;
+    a.tiles_m = (a.o.m + S::BM - 1) / S::BM;
     a.tiles_n = (a.N + S::BN - 1) / S::BN;
     a.group = 8;
     const dim3 grid((unsigned)(a.tiles_m * a.tiles_n));
@@ -380,14 +369,15 @@ void launch_grad(GradArgs a, int slices, hipStream_t stream)
     a.group = 8;
     hipLaunchKernelGGL(grad_tiles<S>, dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)slices), dim3(S::kThreads), S::kLds, stream, a);
 }
-template <class T>
+// (the hidden rows': the weights as columns; the weights': both operands)
+template <class T, bool COLS_B>
 void launch_grad(int shape, const GradArgs &a, int slices, hipStream_t stream)
 {
     switch (shape) {
-        case 0: launch_grad<Shape0<T>>(a, slices, stream); break;
-        case 1: launch_grad<Shape1<T>>(a, slices, stream); break;
-        case 2: launch_grad<Shape2<T>>(a, slices, stream); break;
-        default: launch_grad<Shape3<T>>(a, slices, stream); break;
+        case 0: launch_grad<Shape0<T, true, COLS_B>>(a, slices, stream); break;
+        case 1: launch_grad<Shape1<T, true, COLS_B>>(a, slices, stream); break;
+        case 2: launch_grad<Shape2<T, true, COLS_B>>(a, slices, stream); break;
+        default: launch_grad<Shape3<T, true, COLS_B>>(a, slices, stream); break;
     }
 }
 
@@ -407,7 +397,7 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
         return status_of(hipGetLastError());
     }
     if (p.pack_hidden) {
-        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * p.d_pad)), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad);
+        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * p.d_pad / (16 / e))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
         hidden = ws + p.hidden;
     }
     LogitArgs a = {};
@@ -418,16 +408,16 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
     a.picked = (float *)(ws + p.picked);
     a.o.b = hidden;
     a.o.ldb = ld_h * e;
-    a.o.rows_b = N;
+    a.o.n = N;
     a.o.lda = ld_w * e;
-    a.o.k_bytes = (int)(p.d_pad * e);      // (where D is padded, both operands are packed)
+    a.o.k = (int)p.d_pad;                  // (where D is padded, both operands are packed)
     int tiles = 0;
     for (int k = 0; k < p.pieces; ++k) {
         a.first = k * p.piece;
-        a.rows = a.o.rows_a = std::min(p.piece, d.V - a.first);
+        a.rows = a.o.m = std::min(p.piece, d.V - a.first);
         const char *from = weight + (int64_t)a.first * d.weight_stride * e;
         if (p.pack_weight) {
-            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * p.d_pad)), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad);
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * p.d_pad / (16 / e))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
             from = ws + p.weight;
         }
         a.o.a = from;
@@ -456,24 +446,17 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
     if (N == 0) {
         if (weight_grad && !(d.flags & PX_FLAG_ACCUMULATE)) {      // products over no tokens
             GradArgs g = {};
-            g.o.rows_a = g.cols = d.D;
-            g.o.rows_b = g.rows = d.V;
+            g.o.m = g.cols = d.D;
+            g.o.n = g.rows = d.V;
             g.out = weight_grad;
             g.ld = d.weight_grad_stride;
-            launch_grad<T>(0, g, 1, stream);
+            launch_grad<T, true>(0, g, 1, stream);
         }
         return status_of(hipGetLastError());
     }
-    if (weight_grad)
-        hipLaunchKernelGGL(transpose_rows<type>, dim3((unsigned)((p.n_pad + 63) / 64), (d.D + 63) / 64), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, N, d.D,
-                           (type *)(ws + p.ht), p.n_pad, targets, row_weight, i64, d.V);
-    const char *logit_hidden = hidden;
-    int64_t ld_h = d.hidden_stride;
-    if (p.pack_hidden) {
-        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * p.d_pad)), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad);
-        logit_hidden = ws + p.hidden;
-        ld_h = p.d_pad;
-    }
+    // (a product with q's zeros would still be NaN where a row that counts for nothing holds one)
+    hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * p.d_pad / (16 / e))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D,
+                       (type *)(ws + p.hidden), p.d_pad, targets, row_weight, i64, d.V);
     LogitArgs a = {};
     a.targets = targets;
     a.i64 = i64;
@@ -483,35 +466,29 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
     a.row_weight = row_weight;
     a.scale = scale;
     a.q = ws + p.q;
-    a.qt = ws + p.qt;
     a.ld_q = p.v_pad;
-    a.ld_qt = p.n_pad;
-    a.o.b = logit_hidden;
-    a.o.ldb = ld_h * e;
-    a.o.rows_b = N;
+    a.o.b = ws + p.hidden;
+    a.o.ldb = p.d_pad * e;
+    a.o.n = N;
     a.o.lda = (p.pack_weight ? p.d_pad : d.weight_stride) * e;
-    a.o.k_bytes = (int)(p.d_pad * e);      // (where D is padded, both operands are packed)
+    a.o.k = (int)p.d_pad;                  // (where D is padded, both operands are packed)
     for (int k = 0; k < p.pieces; ++k) {
         a.first = k * p.piece;
-        a.rows = a.o.rows_a = std::min(p.piece, d.V - a.first);
-        const char *piece = weight + (int64_t)a.first * d.weight_stride * e, *from = piece;
+        a.rows = a.o.m = std::min(p.piece, d.V - a.first);
+        const char *from = weight + (int64_t)a.first * d.weight_stride * e;
         if (p.pack_weight) {
-            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * p.d_pad)), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad);
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * p.d_pad / (16 / e))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
             from = ws + p.weight;
         }
         a.o.a = from;
-        const int64_t pad = 16 / e, v_pad = (a.rows + pad - 1) / pad * pad;      // of this piece
-        a.ld_q = v_pad;
         launch_logits<T>(p.tiles, kQ, a, stream);
         if (hidden_grad) {
-            hipLaunchKernelGGL(transpose_rows<type>, dim3((unsigned)((v_pad + 63) / 64), (d.D + 63) / 64), dim3(256), 0, stream, (const type *)piece, d.weight_stride, a.rows, d.D,
-                               (type *)(ws + p.wt), v_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
             GradArgs g = {};
-            g.o = {ws + p.wt, ws + p.q, v_pad * e, v_pad * e, d.D, N, (int)(v_pad * e)};
+            g.o = {from, ws + p.q, a.o.lda, p.v_pad * e, d.D, N, a.rows};
             g.cols = d.D;
             g.rows = N;
-            const int stages = (int)((v_pad * e + kRowBytes - 1) / kRowBytes);
-            g.slice_k = (stages + p.slices - 1) / p.slices * kRowBytes;
+            const int depth = kRowBytes / e, stages = (a.rows + depth - 1) / depth;
+            g.slice_k = (stages + p.slices - 1) / p.slices * depth;
             g.scale = scale;
             g.targets = targets;
             g.row_weight = row_weight;
@@ -520,19 +497,19 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
             g.sums = p.slices == 1 && p.pieces == 1 ? 0 : k == 0 ? 1 : 2;
             g.out = g.sums ? (void *)(ws + p.sums) : (void *)hidden_grad;
             g.ld = d.hidden_grad_stride;
-            launch_grad<T>(p.grad_tiles, g, p.slices, stream);
+            launch_grad<T, false>(p.grad_tiles, g, p.slices, stream);
         }
         if (weight_grad) {
             GradArgs g = {};
-            g.o = {ws + p.ht, ws + p.qt, p.n_pad * e, p.n_pad * e, d.D, a.rows, (int)(p.n_pad * e)};
+            g.o = {ws + p.hidden, ws + p.q, p.d_pad * e, p.v_pad * e, d.D, a.rows, N};
             g.cols = d.D;
             g.rows = a.rows;
-            g.slice_k = (int)((p.n_pad * e + kRowBytes - 1) / kRowBytes) * kRowBytes;
+            g.slice_k = N;
             g.scale = scale;
             g.out = weight_grad + (int64_t)a.first * d.weight_grad_stride * e;
             g.ld = d.weight_grad_stride;
             g.add = d.flags & PX_FLAG_ACCUMULATE;
-            launch_grad<T>(shape_for(d.D, a.rows, 1, e == 4), g, 1, stream);
+            launch_grad<T, true>(shape_for(d.D, a.rows, 1, e == 4), g, 1, stream);
         }
     }
     if (hidden_grad && (p.slices > 1 || p.pieces > 1))
@@ -551,20 +528,20 @@ LossPlan loss_plan(const pollux_loss_dims &d, bool grad)
     auto padded = [&](int64_t x) { return (x + pad - 1) / pad * pad; };
     p.grad = grad;
     p.d_pad = padded(d.D);
-    p.n_pad = padded(N);
     p.pack_hidden = d.hidden_stride % pad != 0 || d.D % pad != 0;
     p.pack_weight = d.weight_stride % pad != 0 || d.D % pad != 0;
-    // A piece's q and its transpose, and its transposed or packed weights, are held to 512 and 256 MiB: pieces that large keep the
-    // matrix kernels' ends and the sums' passes over memory to a few per cent.
+    // A piece's q is held to 512 MiB, packed weights to 256: pieces that large keep the matrix kernels' ends and the sums' passes over
+    // memory to a few per cent.
     int64_t piece = (d.V + 255) / 256 * 256;
     if (grad) piece = std::min(piece, std::max<int64_t>(256, ((512ll << 20) / (std::max<int64_t>(N, 1) * e)) / 256 * 256));
-    if (grad || p.pack_weight) piece = std::min(piece, std::max<int64_t>(256, ((256ll << 20) / (p.d_pad * e)) / 256 * 256));
+    if (p.pack_weight) piece = std::min(piece, std::max<int64_t>(256, ((256ll << 20) / (p.d_pad * e)) / 256 * 256));
     p.pieces = (int)((d.V + piece - 1) / piece);
     // (even shares)
     piece = ((d.V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
     p.piece = (int)piece;
     p.pieces = (int)((d.V + piece - 1) / piece);
-    p.v_pad = padded(std::min<int64_t>(piece, d.V));
+    // (rows of q a stage longer than a power of two: those of one tile then begin in different channels of memory)
+    p.v_pad = padded(std::min<int64_t>(piece, d.V)) + kRowBytes / e;
     p.tiles = shape_for(std::min<int64_t>(piece, d.V), N, 1, f32);
     p.slices = 1;
     if (grad) {
@@ -588,13 +565,10 @@ LossPlan loss_plan(const pollux_loss_dims &d, bool grad)
         p.parts = take(8 * tiles * (size_t)N);
         p.picked = take(4 * (size_t)N);
     }
-    if (p.pack_hidden) p.hidden = take((size_t)N * p.d_pad * e);
+    if (grad || p.pack_hidden) p.hidden = take((size_t)N * p.d_pad * e);
     if (p.pack_weight) p.weight = take((size_t)piece * p.d_pad * e);
     if (grad) {
         p.q = take((size_t)N * p.v_pad * e);
-        p.qt = take((size_t)p.v_pad * p.n_pad * e);
-        p.ht = take((size_t)d.D * p.n_pad * e);
-        p.wt = take((size_t)d.D * p.v_pad * e);
         if (p.slices > 1 || p.pieces > 1) p.sums = take((size_t)p.slices * N * d.D * 4);
     }
     p.total = o;

@@ -1,9 +1,8 @@
 // Orthogonalised updates: X = G / |G|_F, then `steps` times  A = X X',  B = b A + c A^2,  X <- a X + B X.
 //
-// All three products are of the matrix kernels' form (k contiguous in both operands) when X is held both as it is and
-// transposed: A[i,j] = <X_i, X_j>; A^2 and B X use that A and B are symmetric, so that a row is a column.  The product that
-// forms the next X writes both layouts, the second through turned 4 x 4 blocks.  Three launches a step, for all matrices of the
-// batch together.
+// X is held as the gradients lie.  Of at most as many rows as columns: A = X X' takes rows, and B X the columns of X; of more rows
+// than columns (the formula on the transposes): A = X' X takes columns, and X B the rows.  A^2, A and B are symmetric, so that a row is
+// a column.  Three launches a step, for all matrices of the batch together.
 //
 // X is held in fp16, times a power of two near the root of its longer side, so that its elements lie well within fp16's range
 // whatever the matrix's shape: an element's rounding is then 2^-11 of it, a quarter of what bfloat16 would leave, and the
@@ -40,14 +39,12 @@ __global__ __launch_bounds__(kThreads) void square_sums(const E *grads, int rows
     if (threadIdx.x == 0) sums[blockIdx.y * gridDim.x + blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
 }
 
-// X and its transpose from the gradients (tall: of their transposes), 64 x 64 at a time, rows padded with zeros.
+// X from the gradients, rows padded with zeros.
 template <class E>
-__global__ __launch_bounds__(kThreads) void normalise(const E *grads, int rows, int cols, int64_t ld, int64_t ld_batch, const double *sums, int parts, double unit, _Float16 *as_is,
-                                                      int64_t ld_as, _Float16 *turned_to, int64_t ld_turned)
+__global__ __launch_bounds__(kThreads) void normalise(const E *grads, int rows, int cols, int64_t ld, int64_t ld_batch, const double *sums, int parts, double unit, _Float16 *x, int64_t ld_x)
 {
-    __shared__ float tile[64][65];
     __shared__ double waves[kThreads / 64];
-    const int64_t batch = blockIdx.z;
+    const int64_t batch = blockIdx.y;
     double sum = 0.0;
     for (int i = threadIdx.x; i < parts; i += kThreads) sum += sums[batch * parts + i];
 #pragma unroll
@@ -56,18 +53,23 @@ __global__ __launch_bounds__(kThreads) void normalise(const E *grads, int rows, 
     __syncthreads();
     sum = waves[0] + waves[1] + waves[2] + waves[3];
     const double by = sum == 0.0 ? 0.0 : unit / sqrt(sum);
-    const E *g = grads + batch * ld_batch;
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    for (int i = y; i < 64; i += 4) {
-        const int r = r0 + i, c = c0 + x;
-        const float v = r < rows && c < cols ? (float)((double)(float)g[r * ld + c] * by) : 0.f;
-        tile[i][x] = v;
-        if (r < rows && c < ld_as) as_is[(batch * rows + r) * ld_as + c] = (_Float16)v;
-    }
-    __syncthreads();
-    for (int i = y; i < 64; i += 4) {
-        const int c = c0 + i, r = r0 + x;
-        if (c < cols && r < ld_turned) turned_to[(batch * cols + c) * ld_turned + r] = (_Float16)tile[x][i];
+    const int groups = (int)(ld_x / 8);
+    const int64_t total = (int64_t)rows * groups;
+    for (int64_t at = blockIdx.x * (int64_t)kThreads + threadIdx.x; at < total; at += gridDim.x * (int64_t)kThreads) {
+        const int64_t r = at / groups;
+        const int c = (int)(at - r * groups) * 8;
+        const E *from = grads + batch * ld_batch + r * ld + c;
+        struct {
+            E v[8];
+        } g;
+        if (c + 8 <= cols) __builtin_memcpy(&g, from, sizeof(g));
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g.v[i] = c + i < cols ? from[i] : E(0.f);
+        f16x8 h;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = (_Float16)(float)((double)(float)g.v[i] * by);
+        *(f16x8 *)(x + (batch * rows + r) * ld_x + c) = h;
     }
 }
 
@@ -80,13 +82,12 @@ struct StepArgs {
     float plus;                         // of `base`
     const _Float16 *base;               // [rows, ld]: added; null: nothing
     _Float16 *out;                      // [rows, ld]
-    _Float16 *out_turned;               // [cols, ld_turned], or null
-    int64_t ld, ld_turned;              // elements, padded
+    int64_t ld;                         // elements, padded
     __bf16 *last;                       // the update itself in place of `out`: [rows, ld_last]
     int64_t ld_last, batch_last;
 };
 
-// out = plus base + by (product), and its transpose; or the update.
+// out = plus base + by (product); or the update.
 template <class S>
 __global__ __launch_bounds__(S::kThreads) void step_tiles(const StepArgs A)
 {
@@ -124,11 +125,6 @@ __global__ __launch_bounds__(S::kThreads) void step_tiles(const StepArgs A)
             for (int r = 0; r < 4; ++r)
                 if (m + r >= A.cols || n >= A.rows) v[r] = 0.f;
             if (inside) store4<F16>(A.out + here, v);
-            if (A.out_turned) {
-                const f32x4 w = turned(v);
-                const int row = m + (threadIdx.x & 3), col = n & ~3;
-                if (row < A.cols && col < A.ld_turned) store4<F16>(A.out_turned + (batch * A.cols + row) * A.ld_turned + col, w);
-            }
         }
     }
 #endif
@@ -142,12 +138,13 @@ void launch_step(StepArgs a, int batch, hipStream_t stream)
     a.group = 8;
     hipLaunchKernelGGL(step_tiles<S>, dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)batch), dim3(S::kThreads), S::kLds, stream, a);
 }
+template <bool COLS_A, bool COLS_B>
 void launch_step(int shape, const StepArgs &a, int batch, hipStream_t stream)
 {
     switch (shape) {
-        case 0: launch_step<Shape0<F16>>(a, batch, stream); break;
-        case 1: launch_step<Shape1<F16>>(a, batch, stream); break;
-        default: launch_step<Shape2<F16>>(a, batch, stream); break;
+        case 0: launch_step<Shape0<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        case 1: launch_step<Shape1<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        default: launch_step<Shape2<F16, COLS_A, COLS_B>>(a, batch, stream); break;
     }
 }
 
@@ -175,63 +172,57 @@ int orthogonalize(const pollux_ortho_dims &d, const OrthoPlan &p, const E *grads
                            grads, d.rows, d.cols, d.grads_stride, d.grads_batch_stride, (const double *)norms, p.norm_blocks, update, d.update_stride, d.update_batch_stride);
         return status_of(hipGetLastError());
     }
-    _Float16 *x[2] = {(_Float16 *)(ws + p.x[0]), (_Float16 *)(ws + p.x[1])}, *xt[2] = {(_Float16 *)(ws + p.xt[0]), (_Float16 *)(ws + p.xt[1])};
-    _Float16 *gram = (_Float16 *)(ws + p.gram), *poly = (_Float16 *)(ws + p.poly);
-    // X is [m, n]: the gradients as they are, or, of more rows than columns, transposed
-    const int64_t pad_as = p.tall ? p.m_pad : p.n_pad, pad_turned = p.tall ? p.n_pad : p.m_pad;
-    hipLaunchKernelGGL(normalise<E>, dim3((unsigned)((pad_as + 63) / 64), (unsigned)((pad_turned + 63) / 64), (unsigned)d.batch), dim3(kThreads), 0, stream, grads, d.rows, d.cols,
-                       d.grads_stride, d.grads_batch_stride, (const double *)norms, p.norm_blocks, p.unit, p.tall ? xt[0] : x[0], pad_as, p.tall ? x[0] : xt[0], pad_turned);
+    _Float16 *x[2] = {(_Float16 *)(ws + p.x[0]), (_Float16 *)(ws + p.x[1])}, *gram = (_Float16 *)(ws + p.gram), *poly = (_Float16 *)(ws + p.poly);
+    const unsigned blocks = (unsigned)std::min<int64_t>(std::max<int64_t>(2048 / d.batch, 16), ((int64_t)d.rows * (p.x_pad / 8) + kThreads - 1) / kThreads);
+    hipLaunchKernelGGL(normalise<E>, dim3(blocks, (unsigned)d.batch), dim3(kThreads), 0, stream, grads, d.rows, d.cols, d.grads_stride, d.grads_batch_stride, (const double *)norms,
+                       p.norm_blocks, p.unit, x[0], p.x_pad);
+    const int64_t ld_x = p.x_pad * 2, ld_m = p.m_pad * 2, batch_x = d.rows * ld_x, batch_m = p.m * ld_m;      // bytes
     for (int s = 0; s < d.steps; ++s) {
-        const _Float16 *from = x[s & 1], *from_t = xt[s & 1];
+        const char *from = (const char *)x[s & 1];
         StepArgs a = {};
         // gram = X X'
-        a.o = {(const char *)from, (const char *)from, p.n_pad * 2, p.n_pad * 2, p.m, p.m, (int)p.n_pad * 2};
-        a.batch_a = a.batch_b = p.m * p.n_pad * 2;
+        a.o = {from, from, ld_x, ld_x, p.m, p.m, p.n};
+        a.batch_a = a.batch_b = batch_x;
         a.cols = a.rows = p.m;
         a.by = (float)(1.0 / (p.unit * p.unit));
         a.out = gram;
         a.ld = p.m_pad;
-        launch_step(p.shape_square, a, d.batch, stream);
+        if (p.tall) launch_step<true, true>(p.shape_square, a, d.batch, stream);
+        else launch_step<false, false>(p.shape_square, a, d.batch, stream);
         // poly = b gram + c gram gram
-        a.o = {(const char *)gram, (const char *)gram, p.m_pad * 2, p.m_pad * 2, p.m, p.m, (int)p.m_pad * 2};
-        a.batch_a = a.batch_b = p.m * p.m_pad * 2;
+        a.o = {(const char *)gram, (const char *)gram, ld_m, ld_m, p.m, p.m, p.m};
+        a.batch_a = a.batch_b = batch_m;
         a.by = (float)d.c;
         a.plus = (float)d.b;
         a.base = gram;
         a.out = poly;
-        launch_step(p.shape_square, a, d.batch, stream);
-        // X = a X + poly X; the last one as the update, in the gradients' own layout
-        const bool last = s + 1 == d.steps;
+        launch_step<false, false>(p.shape_square, a, d.batch, stream);
+        // X = a X + poly X (tall: + X poly); the last one as the update
         a.by = 1.f;
         a.plus = (float)d.a;
-        if (last) {
+        a.base = x[s & 1];
+        a.out = x[(s + 1) & 1];
+        a.ld = p.x_pad;
+        a.cols = d.cols;
+        a.rows = d.rows;
+        if (s + 1 == d.steps) {
             a.by /= (float)p.unit;
             a.plus /= (float)p.unit;
             a.last = update;
             a.ld_last = d.update_stride;
             a.batch_last = d.update_batch_stride;
         }
-        if (last && p.tall) {                   // X' [n, m] = a X' + X' poly
-            a.o = {(const char *)poly, (const char *)from_t, p.m_pad * 2, p.m_pad * 2, p.m, p.n, (int)p.m_pad * 2};
-            a.batch_a = p.m * p.m_pad * 2;
-            a.batch_b = p.n * p.m_pad * 2;
-            a.cols = p.m;
-            a.rows = p.n;
-            a.base = from_t;
-            a.ld = p.m_pad;
+        if (p.tall) {
+            a.o = {(const char *)poly, from, ld_m, ld_x, d.cols, d.rows, p.m};
+            a.batch_a = batch_m;
+            a.batch_b = batch_x;
+            launch_step<false, false>(p.shape_wide, a, d.batch, stream);
         } else {
-            a.o = {(const char *)from_t, (const char *)poly, p.m_pad * 2, p.m_pad * 2, p.n, p.m, (int)p.m_pad * 2};
-            a.batch_a = p.n * p.m_pad * 2;
-            a.batch_b = p.m * p.m_pad * 2;
-            a.cols = p.n;
-            a.rows = p.m;
-            a.base = from;
-            a.out = x[(s + 1) & 1];
-            a.ld = p.n_pad;
-            a.out_turned = xt[(s + 1) & 1];
-            a.ld_turned = p.m_pad;
+            a.o = {from, (const char *)poly, ld_x, ld_m, d.cols, d.rows, p.m};
+            a.batch_a = batch_x;
+            a.batch_b = batch_m;
+            launch_step<true, false>(p.shape_wide, a, d.batch, stream);
         }
-        launch_step(p.shape_wide, a, d.batch, stream);
     }
     return status_of(hipGetLastError());
 }
@@ -245,19 +236,16 @@ OrthoPlan ortho_plan(const pollux_ortho_dims &d)
     p.m = std::min(d.rows, d.cols);
     p.n = std::max(d.rows, d.cols);
     p.m_pad = (p.m + 7) / 8 * 8;
-    p.n_pad = (p.n + 7) / 8 * 8;
+    p.x_pad = (d.cols + 7) / 8 * 8;
     p.unit = ldexp(1.0, (int)lround(0.5 * log2((double)p.n)));
     p.norm_blocks = (int)std::min<int64_t>(d.rows, std::max<int64_t>(1, std::min<int64_t>(1024 / std::max(d.batch, 1) + 1, (int64_t)d.rows * d.cols / 4096)));
     p.shape_square = std::min(2, shape_for(p.m, p.m, d.batch, false));
-    p.shape_wide = std::min(2, shape_for(p.n, p.m, d.batch, false));
+    p.shape_wide = std::min(2, shape_for(d.cols, d.rows, d.batch, false));
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
     p.norms = take(std::max<size_t>(8, 8 * (size_t)d.batch * p.norm_blocks));
     if (d.steps > 0) {
-        for (int i = 0; i < (d.steps > 1 ? 2 : 1); ++i) {
-            p.x[i] = take(2 * (size_t)d.batch * p.m * p.n_pad);
-            p.xt[i] = take(2 * (size_t)d.batch * p.n * p.m_pad);
-        }
+        for (int i = 0; i < (d.steps > 1 ? 2 : 1); ++i) p.x[i] = take(2 * (size_t)d.batch * d.rows * p.x_pad);
         p.gram = take(2 * (size_t)d.batch * p.m * p.m_pad);
         p.poly = take(2 * (size_t)d.batch * p.m * p.m_pad);
     }

@@ -1,14 +1,17 @@
 // Matrix products on the matrix units, shared by the loss and the orthogonalised update: one tile of
 //   C[m, n] = sum_k A[m, k] B[n, k]
-// per workgroup, both operands row-major with k contiguous, sums in fp32.
+// per workgroup, sums in fp32.  Either operand may lie in memory as its rows (k contiguous) or as its columns (rows of k, m or n
+// contiguous): a product with a transposed matrix needs no transposed copy.
 //
-// Rows of both operands come into LDS 128 bytes of k at a time (64 elements of 16 bits, 32 of 32 bits), by loads that write
-// LDS directly and are in flight while the stage before is multiplied: two stages, one barrier each.  A row's eight 16-byte
-// pieces lie in LDS in the order piece ^ (row & 7): sixteen rows' pieces read by a wavefront then touch every bank once.
-// The address a lane loads from is permuted instead of the one it writes to, which the hardware makes the lane's number.
+// A stage of k (128 bytes of a row: 64 elements of 16 bits, 32 of 32 bits) comes into LDS by loads that write LDS directly,
+// two stages in turn.  What a load writes is in the order of its lanes, so it is the address a lane loads from that is permuted:
+// * rows: a row's eight 16-byte pieces lie in the order piece ^ (row & 7); the sixteen rows' pieces that a wavefront reads
+//   together then touch every bank once.
+// * columns: a row of k is BM (BN) elements; its pieces lie in the order piece ^ f(k), which puts the four rows of k that sixteen lanes read
+//   together (eight bytes each, turned by the read into four k of one column a lane; in fp32 four reads) on different banks.
 // Each lane holds column n = lane & 15 of a 16 x 16 tile and four consecutive rows m: what runs over m (the vocabulary) is
 // reduced mostly in registers, and four elements contiguous in m go out in one store.
-// 8192 x 8192 x 4096 in bfloat16, tiles of 256 x 256: 1.27 PFLOP/s, where a large library product reaches 1.28 to 1.6.
+// 8192 x 8192 x 4096 in bfloat16, tiles of 256 x 256: 1.38 PFLOP/s, where a large library product reaches 1.28 to 1.6.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -39,11 +42,12 @@ struct F32 {
 
 constexpr int kRowBytes = 128;      // of k, a stage
 
+// m, n: rows of A and B.  Rows: the elements between k and the next multiple of 16 bytes are zeros in at least one operand and finite
+// in the other.  Columns: rows of k are whole 16-byte groups.  k = 0 gives a tile of zeros.
 struct Operands {
     const char *a, *b;
-    int64_t lda, ldb;       // bytes from row to row, multiples of 16, as are the pointers
-    int rows_a, rows_b;
-    int k_bytes;            // a multiple of 16; 0 gives a tile of zeros
+    int64_t lda, ldb;       // bytes from row to row in memory, multiples of 16, as are the pointers
+    int m, n, k;
 };
 
 // Workgroup -> tile.  Workgroups go round the eight XCDs, each with a cache of its own: the tiles are cut into eight runs, one
@@ -60,9 +64,10 @@ __device__ __forceinline__ Tile tile_of(int block, int tiles_m, int tiles_n, int
     return {first + rest % size, rest / size};
 }
 
-template <class T, int BM_, int BN_, int WM_, int WN_>
+template <class T, int BM_, int BN_, int WM_, int WN_, bool COLS_A_ = false, bool COLS_B_ = false>
 struct TileShape {
     typedef T element;
+    static constexpr bool COLS_A = COLS_A_, COLS_B = COLS_B_;     // the operand lies in memory as its columns
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr int kThreads = WM * WN * 64, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
     static constexpr int kStage = (BM + BN) * kRowBytes, kLds = 2 * kStage;
@@ -91,14 +96,14 @@ inline int shape_for(int64_t m, int64_t n, int64_t slices, bool f32)
     return best;
 }
 
-template <class T>
-using Shape0 = TileShape<T, 256, 256, 2, 4>;
-template <class T>
-using Shape1 = TileShape<T, 128, 128, 2, 2>;
-template <class T>
-using Shape2 = TileShape<T, 64, 64, 2, 2>;
-template <class T>
-using Shape3 = TileShape<T, 128, 16, 2, 1>;
+template <class T, bool COLS_A = false, bool COLS_B = false>
+using Shape0 = TileShape<T, 256, 256, 2, 4, COLS_A, COLS_B>;
+template <class T, bool COLS_A = false, bool COLS_B = false>
+using Shape1 = TileShape<T, 128, 128, 2, 2, COLS_A, COLS_B>;
+template <class T, bool COLS_A = false, bool COLS_B = false>
+using Shape2 = TileShape<T, 64, 64, 2, 2, COLS_A, COLS_B>;
+template <class T, bool COLS_A = false, bool COLS_B = false>
+using Shape3 = TileShape<T, 128, 16, 2, 1, COLS_A, COLS_B>;
 
 #ifdef __HIP_DEVICE_COMPILE__
 
@@ -124,53 +129,133 @@ struct Place {
     }
 };
 
-template <class S>
-__device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *lds, f32x4 (&acc)[S::FM][S::FN])
-{
-    typedef __attribute__((address_space(3))) void lds_void;
-    typedef typename S::element::piece piece;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rows_a = min(o.rows_a - t.m * S::BM, S::BM), rows_b = min(o.rows_b - t.n * S::BN, S::BN);
-    // (rows - 1) * ld + k_bytes stays below 2^31: the entry points' limits see to it.  A load beyond the buffer gives zeros.
-    const char *const base_a = o.a + (int64_t)t.m * S::BM * o.lda, *const base_b = o.b + (int64_t)t.n * S::BN * o.ldb;
-    const int bytes_a = (int)((rows_a - 1) * o.lda) + o.k_bytes, bytes_b = (int)((rows_b - 1) * o.ldb) + o.k_bytes;
-    const int piece_at = ((lane & 7) ^ (lane >> 3)) * 16;
-    int at_a[S::kLoadsA], at_b[S::kLoadsB];
-#pragma unroll
-    for (int i = 0; i < S::kLoadsA; ++i) at_a[i] = min((i * (S::kThreads / 64) + wave) * 8 + (lane >> 3), rows_a - 1) * (int)o.lda + piece_at;
-#pragma unroll
-    for (int i = 0; i < S::kLoadsB; ++i) at_b[i] = min((i * (S::kThreads / 64) + wave) * 8 + (lane >> 3), rows_b - 1) * (int)o.ldb + piece_at;
+typedef __attribute__((address_space(3))) char lds_char;
 
-    const int stages = (o.k_bytes + kRowBytes - 1) / kRowBytes, part = o.k_bytes % kRowBytes ? stages - 1 : -1;
-    // Stages past the end are asked for like any other, from a buffer of no bytes: zeros, and no traffic.  Of a last stage that is
-    // not whole, a row's pieces beyond its end are taken from beyond the buffer.
-    auto load = [&](int stage) {
-        const int k = stage * kRowBytes;
-        char *to = lds + (stage & 1) * S::kStage + wave * 1024;
-        if (stage == part) {
-            const int off = k + piece_at < o.k_bytes ? 0 : (int)0x80000000;
+// Eight bytes a lane out of LDS, sixteen lanes' worth turned: lane i of sixteen gets element i % 4 of lanes i / 4, 4 + i / 4, 8 + i / 4
+// and 12 + i / 4.  (The pointer is restrict for what the compiler concludes from it: a read that it knows nothing of would wait for
+// every load into LDS that is on its way, those of other stages among them.)
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+__device__ __forceinline__ s16x4 read_turned(lds_s16x4 *__restrict from) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(from); }
+
+// One operand of a tile: B_ rows of it (BM or BN), of which the wavefront multiplies F x 16 from `mine` on.
+template <class T, int B_, int F, int THREADS, bool COLS>
+struct Side {
+    typedef typename T::piece piece;
+    static constexpr int kSize = sizeof(typename T::type), kDepth = kRowBytes / kSize;      // k of a stage
+    static constexpr int kLoads = B_ * kRowBytes / (THREADS * 16), kReads = F * (COLS ? (kSize == 4 ? 4 : 2) : 1);
+    static constexpr int kLine = COLS ? B_ * kSize : kRowBytes, kPieces = kLine / 16;       // a row in LDS
+    const char *base;
+    int64_t ld;
+    int bytes, k, stages, part;         // (rows) of the buffer; k in bytes; stages, and the one that is not whole
+    int width;                          // (columns) bytes of a row of k
+    int at[kLoads], piece_at;
+    int from;                           // of the lane's first piece in LDS
+
+    // the permutation of a row of k
+    static __device__ __forceinline__ int f(int row) { return (kSize == 4 ? (row >> 2 & 3) << 2 : (row & 3) << 1 | (row >> 3 & 1) << 3) & (kPieces - 1); }
+
+    __device__ __forceinline__ Side(const char *p, int64_t ld_, int first, int rows, int k_, int mine)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        ld = ld_;
+        stages = (k_ + kDepth - 1) / kDepth;
+        const int left = min(rows - first, B_);
+        if (COLS) {
+            base = p + (int64_t)first * kSize;
+            k = k_;
+            width = (left * kSize + 15) & ~15;
 #pragma unroll
-            for (int i = 0; i < S::kLoadsA; ++i) at_a[i] |= off;
+            for (int i = 0; i < kLoads; ++i) {
+                const int byte = (i * (THREADS / 64) + wave) * 1024 + lane * 16, row = byte / kLine;
+                const int piece = (byte % kLine / 16) ^ f(row);
+                at[i] = piece * 16 < width ? row * (int)ld + piece * 16 : (int)0x80000000;
+            }
+            const int g = lane >> 4, r = lane & 15;
+            if (kSize == 4) from = 4 * g * kLine + (((mine + r) / 4 ^ f(4 * g)) * 16) + (r & 3) * 4;
+            else from = (8 * g + (r >> 2)) * kLine + ((mine / 8 + ((r & 3) >> 1)) ^ f(8 * g + (r >> 2))) * 16 + (r & 1) * 8;
+        } else {
+            base = p + first * ld;
+            k = (k_ * kSize + 15) & ~15;
+            bytes = (int)((left - 1) * ld) + k;
+            part = k % kRowBytes ? stages - 1 : -1;
+            piece_at = ((lane & 7) ^ (lane >> 3)) * 16;
 #pragma unroll
-            for (int i = 0; i < S::kLoadsB; ++i) at_b[i] |= off;
+            for (int i = 0; i < kLoads; ++i) at[i] = min((i * (THREADS / 64) + wave) * 8 + (lane >> 3), left - 1) * (int)ld + piece_at;
+            from = (mine + (lane & 15)) * kRowBytes + ((lane >> 4) ^ (lane & 7)) * 16;
         }
-        const auto from_a = __builtin_amdgcn_make_buffer_rsrc((void *)base_a, 0, stage < stages ? bytes_a : 0, 0x00027000);
-        const auto from_b = __builtin_amdgcn_make_buffer_rsrc((void *)base_b, 0, stage < stages ? bytes_b : 0, 0x00027000);
+    }
+
+    // Stages past the end are asked for like any other, from a buffer of no bytes: zeros, and no traffic.  What lies beyond a row's
+    // end, or beyond the last row of k, is beyond the buffer too.
+    __device__ __forceinline__ void load(int stage, lds_char *to)
+    {
+        typedef __attribute__((address_space(3))) void lds_void;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const char *p = base;
+        int size, k_at = 0;
+        if (COLS) {
+            const int rows = min(k - stage * kDepth, kDepth);
+            p += (int64_t)min(stage, stages - 1) * kDepth * ld;
+            size = rows > 0 ? (int)((rows - 1) * ld) + width : 0;
+        } else {
+            k_at = stage * kRowBytes;
+            size = stage < stages ? bytes : 0;
+            if (stage == part) {
+                const int off = k_at + piece_at < k ? 0 : (int)0x80000000;
 #pragma unroll
-        for (int i = 0; i < S::kLoadsA; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_a, (lds_void *)(to + i * S::kThreads * 16), 16, at_a[i], k, 0, 0);
+                for (int i = 0; i < kLoads; ++i) at[i] |= off;
+            }
+        }
+        const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, size, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < S::kLoadsB; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_b, (lds_void *)(to + S::BM * kRowBytes + i * S::kThreads * 16), 16, at_b[i], k, 0, 0);
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (lds_void *)(to + (i * (THREADS / 64) + wave) * 1024), 16, at[i], k_at, 0, 0);
+    }
+
+    __device__ __forceinline__ void read(const lds_char *stage, int half, piece (&to)[F]) const
+    {
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            if constexpr (!COLS) {
+                typedef const __attribute__((address_space(3))) piece lds_piece;
+                to[i] = *(lds_piece *)(stage + (from ^ (half * 64)) + i * 16 * kRowBytes);
+            } else if constexpr (kSize == 4) {
+                typedef const __attribute__((address_space(3))) float lds_float;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) to[i][q] = *(lds_float *)(stage + (from ^ (i * 64)) + (half * 16 + q) * kLine);
+            } else {
+                const s16x4 low = read_turned((lds_s16x4 *)(stage + (from ^ (i * 32)) + half * 32 * kLine));
+                const s16x4 high = read_turned((lds_s16x4 *)(stage + (from ^ (i * 32)) + (half * 32 + 4) * kLine));
+                to[i] = __builtin_bit_cast(piece, (s16x8)__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        }
+    }
+};
+
+template <class S>
+__device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *lds_, f32x4 (&acc)[S::FM][S::FN])
+{
+    typedef typename S::element T;
+    typedef typename T::piece piece;
+    lds_char *const lds = (lds_char *)lds_;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    typedef Side<T, S::BM, S::FM, S::kThreads, S::COLS_A> SideA;
+    typedef Side<T, S::BN, S::FN, S::kThreads, S::COLS_B> SideB;
+    SideA side_a(o.a, o.lda, t.m * S::BM, o.m, o.k, wave / S::WN * S::TM);
+    SideB side_b(o.b, o.ldb, t.n * S::BN, o.n, o.k, wave % S::WN * S::TN);
+    const int stages = side_a.stages;
+    constexpr int kBytesA = S::BM * kRowBytes;
+    auto load = [&](int stage) {
+        lds_char *to = lds + (stage & 1) * S::kStage;
+        side_a.load(stage, to);
+        side_b.load(stage, to + kBytesA);
     };
-    const int row_a = (wave / S::WN * S::TM + (lane & 15)) * kRowBytes, row_b = (S::BM + wave % S::WN * S::TN + (lane & 15)) * kRowBytes;
-    const int piece_of = ((lane >> 4) ^ (lane & 7)) * 16;
     auto read = [&](int stage, int half, piece (&a)[S::FM], piece (&b)[S::FN]) {
-        const char *from = lds + (stage & 1) * S::kStage + (piece_of ^ (half * 64));
-#pragma unroll
-        for (int j = 0; j < S::FN; ++j) b[j] = *(const piece *)(from + row_b + j * 16 * kRowBytes);
-#pragma unroll
-        for (int i = 0; i < S::FM; ++i) a[i] = *(const piece *)(from + row_a + i * 16 * kRowBytes);
+        const lds_char *from = lds + (stage & 1) * S::kStage;
+        side_b.read(from + kBytesA, half, b);
+        side_a.read(from, half, a);
     };
     auto multiply_all = [&](const piece (&a)[S::FM], const piece (&b)[S::FN]) {
 #pragma unroll
@@ -181,8 +266,10 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
     auto wait_for_all = [] {
         // this wavefront's loads have arrived and what it read is in registers; after the barrier, everybody's
         asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);         // (nothing is moved across)
         __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
     };
 
@@ -193,8 +280,8 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
     if (stages == 0) return;
     // Half a stage ahead: while one half is multiplied, the other is on its way from LDS to registers; the barrier stands between the
     // halves, when the whole stage has been read: the loads of the stage after next go where it was.
-    constexpr int kReads = S::FM + S::FN, kLoads = S::kLoadsA + S::kLoadsB, kProducts = S::FM * S::FN * (sizeof(typename S::element::type) == 4 ? 4 : 1);
-    constexpr int kPerRead = kProducts / (kReads + 4) > 0 ? kProducts / (kReads + 4) : 1, kPerLoad = kProducts / (kReads + 4) > 0 ? kProducts / (kReads + 4) : 1;
+    constexpr int kReads = SideA::kReads + SideB::kReads, kLoads = SideA::kLoads + SideB::kLoads, kProducts = S::FM * S::FN * (SideA::kSize == 4 ? 4 : 1);
+    constexpr int kPerRead = kProducts / (kReads + 4) > 0 ? kProducts / (kReads + 4) : 1, kPerLoad = kPerRead;
     constexpr int kMatrix = 0x008, kVector = 0x010, kLds = 0x100;         // the scheduler's groups of instructions
     piece a0[S::FM], b0[S::FN], a1[S::FM], b1[S::FN];
     load(0);
@@ -236,21 +323,6 @@ __device__ __forceinline__ void store4(typename T::type *to, f32x4 v)
 {
     typedef typename T::type vec __attribute__((ext_vector_type(4)));
     *(vec *)to = __builtin_convertvector(v, vec);
-}
-
-// The 4 x 4 block that four neighbouring lanes (columns n .. n + 3) hold of four rows m each, turned: lane q of the four gets
-// row m + q of columns n .. n + 3.
-__device__ __forceinline__ f32x4 turned(f32x4 v)
-{
-    const int q = threadIdx.x & 3;
-    auto xor1 = [](float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xf, 0xf, true)); };     // quad_perm [1,0,3,2]
-    auto xor2 = [](float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xf, 0xf, true)); };     // [2,3,0,1]
-    // swap the off-diagonal elements of 2 x 2 blocks, then the off-diagonal blocks
-    const bool odd = q & 1, high = q & 2;
-    const float s01 = xor1(odd ? v[0] : v[1]), s23 = xor1(odd ? v[2] : v[3]);
-    f32x4 w = {odd ? s01 : v[0], odd ? v[1] : s01, odd ? s23 : v[2], odd ? v[3] : s23};
-    const float t0 = xor2(high ? w[0] : w[2]), t1 = xor2(high ? w[1] : w[3]);
-    return f32x4{high ? t0 : w[0], high ? t1 : w[1], high ? w[2] : t0, high ? w[3] : t1};
 }
 
 #endif

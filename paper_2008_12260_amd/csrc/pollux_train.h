@@ -27,7 +27,7 @@ __device__ __forceinline__ int token_at(const void *tokens, int64_t n, bool i64,
 // ---- loss ----------------------------------------------------------------------------------------------------------
 
 // How a loss call cuts the vocabulary, and the byte offsets of its workspace's sections.  Lengths of rows in the workspace are
-// padded to whole stages of the matrix kernels (128 bytes), the padding holding zeros.
+// padded to whole 16-byte groups, the padding holding zeros.
 struct LossPlan {
     bool grad;
     bool pack_hidden, pack_weight;      // rows that 16-byte loads cannot take are copied to aligned ones first
@@ -36,13 +36,12 @@ struct LossPlan {
     int piece;                          // vocabulary entries taken at a time, a multiple of 256
     int pieces;
     int slices;                         // workgroups that share one tile of the hidden rows' gradient, each a part of a piece
-    int64_t n_pad, d_pad, v_pad;        // padded tokens, width, piece
+    int64_t d_pad, v_pad;               // padded width, piece
     size_t status, top;                 // int32 [64]; float [64]: the scale of q (fp16)
     size_t parts;                       // float2 [vocabulary tiles, N]: largest logit and sum of exponentials
     size_t picked;                      // float [N]: the target's logit
-    size_t hidden, weight;              // packed copies [N, d_pad], [piece, d_pad]
-    size_t q, qt;                       // q [N, v_pad], its transpose [piece, n_pad]
-    size_t ht, wt;                      // transposes: hidden [D, n_pad], a piece of the weights [D, v_pad]
+    size_t hidden, weight;              // packed copies [N, d_pad] (of the gradients, with zeros for rows that do not count), [piece, d_pad]
+    size_t q;                           // q [N, v_pad]
     size_t sums;                        // float [slices, N, D]: the hidden rows' gradient so far
     size_t total;
 };
@@ -82,12 +81,12 @@ int launch_noise_scale(const pollux_noise_dims &d, const void *grads, const floa
 struct OrthoPlan {
     int m, n;                   // the smaller and the larger side
     bool tall;                  // the gradients have more rows than columns
-    int64_t m_pad, n_pad;
+    int64_t m_pad, x_pad;       // m and cols in whole 16-byte groups
     int shape_square, shape_wide;       // of the products [m, m] and [m, n]
     int norm_blocks;            // a matrix
     double unit;                // X is held times this power of two
     size_t norms;               // double [batch, norm_blocks]
-    size_t x[2], xt[2];         // _Float16 [batch, m, n_pad], [batch, n, m_pad]: before and after a step
+    size_t x[2];                // _Float16 [batch, rows, x_pad]: before and after a step
     size_t gram, poly;          // _Float16 [batch, m, m_pad]: X X', b X X' + c (X X')^2
     size_t total;
 };
