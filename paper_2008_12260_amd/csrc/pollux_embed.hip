@@ -8,6 +8,7 @@
 // the order in which atomics arrive, and rows that no token names are zeroed by further workgroups of the first launch.
 
 #include "pollux_host.h"
+#include "pollux_rows.h"
 #include "pollux_train.h"
 
 #include <algorithm>
@@ -30,48 +31,13 @@ struct ElementOf<PX_TYPE_F16> {
     typedef _Float16 type;
 };
 
-constexpr int kVec = 8;         // columns a lane takes at a time
-
-// Eight neighbouring columns as fp32; `left` of them are the row's.  Rows may begin at any element: whole groups of eight are one
-// load of 16 bytes (two of a row in fp32) at whatever alignment.
-template <class E>
-struct Eight {
-    E v[kVec];
-};
-template <class E>
-__device__ __forceinline__ void load8(const E *from, int left, float (&to)[kVec])
-{
-    if (left >= kVec) {
-        Eight<E> t;
-        __builtin_memcpy(&t, from, sizeof(t));
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) to[i] = (float)t.v[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) to[i] = i < left ? (float)from[i] : 0.f;
-    }
-}
-template <class E>
-__device__ __forceinline__ void store8(E *to, int left, const float (&v)[kVec])
-{
-    if (left >= kVec) {
-        Eight<E> t;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) t.v[i] = (E)v[i];
-        __builtin_memcpy(to, &t, sizeof(t));
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (i < left) to[i] = (E)v[i];
-    }
-}
-
 // A wavefront a row, or, of wide rows, kRowPart columns of one (blockIdx.y).
 constexpr int kRowPart = 64 * kVec * 8;
 template <class T, class R>
 __global__ __launch_bounds__(256) void embed_rows(const void *tokens, bool i64, int64_t N, int V, int D, const T *table, int64_t ld_table, float scale, R *rows,
                                                   int64_t ld_rows, int32_t *status)
 {
+#ifdef __HIP_DEVICE_COMPILE__
     const int64_t n = blockIdx.x * 4ll + (threadIdx.x >> 6);
     if (n >= N) return;
     bool bad;
@@ -82,12 +48,11 @@ __global__ __launch_bounds__(256) void embed_rows(const void *tokens, bool i64, 
     R *to = rows + n * ld_rows;
 #pragma unroll 4
     for (int c = first + (threadIdx.x & 63) * kVec; c < last; c += 64 * kVec) {
-        float x[kVec];
-        if (v >= 0) load8(from + c, last - c, x);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = v >= 0 ? x[i] * scale : 0.f;
-        store8(to + c, last - c, x);
+        f32x8 x = {};
+        if (v >= 0) x = load8f(from + c, last - c) * scale;
+        store8f(to + c, last - c, x);
     }
+#endif
 }
 
 // ---- sort ----------------------------------------------------------------------------------------------------------
@@ -158,6 +123,7 @@ __global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, boo
     // digit `tid`: tokens of it in all workgroups and in those before this one
     int all = 0, before = 0;
     if (tid < size)
+#pragma unroll 8
         for (int b = 0; b < blocks; ++b) {
             const int c = counts[b * size + tid];
             all += c;
@@ -243,6 +209,7 @@ constexpr int kZeroRows = 32;
 template <class R, class T>
 __global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *rows, T *table)
 {
+#ifdef __HIP_DEVICE_COMPILE__
     if ((int)blockIdx.x >= A.window_blocks) {
         // the first place of a token not below row v: is it v's?
         __shared__ unsigned char named[kZeroRows];
@@ -258,10 +225,10 @@ __global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *row
             named[threadIdx.x] = lo < A.N && A.keys[lo] == v;
         }
         __syncthreads();
-        const float zeros[kVec] = {};
+        const f32x8 zeros = {};
         for (int i = threadIdx.x; i < kZeroRows * A.lanes; i += 256) {
             const int r = i / A.lanes, c = (blockIdx.y * A.lanes + i % A.lanes) * kVec;
-            if (v0 + r < A.V && c < A.D && !named[r]) store8(table + (int64_t)(v0 + r) * A.ld_table + c, A.D - c, zeros);
+            if (v0 + r < A.V && c < A.D && !named[r]) store8f(table + (int64_t)(v0 + r) * A.ld_table + c, A.D - c, zeros);
         }
         return;
     }
@@ -269,18 +236,18 @@ __global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *row
     const int c = (blockIdx.y * A.lanes + threadIdx.x % A.lanes) * kVec;
     if (w >= A.windows || c >= A.D) return;
     const int first = w * A.window, last = min(A.N, first + A.window), left = A.D - c;
-    float sum[kVec] = {};
+    f32x8 sum = {};
     int run = A.keys[first];
     bool cut = first > 0 && A.keys[first - 1] == run;         // by the window's first place
     constexpr int kAhead = 8;
     for (int at = first; at < last; at += kAhead) {
-        float x[kAhead][kVec];
+        f32x8 x[kAhead];
         int key[kAhead + 1];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int p = min(at + i, A.N - 1);
             key[i] = A.keys[p];
-            if (at + i < last && key[i] < A.V) load8(rows + (int64_t)A.places[p] * A.ld_rows + c, left, x[i]);
+            if (at + i < last && key[i] < A.V) x[i] = load8f(rows + (int64_t)A.places[p] * A.ld_rows + c, left);
         }
         key[kAhead] = at + kAhead < A.N ? A.keys[at + kAhead] : -1;
 #pragma unroll
@@ -290,45 +257,35 @@ __global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *row
             if (key[i] != run) {
                 run = key[i];
                 cut = false;
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) sum[k] = 0.f;
+                sum = f32x8{};
             }
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) sum[k] += x[i][k];
+            sum += x[i];
             const bool ends = at + i + 1 >= A.N || key[i + 1] != run, final = at + i + 1 >= last;
             if (!ends && !final) continue;
             if (ends && !cut) {
                 T *to = table + (int64_t)run * A.ld_table + c;
-                float out[kVec];
-                if (A.add) {
-                    float held[kVec];
-                    load8(to, left, held);
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k) out[k] = held[k] + sum[k] * A.scale;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < kVec; ++k) out[k] = sum[k] * A.scale;
-                }
-                store8(to, left, out);
+                f32x8 out = sum * A.scale;
+                if (A.add) out += load8f(to, left);
+                store8f(to, left, out);
             } else {
-                store8(A.partial + ((int64_t)(cut ? 0 : A.windows) + w) * A.D + c, left, sum);
+                store8f(A.partial + ((int64_t)(cut ? 0 : A.windows) + w) * A.D + c, left, sum);
             }
         }
     }
+#endif
 }
 
-// The runs that windows cut: the window in which one begins adds up the pieces, its own and those of the windows after it.
+// The runs that windows cut: the window in which one begins adds up the pieces, its own and those of the windows after it, a
+// quarter of them each of four wavefronts, and these in their order.
 template <class T>
 __global__ __launch_bounds__(256) void join_runs(const SumArgs A, T *table)
 {
-    const int w = blockIdx.x * A.groups + threadIdx.x / A.lanes;
-    const int c = (blockIdx.y * A.lanes + threadIdx.x % A.lanes) * kVec;
-    if (w + 1 >= A.windows || c >= A.D) return;
-    const int first = w * A.window, last = first + A.window, run = A.keys[last - 1], left = A.D - c;
+#ifdef __HIP_DEVICE_COMPILE__
+    __shared__ f32x8 shared[3][64];
+    const int w = blockIdx.x, part = threadIdx.x >> 6, c = (blockIdx.y * 64 + (threadIdx.x & 63)) * kVec, left = A.D - c;
+    const int first = w * A.window, last = first + A.window, run = A.keys[last - 1];
     if (run >= A.V || A.keys[last] != run) return;            // nothing is cut by this window's end
     if (A.keys[first] == run && first > 0 && A.keys[first - 1] == run) return;      // it began before
-    float sum[kVec];
-    load8(A.partial + ((int64_t)A.windows + w) * A.D + c, left, sum);
     // windows that the run reaches: up to the one that holds its last place
     int lo = last, hi = A.N;
     while (lo < hi) {
@@ -336,25 +293,23 @@ __global__ __launch_bounds__(256) void join_runs(const SumArgs A, T *table)
         if (A.keys[mid] <= run) lo = mid + 1;
         else hi = mid;
     }
-    const int end = (lo - 1) / A.window;
-#pragma unroll 4
-    for (int u = w + 1; u <= end; ++u) {
-        float x[kVec];
-        load8(A.partial + (int64_t)u * A.D + c, left, x);
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) sum[k] += x[k];
+    const int count = (lo - 1) / A.window - w, each = (count + 3) >> 2, u0 = w + 1 + part * each, u1 = min(w + 1 + count, u0 + each);
+    f32x8 sum = {};
+    if (c < A.D) {
+        if (part == 0) sum = load8f(A.partial + ((int64_t)A.windows + w) * A.D + c, left);
+#pragma unroll 8
+        for (int u = u0; u < u1; ++u) sum += load8f(A.partial + (int64_t)u * A.D + c, left);
     }
+    if (part > 0) shared[part - 1][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (part > 0 || c >= A.D) return;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) sum += shared[i][threadIdx.x];
     T *to = table + (int64_t)run * A.ld_table + c;
-    if (A.add) {
-        float held[kVec];
-        load8(to, left, held);
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) sum[k] = held[k] + sum[k] * A.scale;
-    } else {
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) sum[k] *= A.scale;
-    }
-    store8(to, left, sum);
+    sum *= A.scale;
+    if (A.add) sum += load8f(to, left);
+    store8f(to, left, sum);
+#endif
 }
 
 template <class R, class T>
@@ -395,7 +350,7 @@ int embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *token
     const int zero_blocks = a.add ? 0 : (d.V + kZeroRows - 1) / kZeroRows;
     if (a.window_blocks + zero_blocks > 0)
         hipLaunchKernelGGL((sum_windows<R, T>), dim3((unsigned)(a.window_blocks + zero_blocks), parts), dim3(256), 0, stream, a, rows, table);
-    if (p.windows > 1) hipLaunchKernelGGL(join_runs<T>, dim3((unsigned)a.window_blocks, parts), dim3(256), 0, stream, a, table);
+    if (p.windows > 1) hipLaunchKernelGGL(join_runs<T>, dim3((unsigned)(p.windows - 1), (unsigned)((d.D + 64 * kVec - 1) / (64 * kVec))), dim3(256), 0, stream, a, table);
     return status_of(hipGetLastError());
 }
 

@@ -16,6 +16,7 @@
 // scaled by the power of two that brings the largest row weight to 2^13, and the gradients are scaled back in fp32.
 
 #include "pollux_host.h"
+#include "pollux_rows.h"
 #include "pollux_tiles.h"
 #include "pollux_train.h"
 
@@ -116,32 +117,38 @@ __global__ __launch_bounds__(S::kThreads) void loss_tiles(const LogitArgs A)
 #endif
 }
 
-// Each token's tiles joined: kJoinTokens neighbouring tokens (a line of a tile's values) by kJoinParts parts of the list.
-constexpr int kJoinTokens = 16, kJoinParts = 16;
-__global__ __launch_bounds__(kJoinTokens *kJoinParts) void loss_join(const float2 *parts, int tiles, int N, const float *picked,
-                                                                     const void *targets, bool i64, int V, float *loss, float *lse,
-                                                                     int32_t *status)
+// Each token's tiles joined: TOKENS neighbouring tokens (a line of a tile's values) by 256 / TOKENS parts of the list.
+constexpr int kJoinThreads = 256;
+template <int TOKENS>
+__global__ __launch_bounds__(kJoinThreads) void loss_join(const float2 *parts, int tiles, int N, const float *picked, const void *targets, bool i64, int V, float *loss,
+                                                          float *lse, int32_t *status)
 {
-    __shared__ float2 shared[kJoinParts][kJoinTokens];
-    const int c = threadIdx.x % kJoinTokens, k = threadIdx.x / kJoinTokens, n = blockIdx.x * kJoinTokens + c;
+    constexpr int kParts = kJoinThreads / TOKENS, kAhead = 4;
+    __shared__ float2 shared[kParts][TOKENS];
+    const int c = threadIdx.x % TOKENS, k = threadIdx.x / TOKENS, n = blockIdx.x * TOKENS + c;
     float top = -__builtin_inff(), sum = 0.f;
     if (n < N)
-        for (int t = k; t < tiles; t += kJoinParts) {
-            const float2 p = parts[(int64_t)t * N + n];
-            const float most = fmaxf(top, p.x), from = finite_or_zero(most);
-            const float x = sum == __builtin_inff() ? sum : sum * __builtin_amdgcn_exp2f((finite_or_zero(top) - from) * kLog2e);
-            const float y = p.y == __builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
-            // (the sum from a maximum of -inf is 0, or NaN)
-            sum = (top == -__builtin_inff() ? sum : x) + (p.x == -__builtin_inff() ? p.y : y);
-            top = most;
+        for (int t0 = k; t0 < tiles; t0 += kParts * kAhead) {
+            float2 p[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) p[i] = t0 + i * kParts < tiles ? parts[(int64_t)(t0 + i * kParts) * N + n] : make_float2(-__builtin_inff(), 0.f);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const float most = fmaxf(top, p[i].x), from = finite_or_zero(most);
+                const float x = sum == __builtin_inff() ? sum : sum * __builtin_amdgcn_exp2f((finite_or_zero(top) - from) * kLog2e);
+                const float y = p[i].y == __builtin_inff() ? p[i].y : p[i].y * __builtin_amdgcn_exp2f((finite_or_zero(p[i].x) - from) * kLog2e);
+                // (the sum from a maximum of -inf is 0, or NaN)
+                sum = (top == -__builtin_inff() ? sum : x) + (p[i].x == -__builtin_inff() ? p[i].y : y);
+                top = most;
+            }
         }
     shared[k][c] = make_float2(top, sum);
     __syncthreads();
     if (k != 0 || n >= N) return;
-    for (int i = 1; i < kJoinParts; ++i) top = fmaxf(top, shared[i][c].x);
+    for (int i = 1; i < kParts; ++i) top = fmaxf(top, shared[i][c].x);
     const float from = finite_or_zero(top);
     sum = 0.f;
-    for (int i = 0; i < kJoinParts; ++i) {
+    for (int i = 0; i < kParts; ++i) {
         const float2 p = shared[i][c];
         sum += p.y == __builtin_inff() || p.x == -__builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
     }
@@ -313,29 +320,23 @@ __global__ __launch_bounds__(256) void join_slices(const float *sums, int slices
     }
 }
 
-// Rows copied to aligned ones, `cols` padded with zeros to ld_to; rows without a target, or of weight 0, are copied as zeros.  Eight
-// bytes at a time where rows allow it.
+// Rows copied to aligned ones, `cols` padded with zeros to ld_to; rows without a target, or of weight 0, are copied as zeros.
 template <class E>
 __global__ __launch_bounds__(256) void pack_rows(const E *from, int64_t ld_from, int64_t rows, int cols, E *to, int64_t ld_to, const void *targets, const float *row_weight,
                                                  bool i64, int V)
 {
-    constexpr int kVec = 16 / sizeof(E);
-    struct Vec {
-        E v[kVec];
-    };
-    const int groups = (int)(ld_to / kVec);
+#ifdef __HIP_DEVICE_COMPILE__
+    const int groups = (int)((ld_to + kVec - 1) / kVec);
     const int64_t total = rows * groups;
     for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
         const int64_t n = at / groups;
         const int c = (int)(at - n * groups) * kVec;
         const bool there = !targets || (target_of(targets, n, i64, V) >= 0 && !(row_weight && row_weight[n] == 0.f));
-        Vec t;
-        if (there && c + kVec <= cols) __builtin_memcpy(&t, from + n * ld_from + c, sizeof(t));
-        else
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) t.v[i] = there && c + i < cols ? from[n * ld_from + c + i] : E(0.f);
-        *(Vec *)(to + n * ld_to + c) = t;
+        typename Eight<E>::type v = {};
+        if (there && c < cols) v = load8(from + n * ld_from + c, cols - c);
+        store8(to + n * ld_to + c, ld_to - c, v);
     }
+#endif
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
@@ -397,7 +398,7 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
         return status_of(hipGetLastError());
     }
     if (p.pack_hidden) {
-        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * p.d_pad / (16 / e))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
+        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
         hidden = ws + p.hidden;
     }
     LogitArgs a = {};
@@ -417,7 +418,7 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
         a.rows = a.o.m = std::min(p.piece, d.V - a.first);
         const char *from = weight + (int64_t)a.first * d.weight_stride * e;
         if (p.pack_weight) {
-            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * p.d_pad / (16 / e))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
             from = ws + p.weight;
         }
         a.o.a = from;
@@ -426,8 +427,13 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
         launch_logits<T>(p.tiles, kLoss, a, stream);
         tiles += (a.rows + kShape[p.tiles].bm - 1) / kShape[p.tiles].bm;
     }
-    hipLaunchKernelGGL(loss_join, dim3((N + kJoinTokens - 1) / kJoinTokens), dim3(kJoinTokens * kJoinParts), 0, stream, (const float2 *)(ws + p.parts),
-                       tiles, N, (const float *)(ws + p.picked), targets, a.i64, d.V, loss, lse, status);
+    auto join = [&](auto kernel, int tokens) {
+        hipLaunchKernelGGL(kernel, dim3((N + tokens - 1) / tokens), dim3(kJoinThreads), 0, stream, (const float2 *)(ws + p.parts), tiles, N, (const float *)(ws + p.picked), targets,
+                           a.i64, d.V, loss, lse, status);
+    };
+    // (few tokens: as many threads for each; three tokens of 1024 tiles 25 us with sixteen parts)
+    if (N <= 1024) join(loss_join<2>, 2);
+    else join(loss_join<16>, 16);
     return status_of(hipGetLastError());
 }
 
@@ -455,7 +461,7 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
         return status_of(hipGetLastError());
     }
     // (a product with q's zeros would still be NaN where a row that counts for nothing holds one)
-    hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * p.d_pad / (16 / e))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D,
+    hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D,
                        (type *)(ws + p.hidden), p.d_pad, targets, row_weight, i64, d.V);
     LogitArgs a = {};
     a.targets = targets;
@@ -477,7 +483,7 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
         a.rows = a.o.m = std::min(p.piece, d.V - a.first);
         const char *from = weight + (int64_t)a.first * d.weight_stride * e;
         if (p.pack_weight) {
-            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * p.d_pad / (16 / e))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
             from = ws + p.weight;
         }
         a.o.a = from;

@@ -6,6 +6,7 @@
 // and a second launch adds them up in their order, so that the result depends on nothing but the gradients.
 
 #include "pollux_host.h"
+#include "pollux_rows.h"
 #include "pollux_train.h"
 
 #include <algorithm>
@@ -13,67 +14,49 @@
 namespace px {
 namespace {
 
-constexpr int kVec = 8, kAhead = 4, kThreads = 256;
-
-template <class E>
-struct Eight {
-    E v[kVec];
-};
-
-template <class E>
-__device__ __forceinline__ void load8(const E *from, int64_t left, Eight<E> &to)
-{
-    if (left >= kVec) __builtin_memcpy(&to, from, sizeof(to));      // one load of 16 bytes (two in fp32) at any alignment of the element
-    else
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) to.v[i] = i < left ? from[i] : E(0.f);
-}
+constexpr int kThreads = 256;
 
 template <class E, class M>
 __global__ __launch_bounds__(kThreads) void noise_sums(const E *grads, int64_t n, int B, int64_t stride, const float *precondition, M *mean, double2 *sums)
 {
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int kAhead = 4;
     double trace = 0.0, norm = 0.0;
     const double over_b = 1.0 / B;
     for (int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kVec; at < n; at += (int64_t)gridDim.x * kThreads * kVec) {
         const int64_t left = n - at;
-        Eight<E> g0;
-        load8(grads + at, left, g0);
+        const f32x8 g0 = load8f(grads + at, left);
         double s1[kVec] = {}, s2[kVec] = {};
         for (int b = 1; b < B; b += kAhead) {
-            Eight<E> g[kAhead];
+            f32x8 g[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
-                if (b + k < B) load8(grads + (b + k) * stride + at, left, g[k]);
+                if (b + k < B) g[k] = load8f(grads + (b + k) * stride + at, left);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
                 if (b + k < B) {
 #pragma unroll
                     for (int i = 0; i < kVec; ++i) {
-                        const double d = (double)(float)g[k].v[i] - (double)(float)g0.v[i];
+                        const double d = (double)g[k][i] - (double)g0[i];
                         s1[i] += d;
                         s2[i] = fma(d, d, s2[i]);
                     }
                 }
         }
-        Eight<float> p;
-        if (precondition) load8(precondition + at, left, p);
-        Eight<M> out;
+        f32x8 p, out;
+        if (precondition) p = load8f(precondition + at, left);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const double m = (double)(float)g0.v[i] + s1[i] * over_b;
-            out.v[i] = (M)(float)m;
+            const double m = (double)g0[i] + s1[i] * over_b;
+            out[i] = (float)m;
             if (i < left) {
-                const double w = precondition ? (double)p.v[i] * (double)p.v[i] : 1.0;
+                const double w = precondition ? (double)p[i] * (double)p[i] : 1.0;
                 const double v = fma(-s1[i] * over_b, s1[i], s2[i]);
                 trace += w * (v < 0.0 ? 0.0 : v);              // (NaN stays)
                 norm += w * (m * m);
             }
         }
-        if (mean) {
-            if (left >= kVec) __builtin_memcpy(mean + at, &out, sizeof(out));
-            else
-                for (int i = 0; i < left; ++i) mean[at + i] = out.v[i];
-        }
+        if (mean) store8f(mean + at, left, out);
     }
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) {
@@ -89,6 +72,7 @@ __global__ __launch_bounds__(kThreads) void noise_sums(const E *grads, int64_t n
         norm += waves[i].y;
     }
     sums[blockIdx.x] = make_double2(trace, norm);
+#endif
 }
 
 __global__ __launch_bounds__(kThreads) void noise_join(const double2 *sums, int blocks, int B, double examples, double *scale)

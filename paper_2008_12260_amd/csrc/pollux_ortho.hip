@@ -10,6 +10,7 @@
 // elements of 1 or so.  Sums in fp32, the norm in fp64.
 
 #include "pollux_host.h"
+#include "pollux_rows.h"
 #include "pollux_tiles.h"
 #include "pollux_train.h"
 
@@ -23,26 +24,33 @@ constexpr int kThreads = 256;
 template <class E>
 __global__ __launch_bounds__(kThreads) void square_sums(const E *grads, int rows, int cols, int64_t ld, int64_t ld_batch, double *sums)
 {
+#ifdef __HIP_DEVICE_COMPILE__
     const E *g = grads + blockIdx.y * ld_batch;
     double sum = 0.0;
-    for (int r = blockIdx.x; r < rows; r += gridDim.x)
-#pragma unroll 4
-        for (int c = threadIdx.x; c < cols; c += kThreads) {
-            const double v = (double)(float)g[r * ld + c];
-            sum = fma(v, v, sum);
-        }
+    const int groups = (cols + kVec - 1) / kVec;
+    const int64_t total = (int64_t)rows * groups;
+#pragma unroll 2
+    for (int64_t at = blockIdx.x * (int64_t)kThreads + threadIdx.x; at < total; at += gridDim.x * (int64_t)kThreads) {
+        const int64_t r = at / groups;
+        const int c = (int)(at - r * groups) * kVec;
+        const f32x8 v = load8f(g + r * ld + c, cols - c);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sum = fma((double)v[i], (double)v[i], sum);
+    }
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) sum += __shfl_xor(sum, w);
     __shared__ double waves[kThreads / 64];
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) sums[blockIdx.y * gridDim.x + blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
+#endif
 }
 
 // X from the gradients, rows padded with zeros.
 template <class E>
 __global__ __launch_bounds__(kThreads) void normalise(const E *grads, int rows, int cols, int64_t ld, int64_t ld_batch, const double *sums, int parts, double unit, _Float16 *x, int64_t ld_x)
 {
+#ifdef __HIP_DEVICE_COMPILE__
     __shared__ double waves[kThreads / 64];
     const int64_t batch = blockIdx.y;
     double sum = 0.0;
@@ -58,19 +66,13 @@ __global__ __launch_bounds__(kThreads) void normalise(const E *grads, int rows, 
     for (int64_t at = blockIdx.x * (int64_t)kThreads + threadIdx.x; at < total; at += gridDim.x * (int64_t)kThreads) {
         const int64_t r = at / groups;
         const int c = (int)(at - r * groups) * 8;
-        const E *from = grads + batch * ld_batch + r * ld + c;
-        struct {
-            E v[8];
-        } g;
-        if (c + 8 <= cols) __builtin_memcpy(&g, from, sizeof(g));
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) g.v[i] = c + i < cols ? from[i] : E(0.f);
+        const f32x8 g = load8f(grads + batch * ld_batch + r * ld + c, cols - c);
         f16x8 h;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = (_Float16)(float)((double)(float)g.v[i] * by);
+        for (int i = 0; i < 8; ++i) h[i] = (_Float16)(float)((double)g[i] * by);
         *(f16x8 *)(x + (batch * rows + r) * ld_x + c) = h;
     }
+#endif
 }
 
 struct StepArgs {
@@ -238,7 +240,7 @@ OrthoPlan ortho_plan(const pollux_ortho_dims &d)
     p.m_pad = (p.m + 7) / 8 * 8;
     p.x_pad = (d.cols + 7) / 8 * 8;
     p.unit = ldexp(1.0, (int)lround(0.5 * log2((double)p.n)));
-    p.norm_blocks = (int)std::min<int64_t>(d.rows, std::max<int64_t>(1, std::min<int64_t>(1024 / std::max(d.batch, 1) + 1, (int64_t)d.rows * d.cols / 4096)));
+    p.norm_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / std::max(d.batch, 1), (int64_t)d.rows * d.cols / 8192));
     p.shape_square = std::min(2, shape_for(p.m, p.m, d.batch, false));
     p.shape_wide = std::min(2, shape_for(d.cols, d.rows, d.batch, false));
     size_t o = 0;

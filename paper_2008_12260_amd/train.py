@@ -16,13 +16,14 @@ import os
 import paper_2008_12260_amd as _px
 
 
-def _types():
-    import torch
-    return {torch.float32: _px.PX_TYPE_F32, torch.bfloat16: _px.PX_TYPE_BF16, torch.float16: _px.PX_TYPE_F16}
+_TYPES = {}              # torch's types to the library's, filled at the first call
 
 
 def _type(t, name):
-    code = _types().get(t.dtype)
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: _px.PX_TYPE_F32, torch.bfloat16: _px.PX_TYPE_BF16, torch.float16: _px.PX_TYPE_F16})
+    code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} is {t.dtype}: float32, bfloat16 or float16 is wanted")
     return code
@@ -33,7 +34,7 @@ def _on_device(**tensors):
     import torch
     here = torch.cuda.current_device()
     for name, t in tensors.items():
-        if t is not None and (not t.is_cuda or t.device.index != here):
+        if t is not None and t.get_device() != here:
             raise ValueError(f"{name} is on {t.device}: it has to be on the current GPU, cuda:{here}")
 
 
@@ -70,15 +71,20 @@ def _tokens(t, name, count):
     return t.contiguous(), _px.PX_FLAG_TOKENS_I64 if t.dtype == torch.int64 else 0
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(stream):
+    if stream is None:
+        return _HERE
     import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return torch.cuda.stream(stream)
 
 
 def _scratch(bytes_, device):
     import torch
     ws = torch.empty(bytes_, dtype=torch.uint8, device=device)
-    if os.environ.get("POLLUX_POISON_WORKSPACE"):
+    if "POLLUX_POISON_WORKSPACE" in os.environ:
         # for tests: nothing in the library may depend on what a fresh workspace holds (0xFF bytes read as NaN / -1)
         ws.fill_(0xFF)
     return ws
