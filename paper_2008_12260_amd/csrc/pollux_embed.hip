@@ -61,13 +61,16 @@ __global__ __launch_bounds__(256) void embed_rows(const void *tokens, bool i64, 
 
 constexpr int kFew = 1024, kThreads = 1024, kWaves = kThreads / 64, kMaxBits = 10;
 
-__global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i64, int N, int V, int32_t *status, int *keys, int *places)
+__global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i64, int N, int V, int32_t *status, int *keys, int *places, unsigned char *named)
 {
     __shared__ int shared[kFew];
     __shared__ int bad_any;
     const int n = threadIdx.x;
     if (n == 0) bad_any = 0;
     if (n < kStatusWords) status[n] = 0;
+    if (named)
+        for (int i = n; i < (V + 3) / 4; i += kThreads) ((unsigned *)named)[i] = 0;
+    __threadfence();
     bool bad = false;
     int key = 0x7fffffff;
     if (n < N) {
@@ -85,18 +88,22 @@ __global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i6
     if (n < N) {
         keys[before] = key;
         places[before] = n;
+        if (named && key < V) named[key] = 1;
     }
     __syncthreads();
     if (n == 0 && bad_any) *status = PX_ST_BAD_TOKEN;
 }
 
-// A workgroup's tokens counted by their lowest digit; the second pass's counts and the status word are cleared.
-__global__ __launch_bounds__(kThreads) void count_digits(const void *tokens, bool i64, int N, int V, int per_block, int bits, int *counts, int *counts2, int32_t *status)
+// A workgroup's tokens counted by their lowest digit; the second pass's counts, the marks of the entries that are named and the
+// status word are cleared.
+__global__ __launch_bounds__(kThreads) void count_digits(const void *tokens, bool i64, int N, int V, int per_block, int bits, int *counts, int *counts2, unsigned char *named, int32_t *status)
 {
     __shared__ int bins[1 << kMaxBits];
     const int size = 1 << bits, first = blockIdx.x * per_block, last = min(N, first + per_block);
     for (int i = threadIdx.x; i < size; i += kThreads) bins[i] = 0;
     if (blockIdx.x == 0 && threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
+    if (named)
+        for (int i = blockIdx.x * kThreads + threadIdx.x; i < (V + 3) / 4; i += gridDim.x * kThreads) ((unsigned *)named)[i] = 0;
     __syncthreads();
     for (int n = first + threadIdx.x; n < last; n += kThreads) {
         bool bad;
@@ -114,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void count_digits(const void *tokens, boo
 // order.  The first pass reads the tokens themselves and counts, for the second, the next digits of the places it fills.
 template <bool FIRST>
 __global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, bool i64, const int *keys_in, const int *places_in, int N, int V, int blocks, int per_block,
-                                                         int bits, const int *counts, int *counts2, int *keys, int *places, int32_t *status)
+                                                         int bits, const int *counts, int *counts2, int *keys, int *places, unsigned char *named, int32_t *status)
 {
     __shared__ int base[1 << kMaxBits];
     __shared__ int in_wave[kWaves][1 << kMaxBits];
@@ -182,7 +189,10 @@ __global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, boo
             const int to = base[digit] + in_wave[wave][digit] + rank;
             keys[to] = key;
             places[to] = place;
-            if (FIRST) atomicAdd(&counts2[to / per_block * size + ((key >> bits) & (size - 1))], 1);
+            if (FIRST) {
+                atomicAdd(&counts2[to / per_block * size + ((key >> bits) & (size - 1))], 1);
+                if (named && key < V) named[key] = 1;
+            }
         }
         __syncthreads();
         if (tid < size) base[tid] += total;
@@ -195,6 +205,7 @@ __global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, boo
 
 struct SumArgs {
     const int *keys, *places;
+    const unsigned char *named;      // [V / 32]: bits of the entries that tokens name
     int64_t ld_rows, ld_table;
     float *partial;             // [2][windows][D]: the run cut by a window's first place, by its last
     int N, V, D, window, windows;
@@ -211,24 +222,11 @@ __global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *row
 {
 #ifdef __HIP_DEVICE_COMPILE__
     if ((int)blockIdx.x >= A.window_blocks) {
-        // the first place of a token not below row v: is it v's?
-        __shared__ unsigned char named[kZeroRows];
         const int v0 = ((int)blockIdx.x - A.window_blocks) * kZeroRows;
-        if (threadIdx.x < kZeroRows) {
-            const int v = v0 + threadIdx.x;
-            int lo = 0, hi = A.N;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (A.keys[mid] < v) lo = mid + 1;
-                else hi = mid;
-            }
-            named[threadIdx.x] = lo < A.N && A.keys[lo] == v;
-        }
-        __syncthreads();
         const f32x8 zeros = {};
         for (int i = threadIdx.x; i < kZeroRows * A.lanes; i += 256) {
             const int r = i / A.lanes, c = (blockIdx.y * A.lanes + i % A.lanes) * kVec;
-            if (v0 + r < A.V && c < A.D && !named[r]) store8f(table + (int64_t)(v0 + r) * A.ld_table + c, A.D - c, zeros);
+            if (v0 + r < A.V && c < A.D && !A.named[v0 + r]) store8f(table + (int64_t)(v0 + r) * A.ld_table + c, A.D - c, zeros);
         }
         return;
     }
@@ -319,19 +317,21 @@ int embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *token
     const bool i64 = d.flags & PX_FLAG_TOKENS_I64;
     int32_t *status = (int32_t *)(ws + p.status);
     int *keys[2] = {(int *)(ws + p.keys[0]), (int *)(ws + p.keys[1])}, *places[2] = {(int *)(ws + p.places[0]), (int *)(ws + p.places[1])};
+    unsigned char *named = d.flags & PX_FLAG_ACCUMULATE ? nullptr : (unsigned char *)(ws + p.named);
     if (p.passes == 0) {
-        hipLaunchKernelGGL(rank_few, dim3(1), dim3(kThreads), 0, stream, tokens, i64, N, d.V, status, keys[1], places[1]);
+        hipLaunchKernelGGL(rank_few, dim3(1), dim3(kThreads), 0, stream, tokens, i64, N, d.V, status, keys[1], places[1], named);
     } else {
         int *counts = (int *)(ws + p.counts), *counts2 = counts + ((size_t)p.blocks << p.bits);
-        hipLaunchKernelGGL(count_digits, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, N, d.V, p.per_block, p.bits, counts, counts2, status);
+        hipLaunchKernelGGL(count_digits, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, N, d.V, p.per_block, p.bits, counts, counts2, named, status);
         hipLaunchKernelGGL(place_digits<true>, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, (const int *)nullptr, (const int *)nullptr, N, d.V, p.blocks,
-                           p.per_block, p.bits, (const int *)counts, counts2, keys[0], places[0], status);
+                           p.per_block, p.bits, (const int *)counts, counts2, keys[0], places[0], named, status);
         hipLaunchKernelGGL(place_digits<false>, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, (const int *)keys[0], (const int *)places[0], N, d.V, p.blocks,
-                           p.per_block, p.bits, (const int *)counts2, (int *)nullptr, keys[1], places[1], status);
+                           p.per_block, p.bits, (const int *)counts2, (int *)nullptr, keys[1], places[1], (unsigned char *)nullptr, status);
     }
     SumArgs a = {};
     a.keys = keys[1];
     a.places = places[1];
+    a.named = named;
     a.ld_rows = d.rows_stride;
     a.ld_table = d.table_stride;
     a.partial = (float *)(ws + p.partial);
@@ -373,6 +373,7 @@ EmbedPlan embed_plan(const pollux_embed_dims &d)
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
     p.status = take(4 * kStatusWords);
+    if (!(d.flags & PX_FLAG_ACCUMULATE)) p.named = take(((size_t)d.V + 3) / 4 * 4);
     if (N > kFew) {
         int bits = 1;
         while (((int64_t)1 << (2 * bits)) <= d.V) ++bits;       // keys 0 .. V
@@ -387,7 +388,7 @@ EmbedPlan embed_plan(const pollux_embed_dims &d)
     }
     p.keys[1] = take(4 * (size_t)N);
     p.places[1] = take(4 * (size_t)N);
-    p.window = N <= 1 << 16 ? 32 : 128;
+    p.window = N <= 1 << 13 ? 8 : N <= 1 << 15 ? 16 : N <= 1 << 17 ? 32 : 128;
     p.windows = (N + p.window - 1) / p.window;
     p.partial = take(2 * (size_t)p.windows * d.D * 4);
     p.total = o;

@@ -110,7 +110,8 @@ __global__ __launch_bounds__(S::kThreads) void loss_tiles(const LogitArgs A)
 #pragma unroll
         for (int w = 0; w < S::WM; ++w) {
             const float2 p = shared[w * S::BN + c];
-            sum += p.y == __builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
+            // (the sum from a maximum of -inf is 0, or NaN)
+            sum += p.y == __builtin_inff() || p.x == -__builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
         }
         A.parts[(int64_t)t.m * A.N + n] = make_float2(top, sum);
     }
@@ -515,7 +516,7 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
             g.out = weight_grad + (int64_t)a.first * d.weight_grad_stride * e;
             g.ld = d.weight_grad_stride;
             g.add = d.flags & PX_FLAG_ACCUMULATE;
-            launch_grad<T, true>(shape_for(d.D, a.rows, 1, e == 4), g, 1, stream);
+            launch_grad<T, true>(shape_for(d.D, a.rows, N, 1, e == 4), g, 1, stream);
         }
     }
     if (hidden_grad && (p.slices > 1 || p.pieces > 1))
@@ -548,18 +549,18 @@ LossPlan loss_plan(const pollux_loss_dims &d, bool grad)
     p.pieces = (int)((d.V + piece - 1) / piece);
     // (rows of q a stage longer than a power of two: those of one tile then begin in different channels of memory)
     p.v_pad = padded(std::min<int64_t>(piece, d.V)) + kRowBytes / e;
-    p.tiles = shape_for(std::min<int64_t>(piece, d.V), N, 1, f32);
+    p.tiles = shape_for(std::min<int64_t>(piece, d.V), N, d.D, 1, f32);
     p.slices = 1;
     if (grad) {
-        // the hidden rows' gradient has few tiles and a long sum: the number of workgroups a tile that takes least
+        // the hidden rows' gradient has few tiles and a long sum: in as many slices as takes least, their sums being written and read at some
+        // 4 and 3 TB/s (2048 x 32768 x 1024 in one slice 579 us, in eight 117 and 23)
         double least = 1e300;
-        for (int slices = 1; slices <= 16; slices *= 2) {
-            if (slices > 1 && (p.v_pad * e / kRowBytes < 8 * slices || (int64_t)slices * N * d.D * 4 > (512ll << 20))) break;
-            const int shape = shape_for(d.D, N, slices, f32);
-            const ShapeOf &h = kShape[shape];
-            const double tiles = (double)((d.D + h.bm - 1) / h.bm) * ((N + h.bn - 1) / h.bn) * slices;
-            const double cost = ceil(tiles / (256.0 * h.per_cu)) * h.per_cu * h.bm * h.bn / (f32 ? 1.0 : h.rate) / slices;
-            if (cost < 0.9 * least) least = cost, p.slices = slices, p.grad_tiles = shape;
+        for (int slices = 1; slices <= 32; slices *= 2) {
+            if (slices > 1 && (p.v_pad * e / kRowBytes < 4 * slices || (int64_t)slices * N * d.D * 4 > (512ll << 20))) break;
+            double cost;
+            const int shape = shape_for(d.D, N, (double)piece / slices, slices, f32, &cost);
+            if (slices > 1) cost += 4.0 + 4.0 * slices * N * d.D * (1 / 4e6 + 1 / 3e6);
+            if (cost < least) least = cost, p.slices = slices, p.grad_tiles = shape;
         }
     }
     size_t o = 0;

@@ -241,8 +241,8 @@ OrthoPlan ortho_plan(const pollux_ortho_dims &d)
     p.x_pad = (d.cols + 7) / 8 * 8;
     p.unit = ldexp(1.0, (int)lround(0.5 * log2((double)p.n)));
     p.norm_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / std::max(d.batch, 1), (int64_t)d.rows * d.cols / 8192));
-    p.shape_square = std::min(2, shape_for(p.m, p.m, d.batch, false));
-    p.shape_wide = std::min(2, shape_for(d.cols, d.rows, d.batch, false));
+    p.shape_square = shape_for(p.m, p.m, 0.5 * (p.m + p.n), d.batch, false, nullptr, 3);
+    p.shape_wide = shape_for(d.cols, d.rows, p.m, d.batch, false, nullptr, 3);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
     p.norms = take(std::max<size_t>(8, 8 * (size_t)d.batch * p.norm_blocks));

@@ -75,24 +75,34 @@ struct TileShape {
     static_assert(kLoadsA * kThreads * 16 == BM * kRowBytes && kLoadsB * kThreads * 16 == BN * kRowBytes, "whole loads");
 };
 
+// Which shape of tile a product is formed in, and in how many slices of k: by what it is estimated to take, in microseconds.  A compute unit works on
+// per_cu tiles of a shape at once, at `rate` of 5.5 TFLOP/s (fp32: rate32 of 0.6) together, r of them at (r / per_cu)^(1/2) of that, and a
+// round of tiles begins and ends in `ends`: fitted to products of 64 to 2048 x 8192 to 65536 x 512 to 2048 and within about 15 % of them (bfloat16
+// 2048 x 32768 x 1024: 133, 170, 235, 407 us in the four shapes, 512 x 8192 x 512: 21, 12.5, 11.6, 19.6).
 constexpr int kShapes = 4;
 struct ShapeOf {
-    int bm, bn, per_cu;         // tile, workgroups a compute unit holds
-    float rate;                 // of the matrix units' while it runs, relative
+    int bm, bn, per_cu;
+    double rate, rate32, ends;
 };
-constexpr ShapeOf kShape[kShapes] = {{256, 256, 1, 1.0f}, {128, 128, 2, 0.75f}, {64, 64, 4, 0.45f}, {128, 16, 4, 0.15f}};
+constexpr ShapeOf kShape[kShapes] = {{256, 256, 1, 1.0, 0.9, 8.7}, {128, 128, 2, 0.82, 1.0, 6.0}, {64, 64, 4, 0.57, 0.97, 6.0}, {128, 16, 4, 0.35, 0.65, 4.0}};
 
-// The shape whose rounds over the compute units take least: ceil(tiles / (256 x per_cu)) rounds of per_cu tiles.
-inline int shape_for(int64_t m, int64_t n, int64_t slices, bool f32)
+inline double shape_cost(const ShapeOf &s, int64_t m, int64_t n, double k, int64_t count, bool f32)
+{
+    const double tiles = (double)((m + s.bm - 1) / s.bm) * (double)((n + s.bn - 1) / s.bn) * count, each = ceil(tiles / 256);
+    const double work = 2.0 * s.bm * s.bn * k / (f32 ? 0.6e6 * s.rate32 : 5.5e6 * s.rate), rounds = floor(each / s.per_cu), rest = each - rounds * s.per_cu;
+    return rounds * (s.per_cu * work + s.ends) + (rest > 0 ? rest * work / sqrt(rest / s.per_cu) + s.ends : 0.0);
+}
+
+// `count` products [m, n] over k; the least estimate goes to *cost, if that is given.  Shapes from `shapes` on are left out.
+inline int shape_for(int64_t m, int64_t n, double k, int64_t count, bool f32, double *cost = nullptr, int shapes = kShapes)
 {
     int best = 0;
     double least = 1e300;
-    for (int s = 0; s < kShapes; ++s) {
-        const ShapeOf &h = kShape[s];
-        const double tiles = (double)((m + h.bm - 1) / h.bm) * ((n + h.bn - 1) / h.bn) * slices;
-        const double cost = ceil(tiles / (256.0 * h.per_cu)) * h.per_cu * h.bm * h.bn / (f32 ? 1.0 : h.rate);
-        if (cost < least) least = cost, best = s;
+    for (int s = 0; s < shapes; ++s) {
+        const double c = shape_cost(kShape[s], m, n, k, count, f32);
+        if (c < least) least = c, best = s;
     }
+    if (cost) *cost = least;
     return best;
 }
 

@@ -29,13 +29,13 @@ def _type(t, name):
     return code
 
 
-def _on_device(**tensors):
+def _on_device(*tensors):
     """All given tensors on the current GPU: the library launches there, and reads what it is given there."""
     import torch
     here = torch.cuda.current_device()
-    for name, t in tensors.items():
+    for t in tensors:
         if t is not None and t.get_device() != here:
-            raise ValueError(f"{name} is on {t.device}: it has to be on the current GPU, cuda:{here}")
+            raise ValueError(f"a tensor {tuple(t.shape)} is on {t.device}: it has to be on the current GPU, cuda:{here}")
 
 
 def _rows(t, name):
@@ -96,7 +96,7 @@ def _check(rc, where):
 
 
 def _loss_call(hidden, weight, targets):
-    _on_device(hidden=hidden, weight=weight, targets=targets)
+    _on_device(hidden, weight, targets)
     if hidden.dtype != weight.dtype:
         raise TypeError(f"hidden is {hidden.dtype} and weight {weight.dtype}: one type is wanted")
     type_ = _type(hidden, "hidden")
@@ -145,7 +145,7 @@ def token_loss_grad(hidden, weight, targets, lse, row_weight=None, hidden_grad=N
         for name, t in (("lse", lse), ("row_weight", row_weight)):
             if t is not None and (t.dtype != torch.float32 or t.shape != (dims.N,) or not t.is_contiguous()):
                 raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}: contiguous float32 ({dims.N},) is wanted")
-        _on_device(lse=lse, row_weight=row_weight, hidden_grad=hidden_grad, weight_grad=weight_grad)
+        _on_device(lse, row_weight, hidden_grad, weight_grad)
         if accumulate and weight_grad is None:
             raise ValueError("accumulate needs a weight_grad to add to")
         if hidden_grad is None and need[0]:
@@ -173,7 +173,7 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
     of one element that the caller clears."""
     import torch
     with _on(stream):
-        _on_device(tokens=tokens, table=table, out=out, status=status)
+        _on_device(tokens, table, out, status)
         dtype = table.dtype if dtype is None else dtype
         table_type = _type(table, "table")
         table, table_stride = _rows(table, "table")
@@ -182,13 +182,15 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
             raise ValueError("status is one int32")
         shape = tuple(tokens.shape) + (D,)
         flat, flag = _tokens(tokens, "tokens", count)
-        rows = torch.empty((count, D), dtype=dtype, device=table.device) if out is None else out.view(count, D)
+        if out is None:
+            rows, rows_stride = torch.empty(shape, dtype=dtype, device=table.device), D
+        else:
+            rows, rows_stride = _result(out.view(count, D), "out", (count, D), dtype)
         rows_type = _type(rows, "rows")
-        rows, rows_stride = _result(rows, "out", (count, D), dtype)
         dims = _px.EmbedDims(count, table.shape[0], D, table_type, rows_type, flag, float(scale), table_stride, rows_stride)
         _check(_px.lib().pollux_embed(ctypes.byref(dims), flat.data_ptr(), table.data_ptr(), rows.data_ptr(), _px._ptr(status),
                                       _px._stream_handle(stream)), "pollux_embed")
-    return rows.view(shape) if out is None else out
+    return rows if out is None else out
 
 
 def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, accumulate=False, workspace=None, stream=None):
@@ -197,7 +199,7 @@ def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, acc
     are then not touched."""
     import torch
     with _on(stream):
-        _on_device(tokens=tokens, rows_grad=rows_grad, table_grad=table_grad)
+        _on_device(tokens, rows_grad, table_grad)
         count, D = tokens.numel(), rows_grad.shape[-1]
         if rows_grad.shape[:-1] != tokens.shape and rows_grad.numel() != count * D:
             raise ValueError(f"rows_grad {tuple(rows_grad.shape)} has not a row for each of the tokens {tuple(tokens.shape)}")
@@ -227,7 +229,7 @@ def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=T
     want_mean False: None in the place of the mean."""
     import torch
     with _on(stream):
-        _on_device(grads=grads, precondition=precondition)
+        _on_device(grads, precondition)
         if grads.dim() < 2:
             raise ValueError("grads holds one gradient a row: [B, ...]")
         type_, B, shape = _type(grads, "grads"), grads.shape[0], tuple(grads.shape[1:])
@@ -258,7 +260,7 @@ def orthogonalize(grads, steps=5, coefficients=(3.4445, -4.7750, 2.0315), out=No
     coefficients bring those above 1e-3 of the norm to 0.7 .. 1.2 in five steps; (1.5, -0.5, 0) converges to 1)."""
     import torch
     with _on(stream):
-        _on_device(grads=grads, out=out)
+        _on_device(grads, out)
         if grads.dim() < 2:
             raise ValueError("grads holds matrices: [..., rows, cols]")
         type_ = _type(grads, "grads")
