@@ -284,14 +284,17 @@ __global__ __launch_bounds__(256) void join_runs(const SumArgs A, T *table)
     const int first = w * A.window, last = first + A.window, run = A.keys[last - 1];
     if (run >= A.V || A.keys[last] != run) return;            // nothing is cut by this window's end
     if (A.keys[first] == run && first > 0 && A.keys[first - 1] == run) return;      // it began before
-    // windows that the run reaches: up to the one that holds its last place
-    int lo = last, hi = A.N;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (A.keys[mid] <= run) lo = mid + 1;
-        else hi = mid;
+    // whole windows that the run fills after this one, 64 looked at together, and the one in which it ends
+    int count = 1;
+    for (int u = w + 1;; u += 64) {
+        const int64_t next = ((int64_t)u + (threadIdx.x & 63) + 1) * A.window;      // the first place after a window
+        const unsigned long long over = __ballot(next >= A.N || A.keys[next] != run);
+        if (over) {
+            count += u - (w + 1) + __ffsll(over) - 1;
+            break;
+        }
     }
-    const int count = (lo - 1) / A.window - w, each = (count + 3) >> 2, u0 = w + 1 + part * each, u1 = min(w + 1 + count, u0 + each);
+    const int each = (count + 3) >> 2, u0 = w + 1 + part * each, u1 = min(w + 1 + count, u0 + each);
     f32x8 sum = {};
     if (c < A.D) {
         if (part == 0) sum = load8f(A.partial + ((int64_t)A.windows + w) * A.D + c, left);

@@ -39,6 +39,16 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // A maximum to subtract: 0 stands in for one that is infinite, so that inf - inf is never formed.
 __device__ __forceinline__ float finite_or_zero(float m) { return fabsf(m) < __builtin_inff() ? m : 0.f; }
 
+// (largest logit, sum of exponentials from it) of two sets as that of both.  The sum from a maximum of -inf is 0, or NaN.
+__device__ __forceinline__ float2 joined(float2 a, float2 b)
+{
+    const float top = fmaxf(a.x, b.x), from = finite_or_zero(top);
+    auto part = [&](float2 p) {
+        return p.y == __builtin_inff() || p.x == -__builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
+    };
+    return make_float2(top, part(a) + part(b));
+}
+
 struct LogitArgs {
     Operands o;                 // a: weights of the piece, b: hidden rows
     int first, V, N;            // the piece's first vocabulary entry
@@ -48,7 +58,7 @@ struct LogitArgs {
     // forward
     float2 *parts;              // of the piece's first tile
     float *picked;
-    int32_t *status;            // cleared by the first workgroup; null in all but the first piece
+    int32_t *status;            // of the first piece, else null: forward, the first workgroup clears it; backward, the first tiles report
     // backward
     const float *lse, *row_weight, *scale;
     void *q;
@@ -102,18 +112,10 @@ __global__ __launch_bounds__(S::kThreads) void loss_tiles(const LogitArgs A)
     for (int c = threadIdx.x; c < S::BN; c += S::kThreads) {
         const int n = t.n * S::BN + c;
         if (n >= A.N) break;
-        float top = shared[c].x;
+        float2 all = shared[c];
 #pragma unroll
-        for (int w = 1; w < S::WM; ++w) top = fmaxf(top, shared[w * S::BN + c].x);
-        const float from = finite_or_zero(top);
-        float sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < S::WM; ++w) {
-            const float2 p = shared[w * S::BN + c];
-            // (the sum from a maximum of -inf is 0, or NaN)
-            sum += p.y == __builtin_inff() || p.x == -__builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
-        }
-        A.parts[(int64_t)t.m * A.N + n] = make_float2(top, sum);
+        for (int w = 1; w < S::WM; ++w) all = joined(all, shared[w * S::BN + c]);
+        A.parts[(int64_t)t.m * A.N + n] = all;
     }
 #endif
 }
@@ -125,34 +127,26 @@ __global__ __launch_bounds__(kJoinThreads) void loss_join(const float2 *parts, i
                                                           float *lse, int32_t *status)
 {
     constexpr int kParts = kJoinThreads / TOKENS, kAhead = 4;
-    __shared__ float2 shared[kParts][TOKENS];
+    __shared__ float2 shared[kJoinThreads / 64][TOKENS];
     const int c = threadIdx.x % TOKENS, k = threadIdx.x / TOKENS, n = blockIdx.x * TOKENS + c;
-    float top = -__builtin_inff(), sum = 0.f;
+    const float2 none = make_float2(-__builtin_inff(), 0.f);
+    float2 all = none;
     if (n < N)
         for (int t0 = k; t0 < tiles; t0 += kParts * kAhead) {
             float2 p[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) p[i] = t0 + i * kParts < tiles ? parts[(int64_t)(t0 + i * kParts) * N + n] : make_float2(-__builtin_inff(), 0.f);
+            for (int i = 0; i < kAhead; ++i) p[i] = t0 + i * kParts < tiles ? parts[(int64_t)(t0 + i * kParts) * N + n] : none;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const float most = fmaxf(top, p[i].x), from = finite_or_zero(most);
-                const float x = sum == __builtin_inff() ? sum : sum * __builtin_amdgcn_exp2f((finite_or_zero(top) - from) * kLog2e);
-                const float y = p[i].y == __builtin_inff() ? p[i].y : p[i].y * __builtin_amdgcn_exp2f((finite_or_zero(p[i].x) - from) * kLog2e);
-                // (the sum from a maximum of -inf is 0, or NaN)
-                sum = (top == -__builtin_inff() ? sum : x) + (p[i].x == -__builtin_inff() ? p[i].y : y);
-                top = most;
-            }
+            for (int i = 0; i < kAhead; ++i) all = joined(all, p[i]);
         }
-    shared[k][c] = make_float2(top, sum);
+#pragma unroll
+    for (int w = TOKENS; w < 64; w <<= 1) all = joined(all, make_float2(__shfl_xor(all.x, w), __shfl_xor(all.y, w)));
+    if ((threadIdx.x & 63) < TOKENS) shared[threadIdx.x >> 6][c] = all;
     __syncthreads();
-    if (k != 0 || n >= N) return;
-    for (int i = 1; i < kParts; ++i) top = fmaxf(top, shared[i][c].x);
-    const float from = finite_or_zero(top);
-    sum = 0.f;
-    for (int i = 0; i < kParts; ++i) {
-        const float2 p = shared[i][c];
-        sum += p.y == __builtin_inff() || p.x == -__builtin_inff() ? p.y : p.y * __builtin_amdgcn_exp2f((finite_or_zero(p.x) - from) * kLog2e);
-    }
+    if (threadIdx.x >= TOKENS || n >= N) return;
+#pragma unroll
+    for (int i = 1; i < kJoinThreads / 64; ++i) all = joined(all, shared[i][c]);
+    const float from = finite_or_zero(all.x), sum = all.y;
     const float whole = from + logf(sum);
     lse[n] = whole;
     bool bad;
@@ -163,40 +157,26 @@ __global__ __launch_bounds__(kJoinThreads) void loss_join(const float2 *parts, i
 
 // ---- backward ------------------------------------------------------------------------------------------------------
 
-// Clears the status word, reports targets that are no entry, and, for fp16, finds the power of two that q is scaled by:
-// scale[0] that, scale[1] its inverse.
-template <bool SCALED>
+// Clears the status word, and, for fp16, finds the power of two that q is scaled by: scale[0] that, scale[1] its inverse.
 __global__ __launch_bounds__(1024) void grad_begin(const void *targets, bool i64, int V, int N, const float *row_weight, int32_t *status, float *scale)
 {
-    __shared__ int bad_any;
     __shared__ float tops[16];
-    if (threadIdx.x == 0) bad_any = 0;
     if (threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
-    __syncthreads();
+    if (!scale) return;
     float top = 0.f;
     for (int n = threadIdx.x; n < N; n += 1024) {
-        bool bad;
-        const int y = token_at(targets, n, i64, V, bad);
-        if (bad) bad_any = 1;
-        if (SCALED && y >= 0) {
-            const float g = row_weight ? fabsf(row_weight[n]) : 1.f;
-            if (g < __builtin_inff()) top = fmaxf(top, g);
-        }
+        const float g = target_of(targets, n, i64, V) < 0 ? 0.f : row_weight ? fabsf(row_weight[n]) : 1.f;
+        if (g < __builtin_inff()) top = fmaxf(top, g);
     }
-    if (SCALED) {
 #pragma unroll
-        for (int w = 1; w < 64; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
-        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-    }
+    for (int w = 1; w < 64; w <<= 1) top = fmaxf(top, __shfl_xor(top, w));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
     if (threadIdx.x != 0) return;
-    if (bad_any) *status = PX_ST_BAD_TOKEN;
-    if (SCALED) {
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, tops[i]);
-        const int e = top > 0.f ? min(100, max(-100, 13 - ilogbf(top))) : 0;
-        scale[0] = ldexpf(1.f, e);
-        scale[1] = ldexpf(1.f, -e);
-    }
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, tops[i]);
+    const int e = top > 0.f ? min(100, max(-100, 13 - ilogbf(top))) : 0;
+    scale[0] = ldexpf(1.f, e);
+    scale[1] = ldexpf(1.f, -e);
 }
 
 // One tile of q from the logits' tile.  A token without a target, or of weight 0, has a row of zeros,
@@ -215,7 +195,9 @@ __global__ __launch_bounds__(S::kThreads) void q_tiles(const LogitArgs A)
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
         const int n = at.first_n + j * 16;
-        const int y = n < A.N ? target_of(A.targets, n, A.i64, A.V) : -1;
+        bool bad = false;
+        const int y = n < A.N ? token_at(A.targets, n, A.i64, A.V, bad) : -1;
+        if (bad && A.status && t.m == 0) atomicOr(A.status, PX_ST_BAD_TOKEN);
         const float g = y < 0 ? 0.f : (A.row_weight ? A.row_weight[n] : 1.f) * scale;
         const float lse = y < 0 ? 0.f : A.lse[n];
         const int hit = y - A.first;
@@ -324,9 +306,10 @@ __global__ __launch_bounds__(256) void join_slices(const float *sums, int slices
 // Rows copied to aligned ones, `cols` padded with zeros to ld_to; rows without a target, or of weight 0, are copied as zeros.
 template <class E>
 __global__ __launch_bounds__(256) void pack_rows(const E *from, int64_t ld_from, int64_t rows, int cols, E *to, int64_t ld_to, const void *targets, const float *row_weight,
-                                                 bool i64, int V)
+                                                 bool i64, int V, int32_t *status)
 {
 #ifdef __HIP_DEVICE_COMPILE__
+    if (status && blockIdx.x == 0 && threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
     const int groups = (int)((ld_to + kVec - 1) / kVec);
     const int64_t total = rows * groups;
     for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
@@ -395,11 +378,11 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
     const int64_t ld_h = p.pack_hidden ? p.d_pad : d.hidden_stride, ld_w = p.pack_weight ? p.d_pad : d.weight_stride;
     int32_t *status = (int32_t *)(ws + p.status);
     if (N == 0) {
-        hipLaunchKernelGGL(grad_begin<false>, dim3(1), dim3(1024), 0, stream, targets, false, d.V, 0, (const float *)nullptr, status, (float *)nullptr);
+        hipLaunchKernelGGL(grad_begin, dim3(1), dim3(1024), 0, stream, targets, false, d.V, 0, (const float *)nullptr, status, (float *)nullptr);
         return status_of(hipGetLastError());
     }
     if (p.pack_hidden) {
-        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
+        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr);
         hidden = ws + p.hidden;
     }
     LogitArgs a = {};
@@ -419,7 +402,7 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
         a.rows = a.o.m = std::min(p.piece, d.V - a.first);
         const char *from = weight + (int64_t)a.first * d.weight_stride * e;
         if (p.pack_weight) {
-            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr);
             from = ws + p.weight;
         }
         a.o.a = from;
@@ -449,7 +432,8 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
     const bool i64 = d.flags & PX_FLAG_TOKENS_I64;
     int32_t *status = (int32_t *)(ws + p.status);
     float *scale = scaled ? (float *)(ws + p.top) : nullptr;
-    hipLaunchKernelGGL(grad_begin<scaled>, dim3(1), dim3(1024), 0, stream, targets, i64, d.V, N, row_weight, status, scale);
+    // (elsewhere the first of the copies below clears the status word)
+    if (scaled || N == 0) hipLaunchKernelGGL(grad_begin, dim3(1), dim3(1024), 0, stream, targets, i64, d.V, N, row_weight, status, scale);
     if (N == 0) {
         if (weight_grad && !(d.flags & PX_FLAG_ACCUMULATE)) {      // products over no tokens
             GradArgs g = {};
@@ -463,7 +447,7 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
     }
     // (a product with q's zeros would still be NaN where a row that counts for nothing holds one)
     hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D,
-                       (type *)(ws + p.hidden), p.d_pad, targets, row_weight, i64, d.V);
+                       (type *)(ws + p.hidden), p.d_pad, targets, row_weight, i64, d.V, status);
     LogitArgs a = {};
     a.targets = targets;
     a.i64 = i64;
@@ -484,10 +468,11 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
         a.rows = a.o.m = std::min(p.piece, d.V - a.first);
         const char *from = weight + (int64_t)a.first * d.weight_stride * e;
         if (p.pack_weight) {
-            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0);
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr);
             from = ws + p.weight;
         }
         a.o.a = from;
+        a.status = k == 0 ? status : nullptr;
         launch_logits<T>(p.tiles, kQ, a, stream);
         if (hidden_grad) {
             GradArgs g = {};
