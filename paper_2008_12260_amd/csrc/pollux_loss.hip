@@ -343,7 +343,8 @@ void launch_logits(int shape, LogitKind kind, const LogitArgs &a, hipStream_t st
         case 0: launch_logits<Shape0<T>>(kind, a, stream); break;
         case 1: launch_logits<Shape1<T>>(kind, a, stream); break;
         case 2: launch_logits<Shape2<T>>(kind, a, stream); break;
-        default: launch_logits<Shape3<T>>(kind, a, stream); break;
+        case 3: launch_logits<Shape3<T>>(kind, a, stream); break;
+        default: launch_logits<Shape4<T>>(kind, a, stream); break;
     }
 }
 template <class S>
@@ -362,7 +363,8 @@ void launch_grad(int shape, const GradArgs &a, int slices, hipStream_t stream)
         case 0: launch_grad<Shape0<T, true, COLS_B>>(a, slices, stream); break;
         case 1: launch_grad<Shape1<T, true, COLS_B>>(a, slices, stream); break;
         case 2: launch_grad<Shape2<T, true, COLS_B>>(a, slices, stream); break;
-        default: launch_grad<Shape3<T, true, COLS_B>>(a, slices, stream); break;
+        case 3: launch_grad<Shape3<T, true, COLS_B>>(a, slices, stream); break;
+        default: launch_grad<Shape4<T, true, COLS_B>>(a, slices, stream); break;
     }
 }
 

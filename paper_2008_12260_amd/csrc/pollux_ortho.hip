@@ -146,7 +146,9 @@ void launch_step(int shape, const StepArgs &a, int batch, hipStream_t stream)
     switch (shape) {
         case 0: launch_step<Shape0<F16, COLS_A, COLS_B>>(a, batch, stream); break;
         case 1: launch_step<Shape1<F16, COLS_A, COLS_B>>(a, batch, stream); break;
-        default: launch_step<Shape2<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        case 2: launch_step<Shape2<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        case 3: launch_step<Shape3<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        default: launch_step<Shape4<F16, COLS_A, COLS_B>>(a, batch, stream); break;
     }
 }
 
@@ -241,8 +243,8 @@ OrthoPlan ortho_plan(const pollux_ortho_dims &d)
     p.x_pad = (d.cols + 7) / 8 * 8;
     p.unit = ldexp(1.0, (int)lround(0.5 * log2((double)p.n)));
     p.norm_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / std::max(d.batch, 1), (int64_t)d.rows * d.cols / 8192));
-    p.shape_square = shape_for(p.m, p.m, 0.5 * (p.m + p.n), d.batch, false, nullptr, 3);
-    p.shape_wide = shape_for(d.cols, d.rows, p.m, d.batch, false, nullptr, 3);
+    p.shape_square = shape_for(p.m, p.m, 0.5 * (p.m + p.n), d.batch, false);
+    p.shape_wide = shape_for(d.cols, d.rows, p.m, d.batch, false);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
     p.norms = take(std::max<size_t>(8, 8 * (size_t)d.batch * p.norm_blocks));

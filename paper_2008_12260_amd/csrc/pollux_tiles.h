@@ -4,7 +4,7 @@
 // contiguous): a product with a transposed matrix needs no transposed copy.
 //
 // A stage of k (128 bytes of a row: 64 elements of 16 bits, 32 of 32 bits) comes into LDS by loads that write LDS directly,
-// two stages in turn.  What a load writes is in the order of its lanes, so it is the address a lane loads from that is permuted:
+// two stages in turn, five of the smallest tiles, which would otherwise wait for every one.  What a load writes is in the order of its lanes, so it is the address a lane loads from that is permuted:
 // * rows: a row's eight 16-byte pieces lie in the order piece ^ (row & 7); the sixteen rows' pieces that a wavefront reads
 //   together then touch every bank once.
 // * columns: a row of k is BM (BN) elements; its pieces lie in the order piece ^ f(k), which puts the four rows of k that sixteen lanes read
@@ -17,6 +17,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 namespace px {
 
@@ -64,33 +66,40 @@ __device__ __forceinline__ Tile tile_of(int block, int tiles_m, int tiles_n, int
     return {first + rest % size, rest / size};
 }
 
-template <class T, int BM_, int BN_, int WM_, int WN_, bool COLS_A_ = false, bool COLS_B_ = false>
+template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool COLS_A_ = false, bool COLS_B_ = false>
 struct TileShape {
     typedef T element;
     static constexpr bool COLS_A = COLS_A_, COLS_B = COLS_B_;     // the operand lies in memory as its columns
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr int kThreads = WM * WN * 64, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-    static constexpr int kStage = (BM + BN) * kRowBytes, kLds = 2 * kStage;
+    static constexpr int kStages = STAGES_, kStage = (BM + BN) * kRowBytes, kLds = kStages * kStage;
     static constexpr int kLoadsA = BM * kRowBytes / (kThreads * 16), kLoadsB = BN * kRowBytes / (kThreads * 16);
     static_assert(kLoadsA * kThreads * 16 == BM * kRowBytes && kLoadsB * kThreads * 16 == BN * kRowBytes, "whole loads");
 };
 
 // Which shape of tile a product is formed in, and in how many slices of k: by what it is estimated to take, in microseconds.  A compute unit works on
-// per_cu tiles of a shape at once, at `rate` of 5.5 TFLOP/s (fp32: rate32 of 0.6) together, r of them at (r / per_cu)^(1/2) of that, and a
-// round of tiles begins and ends in `ends`: fitted to products of 64 to 2048 x 8192 to 65536 x 512 to 2048 and within about 15 % of them (bfloat16
-// 2048 x 32768 x 1024: 133, 170, 235, 407 us in the four shapes, 512 x 8192 x 512: 21, 12.5, 11.6, 19.6).
-constexpr int kShapes = 4;
+// per_cu tiles of a shape at once; a stage takes `alone` for one of them and `full` for per_cu (16 bits; in fp32 the matrix units are the bound, at
+// rate32 of 0.6 TFLOP/s), and a round of tiles begins and ends in `ends`.  Fitted to products of 64 to 2048 x 384 to 65536 x 64 to 8192 and within some 20 % of
+// them: bfloat16 2048 x 32768 x 1024 133, 170, 235, 407, 275 us in the five shapes, 1500 x 50000 x 1000 180, 229, 328, 624, 352, 512 x 8192 x 512 21, 12.5,
+// 11.5, 19.4, 15, 1024 x 1024 x 1024 31, 16, 12, 12, 9.
+constexpr int kShapes = 5;
 struct ShapeOf {
     int bm, bn, per_cu;
-    double rate, rate32, ends;
+    double alone, full, rate32, ends;
 };
-constexpr ShapeOf kShape[kShapes] = {{256, 256, 1, 1.0, 0.9, 8.7}, {128, 128, 2, 0.82, 1.0, 6.0}, {64, 64, 4, 0.57, 0.97, 6.0}, {128, 16, 4, 0.35, 0.65, 4.0}};
+constexpr ShapeOf kShape[kShapes] = {
+    {256, 256, 1, 1.53, 1.53, 0.90, 8.7}, {128, 128, 2, 0.80, 0.93, 1.00, 6.0}, {64, 64, 4, 0.45, 0.67, 0.97, 4.5}, {128, 16, 4, 0.45, 0.65, 0.65, 5.5}, {64, 64, 2, 0.28, 0.60, 0.92, 4.5}};
 
 inline double shape_cost(const ShapeOf &s, int64_t m, int64_t n, double k, int64_t count, bool f32)
 {
     const double tiles = (double)((m + s.bm - 1) / s.bm) * (double)((n + s.bn - 1) / s.bn) * count, each = ceil(tiles / 256);
-    const double work = 2.0 * s.bm * s.bn * k / (f32 ? 0.6e6 * s.rate32 : 5.5e6 * s.rate), rounds = floor(each / s.per_cu), rest = each - rounds * s.per_cu;
-    return rounds * (s.per_cu * work + s.ends) + (rest > 0 ? rest * work / sqrt(rest / s.per_cu) + s.ends : 0.0);
+    const double stages = ceil(k / (f32 ? 32 : 64)), rounds = floor(each / s.per_cu), rest = each - rounds * s.per_cu;
+    auto round = [&](double at_once) {
+        double stage = s.per_cu > 1 ? s.alone + (s.full - s.alone) * (at_once - 1) / (s.per_cu - 1) : s.full;
+        if (f32) stage = fmax(stage, at_once * 2.0 * s.bm * s.bn * 32 / (0.6e6 * s.rate32));
+        return stages * stage + s.ends;
+    };
+    return rounds * round(s.per_cu) + (rest > 0 ? round(rest) : 0.0);
 }
 
 // `count` products [m, n] over k; the least estimate goes to *cost, if that is given.  Shapes from `shapes` on are left out.
@@ -107,13 +116,15 @@ inline int shape_for(int64_t m, int64_t n, double k, int64_t count, bool f32, do
 }
 
 template <class T, bool COLS_A = false, bool COLS_B = false>
-using Shape0 = TileShape<T, 256, 256, 2, 4, COLS_A, COLS_B>;
+using Shape0 = TileShape<T, 256, 256, 2, 4, 2, COLS_A, COLS_B>;
 template <class T, bool COLS_A = false, bool COLS_B = false>
-using Shape1 = TileShape<T, 128, 128, 2, 2, COLS_A, COLS_B>;
+using Shape1 = TileShape<T, 128, 128, 2, 2, 2, COLS_A, COLS_B>;
 template <class T, bool COLS_A = false, bool COLS_B = false>
-using Shape2 = TileShape<T, 64, 64, 2, 2, COLS_A, COLS_B>;
+using Shape2 = TileShape<T, 64, 64, 2, 2, 2, COLS_A, COLS_B>;
 template <class T, bool COLS_A = false, bool COLS_B = false>
-using Shape3 = TileShape<T, 128, 16, 2, 1, COLS_A, COLS_B>;
+using Shape3 = TileShape<T, 128, 16, 2, 1, 2, COLS_A, COLS_B>;
+template <class T, bool COLS_A = false, bool COLS_B = false>
+using Shape4 = TileShape<T, 64, 64, 2, 2, 5, COLS_A, COLS_B>;
 
 #ifdef __HIP_DEVICE_COMPILE__
 
@@ -257,13 +268,13 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
     SideB side_b(o.b, o.ldb, t.n * S::BN, o.n, o.k, wave % S::WN * S::TN);
     const int stages = side_a.stages;
     constexpr int kBytesA = S::BM * kRowBytes;
-    auto load = [&](int stage) {
-        lds_char *to = lds + (stage & 1) * S::kStage;
+    auto load = [&](int stage, int at) {
+        lds_char *to = lds + at * S::kStage;
         side_a.load(stage, to);
         side_b.load(stage, to + kBytesA);
     };
-    auto read = [&](int stage, int half, piece (&a)[S::FM], piece (&b)[S::FN]) {
-        const lds_char *from = lds + (stage & 1) * S::kStage;
+    auto read = [&](int at, int half, piece (&a)[S::FM], piece (&b)[S::FN]) {
+        const lds_char *from = lds + at * S::kStage;
         side_b.read(from + kBytesA, half, b);
         side_a.read(from, half, a);
     };
@@ -273,11 +284,14 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
 #pragma unroll
             for (int j = 0; j < S::FN; ++j) acc[i][j] = multiply(a[i], b[j], acc[i][j]);
     };
-    auto wait_for_all = [] {
-        // this wavefront's loads have arrived and what it read is in registers; after the barrier, everybody's
+    constexpr int kLoads = SideA::kLoads + SideB::kLoads, kAhead = (S::kStages - 2) * kLoads;
+    static_assert(kAhead < 64, "counted by the hardware");
+    auto wait = [](auto ahead) {
+        // all but `ahead` of this wavefront's loads have arrived and what it read is in registers; after the barrier, everybody's
+        constexpr int n = decltype(ahead)::value;
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);         // (nothing is moved across)
-        __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt((n & 15) | 0x70 | n >> 4 << 14);        // vmcnt(n) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
@@ -289,17 +303,21 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
         for (int j = 0; j < S::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (stages == 0) return;
     // Half a stage ahead: while one half is multiplied, the other is on its way from LDS to registers; the barrier stands between the
-    // halves, when the whole stage has been read: the loads of the stage after next go where it was.
-    constexpr int kReads = SideA::kReads + SideB::kReads, kLoads = SideA::kLoads + SideB::kLoads, kProducts = S::FM * S::FN * (SideA::kSize == 4 ? 4 : 1);
+    // halves, when the whole stage has been read: the loads of the stage kStages later go where it was.
+    constexpr int kReads = SideA::kReads + SideB::kReads, kProducts = S::FM * S::FN * (SideA::kSize == 4 ? 4 : 1);
     constexpr int kPerRead = kProducts / (kReads + 4) > 0 ? kProducts / (kReads + 4) : 1, kPerLoad = kPerRead;
     constexpr int kMatrix = 0x008, kVector = 0x010, kLds = 0x100;         // the scheduler's groups of instructions
     piece a0[S::FM], b0[S::FN], a1[S::FM], b1[S::FN];
-    load(0);
-    wait_for_all();
-    load(1);
+    typedef std::integral_constant<int, kAhead> some;
+    typedef std::integral_constant<int, 0> all;
+#pragma unroll
+    for (int s = 0; s < S::kStages - 1; ++s) load(s, s);
+    wait(some());
+    load(S::kStages - 1, S::kStages - 1);
     read(0, 0, a0, b0);
+    int at = 0;
     for (int s = 0; s < stages; ++s) {
-        read(s, 1, a1, b1);
+        read(at, 1, a1, b1);
         multiply_all(a0, b0);
 #pragma unroll
         for (int i = 0; i < kReads; ++i) {
@@ -307,9 +325,10 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
             __builtin_amdgcn_sched_group_barrier(kMatrix, kPerRead, 0);
         }
         __builtin_amdgcn_sched_group_barrier(kMatrix, kProducts, 0);
-        wait_for_all();
-        load(s + 2);
-        read(s + 1, 0, a0, b0);
+        wait(some());
+        load(s + S::kStages, at);
+        at = at + 1 == S::kStages ? 0 : at + 1;
+        read(at, 0, a0, b0);
         multiply_all(a1, b1);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -324,7 +343,7 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
         __builtin_amdgcn_sched_group_barrier(kMatrix, kProducts, 1);
     }
     // the loads of stages past the end write zeros: nobody else's data may be there before they have
-    wait_for_all();
+    wait(all());
 }
 
 // Four values in the lane's own row n, as stored: contiguous in m.
