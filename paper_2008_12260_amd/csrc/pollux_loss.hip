@@ -80,6 +80,7 @@ __global__ __launch_bounds__(S::kThreads) void loss_tiles(const LogitArgs A)
     tile_product<S>(A.o, t, lds, acc);
     const Place<S> at(t);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, left = A.o.m;
+    const bool edge = (t.m + 1) * S::BM > left;
     float2 *const shared = (float2 *)lds;        // [WM][BN]
     __syncthreads();
 #pragma unroll
@@ -88,14 +89,16 @@ __global__ __launch_bounds__(S::kThreads) void loss_tiles(const LogitArgs A)
         const int y = n < A.N ? target_of(A.targets, n, A.i64, A.V) - A.first : -1;
         float top = -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i)
+        for (int i = 0; i < S::FM; ++i) {
+            const int v = at.first_m + 16 * i;
+            if (edge)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int v = at.first_m + 16 * i + r;
-                if (v >= left) acc[i][j][r] = -__builtin_inff();
-                top = fmaxf(top, acc[i][j][r]);
-                if (v == y && v < left) A.picked[n] = acc[i][j][r];
-            }
+                for (int r = 0; r < 4; ++r)
+                    if (v + r >= left) acc[i][j][r] = -__builtin_inff();
+            if (y >= v && y < min(v + 4, left)) A.picked[n] = y == v ? acc[i][j][0] : y == v + 1 ? acc[i][j][1] : y == v + 2 ? acc[i][j][2] : acc[i][j][3];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
+        }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float from = finite_or_zero(top);
@@ -192,6 +195,9 @@ __global__ __launch_bounds__(S::kThreads) void q_tiles(const LogitArgs A)
     tile_product<S>(A.o, t, lds, acc);
     const Place<S> at(t);
     const float scale = A.scale ? A.scale[0] : 1.f;
+    const bool edge = (t.m + 1) * S::BM > A.rows;
+    const Pair pair;
+    const int wave_m = at.first_m - (threadIdx.x >> 4 & 3) * 4;
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
         const int n = at.first_n + j * 16;
@@ -199,18 +205,34 @@ __global__ __launch_bounds__(S::kThreads) void q_tiles(const LogitArgs A)
         const int y = n < A.N ? token_at(A.targets, n, A.i64, A.V, bad) : -1;
         if (bad && A.status && t.m == 0) atomicOr(A.status, PX_ST_BAD_TOKEN);
         const float g = y < 0 ? 0.f : (A.row_weight ? A.row_weight[n] : 1.f) * scale;
-        const float lse = y < 0 ? 0.f : A.lse[n];
+        const float lse = g == 0.f ? 0.f : A.lse[n];
         const int hit = y - A.first;
-#pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
+        auto value = [&](int i) {
             const int v = at.first_m + 16 * i;
             f32x4 q;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e) - (v + r == hit ? 1.f : 0.f);
-                q[r] = g != 0.f && v + r < A.rows ? p * g : 0.f;
+            for (int r = 0; r < 4; ++r) q[r] = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * kLog2e) * g;
+            if (hit >= v && hit < v + 4)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) q[r] -= v + r == hit ? g : 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) q[r] = g != 0.f && (!edge || v + r < A.rows) ? q[r] : 0.f;
+            return q;
+        };
+        type *const row = (type *)A.q + (int64_t)n * A.ld_q;
+        if constexpr (sizeof(type) == 2 && S::FM % 2 == 0) {
+#pragma unroll
+            for (int i = 0; i < S::FM; i += 2) {
+                const auto both = paired<typename S::element>(value(i), value(i + 1));
+                const int v = wave_m + 16 * (i + pair.tile) + pair.row;
+                if (n < A.N && v < A.ld_q) *(typename S::element::piece *)(row + v) = both;
             }
-            if (n < A.N && v < A.ld_q) store4<typename S::element>((type *)A.q + (int64_t)n * A.ld_q + v, q);
+        } else {
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int v = at.first_m + 16 * i;
+                if (n < A.N && v < A.ld_q) store4<typename S::element>(row + v, value(i));
+            }
         }
     }
 #endif
@@ -233,17 +255,21 @@ struct GradArgs {
 };
 
 #ifdef __HIP_DEVICE_COMPILE__
-template <class T>
-__device__ __forceinline__ void put(typename T::type *to, f32x4 v, int left, bool whole, bool add)
+// Neighbouring values into a row of which `left` elements remain, added to what it holds if `add`; whole: such groups are aligned.
+template <class T, int COUNT>
+__device__ __forceinline__ void put(typename T::type *to, const float (&v)[COUNT], int left, bool whole, bool add)
 {
     typedef typename T::type type;
-    typedef type vec __attribute__((ext_vector_type(4)));
-    if (whole && left >= 4) {
-        if (add) v += __builtin_convertvector(*(const vec *)to, f32x4);
-        store4<T>(to, v);
+    typedef type vec __attribute__((ext_vector_type(COUNT)));
+    if (whole && left >= COUNT) {
+        vec old = {}, t;
+        if (add) old = *(const vec *)to;
+#pragma unroll
+        for (int r = 0; r < COUNT; ++r) t[r] = (type)(add ? v[r] + (float)old[r] : v[r]);
+        *(vec *)to = t;
     } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < COUNT; ++r)
             if (r < left) to[r] = (type)(add ? v[r] + (float)to[r] : v[r]);
     }
 }
@@ -265,23 +291,49 @@ __global__ __launch_bounds__(S::kThreads) void grad_tiles(const GradArgs A)
     tile_product<S>(o, t, lds, acc);
     const Place<S> at(t);
     const float scale = A.scale ? A.scale[1] : 1.f;
-    const bool whole = A.sums ? (A.cols & 3) == 0 : (A.ld & 3) == 0 && ((uintptr_t)A.out & (4 * sizeof(type) - 1)) == 0;
+    constexpr bool kPairs = sizeof(type) == 2 && S::FM % 2 == 0;
+    const Pair pair;
+    const int wave_m = at.first_m - (threadIdx.x >> 4 & 3) * 4;
+    const int group = A.sums || !kPairs ? 3 : 7;
+    const bool whole = A.sums ? (A.cols & group) == 0 : (A.ld & group) == 0 && ((uintptr_t)A.out & 15) == 0;
+    const bool plain = whole && !A.add && (t.m + 1) * S::BM <= A.cols;
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
         const int n = at.first_n + j * 16;
         if (n >= A.rows) continue;
         bool none = false;
         if (A.targets && !A.sums) none = target_of(A.targets, n, A.i64, A.V) < 0 || (A.row_weight && A.row_weight[n] == 0.f);
+        if (A.sums) {
+            float *const row = (float *)A.out + ((int64_t)blockIdx.y * A.rows + n) * A.cols;
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
-            const int m = at.first_m + 16 * i, left = A.cols - m;
-            if (left <= 0) continue;
-            if (A.sums) {
-                put<F32>((float *)A.out + ((int64_t)blockIdx.y * A.rows + n) * A.cols + m, acc[i][j], left, whole, A.sums == 2);
-            } else {
-                f32x4 v = acc[i][j] * scale;
-                if (none) v = f32x4{0.f, 0.f, 0.f, 0.f};
-                put<typename S::element>((type *)A.out + (int64_t)n * A.ld + m, v, left, whole, A.add);
+            for (int i = 0; i < S::FM; ++i) {
+                const int m = at.first_m + 16 * i;
+                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                put<F32>(row + m, v, A.cols - m, whole, A.sums == 2);
+            }
+            continue;
+        }
+        type *const row = (type *)A.out + (int64_t)n * A.ld;
+        auto value = [&](int i, int r) { return none ? 0.f : acc[i][j][r] * scale; };
+        if constexpr (kPairs) {
+#pragma unroll
+            for (int i = 0; i < S::FM; i += 2) {
+                const f32x4 first = {value(i, 0), value(i, 1), value(i, 2), value(i, 3)}, second = {value(i + 1, 0), value(i + 1, 1), value(i + 1, 2), value(i + 1, 3)};
+                const int m = wave_m + 16 * (i + pair.tile) + pair.row;
+                if (plain) {                               // (the same for all lanes, which change places)
+                    *(typename S::element::piece *)(row + m) = paired<typename S::element>(first, second);
+                } else {
+                    float v[8];
+                    paired32(first, second, v);
+                    put<typename S::element>(row + m, v, A.cols - m, whole, A.add);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int m = at.first_m + 16 * i;
+                const float v[4] = {value(i, 0), value(i, 1), value(i, 2), value(i, 3)};
+                put<typename S::element>(row + m, v, A.cols - m, whole, A.add);
             }
         }
     }

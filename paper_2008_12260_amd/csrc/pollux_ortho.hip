@@ -103,30 +103,42 @@ __global__ __launch_bounds__(S::kThreads) void step_tiles(const StepArgs A)
     f32x4 acc[S::FM][S::FN];
     tile_product<S>(o, t, lds, acc);
     const Place<S> at(t);
-    const bool whole = (A.ld_last & 3) == 0 && (A.batch_last & 3) == 0 && ((uintptr_t)A.last & 7) == 0;
+    const bool whole = (A.ld_last & 7) == 0 && (A.batch_last & 7) == 0 && ((uintptr_t)A.last & 15) == 0;
+    static_assert(S::FM % 2 == 0, "tiles in pairs");
+    const Pair pair;
+    const int wave_m = at.first_m - (threadIdx.x >> 4 & 3) * 4;
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
         const int n = at.first_n + j * 16;
+        if (n >= A.rows) continue;
 #pragma unroll
-        for (int i = 0; i < S::FM; ++i) {
-            const int m = at.first_m + 16 * i;
-            f32x4 v = acc[i][j] * A.by;
+        for (int i = 0; i < S::FM; i += 2) {
+            float v[8];
+            paired32(acc[i][j], acc[i + 1][j], v);
+            const int m = wave_m + 16 * (i + pair.tile) + pair.row;
+            if (m >= A.ld) continue;
             const int64_t here = (batch * A.rows + n) * A.ld + m;
-            const bool inside = n < A.rows && m < A.ld;
-            if (A.base && inside) v += A.plus * __builtin_convertvector(*(const f16x4 *)(A.base + here), f32x4);
-            if (A.last) {
-                if (n >= A.rows) continue;
-                __bf16 *to = A.last + batch * A.batch_last + (int64_t)n * A.ld_last + m;
-                if (whole && m + 4 <= A.cols) store4<Bf16>(to, v);
-                else
-                    for (int r = 0; r < 4; ++r)
-                        if (m + r < A.cols) to[r] = (__bf16)v[r];
-                continue;
-            }
+            f16x8 base = {};
+            if (A.base) base = *(const f16x8 *)(A.base + here);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (m + r >= A.cols || n >= A.rows) v[r] = 0.f;
-            if (inside) store4<F16>(A.out + here, v);
+            for (int r = 0; r < 8; ++r) v[r] = v[r] * A.by + A.plus * (float)base[r];
+            if (A.last) {
+                __bf16 *to = A.last + batch * A.batch_last + (int64_t)n * A.ld_last + m;
+                if (whole && m + 8 <= A.cols) {
+                    bf16x8 t;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) t[r] = (__bf16)v[r];
+                    *(bf16x8 *)to = t;
+                } else {
+                    for (int r = 0; r < 8; ++r)
+                        if (m + r < A.cols) to[r] = (__bf16)v[r];
+                }
+            } else {
+                f16x8 t;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) t[r] = (_Float16)(m + r < A.cols ? v[r] : 0.f);
+                *(f16x8 *)(A.out + here) = t;
+            }
         }
     }
 #endif

@@ -354,6 +354,35 @@ __device__ __forceinline__ void store4(typename T::type *to, f32x4 v)
     *(vec *)to = __builtin_convertvector(v, vec);
 }
 
+// Of 16 bits, two neighbouring tiles' values as eight contiguous in m: the sixteen lanes of rows 4 .. 7 (12 .. 15) of the first tile change places with
+// those of rows 0 .. 3 (8 .. 11) of the second.  The lane's values are then of tile first + `tile`, rows `row` .. row + 7, and a row's 64 bytes go out in one store
+// where two would write 32 each.
+struct Pair {
+    int tile, row;
+    __device__ __forceinline__ Pair() : tile(threadIdx.x >> 4 & 1), row((threadIdx.x >> 5 & 1) * 8) {}
+};
+template <class T>
+__device__ __forceinline__ typename T::piece paired(f32x4 first, f32x4 second)
+{
+    typedef typename T::type vec __attribute__((ext_vector_type(4)));
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_convertvector(first, vec)), b = __builtin_bit_cast(u32x2, __builtin_convertvector(second, vec));
+    const auto low = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), high = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    return __builtin_bit_cast(typename T::piece, u32x4{low[0], high[0], low[1], high[1]});
+}
+
+// The same before rounding.
+__device__ __forceinline__ void paired32(f32x4 first, f32x4 second, float (&to)[8])
+{
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(first[r]), __float_as_uint(second[r]), false, false);
+        to[r] = __uint_as_float(both[0]);
+        to[r + 4] = __uint_as_float(both[1]);
+    }
+}
+
 #endif
 
 }  // namespace px
