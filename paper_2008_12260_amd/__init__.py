@@ -156,6 +156,11 @@ def _ptr(t):
 _raw_stream = None
 
 
+def _current_device():
+    import torch
+    return torch._C._cuda_getDevice() if _raw_stream is not None and hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device()
+
+
 def _stream_handle(stream):
     if stream is not None:
         return stream.cuda_stream

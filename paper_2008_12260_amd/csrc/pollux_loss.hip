@@ -11,8 +11,10 @@
 // gradient is summed over pieces in fp32 (and over slices of a piece where few tiles would leave the chip idle), in a
 // fixed order, and rounded once (join_slices).
 //
-// q is rounded to the type of the inputs because the matrix units take it so: half a step of that type per element, as large
-// as the rounding of the result.  fp16 has too few exponents for q (a mean over 10^4 tokens of probabilities of 10^-6): there q is
+// q is rounded to the type of the inputs because the matrix units take it so: half a step of that type per element.  A token's
+// largest q by far is its target's, as large as all others together: what its rounding leaves is kept in fp32 (`rest`) and multiplied with the target's weights
+// where the hidden rows' gradient is rounded, which brings that gradient's error from 1.35 times that of its own rounding to what the rounding leaves.
+// fp16 has too few exponents for q (a mean over 10^4 tokens of probabilities of 10^-6): there q is
 // scaled by the power of two that brings the largest row weight to 2^13, and the gradients are scaled back in fp32.
 
 #include "pollux_host.h"
@@ -62,6 +64,7 @@ struct LogitArgs {
     // backward
     const float *lse, *row_weight, *scale;
     void *q;
+    float *rest;                // [N]: the target's q less what it was rounded to; null (fp32): nothing is lost
     int64_t ld_q;               // elements
     int rows;                   // entries of the piece
 };
@@ -217,6 +220,11 @@ __global__ __launch_bounds__(S::kThreads) void q_tiles(const LogitArgs A)
                 for (int r = 0; r < 4; ++r) q[r] -= v + r == hit ? g : 0.f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) q[r] = g != 0.f && (!edge || v + r < A.rows) ? q[r] : 0.f;
+            if constexpr (sizeof(type) == 2)
+                if (hit >= v && hit < v + 4) {
+                    const float whole = hit == v ? q[0] : hit == v + 1 ? q[1] : hit == v + 2 ? q[2] : q[3], lost = whole - (float)(type)whole;
+                    A.rest[n] = fabsf(lost) < __builtin_inff() ? lost : 0.f;
+                }
             return q;
         };
         type *const row = (type *)A.q + (int64_t)n * A.ld_q;
@@ -252,9 +260,24 @@ struct GradArgs {
     const float *row_weight;
     bool i64;
     int V;
+    const float *rest;          // [N], and the weights it multiplies (elements from row to row); null: nothing
+    const void *weight;
+    int64_t ld_weight;
 };
 
 #ifdef __HIP_DEVICE_COMPILE__
+// v += rest * the target's weights, of which `left` remain in the row.  (An infinite weight has made its logit, and the row, what it is already.)
+template <class E, class V>
+__device__ __forceinline__ void add_rest(V &v, float rest, const E *weight, int64_t left)
+{
+    const f32x8 w = load8f(weight, left);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const float more = rest * w[r];
+        v[r] += fabsf(more) < __builtin_inff() ? more : 0.f;
+    }
+}
+
 // Neighbouring values into a row of which `left` elements remain, added to what it holds if `add`; whole: such groups are aligned.
 template <class T, int COUNT>
 __device__ __forceinline__ void put(typename T::type *to, const float (&v)[COUNT], int left, bool whole, bool add)
@@ -296,13 +319,17 @@ __global__ __launch_bounds__(S::kThreads) void grad_tiles(const GradArgs A)
     const int wave_m = at.first_m - (threadIdx.x >> 4 & 3) * 4;
     const int group = A.sums || !kPairs ? 3 : 7;
     const bool whole = A.sums ? (A.cols & group) == 0 : (A.ld & group) == 0 && ((uintptr_t)A.out & 15) == 0;
-    const bool plain = whole && !A.add && (t.m + 1) * S::BM <= A.cols;
+    const bool plain = whole && !A.add && !A.rest && (t.m + 1) * S::BM <= A.cols;
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
         const int n = at.first_n + j * 16;
         if (n >= A.rows) continue;
         bool none = false;
-        if (A.targets && !A.sums) none = target_of(A.targets, n, A.i64, A.V) < 0 || (A.row_weight && A.row_weight[n] == 0.f);
+        int y = -1;
+        if (A.targets && !A.sums) {
+            y = target_of(A.targets, n, A.i64, A.V);
+            none = y < 0 || (A.row_weight && A.row_weight[n] == 0.f);
+        }
         if (A.sums) {
             float *const row = (float *)A.out + ((int64_t)blockIdx.y * A.rows + n) * A.cols;
 #pragma unroll
@@ -316,6 +343,8 @@ __global__ __launch_bounds__(S::kThreads) void grad_tiles(const GradArgs A)
         type *const row = (type *)A.out + (int64_t)n * A.ld;
         auto value = [&](int i, int r) { return none ? 0.f : acc[i][j][r] * scale; };
         if constexpr (kPairs) {
+            const float rest = A.rest && !none ? A.rest[n] * scale : 0.f;
+            const type *const target = (const type *)A.weight + (int64_t)max(y, 0) * A.ld_weight;
 #pragma unroll
             for (int i = 0; i < S::FM; i += 2) {
                 const f32x4 first = {value(i, 0), value(i, 1), value(i, 2), value(i, 3)}, second = {value(i + 1, 0), value(i + 1, 1), value(i + 1, 2), value(i + 1, 3)};
@@ -325,6 +354,7 @@ __global__ __launch_bounds__(S::kThreads) void grad_tiles(const GradArgs A)
                 } else {
                     float v[8];
                     paired32(first, second, v);
+                    if (rest != 0.f && m < A.cols) add_rest(v, rest, target + m, A.cols - m);
                     put<typename S::element>(row + m, v, A.cols - m, whole, A.add);
                 }
             }
@@ -340,19 +370,28 @@ __global__ __launch_bounds__(S::kThreads) void grad_tiles(const GradArgs A)
 #endif
 }
 
-// The slices' sums, added in their order and rounded.
+// The slices' sums, added in their order, and the targets' rests; rounded.
 template <class T>
-__global__ __launch_bounds__(256) void join_slices(const float *sums, int slices, int64_t N, int D, const float *scale, const void *targets,
-                                                   const float *row_weight, bool i64, int V, typename T::type *out, int64_t ld)
+__global__ __launch_bounds__(256) void join_slices(const GradArgs A, const float *sums, int slices, int64_t N, int D)
 {
-    const int64_t total = N * D;
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef typename T::type type;
+    const int groups = (D + kVec - 1) / kVec;
+    const int64_t total = N * groups;
     for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
-        const int64_t n = at / D;
-        float v = sums[at];
-        for (int s = 1; s < slices; ++s) v += sums[s * total + at];
-        const bool none = target_of(targets, n, i64, V) < 0 || (row_weight && row_weight[n] == 0.f);
-        out[n * ld + (at - n * D)] = (typename T::type)(none ? 0.f : v * (scale ? scale[1] : 1.f));
+        const int64_t n = at / groups;
+        const int c = (int)(at - n * groups) * kVec;
+        const float *from = sums + n * D + c;
+        f32x8 v = load8f(from, D - c);
+#pragma unroll 4
+        for (int s = 1; s < slices; ++s) v += load8f(from + s * N * D, D - c);
+        const int y = target_of(A.targets, n, A.i64, A.V);
+        const bool none = y < 0 || (A.row_weight && A.row_weight[n] == 0.f);
+        if (A.rest && !none) add_rest(v, A.rest[n], (const type *)A.weight + y * A.ld_weight + c, D - c);
+        const f32x8 zeros = {};
+        store8f((type *)A.out + n * A.ld + c, D - c, none ? zeros : v * (A.scale ? A.scale[1] : 1.f));
     }
+#endif
 }
 
 // Rows copied to aligned ones, `cols` padded with zeros to ld_to; rows without a target, or of weight 0, are copied as zeros.
@@ -440,38 +479,40 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
         hidden = ws + p.hidden;
     }
     LogitArgs a = {};
-    a.targets = targets;
     a.i64 = d.flags & PX_FLAG_TOKENS_I64;
     a.V = d.V;
-    a.N = N;
     a.picked = (float *)(ws + p.picked);
-    a.o.b = hidden;
     a.o.ldb = ld_h * e;
-    a.o.n = N;
     a.o.lda = ld_w * e;
     a.o.k = (int)p.d_pad;                  // (where D is padded, both operands are packed)
-    int tiles = 0;
-    for (int k = 0; k < p.pieces; ++k) {
-        a.first = k * p.piece;
-        a.rows = a.o.m = std::min(p.piece, d.V - a.first);
-        const char *from = weight + (int64_t)a.first * d.weight_stride * e;
-        if (p.pack_weight) {
-            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr);
-            from = ws + p.weight;
+    for (int first = 0; first < N; first += p.tokens) {
+        a.targets = (const char *)targets + (int64_t)first * (a.i64 ? 8 : 4);
+        a.N = a.o.n = std::min(p.tokens, N - first);
+        a.o.b = hidden + first * a.o.ldb;
+        int tiles = 0;
+        for (int k = 0; k < p.pieces; ++k) {
+            a.first = k * p.piece;
+            a.rows = a.o.m = std::min(p.piece, d.V - a.first);
+            const char *from = weight + (int64_t)a.first * d.weight_stride * e;
+            if (p.pack_weight) {
+                if (first == 0 || p.pieces > 1)
+                    hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr);
+                from = ws + p.weight;
+            }
+            a.o.a = from;
+            a.parts = (float2 *)(ws + p.parts) + (int64_t)tiles * a.N;
+            a.status = first == 0 && k == 0 ? status : nullptr;
+            launch_logits<T>(p.tiles, kLoss, a, stream);
+            tiles += (a.rows + kShape[p.tiles].bm - 1) / kShape[p.tiles].bm;
         }
-        a.o.a = from;
-        a.parts = (float2 *)(ws + p.parts) + (int64_t)tiles * N;
-        a.status = k == 0 ? status : nullptr;
-        launch_logits<T>(p.tiles, kLoss, a, stream);
-        tiles += (a.rows + kShape[p.tiles].bm - 1) / kShape[p.tiles].bm;
+        auto join = [&](auto kernel, int tokens) {
+            hipLaunchKernelGGL(kernel, dim3((a.N + tokens - 1) / tokens), dim3(kJoinThreads), 0, stream, (const float2 *)(ws + p.parts), tiles, a.N, (const float *)(ws + p.picked), a.targets,
+                               a.i64, d.V, loss + first, lse + first, status);
+        };
+        // (few tokens: as many threads for each; three tokens of 1024 tiles 25 us with sixteen parts)
+        if (a.N <= 1024) join(loss_join<2>, 2);
+        else join(loss_join<16>, 16);
     }
-    auto join = [&](auto kernel, int tokens) {
-        hipLaunchKernelGGL(kernel, dim3((N + tokens - 1) / tokens), dim3(kJoinThreads), 0, stream, (const float2 *)(ws + p.parts), tiles, N, (const float *)(ws + p.picked), targets,
-                           a.i64, d.V, loss, lse, status);
-    };
-    // (few tokens: as many threads for each; three tokens of 1024 tiles 25 us with sixteen parts)
-    if (N <= 1024) join(loss_join<2>, 2);
-    else join(loss_join<16>, 16);
     return status_of(hipGetLastError());
 }
 
@@ -511,12 +552,25 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
     a.row_weight = row_weight;
     a.scale = scale;
     a.q = ws + p.q;
+    a.rest = e == 2 ? (float *)(ws + p.rest) : nullptr;
     a.ld_q = p.v_pad;
     a.o.b = ws + p.hidden;
     a.o.ldb = p.d_pad * e;
     a.o.n = N;
     a.o.lda = (p.pack_weight ? p.d_pad : d.weight_stride) * e;
     a.o.k = (int)p.d_pad;                  // (where D is padded, both operands are packed)
+    GradArgs h = {};                       // the hidden rows' gradient
+    h.cols = d.D;
+    h.rows = N;
+    h.scale = scale;
+    h.targets = targets;
+    h.row_weight = row_weight;
+    h.i64 = i64;
+    h.V = d.V;
+    h.rest = a.rest;
+    h.weight = weight;
+    h.ld_weight = d.weight_stride;
+    h.ld = d.hidden_grad_stride;
     for (int k = 0; k < p.pieces; ++k) {
         a.first = k * p.piece;
         a.rows = a.o.m = std::min(p.piece, d.V - a.first);
@@ -529,21 +583,12 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
         a.status = k == 0 ? status : nullptr;
         launch_logits<T>(p.tiles, kQ, a, stream);
         if (hidden_grad) {
-            GradArgs g = {};
-            g.o = {from, ws + p.q, a.o.lda, p.v_pad * e, d.D, N, a.rows};
-            g.cols = d.D;
-            g.rows = N;
+            h.o = {from, ws + p.q, a.o.lda, p.v_pad * e, d.D, N, a.rows};
             const int depth = kRowBytes / e, stages = (a.rows + depth - 1) / depth;
-            g.slice_k = (stages + p.slices - 1) / p.slices * depth;
-            g.scale = scale;
-            g.targets = targets;
-            g.row_weight = row_weight;
-            g.i64 = i64;
-            g.V = d.V;
-            g.sums = p.slices == 1 && p.pieces == 1 ? 0 : k == 0 ? 1 : 2;
-            g.out = g.sums ? (void *)(ws + p.sums) : (void *)hidden_grad;
-            g.ld = d.hidden_grad_stride;
-            launch_grad<T, false>(p.grad_tiles, g, p.slices, stream);
+            h.slice_k = (stages + p.slices - 1) / p.slices * depth;
+            h.sums = p.slices == 1 && p.pieces == 1 ? 0 : k == 0 ? 1 : 2;
+            h.out = h.sums ? (void *)(ws + p.sums) : (void *)hidden_grad;
+            launch_grad<T, false>(p.grad_tiles, h, p.slices, stream);
         }
         if (weight_grad) {
             GradArgs g = {};
@@ -558,9 +603,10 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
             launch_grad<T, true>(shape_for(d.D, a.rows, N, 1, e == 4), g, 1, stream);
         }
     }
-    if (hidden_grad && (p.slices > 1 || p.pieces > 1))
-        hipLaunchKernelGGL(join_slices<T>, dim3(blocks_for((int64_t)N * d.D)), dim3(256), 0, stream, (const float *)(ws + p.sums), p.slices, (int64_t)N, d.D, scale, targets,
-                           row_weight, i64, d.V, (type *)hidden_grad, d.hidden_grad_stride);
+    if (hidden_grad && (p.slices > 1 || p.pieces > 1)) {
+        h.out = hidden_grad;
+        hipLaunchKernelGGL(join_slices<T>, dim3(blocks_for((int64_t)N * ((d.D + kVec - 1) / kVec))), dim3(256), 0, stream, h, (const float *)(ws + p.sums), p.slices, (int64_t)N, d.D);
+    }
     return status_of(hipGetLastError());
 }
 
@@ -579,6 +625,8 @@ LossPlan loss_plan(const pollux_loss_dims &d, bool grad)
     // A piece's q is held to 512 MiB, packed weights to 256: pieces that large keep the matrix kernels' ends and the sums' passes over
     // memory to a few per cent.
     int64_t piece = (d.V + 255) / 256 * 256;
+    // Forward, tokens are taken so many at a time that no launch has 2^32 threads, whatever its tiles; the lists of tiles are held to 4 GiB by it too.
+    p.tokens = 1 << 15;
     if (grad) piece = std::min(piece, std::max<int64_t>(256, ((512ll << 20) / (std::max<int64_t>(N, 1) * e)) / 256 * 256));
     if (p.pack_weight) piece = std::min(piece, std::max<int64_t>(256, ((256ll << 20) / (p.d_pad * e)) / 256 * 256));
     p.pieces = (int)((d.V + piece - 1) / piece);
@@ -588,7 +636,7 @@ LossPlan loss_plan(const pollux_loss_dims &d, bool grad)
     p.pieces = (int)((d.V + piece - 1) / piece);
     // (rows of q a stage longer than a power of two: those of one tile then begin in different channels of memory)
     p.v_pad = padded(std::min<int64_t>(piece, d.V)) + kRowBytes / e;
-    p.tiles = shape_for(std::min<int64_t>(piece, d.V), N, d.D, 1, f32);
+    p.tiles = shape_for(std::min<int64_t>(piece, d.V), grad ? N : std::min<int64_t>(N, p.tokens), d.D, 1, f32);
     p.slices = 1;
     if (grad) {
         // the hidden rows' gradient has few tiles and a long sum: in as many slices as takes least, their sums being written and read at some
@@ -608,13 +656,15 @@ LossPlan loss_plan(const pollux_loss_dims &d, bool grad)
     p.top = take(256);
     if (!grad) {
         const size_t tiles = (size_t)p.pieces * ((piece + kShape[p.tiles].bm - 1) / kShape[p.tiles].bm);
-        p.parts = take(8 * tiles * (size_t)N);
-        p.picked = take(4 * (size_t)N);
+        const size_t tokens = (size_t)std::min<int64_t>(N, p.tokens);
+        p.parts = take(8 * tiles * tokens);
+        p.picked = take(4 * tokens);
     }
     if (grad || p.pack_hidden) p.hidden = take((size_t)N * p.d_pad * e);
     if (p.pack_weight) p.weight = take((size_t)piece * p.d_pad * e);
     if (grad) {
         p.q = take((size_t)N * p.v_pad * e);
+        if (!f32) p.rest = take(4 * (size_t)N);
         if (p.slices > 1 || p.pieces > 1) p.sums = take((size_t)p.slices * N * d.D * 4);
     }
     p.total = o;

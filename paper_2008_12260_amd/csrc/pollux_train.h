@@ -35,13 +35,15 @@ struct LossPlan {
     int grad_tiles;                     // and the gradients
     int piece;                          // vocabulary entries taken at a time, a multiple of 256
     int pieces;
+    int tokens;                         // forward: taken at a time
     int slices;                         // workgroups that share one tile of the hidden rows' gradient, each a part of a piece
     int64_t d_pad, v_pad;               // padded width, piece
     size_t status, top;                 // int32 [64]; float [64]: the scale of q (fp16)
-    size_t parts;                       // float2 [vocabulary tiles, N]: largest logit and sum of exponentials
-    size_t picked;                      // float [N]: the target's logit
+    size_t parts;                       // float2 [vocabulary tiles, tokens]: largest logit and sum of exponentials
+    size_t picked;                      // float [tokens]: the target's logit
     size_t hidden, weight;              // packed copies [N, d_pad] (of the gradients, with zeros for rows that do not count), [piece, d_pad]
     size_t q;                           // q [N, v_pad]
+    size_t rest;                        // float [N] (16 bits): what rounding took from the target's q
     size_t sums;                        // float [slices, N, D]: the hidden rows' gradient so far
     size_t total;
 };

@@ -31,8 +31,7 @@ def _type(t, name):
 
 def _on_device(*tensors):
     """All given tensors on the current GPU: the library launches there, and reads what it is given there."""
-    import torch
-    here = torch.cuda.current_device()
+    here = _px._current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor {tuple(t.shape)} is on {t.device}: it has to be on the current GPU, cuda:{here}")
@@ -40,11 +39,14 @@ def _on_device(*tensors):
 
 def _rows(t, name):
     """(the tensor, its stride in elements): a matrix whose rows are contiguous and begin at a multiple of 16 bytes, as it is or copied."""
-    if t.dim() != 2:
-        raise ValueError(f"{name} has {t.dim()} dimensions: 2 are wanted")
-    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and (t.stride(0) < t.shape[1] or t.stride(0) >= 1 << 20) or t.data_ptr() % 16:
-        t = t.clone(memory_format=_contiguous())
-    return t, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} has {len(shape)} dimensions: 2 are wanted")
+    rows, width = shape
+    ld, step = t.stride()
+    if width > 1 and step != 1 or rows > 1 and not width <= ld < 1 << 20 or t.data_ptr() & 15:
+        t, ld = t.clone(memory_format=_contiguous()), width
+    return t, ld if rows > 1 else width
 
 
 def _contiguous():
@@ -54,21 +56,24 @@ def _contiguous():
 
 def _result(t, name, shape, dtype):
     """(a caller's result, its stride): written in place, so it has to be as the library takes it."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}: {dtype} {tuple(shape)} is wanted")
-    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1] or t.data_ptr() % 16:
+    rows, width = shape
+    ld, step = t.stride()
+    if width > 1 and step != 1 or rows > 1 and ld < width or t.data_ptr() & 15:
         raise ValueError(f"{name} needs contiguous rows and a base aligned to 16 bytes")
-    return t, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t, ld if rows > 1 else width
 
 
 def _tokens(t, name, count):
     """(the tensor, its flag): int64 or int32, one for each row."""
     import torch
-    if t.dtype not in (torch.int64, torch.int32):
-        raise TypeError(f"{name} is {t.dtype}: int64 or int32 is wanted")
+    dtype = t.dtype
+    if dtype is not torch.int64 and dtype is not torch.int32:
+        raise TypeError(f"{name} is {dtype}: int64 or int32 is wanted")
     if t.numel() != count:
         raise ValueError(f"{name} has {t.numel()} elements for {count} rows")
-    return t.contiguous(), _px.PX_FLAG_TOKENS_I64 if t.dtype == torch.int64 else 0
+    return t.contiguous(), _px.PX_FLAG_TOKENS_I64 if dtype is torch.int64 else 0
 
 
 _HERE = contextlib.nullcontext()
@@ -81,13 +86,19 @@ def _on(stream):
     return torch.cuda.stream(stream)
 
 
-def _scratch(bytes_, device):
+def _scratch(workspace, need, device):
+    """Scratch memory of `need` bytes: the caller's, if it is given (its size is checked by the library), else a tensor."""
+    if workspace is not None:
+        _on_device(workspace)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace needs to be contiguous")
+        return workspace, workspace.numel() * workspace.element_size()
     import torch
-    ws = torch.empty(bytes_, dtype=torch.uint8, device=device)
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
     if "POLLUX_POISON_WORKSPACE" in os.environ:
         # for tests: nothing in the library may depend on what a fresh workspace holds (0xFF bytes read as NaN / -1)
         ws.fill_(0xFF)
-    return ws
+    return ws, need
 
 
 def _check(rc, where):
@@ -112,7 +123,7 @@ def _loss_call(hidden, weight, targets):
 def _loss_scratch(dims, grad, workspace, device):
     need = ctypes.c_size_t(0)
     _check(_px.lib().pollux_loss_workspace_size(ctypes.byref(dims), grad, ctypes.byref(need)), "pollux_loss_workspace_size")
-    return _scratch(need.value, device) if workspace is None else workspace
+    return _scratch(workspace, need.value, device)
 
 
 def token_loss(hidden, weight, targets, workspace=None, stream=None):
@@ -123,11 +134,11 @@ def token_loss(hidden, weight, targets, workspace=None, stream=None):
     import torch
     with _on(stream):
         dims, hidden, weight, targets = _loss_call(hidden, weight, targets)
-        workspace = _loss_scratch(dims, 0, workspace, hidden.device)
+        workspace, size = _loss_scratch(dims, 0, workspace, hidden.device)
         loss = torch.empty(dims.N, dtype=torch.float32, device=hidden.device)
         lse = torch.empty(dims.N, dtype=torch.float32, device=hidden.device)
         _check(_px.lib().pollux_token_loss(ctypes.byref(dims), hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), workspace.data_ptr(),
-                                           workspace.numel() * workspace.element_size(), loss.data_ptr(), lse.data_ptr(),
+                                           size, loss.data_ptr(), lse.data_ptr(),
                                            _px._stream_handle(stream)), "pollux_token_loss")
     return loss, lse
 
@@ -158,9 +169,9 @@ def token_loss_grad(hidden, weight, targets, lse, row_weight=None, hidden_grad=N
             weight_grad, dims.weight_grad_stride = _result(weight_grad, "weight_grad", (dims.V, dims.D), hidden.dtype)
         if accumulate:
             dims.flags |= _px.PX_FLAG_ACCUMULATE
-        workspace = _loss_scratch(dims, 1, workspace, hidden.device)
+        workspace, size = _loss_scratch(dims, 1, workspace, hidden.device)
         _check(_px.lib().pollux_token_loss_grad(ctypes.byref(dims), hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), lse.data_ptr(),
-                                                _px._ptr(row_weight), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                                _px._ptr(row_weight), workspace.data_ptr(), size,
                                                 _px._ptr(hidden_grad), _px._ptr(weight_grad), _px._stream_handle(stream)),
                "pollux_token_loss_grad")
     return hidden_grad, weight_grad
@@ -174,19 +185,17 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
     import torch
     with _on(stream):
         _on_device(tokens, table, out, status)
-        dtype = table.dtype if dtype is None else dtype
         table_type = _type(table, "table")
         table, table_stride = _rows(table, "table")
         count, D = tokens.numel(), table.shape[1]
         if status is not None and (status.dtype != torch.int32 or status.numel() != 1):
             raise ValueError("status is one int32")
-        shape = tuple(tokens.shape) + (D,)
         flat, flag = _tokens(tokens, "tokens", count)
         if out is None:
-            rows, rows_stride = torch.empty(shape, dtype=dtype, device=table.device), D
+            rows, rows_stride = torch.empty((*tokens.shape, D), dtype=table.dtype if dtype is None else dtype, device=table.device), D
         else:
-            rows, rows_stride = _result(out.view(count, D), "out", (count, D), dtype)
-        rows_type = _type(rows, "rows")
+            rows, rows_stride = _result(out.view(count, D), "out", (count, D), table.dtype if dtype is None else dtype)
+        rows_type = table_type if rows.dtype is table.dtype else _type(rows, "rows")
         dims = _px.EmbedDims(count, table.shape[0], D, table_type, rows_type, flag, float(scale), table_stride, rows_stride)
         _check(_px.lib().pollux_embed(ctypes.byref(dims), flat.data_ptr(), table.data_ptr(), rows.data_ptr(), _px._ptr(status),
                                       _px._stream_handle(stream)), "pollux_embed")
@@ -215,10 +224,9 @@ def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, acc
                              table_stride, rows_stride)
         need = ctypes.c_size_t(0)
         _check(_px.lib().pollux_embed_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_embed_workspace_size")
-        if workspace is None:
-            workspace = _scratch(need.value, rows.device)
+        workspace, size = _scratch(workspace, need.value, rows.device)
         _check(_px.lib().pollux_embed_grad(ctypes.byref(dims), flat.data_ptr(), rows.data_ptr(), workspace.data_ptr(),
-                                           workspace.numel() * workspace.element_size(), table_grad.data_ptr(), _px._stream_handle(stream)),
+                                           size, table_grad.data_ptr(), _px._stream_handle(stream)),
                "pollux_embed_grad")
     return table_grad
 
@@ -248,8 +256,8 @@ def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=T
         dims = _px.NoiseDims(n, B, type_, _px.PX_TYPE_F32 if mean is None else _type(mean, "mean"), 0, flat.stride(0), float(examples))
         need = ctypes.c_size_t(0)
         _check(_px.lib().pollux_noise_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_noise_workspace_size")
-        workspace = _scratch(need.value, flat.device)
-        _check(_px.lib().pollux_noise_scale(ctypes.byref(dims), flat.data_ptr(), _px._ptr(precondition), workspace.data_ptr(), workspace.numel(),
+        workspace, size = _scratch(None, need.value, flat.device)
+        _check(_px.lib().pollux_noise_scale(ctypes.byref(dims), flat.data_ptr(), _px._ptr(precondition), workspace.data_ptr(), size,
                                             _px._ptr(mean), scale.data_ptr(), _px._stream_handle(stream)), "pollux_noise_scale")
     return mean, scale
 
@@ -273,14 +281,13 @@ def orthogonalize(grads, steps=5, coefficients=(3.4445, -4.7750, 2.0315), out=No
             flat = flat.clone(memory_format=_contiguous())
         if out is None:
             out = torch.empty(shape, dtype=torch.bfloat16, device=flat.device)
-        elif tuple(out.shape) != shape or out.dtype != torch.bfloat16 or not out.is_contiguous() or out.data_ptr() % 16:
+        elif out.shape != shape or out.dtype != torch.bfloat16 or not out.is_contiguous() or out.data_ptr() % 16:
             raise ValueError(f"out is {out.dtype} {tuple(out.shape)}: contiguous bfloat16 {shape} is wanted")
         ld = flat.stride(1) if rows > 1 else cols
         dims = _px.OrthoDims(batch, rows, cols, type_, steps, 0, *(float(c) for c in coefficients), ld, 0, flat.stride(0) if batch > 1 else 0, 0)
         need = ctypes.c_size_t(0)
         _check(_px.lib().pollux_ortho_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_ortho_workspace_size")
-        if workspace is None:
-            workspace = _scratch(need.value, flat.device)
-        _check(_px.lib().pollux_orthogonalize(ctypes.byref(dims), flat.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        workspace, size = _scratch(workspace, need.value, flat.device)
+        _check(_px.lib().pollux_orthogonalize(ctypes.byref(dims), flat.data_ptr(), workspace.data_ptr(), size,
                                               out.data_ptr(), _px._stream_handle(stream)), "pollux_orthogonalize")
     return out

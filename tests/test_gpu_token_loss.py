@@ -300,3 +300,51 @@ def test_wrong_tensors_are_refused():
     with pytest.raises(px.PolluxError) as e:
         px.token_loss(hidden, weight, targets, workspace=small)
     assert e.value.code == px.PX_E_WORKSPACE
+
+
+@pytest.mark.parametrize("type_", ("bfloat16", "float16"))
+@pytest.mark.parametrize("N,V,D", [(40, 600, 64), (3, 9, 8), (70, 40001, 72), (300, 3000, 13), (1030, 270000, 24)])
+def test_the_targets_share_of_a_hidden_gradient_is_not_rounded(N, V, D, type_):
+    """Logits near 0: q is 1 / V but at the target, where it is near the row's weight.  The roundings of the other entries (u each), fp32's
+    of the target's, the sum's and the result's are all that is left."""
+    import torch
+    hidden, weight, targets, row_weight = inputs(N, V, D, type_, 51)
+    hidden = hidden * 2.0 ** -9
+    u, f = U[type_], 2.0 ** -24
+    h, w = hidden.double(), weight.double()
+    has = (targets >= 0) & (row_weight != 0)
+    logits = torch.mm(h, w.t())
+    p = torch.softmax(logits, 1)
+    dl = D * f * torch.mm(h.abs(), w.abs().t()).amax(1)
+    dlse = dl + (V / 64 + 256) * f + 4 * f * torch.logsumexp(logits, 1).abs()
+    g = torch.where(has, row_weight.double(), 0.0)[:, None]
+    at = torch.zeros_like(p)
+    at[has] = torch.nn.functional.one_hot(targets[has], V).double()
+    q = g * (p - at)
+    dq = g.abs() * p * (dl + dlse + 8 * f)[:, None] + u * q.abs() * (1 - at) + 4 * f * q.abs() * at
+    if type_ == "float16":
+        dq = dq + torch.where(has[:, None], 2.0 ** -37 * g.abs().max(), 0.0)
+    want = torch.mm(q, w)
+    bound = torch.mm(dq, w.abs()) + (V + 16) * f * torch.mm(q.abs(), w.abs()) + u * want.abs() + SMALLEST[type_]
+    close(run(hidden, weight, targets, row_weight), dict(hidden_grad=(want, bound)), ("hidden_grad",))
+
+
+def test_more_tokens_than_are_taken_at_a_time():
+    args = inputs(32768 + 37, 300, 16, "bfloat16", 53)
+    close(run(*args), reference(*args))
+    args = inputs(65536 + 1, 20, 3, "float32", 54, i64=False)
+    close(run(*args), reference(*args))
+
+
+def test_scratch_memory_has_to_be_on_the_gpu():
+    import torch
+    import paper_2008_12260_amd as px
+    hidden, weight, targets, _ = inputs(8, 50, 64, "bfloat16", 55)
+    _, lse = px.token_loss(hidden, weight, targets)
+    host = torch.empty(1 << 20, dtype=torch.uint8)
+    rows = torch.randn((8, 64), device="cuda")
+    for call in (lambda w: px.token_loss(hidden, weight, targets, workspace=w), lambda w: px.token_loss_grad(hidden, weight, targets, lse, workspace=w),
+                 lambda w: px.embed_grad(targets, rows, 50, workspace=w), lambda w: px.orthogonalize(rows, workspace=w)):
+        for bad in (host, torch.empty((1 << 20, 2), dtype=torch.uint8, device="cuda")[:, 0]):
+            with pytest.raises(ValueError):
+                call(bad)
