@@ -5,7 +5,9 @@
 // order below is one), and the sorted places are cut into windows of equal length: each window sums its runs of equal tokens,
 // writes those that lie within it, and leaves the sums of the two that its ends may cut (sum_windows); a second launch adds
 // up the pieces of the runs that were cut, in their order (join_runs).  Work is even whatever the tokens are, no result depends on
-// the order in which atomics arrive, and rows that no token names are zeroed by further workgroups of the first launch.
+// the order in which atomics arrive.  The sort is a chain of short launches on few compute units; further workgroups of them zero the
+// table meanwhile (the few rows that tokens name are written twice, which costs less than telling them apart: 65536 x 2048 in bfloat16 from 16384
+// rows 107 us with the others zeroed after the sort).
 
 #include "pollux_host.h"
 #include "pollux_rows.h"
@@ -59,18 +61,63 @@ __global__ __launch_bounds__(256) void embed_rows(const void *tokens, bool i64, 
 // Keys are tokens, V for none (sorted last, and dropped).  Up to kFew tokens: one workgroup counts, for every token, those before it.
 // More: two passes, lowest digit first, of ceil(log2(V + 1)) / 2 bits.
 
-constexpr int kFew = 1024, kThreads = 1024, kWaves = kThreads / 64, kMaxBits = 10;
-
-__global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i64, int N, int V, int32_t *status, int *keys, int *places, unsigned char *named)
+// A table's rows from `first` on, `rows` of them, zeroed by the workgroups from `blocks` on, kZeroAhead groups of 16 bytes a thread and turn.
+constexpr int kFew = 1024, kThreads = 1024, kWaves = kThreads / 64, kMaxBits = 10, kZeroAhead = 4;
+struct ZeroArgs {
+    char *table;
+    int64_t ld;                 // bytes
+    int row;                    // bytes of a row, even
+    int first, rows;
+    int blocks;
+    bool past;                  // the stores go past the caches
+};
+// (two loops for the two kinds of stores: of a branch at each store the compiler makes one of the ordinary kind)
+template <bool PAST>
+__device__ __forceinline__ void zero_rows(const ZeroArgs &Z, int64_t block, int64_t blocks)
 {
+#ifdef __HIP_DEVICE_COMPILE__
+    const words none = {};
+    auto put = [&](char *to, int64_t left) {
+        if (left < 16)
+            for (int i = 0; i < left; i += 2) *(short *)(to + i) = 0;
+        else if constexpr (PAST)
+            __builtin_nontemporal_store(none, (at_any *)to);
+        else
+            *(at_any *)to = none;
+    };
+    char *const table = Z.table + Z.first * Z.ld;
+    if (Z.ld == Z.row) {                     // rows without gaps: one long one
+        const int64_t bytes = (int64_t)Z.rows * Z.row, step = kThreads * 16;
+        for (int64_t at = block * step * kZeroAhead + threadIdx.x * 16; at < bytes; at += blocks * step * kZeroAhead)
+#pragma unroll
+            for (int i = 0; i < kZeroAhead; ++i)
+                if (at + i * step < bytes) put(table + at + i * step, bytes - at - i * step);
+    } else {
+        const int64_t groups = (Z.row + 15) / 16, total = groups * Z.rows;
+        for (int64_t at = block * kThreads + threadIdx.x; at < total; at += blocks * kThreads) {
+            const int64_t r = at / groups, byte = (at - r * groups) * 16;
+            put(table + r * Z.ld + byte, Z.row - byte);
+        }
+    }
+#endif
+}
+__device__ __forceinline__ bool zero_rows(const ZeroArgs &Z)
+{
+    const int64_t block = (int64_t)blockIdx.x - Z.blocks, blocks = (int64_t)gridDim.x - Z.blocks;
+    if (block < 0) return false;
+    if (Z.past) zero_rows<true>(Z, block, blocks);
+    else zero_rows<false>(Z, block, blocks);
+    return true;
+}
+
+__global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i64, int N, int V, int32_t *status, int *keys, int *places, const ZeroArgs Z)
+{
+    if (zero_rows(Z)) return;
     __shared__ int shared[kFew];
     __shared__ int bad_any;
     const int n = threadIdx.x;
     if (n == 0) bad_any = 0;
     if (n < kStatusWords) status[n] = 0;
-    if (named)
-        for (int i = n; i < (V + 3) / 4; i += kThreads) ((unsigned *)named)[i] = 0;
-    __threadfence();
     bool bad = false;
     int key = 0x7fffffff;
     if (n < N) {
@@ -88,22 +135,19 @@ __global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i6
     if (n < N) {
         keys[before] = key;
         places[before] = n;
-        if (named && key < V) named[key] = 1;
     }
     __syncthreads();
     if (n == 0 && bad_any) *status = PX_ST_BAD_TOKEN;
 }
 
-// A workgroup's tokens counted by their lowest digit; the second pass's counts, the marks of the entries that are named and the
-// status word are cleared.
-__global__ __launch_bounds__(kThreads) void count_digits(const void *tokens, bool i64, int N, int V, int per_block, int bits, int *counts, int *counts2, unsigned char *named, int32_t *status)
+// A workgroup's tokens counted by their lowest digit; the second pass's counts and the status word are cleared.
+__global__ __launch_bounds__(kThreads) void count_digits(const void *tokens, bool i64, int N, int V, int per_block, int bits, int *counts, int *counts2, int32_t *status, const ZeroArgs Z)
 {
+    if (zero_rows(Z)) return;
     __shared__ int bins[1 << kMaxBits];
     const int size = 1 << bits, first = blockIdx.x * per_block, last = min(N, first + per_block);
     for (int i = threadIdx.x; i < size; i += kThreads) bins[i] = 0;
     if (blockIdx.x == 0 && threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
-    if (named)
-        for (int i = blockIdx.x * kThreads + threadIdx.x; i < (V + 3) / 4; i += gridDim.x * kThreads) ((unsigned *)named)[i] = 0;
     __syncthreads();
     for (int n = first + threadIdx.x; n < last; n += kThreads) {
         bool bad;
@@ -121,8 +165,9 @@ __global__ __launch_bounds__(kThreads) void count_digits(const void *tokens, boo
 // order.  The first pass reads the tokens themselves and counts, for the second, the next digits of the places it fills.
 template <bool FIRST>
 __global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, bool i64, const int *keys_in, const int *places_in, int N, int V, int blocks, int per_block,
-                                                         int bits, const int *counts, int *counts2, int *keys, int *places, unsigned char *named, int32_t *status)
+                                                         int bits, const int *counts, int *counts2, int *keys, int *places, int32_t *status, const ZeroArgs Z)
 {
+    if (zero_rows(Z)) return;
     __shared__ int base[1 << kMaxBits];
     __shared__ int in_wave[kWaves][1 << kMaxBits];
     __shared__ int waves[kWaves];
@@ -185,14 +230,23 @@ __global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, boo
                 total += c;
             }
         __syncthreads();
+        int to = 0;
         if (there) {
-            const int to = base[digit] + in_wave[wave][digit] + rank;
+            to = base[digit] + in_wave[wave][digit] + rank;
             keys[to] = key;
             places[to] = place;
-            if (FIRST) {
-                atomicAdd(&counts2[to / per_block * size + ((key >> bits) & (size - 1))], 1);
-                if (named && key < V) named[key] = 1;
+        }
+        if (FIRST) {
+            // equal keys go to places in a row, in one of the second pass's workgroups or in two: one lane counts for all that share both
+            // (a frequent token is in a wavefront many times, and adding one by one they would wait for each other: 12 us for 16384 tokens, 7 so)
+            const int high = key >> bits, block = to / per_block;
+            for (int b = 0; b < bits; ++b) {
+                const unsigned long long set = __ballot((high >> b) & 1);
+                same &= (high >> b) & 1 ? set : ~set;
             }
+            const unsigned long long odd = __ballot(block & 1);
+            same &= block & 1 ? odd : ~odd;
+            if (there && (same & ((1ull << lane) - 1)) == 0) atomicAdd(&counts2[block * size + (high & (size - 1))], __popcll(same));
         }
         __syncthreads();
         if (tid < size) base[tid] += total;
@@ -205,31 +259,19 @@ __global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, boo
 
 struct SumArgs {
     const int *keys, *places;
-    const unsigned char *named;      // [V / 32]: bits of the entries that tokens name
     int64_t ld_rows, ld_table;
     float *partial;             // [2][windows][D]: the run cut by a window's first place, by its last
     int N, V, D, window, windows;
     int lanes;                  // threads that share a window, kVec columns each: a power of two
     int groups;                 // 256 / lanes windows a workgroup
-    int window_blocks;          // workgroups after these zero the rows that no token names, kZeroRows each
     bool add;
     float scale;
 };
-constexpr int kZeroRows = 32;
 
 template <class R, class T>
 __global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *rows, T *table)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    if ((int)blockIdx.x >= A.window_blocks) {
-        const int v0 = ((int)blockIdx.x - A.window_blocks) * kZeroRows;
-        const f32x8 zeros = {};
-        for (int i = threadIdx.x; i < kZeroRows * A.lanes; i += 256) {
-            const int r = i / A.lanes, c = (blockIdx.y * A.lanes + i % A.lanes) * kVec;
-            if (v0 + r < A.V && c < A.D && !A.named[v0 + r]) store8f(table + (int64_t)(v0 + r) * A.ld_table + c, A.D - c, zeros);
-        }
-        return;
-    }
     const int w = blockIdx.x * A.groups + threadIdx.x / A.lanes;
     const int c = (blockIdx.y * A.lanes + threadIdx.x % A.lanes) * kVec;
     if (w >= A.windows || c >= A.D) return;
@@ -320,21 +362,34 @@ int embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *token
     const bool i64 = d.flags & PX_FLAG_TOKENS_I64;
     int32_t *status = (int32_t *)(ws + p.status);
     int *keys[2] = {(int *)(ws + p.keys[0]), (int *)(ws + p.keys[1])}, *places[2] = {(int *)(ws + p.places[0]), (int *)(ws + p.places[1])};
-    unsigned char *named = d.flags & PX_FLAG_ACCUMULATE ? nullptr : (unsigned char *)(ws + p.named);
+    const bool add = d.flags & PX_FLAG_ACCUMULATE;
+    // rows [V at / 16, V to / 16) of the table zeroed by a launch whose own workgroups are `blocks`; as long as what the sort does in it
+    // (A table that the memory-side cache of 256 MiB holds beside the rows stays there: 29114 x 2048 in fp32 40 us, 54 with stores past the
+    // caches; a larger one only pushes the rows out: 65536 x 2048 in bfloat16 from 16384 rows 95 us, 81 past them.)
+    const bool past = (int64_t)d.V * d.D * (int64_t)sizeof(T) + (int64_t)N * d.D * (int64_t)sizeof(R) > (256ll << 20);
+    auto zero = [&](int at, int to, int blocks) {
+        const int first = (int)((int64_t)d.V * at / 16), last = (int)((int64_t)d.V * to / 16);
+        return ZeroArgs{(char *)table, d.table_stride * (int64_t)sizeof(T), d.D * (int)sizeof(T), first, add ? 0 : last - first, blocks, past};
+    };
+    auto grid = [&](const ZeroArgs &z) {
+        const int64_t groups = ((int64_t)z.row + 15) / 16 * z.rows, each = kThreads * kZeroAhead;
+        return dim3((unsigned)(z.blocks + std::min<int64_t>((groups + each - 1) / each, 512)));
+    };
     if (p.passes == 0) {
-        hipLaunchKernelGGL(rank_few, dim3(1), dim3(kThreads), 0, stream, tokens, i64, N, d.V, status, keys[1], places[1], named);
+        const ZeroArgs z = zero(0, 16, 1);
+        hipLaunchKernelGGL(rank_few, grid(z), dim3(kThreads), 0, stream, tokens, i64, N, d.V, status, keys[1], places[1], z);
     } else {
         int *counts = (int *)(ws + p.counts), *counts2 = counts + ((size_t)p.blocks << p.bits);
-        hipLaunchKernelGGL(count_digits, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, N, d.V, p.per_block, p.bits, counts, counts2, named, status);
-        hipLaunchKernelGGL(place_digits<true>, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, (const int *)nullptr, (const int *)nullptr, N, d.V, p.blocks,
-                           p.per_block, p.bits, (const int *)counts, counts2, keys[0], places[0], named, status);
-        hipLaunchKernelGGL(place_digits<false>, dim3(p.blocks), dim3(kThreads), 0, stream, tokens, i64, (const int *)keys[0], (const int *)places[0], N, d.V, p.blocks,
-                           p.per_block, p.bits, (const int *)counts2, (int *)nullptr, keys[1], places[1], (unsigned char *)nullptr, status);
+        const ZeroArgs z[3] = {zero(0, 4, p.blocks), zero(4, 11, p.blocks), zero(11, 16, p.blocks)};
+        hipLaunchKernelGGL(count_digits, grid(z[0]), dim3(kThreads), 0, stream, tokens, i64, N, d.V, p.per_block, p.bits, counts, counts2, status, z[0]);
+        hipLaunchKernelGGL(place_digits<true>, grid(z[1]), dim3(kThreads), 0, stream, tokens, i64, (const int *)nullptr, (const int *)nullptr, N, d.V, p.blocks,
+                           p.per_block, p.bits, (const int *)counts, counts2, keys[0], places[0], status, z[1]);
+        hipLaunchKernelGGL(place_digits<false>, grid(z[2]), dim3(kThreads), 0, stream, tokens, i64, (const int *)keys[0], (const int *)places[0], N, d.V, p.blocks,
+                           p.per_block, p.bits, (const int *)counts2, (int *)nullptr, keys[1], places[1], status, z[2]);
     }
     SumArgs a = {};
     a.keys = keys[1];
     a.places = places[1];
-    a.named = named;
     a.ld_rows = d.rows_stride;
     a.ld_table = d.table_stride;
     a.partial = (float *)(ws + p.partial);
@@ -346,13 +401,11 @@ int embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *token
     a.lanes = 1;
     while (a.lanes < 256 && a.lanes * kVec < d.D) a.lanes *= 2;
     a.groups = 256 / a.lanes;
-    a.window_blocks = (p.windows + a.groups - 1) / a.groups;
-    a.add = d.flags & PX_FLAG_ACCUMULATE;
+    a.add = add;
     a.scale = d.scale;
     const unsigned parts = (unsigned)((d.D + 256 * kVec - 1) / (256 * kVec));
-    const int zero_blocks = a.add ? 0 : (d.V + kZeroRows - 1) / kZeroRows;
-    if (a.window_blocks + zero_blocks > 0)
-        hipLaunchKernelGGL((sum_windows<R, T>), dim3((unsigned)(a.window_blocks + zero_blocks), parts), dim3(256), 0, stream, a, rows, table);
+    if (p.windows > 0)
+        hipLaunchKernelGGL((sum_windows<R, T>), dim3((unsigned)((p.windows + a.groups - 1) / a.groups), parts), dim3(256), 0, stream, a, rows, table);
     if (p.windows > 1) hipLaunchKernelGGL(join_runs<T>, dim3((unsigned)(p.windows - 1), (unsigned)((d.D + 64 * kVec - 1) / (64 * kVec))), dim3(256), 0, stream, a, table);
     return status_of(hipGetLastError());
 }
@@ -376,7 +429,6 @@ EmbedPlan embed_plan(const pollux_embed_dims &d)
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
     p.status = take(4 * kStatusWords);
-    if (!(d.flags & PX_FLAG_ACCUMULATE)) p.named = take(((size_t)d.V + 3) / 4 * 4);
     if (N > kFew) {
         int bits = 1;
         while (((int64_t)1 << (2 * bits)) <= d.V) ++bits;       // keys 0 .. V

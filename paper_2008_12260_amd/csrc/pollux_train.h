@@ -62,7 +62,6 @@ struct EmbedPlan {
     int blocks, per_block;      // workgroups of a pass, tokens of each
     int window, windows;        // places in sorted order that are summed together, and how many such
     size_t status;
-    size_t named;               // bytes [V]: entries that tokens name (where the others are zeroed)
     size_t counts;              // int32 [2][blocks][1 << bits]: a workgroup's tokens by digit, for both passes
     size_t keys[2], places[2];  // int32 [N]: tokens and their positions, before and after the last pass
     size_t partial;             // float [2][windows][D]: sums of the runs that a window's first and last place cut

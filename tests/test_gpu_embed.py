@@ -215,3 +215,24 @@ def test_wrong_tensors_are_refused():
     with pytest.raises(px.PolluxError) as e:
         px.embed(tokens, table, float("nan"))
     assert e.value.code == px.PX_E_INVALID_ARG
+
+
+def test_tables_of_any_place_are_zeroed_to_their_ends_and_no_further():
+    """Rows with and without gaps, of odd lengths, in fp32 and 16 bits, few and many tokens, within the memory-side cache and beyond: entries that
+    no token names are zeros, what lies between the rows and behind them is left."""
+    import torch
+    import paper_2008_12260_amd as px
+    for N, V, D, gap, type_ in ((5, 1001, 7, 0, "bfloat16"), (5, 1001, 7, 2, "float32"), (2000, 333, 33, 0, "float16"), (2000, 333, 33, 3, "bfloat16"), (3, 4097, 129, 0, "float32"),
+                                (1100, 70001, 2001, 0, "bfloat16"), (9, 70001, 1001, 3, "float32")):
+        tokens = tokens_of(N, V, N)
+        rows = torch.randn((N, D), device="cuda").to(getattr(torch, type_))
+        flat = torch.full((V * (D + gap) + 64,), 7.0, dtype=rows.dtype, device="cuda")
+        table = flat[:V * (D + gap)].view(V, D + gap)
+        got = px.embed_grad(tokens, rows, V, table_grad=table[:, :D])
+        absent = torch.ones(V, dtype=torch.bool, device="cuda")
+        absent[tokens[tokens >= 0]] = False
+        assert not bool(got[absent].any())
+        assert bool((table[:, D:] == 7.0).all()) and bool((flat[V * (D + gap):] == 7.0).all())
+        named = torch.unique(tokens[tokens >= 0])
+        value, bound = gradient(torch.searchsorted(named, tokens.clamp(min=-1)).where(tokens >= 0, -1), rows, len(named), 1.0)
+        close(got[named], value, bound)
