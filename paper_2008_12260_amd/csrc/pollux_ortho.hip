@@ -2,7 +2,7 @@
 //
 // X is held as the gradients lie.  Of at most as many rows as columns: A = X X' takes rows, and B X the columns of X; of more rows
 // than columns (the formula on the transposes): A = X' X takes columns, and X B the rows.  A^2, A and B are symmetric, so that a row is
-// a column.  Three launches a step, for all matrices of the batch together.
+// a column, and where that is less work only the tiles on one side of their diagonals are formed.  Three launches a step, for all matrices of the batch together.
 //
 // X is held in fp16, times a power of two near the root of its longer side, so that its elements lie well within fp16's range
 // whatever the matrix's shape: an element's rounding is then 2^-11 of it, a quarter of what bfloat16 would leave, and the
@@ -89,13 +89,22 @@ struct StepArgs {
     int64_t ld_last, batch_last;
 };
 
-// out = plus base + by (product); or the update.
+// A wavefront's part of a tile on its way to the other side: rows of n, TM elements and a gap that keeps them on different banks.
 template <class S>
+constexpr int kTurnRow = S::TM * 2 + 16;
+template <class S>
+constexpr int kTurnBytes = S::TN * kTurnRow<S>;
+template <class S>
+constexpr int kStepLds = S::kLds > S::WM * S::WN * kTurnBytes<S> ? S::kLds : S::WM * S::WN * kTurnBytes<S>;
+
+// out = plus base + by (product); or the update.  SYMMETRIC: the product is, and its tiles on one side of the diagonal are formed and
+// stored on both sides (4096 x 4096 over 8192: 143 us, 217 with all tiles).
+template <class S, bool SYMMETRIC>
 __global__ __launch_bounds__(S::kThreads) void step_tiles(const StepArgs A)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     extern __shared__ __align__(16) char lds[];
-    const Tile t = tile_of(blockIdx.x, A.tiles_m, A.tiles_n, A.group);
+    const Tile t = SYMMETRIC ? triangle_of(blockIdx.x, A.tiles_m) : tile_of(blockIdx.x, A.tiles_m, A.tiles_n, A.group);
     const int64_t batch = blockIdx.y;
     Operands o = A.o;
     o.a += batch * A.batch_a;
@@ -107,24 +116,27 @@ __global__ __launch_bounds__(S::kThreads) void step_tiles(const StepArgs A)
     static_assert(S::FM % 2 == 0, "tiles in pairs");
     const Pair pair;
     const int wave_m = at.first_m - (threadIdx.x >> 4 & 3) * 4;
+    const bool both = SYMMETRIC && t.m != t.n;
+    lds_char *const turn = (lds_char *)lds + (threadIdx.x >> 6) * kTurnBytes<S>;
+    typedef __attribute__((address_space(3))) f16x8 lds_f16x8;
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
         const int n = at.first_n + j * 16;
-        if (n >= A.rows) continue;
 #pragma unroll
         for (int i = 0; i < S::FM; i += 2) {
             float v[8];
             paired32(acc[i][j], acc[i + 1][j], v);
             const int m = wave_m + 16 * (i + pair.tile) + pair.row;
-            if (m >= A.ld) continue;
+            const bool there = n < A.rows && m < A.ld;
             const int64_t here = (batch * A.rows + n) * A.ld + m;
             f16x8 base = {};
-            if (A.base) base = *(const f16x8 *)(A.base + here);
+            if (A.base && there) base = *(const f16x8 *)(A.base + here);
 #pragma unroll
             for (int r = 0; r < 8; ++r) v[r] = v[r] * A.by + A.plus * (float)base[r];
             if (A.last) {
                 __bf16 *to = A.last + batch * A.batch_last + (int64_t)n * A.ld_last + m;
-                if (whole && m + 8 <= A.cols) {
+                if (!there) {
+                } else if (whole && m + 8 <= A.cols) {
                     bf16x8 t;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) t[r] = (__bf16)v[r];
@@ -136,32 +148,59 @@ __global__ __launch_bounds__(S::kThreads) void step_tiles(const StepArgs A)
             } else {
                 f16x8 t;
 #pragma unroll
-                for (int r = 0; r < 8; ++r) t[r] = (_Float16)(m + r < A.cols ? v[r] : 0.f);
-                *(f16x8 *)(A.out + here) = t;
+                for (int r = 0; r < 8; ++r) t[r] = (_Float16)(there && m + r < A.cols ? v[r] : 0.f);
+                if (there) *(f16x8 *)(A.out + here) = t;
+                if (both) *(lds_f16x8 *)(turn + (j * 16 + (threadIdx.x & 15)) * kTurnRow<S> + (16 * (i + pair.tile) + pair.row) * 2) = t;
             }
         }
+    }
+    if (!both) return;
+    // The wavefront's part turned, sixteen rows m of eight n at a time by sixteen lanes: C[m, n .. n + 7].
+    asm volatile("" ::: "memory");         // (a wavefront's own accesses to LDS keep their order)
+    __builtin_amdgcn_wave_barrier();
+    constexpr int kAcross = S::TN / 8, kUnits = S::TM / 16 * kAcross;
+    const int wave = threadIdx.x >> 6, r = threadIdx.x & 15;
+    static_assert(kUnits % 4 == 0, "four at a time");
+    for (int u = threadIdx.x >> 4 & 3; u < kUnits; u += 4) {
+        const int m = u / kAcross * 16, n = u % kAcross * 8;
+        const lds_char *from = turn + (n + (r >> 2)) * kTurnRow<S> + (m + (r & 3) * 4) * 2;
+        const s16x4 low = read_turned((lds_s16x4 *)from), high = read_turned((lds_s16x4 *)(from + 4 * kTurnRow<S>));
+        const int row = t.m * S::BM + wave / S::WN * S::TM + m + r, col = t.n * S::BN + wave % S::WN * S::TN + n;
+        if (row < A.rows && col < A.ld)
+            *(s16x8 *)(A.out + (batch * A.rows + row) * A.ld + col) = (s16x8)__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
     }
 #endif
 }
 
-template <class S>
+template <bool SYMMETRIC, class S>
 void launch_step(StepArgs a, int batch, hipStream_t stream)
 {
     a.tiles_m = (a.cols + S::BM - 1) / S::BM;
     a.tiles_n = (a.rows + S::BN - 1) / S::BN;
     a.group = 8;
-    hipLaunchKernelGGL(step_tiles<S>, dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)batch), dim3(S::kThreads), S::kLds, stream, a);
+    const int tiles = SYMMETRIC ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
+    hipLaunchKernelGGL((step_tiles<S, SYMMETRIC>), dim3((unsigned)tiles, (unsigned)batch), dim3(S::kThreads), SYMMETRIC ? kStepLds<S> : S::kLds, stream, a);
 }
-template <bool COLS_A, bool COLS_B>
+template <bool SYMMETRIC, bool COLS_A, bool COLS_B>
 void launch_step(int shape, const StepArgs &a, int batch, hipStream_t stream)
 {
     switch (shape) {
-        case 0: launch_step<Shape0<F16, COLS_A, COLS_B>>(a, batch, stream); break;
-        case 1: launch_step<Shape1<F16, COLS_A, COLS_B>>(a, batch, stream); break;
-        case 2: launch_step<Shape2<F16, COLS_A, COLS_B>>(a, batch, stream); break;
-        case 3: launch_step<Shape3<F16, COLS_A, COLS_B>>(a, batch, stream); break;
-        default: launch_step<Shape4<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        case 0: launch_step<SYMMETRIC, Shape0<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        case 1: launch_step<SYMMETRIC, Shape1<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        case 2: launch_step<SYMMETRIC, Shape2<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        case 3:                             // (not square)
+            if constexpr (!SYMMETRIC) launch_step<SYMMETRIC, Shape3<F16, COLS_A, COLS_B>>(a, batch, stream);
+            break;
+        case 4: launch_step<SYMMETRIC, Shape4<F16, COLS_A, COLS_B>>(a, batch, stream); break;
+        default: launch_step<SYMMETRIC, Shape5<F16, COLS_A, COLS_B>>(a, batch, stream); break;
     }
+}
+
+template <bool COLS_A, bool COLS_B>
+void launch_step(StepShape shape, const StepArgs &a, int batch, hipStream_t stream)
+{
+    if (shape.half) launch_step<true, COLS_A, COLS_B>(shape.shape, a, batch, stream);
+    else launch_step<false, COLS_A, COLS_B>(shape.shape, a, batch, stream);
 }
 
 // The update where no step is taken: X itself.
@@ -203,8 +242,8 @@ int orthogonalize(const pollux_ortho_dims &d, const OrthoPlan &p, const E *grads
         a.by = (float)(1.0 / (p.unit * p.unit));
         a.out = gram;
         a.ld = p.m_pad;
-        if (p.tall) launch_step<true, true>(p.shape_square, a, d.batch, stream);
-        else launch_step<false, false>(p.shape_square, a, d.batch, stream);
+        if (p.tall) launch_step<true, true>(p.shape_gram, a, d.batch, stream);
+        else launch_step<false, false>(p.shape_gram, a, d.batch, stream);
         // poly = b gram + c gram gram
         a.o = {(const char *)gram, (const char *)gram, ld_m, ld_m, p.m, p.m, p.m};
         a.batch_a = a.batch_b = batch_m;
@@ -232,12 +271,12 @@ int orthogonalize(const pollux_ortho_dims &d, const OrthoPlan &p, const E *grads
             a.o = {(const char *)poly, from, ld_m, ld_x, d.cols, d.rows, p.m};
             a.batch_a = batch_m;
             a.batch_b = batch_x;
-            launch_step<false, false>(p.shape_wide, a, d.batch, stream);
+            launch_step<false, false, false>(p.shape_wide.shape, a, d.batch, stream);
         } else {
             a.o = {from, (const char *)poly, ld_x, ld_m, d.cols, d.rows, p.m};
             a.batch_a = batch_x;
             a.batch_b = batch_m;
-            launch_step<true, false>(p.shape_wide, a, d.batch, stream);
+            launch_step<false, true, false>(p.shape_wide.shape, a, d.batch, stream);
         }
     }
     return status_of(hipGetLastError());
@@ -255,8 +294,9 @@ OrthoPlan ortho_plan(const pollux_ortho_dims &d)
     p.x_pad = (d.cols + 7) / 8 * 8;
     p.unit = ldexp(1.0, (int)lround(0.5 * log2((double)p.n)));
     p.norm_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / std::max(d.batch, 1), (int64_t)d.rows * d.cols / 8192));
-    p.shape_square = shape_for(p.m, p.m, 0.5 * (p.m + p.n), d.batch, false);
-    p.shape_wide = shape_for(d.cols, d.rows, p.m, d.batch, false);
+    p.shape_gram = step_shape_for(p.m, p.m, p.n, d.batch, true);
+    p.shape_square = step_shape_for(p.m, p.m, p.m, d.batch, true);
+    p.shape_wide = step_shape_for(d.cols, d.rows, p.m, d.batch, false);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
     p.norms = take(std::max<size_t>(8, 8 * (size_t)d.batch * p.norm_blocks));

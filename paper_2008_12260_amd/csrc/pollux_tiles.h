@@ -20,6 +20,8 @@
 
 #include <type_traits>
 
+#include "pollux_train.h"
+
 namespace px {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -66,6 +68,17 @@ __device__ __forceinline__ Tile tile_of(int block, int tiles_m, int tiles_n, int
     return {first + rest % size, rest / size};
 }
 
+// The same of a symmetric product: the tiles with n <= m, row by row of m.
+__device__ __forceinline__ Tile triangle_of(int block, int tiles)
+{
+    const int total = tiles * (tiles + 1) / 2, q = total >> 3, r = total & 7, xcd = block & 7;
+    const int at = xcd * q + min(xcd, r) + (block >> 3);
+    int m = (int)((sqrtf(8.f * at + 1.f) - 1.f) * 0.5f);
+    while (m * (m + 1) / 2 > at) --m;
+    while ((m + 1) * (m + 2) / 2 <= at) ++m;
+    return {m, at - m * (m + 1) / 2};
+}
+
 template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool COLS_A_ = false, bool COLS_B_ = false>
 struct TileShape {
     typedef T element;
@@ -82,17 +95,18 @@ struct TileShape {
 // rate32 of 0.6 TFLOP/s), and a round of tiles begins and ends in `ends`.  Fitted to products of 64 to 2048 x 384 to 65536 x 64 to 8192 and within some 20 % of
 // them: bfloat16 2048 x 32768 x 1024 133, 170, 235, 407, 275 us in the five shapes, 1500 x 50000 x 1000 180, 229, 328, 624, 352, 512 x 8192 x 512 21, 12.5,
 // 11.5, 19.4, 15, 1024 x 1024 x 1024 31, 16, 12, 12, 9.
-constexpr int kShapes = 5;
+constexpr int kShapes = 6;
 struct ShapeOf {
     int bm, bn, per_cu;
     double alone, full, rate32, ends;
 };
 constexpr ShapeOf kShape[kShapes] = {
-    {256, 256, 1, 1.53, 1.53, 0.90, 8.7}, {128, 128, 2, 0.80, 0.93, 1.00, 6.0}, {64, 64, 4, 0.45, 0.67, 0.97, 4.5}, {128, 16, 4, 0.45, 0.65, 0.65, 5.5}, {64, 64, 2, 0.28, 0.60, 0.92, 4.5}};
+    {256, 256, 1, 1.53, 1.53, 0.90, 8.7}, {128, 128, 2, 0.80, 0.93, 1.00, 6.0}, {64, 64, 4, 0.45, 0.67, 0.97, 4.5}, {128, 16, 4, 0.45, 0.65, 0.65, 5.5}, {64, 64, 2, 0.28, 0.60, 0.92, 4.5}, {192, 192, 1, 0.92, 0.92, 0.92, 7.0}};
 
-inline double shape_cost(const ShapeOf &s, int64_t m, int64_t n, double k, int64_t count, bool f32)
+inline double shape_cost(const ShapeOf &s, int64_t m, int64_t n, double k, int64_t count, bool f32, bool symmetric = false)
 {
-    const double tiles = (double)((m + s.bm - 1) / s.bm) * (double)((n + s.bn - 1) / s.bn) * count, each = ceil(tiles / 256);
+    const double tiles_m = (double)((m + s.bm - 1) / s.bm), tiles_n = (double)((n + s.bn - 1) / s.bn);
+    const double tiles = (symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n) * count, each = ceil(tiles / 256);
     const double stages = ceil(k / (f32 ? 32 : 64)), rounds = floor(each / s.per_cu), rest = each - rounds * s.per_cu;
     auto round = [&](double at_once) {
         double stage = s.per_cu > 1 ? s.alone + (s.full - s.alone) * (at_once - 1) / (s.per_cu - 1) : s.full;
@@ -102,16 +116,31 @@ inline double shape_cost(const ShapeOf &s, int64_t m, int64_t n, double k, int64
     return rounds * round(s.per_cu) + (rest > 0 ? round(rest) : 0.0);
 }
 
-// `count` products [m, n] over k; the least estimate goes to *cost, if that is given.  Shapes from `shapes` on are left out.
-inline int shape_for(int64_t m, int64_t n, double k, int64_t count, bool f32, double *cost = nullptr, int shapes = kShapes)
+// `count` products [m, n] over k; the least estimate goes to *cost, if that is given.  The last shape is for orthogonalised updates alone.
+inline int shape_for(int64_t m, int64_t n, double k, int64_t count, bool f32, double *cost = nullptr)
 {
     int best = 0;
     double least = 1e300;
-    for (int s = 0; s < shapes; ++s) {
+    for (int s = 0; s < kShapes - 1; ++s) {
         const double c = shape_cost(kShape[s], m, n, k, count, f32);
         if (c < least) least = c, best = s;
     }
     if (cost) *cost = least;
+    return best;
+}
+
+// For orthogonalised updates, 16 bits.  A symmetric product [m, m] may take the tiles on one side of the diagonal alone (square ones), which
+// pays where all tiles are more than the chip takes at once: turning a tile to store it on the other side takes 0.6 to 0.8 us.
+inline StepShape step_shape_for(int64_t m, int64_t n, double k, int64_t count, bool symmetric)
+{
+    StepShape best = {0, false};
+    double least = 1e300;
+    for (int half = 0; half <= (symmetric ? 1 : 0); ++half)
+        for (int s = 0; s < kShapes; ++s) {
+            if (half && kShape[s].bm != kShape[s].bn) continue;
+            const double c = shape_cost(kShape[s], m, n, k, count, false, half) + (half ? 0.8 : 0.0);
+            if (c < least) least = c, best = {s, half != 0};
+        }
     return best;
 }
 
@@ -125,6 +154,8 @@ template <class T, bool COLS_A = false, bool COLS_B = false>
 using Shape3 = TileShape<T, 128, 16, 2, 1, 2, COLS_A, COLS_B>;
 template <class T, bool COLS_A = false, bool COLS_B = false>
 using Shape4 = TileShape<T, 64, 64, 2, 2, 5, COLS_A, COLS_B>;
+template <class T, bool COLS_A = false, bool COLS_B = false>
+using Shape5 = TileShape<T, 192, 192, 2, 4, 3, COLS_A, COLS_B>;
 
 #ifdef __HIP_DEVICE_COMPILE__
 
@@ -172,9 +203,11 @@ struct Side {
     int bytes, k, stages, part;         // (rows) of the buffer; k in bytes; stages, and the one that is not whole
     int width;                          // (columns) bytes of a row of k
     int at[kLoads], piece_at;
-    int from;                           // of the lane's first piece in LDS
+    // of the lane's pieces in LDS.  Rows, and columns of a power of two: the first one's, the others being a step or a changed bit away
+    static constexpr bool kEach = COLS && (B_ & (B_ - 1)) != 0;
+    int from[kEach ? F : 1];
 
-    // the permutation of a row of k
+    // the permutation of a row of k (of 24 pieces, within eight of them)
     static __device__ __forceinline__ int f(int row) { return (kSize == 4 ? (row >> 2 & 3) << 2 : (row & 3) << 1 | (row >> 3 & 1) << 3) & (kPieces - 1); }
 
     __device__ __forceinline__ Side(const char *p, int64_t ld_, int first, int rows, int k_, int mine)
@@ -194,8 +227,12 @@ struct Side {
                 at[i] = piece * 16 < width ? row * (int)ld + piece * 16 : (int)0x80000000;
             }
             const int g = lane >> 4, r = lane & 15;
-            if (kSize == 4) from = 4 * g * kLine + (((mine + r) / 4 ^ f(4 * g)) * 16) + (r & 3) * 4;
-            else from = (8 * g + (r >> 2)) * kLine + ((mine / 8 + ((r & 3) >> 1)) ^ f(8 * g + (r >> 2))) * 16 + (r & 1) * 8;
+            static_assert(kSize == 2 || !kEach, "whole powers of two in fp32");
+#pragma unroll
+            for (int i = 0; i < (kEach ? F : 1); ++i) {
+                if (kSize == 4) from[i] = 4 * g * kLine + (((mine + r) / 4 ^ f(4 * g)) * 16) + (r & 3) * 4;
+                else from[i] = (8 * g + (r >> 2)) * kLine + ((mine / 8 + 2 * i + ((r & 3) >> 1)) ^ f(8 * g + (r >> 2))) * 16 + (r & 1) * 8;
+            }
         } else {
             base = p + first * ld;
             k = (k_ * kSize + 15) & ~15;
@@ -204,7 +241,7 @@ struct Side {
             piece_at = ((lane & 7) ^ (lane >> 3)) * 16;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) at[i] = min((i * (THREADS / 64) + wave) * 8 + (lane >> 3), left - 1) * (int)ld + piece_at;
-            from = (mine + (lane & 15)) * kRowBytes + ((lane >> 4) ^ (lane & 7)) * 16;
+            from[0] = (mine + (lane & 15)) * kRowBytes + ((lane >> 4) ^ (lane & 7)) * 16;
         }
     }
 
@@ -241,14 +278,14 @@ struct Side {
         for (int i = 0; i < F; ++i) {
             if constexpr (!COLS) {
                 typedef const __attribute__((address_space(3))) piece lds_piece;
-                to[i] = *(lds_piece *)(stage + (from ^ (half * 64)) + i * 16 * kRowBytes);
+                to[i] = *(lds_piece *)(stage + (from[0] ^ (half * 64)) + i * 16 * kRowBytes);
             } else if constexpr (kSize == 4) {
                 typedef const __attribute__((address_space(3))) float lds_float;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) to[i][q] = *(lds_float *)(stage + (from ^ (i * 64)) + (half * 16 + q) * kLine);
+                for (int q = 0; q < 4; ++q) to[i][q] = *(lds_float *)(stage + (from[0] ^ (i * 64)) + (half * 16 + q) * kLine);
             } else {
-                const s16x4 low = read_turned((lds_s16x4 *)(stage + (from ^ (i * 32)) + half * 32 * kLine));
-                const s16x4 high = read_turned((lds_s16x4 *)(stage + (from ^ (i * 32)) + (half * 32 + 4) * kLine));
+                const lds_char *first = stage + (kEach ? from[kEach ? i : 0] : from[0] ^ (i * 32)) + half * 32 * kLine;
+                const s16x4 low = read_turned((lds_s16x4 *)first), high = read_turned((lds_s16x4 *)(first + 4 * kLine));
                 to[i] = __builtin_bit_cast(piece, (s16x8)__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         }

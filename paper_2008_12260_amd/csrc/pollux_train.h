@@ -80,11 +80,15 @@ int launch_noise_scale(const pollux_noise_dims &d, const void *grads, const floa
 
 // ---- orthogonalised update -----------------------------------------------------------------------------------------
 
+struct StepShape {
+    int shape;                  // of tiles
+    bool half;                  // of a symmetric product, only the tiles on one side of the diagonal
+};
 struct OrthoPlan {
     int m, n;                   // the smaller and the larger side
     bool tall;                  // the gradients have more rows than columns
     int64_t m_pad, x_pad;       // m and cols in whole 16-byte groups
-    int shape_square, shape_wide;       // of the products [m, m] and [m, n]
+    StepShape shape_gram, shape_square, shape_wide;       // of the products X X', A A and B X
     int norm_blocks;            // a matrix
     double unit;                // X is held times this power of two
     size_t norms;               // double [batch, norm_blocks]

@@ -142,3 +142,11 @@ def test_wrong_tensors_are_refused():
         with pytest.raises(px.PolluxError) as e:
             px.orthogonalize(grads, steps, coefficients)
         assert e.value.code == px.PX_E_INVALID_ARG
+
+
+@pytest.mark.parametrize("shape", [(1500, 1700), (2100, 1300), (1300, 2100), (2500, 2300), (3, 1000, 1400), (8, 1305, 2497), (8, 2497, 1305), (30, 450, 500)])
+def test_tiles_of_every_shape_on_both_sides_of_the_diagonal(shape):
+    """Sizes whose symmetric products are formed in tiles of 64 to 256, on and off the diagonal, with ends of every kind."""
+    import paper_2008_12260_amd as px
+    grads = gradients(shape, "bfloat16", 41)
+    close(px.orthogonalize(grads, 2), reference(grads, 2, COEFFICIENTS))
