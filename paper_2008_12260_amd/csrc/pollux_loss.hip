@@ -431,7 +431,9 @@ template <class T>
 void launch_logits(int shape, LogitKind kind, const LogitArgs &a, hipStream_t stream)
 {
     switch (shape) {
-        case 0: launch_logits<Shape0<T>>(kind, a, stream); break;
+        case 0:
+            if constexpr (!std::is_same<T, F32>::value) launch_logits<Shape0<T>>(kind, a, stream);
+            break;
         case 1: launch_logits<Shape1<T>>(kind, a, stream); break;
         case 2: launch_logits<Shape2<T>>(kind, a, stream); break;
         case 3: launch_logits<Shape3<T>>(kind, a, stream); break;
@@ -451,7 +453,9 @@ template <class T, bool COLS_B>
 void launch_grad(int shape, const GradArgs &a, int slices, hipStream_t stream)
 {
     switch (shape) {
-        case 0: launch_grad<Shape0<T, true, COLS_B>>(a, slices, stream); break;
+        case 0:
+            if constexpr (!std::is_same<T, F32>::value) launch_grad<Shape0<T, true, COLS_B>>(a, slices, stream);
+            break;
         case 1: launch_grad<Shape1<T, true, COLS_B>>(a, slices, stream); break;
         case 2: launch_grad<Shape2<T, true, COLS_B>>(a, slices, stream); break;
         case 3: launch_grad<Shape3<T, true, COLS_B>>(a, slices, stream); break;
@@ -536,7 +540,7 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
             g.o.n = g.rows = d.V;
             g.out = weight_grad;
             g.ld = d.weight_grad_stride;
-            launch_grad<T, true>(0, g, 1, stream);
+            launch_grad<T, true>(1, g, 1, stream);
         }
         return status_of(hipGetLastError());
     }

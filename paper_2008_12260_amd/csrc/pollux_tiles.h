@@ -90,18 +90,19 @@ struct TileShape {
     static_assert(kLoadsA * kThreads * 16 == BM * kRowBytes && kLoadsB * kThreads * 16 == BN * kRowBytes, "whole loads");
 };
 
-// Which shape of tile a product is formed in, and in how many slices of k: by what it is estimated to take, in microseconds.  A compute unit works on
-// per_cu tiles of a shape at once; a stage takes `alone` for one of them and `full` for per_cu (16 bits; in fp32 the matrix units are the bound, at
-// rate32 of 0.6 TFLOP/s), and a round of tiles begins and ends in `ends`.  Fitted to products of 64 to 2048 x 384 to 65536 x 64 to 8192 and within some 20 % of
-// them: bfloat16 2048 x 32768 x 1024 133, 170, 235, 407, 275 us in the five shapes, 1500 x 50000 x 1000 180, 229, 328, 624, 352, 512 x 8192 x 512 21, 12.5,
-// 11.5, 19.4, 15, 1024 x 1024 x 1024 31, 16, 12, 12, 9.
+// Which shape of tile a product is formed in, and in how many slices of k: by what it is estimated to take, in microseconds.  A compute
+// unit works on per_cu tiles of a shape at once; a stage takes `alone` for one of them and `full` for per_cu (in fp32 alone32 and full32), and
+// a round of tiles begins and ends in `ends`.  Fitted to products of 64 to 2048 x 384 to 65536 x 64 to 8192 and within some 20 % of them: bfloat16 2048 x 32768 x 1024 133, 170,
+// 235, 407, 275 us in the first five shapes, 1500 x 50000 x 1000 180, 229, 328, 624, 352, 512 x 8192 x 512 21, 12.5, 11.5, 19.4, 15, 1024 x 1024 x 1024 31, 16, 12, 12, 9;
+// fp32 512 x 8192 x 512 33 and 41 us in the second and third.
 constexpr int kShapes = 6;
 struct ShapeOf {
     int bm, bn, per_cu;
-    double alone, full, rate32, ends;
+    double alone, full, alone32, full32, ends;
 };
 constexpr ShapeOf kShape[kShapes] = {
-    {256, 256, 1, 1.53, 1.53, 0.90, 8.7}, {128, 128, 2, 0.80, 0.93, 1.00, 6.0}, {64, 64, 4, 0.45, 0.67, 0.97, 4.5}, {128, 16, 4, 0.45, 0.65, 0.65, 5.5}, {64, 64, 2, 0.28, 0.60, 0.92, 4.5}, {192, 192, 1, 0.92, 0.92, 0.92, 7.0}};
+    {256, 256, 1, 1.53, 1.53, 0.00, 0.00, 8.7}, {128, 128, 2, 0.80, 0.93, 1.70, 2.62, 6.0}, {64, 64, 4, 0.45, 0.67, 0.45, 2.24, 4.5},
+    {128, 16, 4, 0.45, 0.65, 0.45, 1.35, 5.5},  {64, 64, 2, 0.28, 0.60, 0.47, 1.17, 4.5},  {192, 192, 1, 0.92, 0.92, 0.00, 0.00, 7.0}};
 
 inline double shape_cost(const ShapeOf &s, int64_t m, int64_t n, double k, int64_t count, bool f32, bool symmetric = false)
 {
@@ -109,8 +110,8 @@ inline double shape_cost(const ShapeOf &s, int64_t m, int64_t n, double k, int64
     const double tiles = (symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n) * count, each = ceil(tiles / 256);
     const double stages = ceil(k / (f32 ? 32 : 64)), rounds = floor(each / s.per_cu), rest = each - rounds * s.per_cu;
     auto round = [&](double at_once) {
-        double stage = s.per_cu > 1 ? s.alone + (s.full - s.alone) * (at_once - 1) / (s.per_cu - 1) : s.full;
-        if (f32) stage = fmax(stage, at_once * 2.0 * s.bm * s.bn * 32 / (0.6e6 * s.rate32));
+        const double alone = f32 ? s.alone32 : s.alone, full = f32 ? s.full32 : s.full;
+        const double stage = s.per_cu > 1 ? alone + (full - alone) * (at_once - 1) / (s.per_cu - 1) : full;
         return stages * stage + s.ends;
     };
     return rounds * round(s.per_cu) + (rest > 0 ? round(rest) : 0.0);
@@ -121,7 +122,7 @@ inline int shape_for(int64_t m, int64_t n, double k, int64_t count, bool f32, do
 {
     int best = 0;
     double least = 1e300;
-    for (int s = 0; s < kShapes - 1; ++s) {
+    for (int s = f32 ? 1 : 0; s < kShapes - 1; ++s) {          // (in fp32 the split's registers leave no room for tiles of 256)
         const double c = shape_cost(kShape[s], m, n, k, count, f32);
         if (c < least) least = c, best = s;
     }
@@ -161,12 +162,41 @@ using Shape5 = TileShape<T, 192, 192, 2, 4, 3, COLS_A, COLS_B>;
 
 __device__ __forceinline__ f32x4 multiply(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-// fp32: four products of k = 4; which four of a row's sixteen k each takes is the same for both operands
+// fp32: four products of k = 4; which four of a row's sixteen k each takes is the same for both operands.  (Where the split below does not hold.)
 __device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
     return c;
+}
+
+// fp32 on the units of 16 bits, which multiply sixteen times as fast: x = p[0] + p[1] + p[2] in bfloat16, each what the ones before leave: the first 8 bits as
+// they are, 8 rounded to nearest, and the rest, so that all 24 are there (of numbers from 2^-109 up).  Of the nine products of two such sums the three of the lowest bits, below 2^-24 of the whole and
+// of either sign, are left out: six products of 16 bits in place of one, exact in the fp32 sums.
+struct Split {
+    bf16x8 p[3];
+};
+__device__ __forceinline__ Split split(f32x4 low, f32x4 high)
+{
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    typedef float f32x2_ __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    u32x4 p[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = i < 2 ? low[2 * i] : high[2 * i - 4], y = i < 2 ? low[2 * i + 1] : high[2 * i - 3];
+        const unsigned tx = __float_as_uint(x) & 0xffff0000u, ty = __float_as_uint(y) & 0xffff0000u;
+        p[0][i] = __builtin_amdgcn_perm(ty, tx, 0x07060302u);
+        const float rx = x - __uint_as_float(tx), ry = y - __uint_as_float(ty);
+        const unsigned second = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2_{rx, ry}, bf16x2));
+        p[1][i] = second;
+        const float sx = rx - __uint_as_float(second << 16), sy = ry - __uint_as_float(second & 0xffff0000u);
+        p[2][i] = __builtin_amdgcn_perm(__float_as_uint(sy), __float_as_uint(sx), 0x07060302u);
+    }
+    Split s;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) s.p[k] = __builtin_bit_cast(bf16x8, p[k]);
+    return s;
 }
 
 // Where the lane's values of acc[i][j] belong: rows m = first_m + 16 i + 0..3 and column n = first_n + 16 j of the product.
@@ -292,8 +322,8 @@ struct Side {
     }
 };
 
-template <class S>
-__device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *lds_, f32x4 (&acc)[S::FM][S::FN])
+template <class S, bool SPLIT>
+__device__ __forceinline__ void form_tile(const Operands &o, Tile t, char *lds_, f32x4 (&acc)[S::FM][S::FN])
 {
     typedef typename S::element T;
     typedef typename T::piece piece;
@@ -343,7 +373,7 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
     // halves, when the whole stage has been read: the loads of the stage kStages later go where it was.
     constexpr int kReads = SideA::kReads + SideB::kReads, kProducts = S::FM * S::FN * (SideA::kSize == 4 ? 4 : 1);
     constexpr int kPerRead = kProducts / (kReads + 4) > 0 ? kProducts / (kReads + 4) : 1, kPerLoad = kPerRead;
-    constexpr int kMatrix = 0x008, kVector = 0x010, kLds = 0x100;         // the scheduler's groups of instructions
+    constexpr int kValu = 0x002, kMatrix = 0x008, kVector = 0x010, kLds = 0x100;         // the scheduler's groups of instructions
     piece a0[S::FM], b0[S::FN], a1[S::FM], b1[S::FN];
     typedef std::integral_constant<int, kAhead> some;
     typedef std::integral_constant<int, 0> all;
@@ -353,6 +383,38 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
     load(S::kStages - 1, S::kStages - 1);
     read(0, 0, a0, b0);
     int at = 0;
+    if constexpr (SPLIT) {
+        for (int s = 0; s < stages; ++s) {
+            read(at, 1, a1, b1);
+            wait(some());
+            load(s + S::kStages, at);
+            at = at + 1 == S::kStages ? 0 : at + 1;
+            Split b[S::FN], a = split(a0[0], a1[0]);
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) b[j] = split(b0[j], b1[j]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                // (the next rows' split between the products of these)
+                const Split next = i + 1 < S::FM ? split(a0[i + 1 < S::FM ? i + 1 : 0], a1[i + 1 < S::FM ? i + 1 : 0]) : a;
+                constexpr int kOf[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};        // the small ones first
+#pragma unroll
+                for (int k = 0; k < 6; ++k)
+#pragma unroll
+                    for (int j = 0; j < S::FN; ++j) acc[i][j] = multiply(a.p[kOf[k][0]], b[j].p[kOf[k][1]], acc[i][j]);
+                a = next;
+                constexpr int kSplit = 48, kEach = (kSplit + 6 * S::FN - 1) / (6 * S::FN);
+#pragma unroll
+                for (int k = 0; k < 6 * S::FN; ++k) {
+                    __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 2);
+                    __builtin_amdgcn_sched_group_barrier(kValu, kEach, 2);
+                }
+            }
+            read(at, 0, a0, b0);
+        }
+        wait(all());
+        return;
+    }
     for (int s = 0; s < stages; ++s) {
         read(at, 1, a1, b1);
         multiply_all(a0, b0);
@@ -381,6 +443,32 @@ __device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *ld
     }
     // the loads of stages past the end write zeros: nobody else's data may be there before they have
     wait(all());
+}
+
+// In fp32 by the split, whose parts of an infinite element are inf - inf: a tile in which something is not finite is formed again
+// without it, and is what the formula says.
+template <class S>
+__device__ __forceinline__ void tile_product(const Operands &o, Tile t, char *lds, f32x4 (&acc)[S::FM][S::FN])
+{
+    constexpr bool kSplit = std::is_same<typename S::element, F32>::value && S::FN >= 4;
+    form_tile<S, kSplit>(o, t, lds, acc);
+    if constexpr (kSplit) {
+        float sum = 0.f;                   // (0 times each: 0, or NaN)
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum = fmaf(acc[i][j][r], 0.f, sum);
+        volatile __attribute__((address_space(3))) int *const bad = (volatile __attribute__((address_space(3))) int *)(lds_char *)lds;
+        if (threadIdx.x == 0) *bad = 0;
+        __syncthreads();
+        if (!(sum == 0.f)) *bad = 1;
+        __syncthreads();
+        const bool again = *bad != 0;
+        __syncthreads();
+        if (again) form_tile<S, false>(o, t, lds, acc);
+    }
 }
 
 // Four values in the lane's own row n, as stored: contiguous in m.

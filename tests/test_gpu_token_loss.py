@@ -348,3 +348,37 @@ def test_scratch_memory_has_to_be_on_the_gpu():
         for bad in (host, torch.empty((1 << 20, 2), dtype=torch.uint8, device="cuda")[:, 0]):
             with pytest.raises(ValueError):
                 call(bad)
+
+
+@pytest.mark.parametrize("N,V,D", [(300, 9000, 300), (600, 5000, 512), (1501, 3001, 77)])
+def test_fp32_in_large_tiles(N, V, D):
+    """Sizes at which fp32 is multiplied in parts of 16 bits: the same tolerances, with elements of very different sizes too."""
+    import torch
+    args = inputs(N, V, D, "float32", 61)
+    close(run(*args), reference(*args))
+    hidden, weight, targets, row_weight = args
+    g = torch.Generator("cuda").manual_seed(62)
+    hidden = hidden * torch.exp2(torch.randint(-20, 1, (1, D), generator=g, device="cuda").float())
+    weight = weight * torch.exp2(torch.randint(-30, 1, (1, D), generator=g, device="cuda").float())
+    close(run(hidden, weight, targets, row_weight), reference(hidden, weight, targets, row_weight))
+
+
+def test_fp32_logits_that_are_not_finite_in_large_tiles():
+    import torch
+    import paper_2008_12260_amd as px
+    inf = float("inf")
+    hidden, weight, targets, _ = inputs(600, 5000, 512, "float32", 63, ignored=0.0)
+    weight = weight.abs()
+    hidden[7, 5] = inf
+    hidden[300, 5] = -inf
+    hidden[431, 9] = float("nan")
+    big = 2.0 ** 127 * (2 - 2.0 ** -23)                 # the largest number, which no bfloat16 holds
+    hidden[511] = 0
+    hidden[511, 0] = big
+    weight[:, 0] = 2.0 ** -124
+    loss, lse = px.token_loss(hidden, weight, targets)
+    want = torch.logsumexp(torch.mm(hidden.double(), weight.double().t()), 1)
+    assert lse[7] == inf and lse[300] == -inf and bool(torch.isnan(lse[431]))
+    rest = torch.ones(600, dtype=torch.bool, device="cuda")
+    rest[[7, 300, 431]] = False
+    assert bool(((lse.double() - want).abs() <= 2.0 ** -10 + 2.0 ** -22 * want.abs())[rest].all())
