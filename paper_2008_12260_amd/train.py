@@ -11,11 +11,13 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 
 import paper_2008_12260_amd as _px
 
 
+_POISON = "POLLUX_POISON_WORKSPACE" in os.environ
 _TYPES = {}              # torch's types to the library's, filled at the first call
 
 
@@ -95,10 +97,19 @@ def _scratch(workspace, need, device):
         return workspace, workspace.numel() * workspace.element_size()
     import torch
     ws = torch.empty(need, dtype=torch.uint8, device=device)
-    if "POLLUX_POISON_WORKSPACE" in os.environ:
+    if _POISON:
         # for tests: nothing in the library may depend on what a fresh workspace holds (0xFF bytes read as NaN / -1)
         ws.fill_(0xFF)
     return ws, need
+
+
+# What a call's sizes, types and strides determine: the library's description of them and the scratch memory it asks for.  (Asking each time is 2 to
+# 4 us of a call's host time.)
+@functools.lru_cache(maxsize=1024)
+def _planned(cls, query, more, *values):
+    dims, need = cls(*values), ctypes.c_size_t(0)
+    _check(getattr(_px.lib(), query)(ctypes.byref(dims), *more, ctypes.byref(need)), query)
+    return ctypes.byref(dims), need.value
 
 
 def _check(rc, where):
@@ -107,23 +118,18 @@ def _check(rc, where):
 
 
 def _loss_call(hidden, weight, targets):
-    _on_device(hidden, weight, targets)
-    if hidden.dtype != weight.dtype:
+    """The tensors as the library takes them, and (N, V, D, type, flag, hidden_stride, weight_stride)."""
+    if hidden.dtype is not weight.dtype:
         raise TypeError(f"hidden is {hidden.dtype} and weight {weight.dtype}: one type is wanted")
     type_ = _type(hidden, "hidden")
     hidden, hidden_stride = _rows(hidden, "hidden")
     weight, weight_stride = _rows(weight, "weight")
-    if hidden.shape[1] != weight.shape[1]:
-        raise ValueError(f"rows of hidden have {hidden.shape[1]} elements, of weight {weight.shape[1]}")
-    targets, flag = _tokens(targets, "targets", hidden.shape[0])
-    dims = _px.LossDims(hidden.shape[0], weight.shape[0], hidden.shape[1], type_, flag, hidden_stride, weight_stride, 0, 0)
-    return dims, hidden, weight, targets
-
-
-def _loss_scratch(dims, grad, workspace, device):
-    need = ctypes.c_size_t(0)
-    _check(_px.lib().pollux_loss_workspace_size(ctypes.byref(dims), grad, ctypes.byref(need)), "pollux_loss_workspace_size")
-    return _scratch(workspace, need.value, device)
+    N, D = hidden.shape
+    V, width = weight.shape
+    if D != width:
+        raise ValueError(f"rows of hidden have {D} elements, of weight {width}")
+    targets, flag = _tokens(targets, "targets", N)
+    return hidden, weight, targets, (N, V, D, type_, flag, hidden_stride, weight_stride)
 
 
 def token_loss(hidden, weight, targets, workspace=None, stream=None):
@@ -133,13 +139,15 @@ def token_loss(hidden, weight, targets, workspace=None, stream=None):
     pollux_last_status(workspace) where the caller gives the workspace."""
     import torch
     with _on(stream):
-        dims, hidden, weight, targets = _loss_call(hidden, weight, targets)
-        workspace, size = _loss_scratch(dims, 0, workspace, hidden.device)
-        loss = torch.empty(dims.N, dtype=torch.float32, device=hidden.device)
-        lse = torch.empty(dims.N, dtype=torch.float32, device=hidden.device)
-        _check(_px.lib().pollux_token_loss(ctypes.byref(dims), hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), workspace.data_ptr(),
-                                           size, loss.data_ptr(), lse.data_ptr(),
-                                           _px._stream_handle(stream)), "pollux_token_loss")
+        _on_device(hidden, weight, targets)
+        hidden, weight, targets, sizes = _loss_call(hidden, weight, targets)
+        dims, need = _planned(_px.LossDims, "pollux_loss_workspace_size", (0,), *sizes, 0, 0)
+        device = hidden.device
+        workspace, size = _scratch(workspace, need, device)
+        loss = torch.empty(sizes[0], dtype=torch.float32, device=device)
+        lse = torch.empty_like(loss)
+        _check(_px.lib().pollux_token_loss(dims, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), workspace.data_ptr(), size, loss.data_ptr(),
+                                           lse.data_ptr(), _px._stream_handle(stream)), "pollux_token_loss")
     return loss, lse
 
 
@@ -152,27 +160,31 @@ def token_loss_grad(hidden, weight, targets, lse, row_weight=None, hidden_grad=N
     added to."""
     import torch
     with _on(stream):
-        dims, hidden, weight, targets = _loss_call(hidden, weight, targets)
+        _on_device(hidden, weight, targets, lse, row_weight, hidden_grad, weight_grad)
+        hidden, weight, targets, sizes = _loss_call(hidden, weight, targets)
+        N, V, D = sizes[:3]
         for name, t in (("lse", lse), ("row_weight", row_weight)):
-            if t is not None and (t.dtype != torch.float32 or t.shape != (dims.N,) or not t.is_contiguous()):
-                raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}: contiguous float32 ({dims.N},) is wanted")
-        _on_device(lse, row_weight, hidden_grad, weight_grad)
+            if t is not None and (t.dtype is not torch.float32 or t.shape != (N,) or not t.is_contiguous()):
+                raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}: contiguous float32 ({N},) is wanted")
         if accumulate and weight_grad is None:
             raise ValueError("accumulate needs a weight_grad to add to")
-        if hidden_grad is None and need[0]:
-            hidden_grad = torch.empty((dims.N, dims.D), dtype=hidden.dtype, device=hidden.device)
-        if weight_grad is None and need[1]:
-            weight_grad = torch.empty((dims.V, dims.D), dtype=hidden.dtype, device=hidden.device)
+        dtype, device = hidden.dtype, hidden.device
+        hidden_stride = weight_stride = 0
         if hidden_grad is not None:
-            hidden_grad, dims.hidden_grad_stride = _result(hidden_grad, "hidden_grad", (dims.N, dims.D), hidden.dtype)
+            hidden_grad, hidden_stride = _result(hidden_grad, "hidden_grad", (N, D), dtype)
+        elif need[0]:
+            hidden_grad = torch.empty((N, D), dtype=dtype, device=device)
         if weight_grad is not None:
-            weight_grad, dims.weight_grad_stride = _result(weight_grad, "weight_grad", (dims.V, dims.D), hidden.dtype)
+            weight_grad, weight_stride = _result(weight_grad, "weight_grad", (V, D), dtype)
+        elif need[1]:
+            weight_grad = torch.empty((V, D), dtype=dtype, device=device)
+        N, V, D, type_, flags, *strides = sizes
         if accumulate:
-            dims.flags |= _px.PX_FLAG_ACCUMULATE
-        workspace, size = _loss_scratch(dims, 1, workspace, hidden.device)
-        _check(_px.lib().pollux_token_loss_grad(ctypes.byref(dims), hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), lse.data_ptr(),
-                                                _px._ptr(row_weight), workspace.data_ptr(), size,
-                                                _px._ptr(hidden_grad), _px._ptr(weight_grad), _px._stream_handle(stream)),
+            flags |= _px.PX_FLAG_ACCUMULATE
+        dims, bytes_ = _planned(_px.LossDims, "pollux_loss_workspace_size", (1,), N, V, D, type_, flags, *strides, hidden_stride, weight_stride)
+        workspace, size = _scratch(workspace, bytes_, device)
+        _check(_px.lib().pollux_token_loss_grad(dims, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), lse.data_ptr(), _px._ptr(row_weight),
+                                                workspace.data_ptr(), size, _px._ptr(hidden_grad), _px._ptr(weight_grad), _px._stream_handle(stream)),
                "pollux_token_loss_grad")
     return hidden_grad, weight_grad
 
@@ -187,7 +199,7 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
         _on_device(tokens, table, out, status)
         table_type = _type(table, "table")
         table, table_stride = _rows(table, "table")
-        count, D = tokens.numel(), table.shape[1]
+        count, (V, D) = tokens.numel(), table.shape
         if status is not None and (status.dtype != torch.int32 or status.numel() != 1):
             raise ValueError("status is one int32")
         flat, flag = _tokens(tokens, "tokens", count)
@@ -196,8 +208,8 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
         else:
             rows, rows_stride = _result(out.view(count, D), "out", (count, D), table.dtype if dtype is None else dtype)
         rows_type = table_type if rows.dtype is table.dtype else _type(rows, "rows")
-        dims = _px.EmbedDims(count, table.shape[0], D, table_type, rows_type, flag, float(scale), table_stride, rows_stride)
-        _check(_px.lib().pollux_embed(ctypes.byref(dims), flat.data_ptr(), table.data_ptr(), rows.data_ptr(), _px._ptr(status),
+        dims, _ = _planned(_px.EmbedDims, "pollux_embed_workspace_size", (), count, V, D, table_type, rows_type, flag, float(scale), table_stride, rows_stride)
+        _check(_px.lib().pollux_embed(dims, flat.data_ptr(), table.data_ptr(), rows.data_ptr(), _px._ptr(status),
                                       _px._stream_handle(stream)), "pollux_embed")
     return rows if out is None else out
 
@@ -220,12 +232,10 @@ def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, acc
         if table_grad is None:
             table_grad = torch.empty((V, D), dtype=rows.dtype if dtype is None else dtype, device=rows.device)
         table_grad, table_stride = _result(table_grad, "table_grad", (V, D), table_grad.dtype if dtype is None else dtype)
-        dims = _px.EmbedDims(count, V, D, _type(table_grad, "table_grad"), rows_type, flag | (_px.PX_FLAG_ACCUMULATE if accumulate else 0), float(scale),
-                             table_stride, rows_stride)
-        need = ctypes.c_size_t(0)
-        _check(_px.lib().pollux_embed_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_embed_workspace_size")
-        workspace, size = _scratch(workspace, need.value, rows.device)
-        _check(_px.lib().pollux_embed_grad(ctypes.byref(dims), flat.data_ptr(), rows.data_ptr(), workspace.data_ptr(),
+        dims, need = _planned(_px.EmbedDims, "pollux_embed_workspace_size", (), count, V, D, _type(table_grad, "table_grad"), rows_type,
+                              flag | (_px.PX_FLAG_ACCUMULATE if accumulate else 0), float(scale), table_stride, rows_stride)
+        workspace, size = _scratch(workspace, need, rows.device)
+        _check(_px.lib().pollux_embed_grad(dims, flat.data_ptr(), rows.data_ptr(), workspace.data_ptr(),
                                            size, table_grad.data_ptr(), _px._stream_handle(stream)),
                "pollux_embed_grad")
     return table_grad
@@ -240,8 +250,8 @@ def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=T
         _on_device(grads, precondition)
         if grads.dim() < 2:
             raise ValueError("grads holds one gradient a row: [B, ...]")
-        type_, B, shape = _type(grads, "grads"), grads.shape[0], tuple(grads.shape[1:])
-        flat = grads.flatten(1)
+        type_, (B, *shape) = _type(grads, "grads"), grads.shape
+        flat = grads if len(shape) == 1 else grads.flatten(1)
         n = flat.shape[1]
         if n > 1 and flat.stride(1) != 1 or flat.stride(0) < n or flat.data_ptr() % 16:
             flat = flat.clone(memory_format=_contiguous())
@@ -253,11 +263,10 @@ def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=T
                 precondition = precondition.clone()
         mean = torch.empty(shape, dtype=torch.float32 if mean_dtype is None else mean_dtype, device=flat.device) if want_mean else None
         scale = torch.empty(3, dtype=torch.float64, device=flat.device)
-        dims = _px.NoiseDims(n, B, type_, _px.PX_TYPE_F32 if mean is None else _type(mean, "mean"), 0, flat.stride(0), float(examples))
-        need = ctypes.c_size_t(0)
-        _check(_px.lib().pollux_noise_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_noise_workspace_size")
-        workspace, size = _scratch(None, need.value, flat.device)
-        _check(_px.lib().pollux_noise_scale(ctypes.byref(dims), flat.data_ptr(), _px._ptr(precondition), workspace.data_ptr(), size,
+        dims, need = _planned(_px.NoiseDims, "pollux_noise_workspace_size", (), n, B, type_, _px.PX_TYPE_F32 if mean is None else _type(mean, "mean"), 0,
+                              flat.stride(0), float(examples))
+        workspace, size = _scratch(None, need, flat.device)
+        _check(_px.lib().pollux_noise_scale(dims, flat.data_ptr(), _px._ptr(precondition), workspace.data_ptr(), size,
                                             _px._ptr(mean), scale.data_ptr(), _px._stream_handle(stream)), "pollux_noise_scale")
     return mean, scale
 
@@ -284,10 +293,9 @@ def orthogonalize(grads, steps=5, coefficients=(3.4445, -4.7750, 2.0315), out=No
         elif out.shape != shape or out.dtype != torch.bfloat16 or not out.is_contiguous() or out.data_ptr() % 16:
             raise ValueError(f"out is {out.dtype} {tuple(out.shape)}: contiguous bfloat16 {shape} is wanted")
         ld = flat.stride(1) if rows > 1 else cols
-        dims = _px.OrthoDims(batch, rows, cols, type_, steps, 0, *(float(c) for c in coefficients), ld, 0, flat.stride(0) if batch > 1 else 0, 0)
-        need = ctypes.c_size_t(0)
-        _check(_px.lib().pollux_ortho_workspace_size(ctypes.byref(dims), ctypes.byref(need)), "pollux_ortho_workspace_size")
-        workspace, size = _scratch(workspace, need.value, flat.device)
-        _check(_px.lib().pollux_orthogonalize(ctypes.byref(dims), flat.data_ptr(), workspace.data_ptr(), size,
+        dims, need = _planned(_px.OrthoDims, "pollux_ortho_workspace_size", (), batch, rows, cols, type_, steps, 0, *(float(c) for c in coefficients), ld, 0,
+                              flat.stride(0) if batch > 1 else 0, 0)
+        workspace, size = _scratch(workspace, need, flat.device)
+        _check(_px.lib().pollux_orthogonalize(dims, flat.data_ptr(), workspace.data_ptr(), size,
                                               out.data_ptr(), _px._stream_handle(stream)), "pollux_orthogonalize")
     return out
