@@ -163,14 +163,20 @@ __global__ __launch_bounds__(kJoinThreads) void loss_join(const float2 *parts, i
 
 // ---- backward ------------------------------------------------------------------------------------------------------
 
-// Clears the status word, and, for fp16, finds the power of two that q is scaled by: scale[0] that, scale[1] its inverse.
-__global__ __launch_bounds__(1024) void grad_begin(const void *targets, bool i64, int V, int N, const float *row_weight, int32_t *status, float *scale)
+// Clears the status word where nothing else is launched.
+__global__ void clear_status(int32_t *status)
 {
-    __shared__ float tops[16];
     if (threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
-    if (!scale) return;
+}
+
+#ifdef __HIP_DEVICE_COMPILE__
+// For fp16, by one workgroup of 256: the power of two that q is scaled by: scale[0] that, scale[1] its inverse.
+__device__ __forceinline__ void find_scale(const void *targets, bool i64, int V, int64_t N, const float *row_weight, float *scale)
+{
+    __shared__ float tops[4];
     float top = 0.f;
-    for (int n = threadIdx.x; n < N; n += 1024) {
+#pragma unroll 8
+    for (int64_t n = threadIdx.x; n < N; n += 256) {
         const float g = target_of(targets, n, i64, V) < 0 ? 0.f : row_weight ? fabsf(row_weight[n]) : 1.f;
         if (g < __builtin_inff()) top = fmaxf(top, g);
     }
@@ -179,11 +185,12 @@ __global__ __launch_bounds__(1024) void grad_begin(const void *targets, bool i64
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
     if (threadIdx.x != 0) return;
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, tops[i]);
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, tops[i]);
     const int e = top > 0.f ? min(100, max(-100, 13 - ilogbf(top))) : 0;
     scale[0] = ldexpf(1.f, e);
     scale[1] = ldexpf(1.f, -e);
 }
+#endif
 
 // One tile of q from the logits' tile.  A token without a target, or of weight 0, has a row of zeros,
 // whatever its logits are.
@@ -394,16 +401,22 @@ __global__ __launch_bounds__(256) void join_slices(const GradArgs A, const float
 #endif
 }
 
-// Rows copied to aligned ones, `cols` padded with zeros to ld_to; rows without a target, or of weight 0, are copied as zeros.
+// Rows copied to aligned ones, `cols` padded with zeros to ld_to; rows without a target, or of weight 0, are copied as zeros.  scale: one more
+// workgroup finds it (a launch of its own took 5 us).
 template <class E>
 __global__ __launch_bounds__(256) void pack_rows(const E *from, int64_t ld_from, int64_t rows, int cols, E *to, int64_t ld_to, const void *targets, const float *row_weight,
-                                                 bool i64, int V, int32_t *status)
+                                                 bool i64, int V, int32_t *status, float *scale)
 {
 #ifdef __HIP_DEVICE_COMPILE__
+    const unsigned blocks = gridDim.x - (scale ? 1 : 0);
+    if (blockIdx.x == blocks) {
+        find_scale(targets, i64, V, rows, row_weight, scale);
+        return;
+    }
     if (status && blockIdx.x == 0 && threadIdx.x < kStatusWords) status[threadIdx.x] = 0;
     const int groups = (int)((ld_to + kVec - 1) / kVec);
     const int64_t total = rows * groups;
-    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += gridDim.x * 256ll) {
+    for (int64_t at = blockIdx.x * 256ll + threadIdx.x; at < total; at += blocks * 256ll) {
         const int64_t n = at / groups;
         const int c = (int)(at - n * groups) * kVec;
         const bool there = !targets || (target_of(targets, n, i64, V) >= 0 && !(row_weight && row_weight[n] == 0.f));
@@ -475,11 +488,11 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
     const int64_t ld_h = p.pack_hidden ? p.d_pad : d.hidden_stride, ld_w = p.pack_weight ? p.d_pad : d.weight_stride;
     int32_t *status = (int32_t *)(ws + p.status);
     if (N == 0) {
-        hipLaunchKernelGGL(grad_begin, dim3(1), dim3(1024), 0, stream, targets, false, d.V, 0, (const float *)nullptr, status, (float *)nullptr);
+        hipLaunchKernelGGL(clear_status, dim3(1), dim3(64), 0, stream, status);
         return status_of(hipGetLastError());
     }
     if (p.pack_hidden) {
-        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr);
+        hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D, (type *)(ws + p.hidden), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr, (float *)nullptr);
         hidden = ws + p.hidden;
     }
     LogitArgs a = {};
@@ -500,7 +513,7 @@ int token_loss(const pollux_loss_dims &d, const LossPlan &p, const char *hidden,
             const char *from = weight + (int64_t)a.first * d.weight_stride * e;
             if (p.pack_weight) {
                 if (first == 0 || p.pieces > 1)
-                    hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr);
+                    hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr, (float *)nullptr);
                 from = ws + p.weight;
             }
             a.o.a = from;
@@ -531,22 +544,21 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
     const bool i64 = d.flags & PX_FLAG_TOKENS_I64;
     int32_t *status = (int32_t *)(ws + p.status);
     float *scale = scaled ? (float *)(ws + p.top) : nullptr;
-    // (elsewhere the first of the copies below clears the status word)
-    if (scaled || N == 0) hipLaunchKernelGGL(grad_begin, dim3(1), dim3(1024), 0, stream, targets, i64, d.V, N, row_weight, status, scale);
     if (N == 0) {
+        hipLaunchKernelGGL(clear_status, dim3(1), dim3(64), 0, stream, status);
         if (weight_grad && !(d.flags & PX_FLAG_ACCUMULATE)) {      // products over no tokens
             GradArgs g = {};
             g.o.m = g.cols = d.D;
             g.o.n = g.rows = d.V;
             g.out = weight_grad;
-            g.ld = d.weight_grad_stride;
+            g.ld = d.weight_grad_stride;            // (no scale: the sums are zeros)
             launch_grad<T, true>(1, g, 1, stream);
         }
         return status_of(hipGetLastError());
     }
-    // (a product with q's zeros would still be NaN where a row that counts for nothing holds one)
-    hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D,
-                       (type *)(ws + p.hidden), p.d_pad, targets, row_weight, i64, d.V, status);
+    // (this clears the status word too; a product with q's zeros would still be NaN where a row that counts for nothing holds one)
+    hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(N * ((p.d_pad + kVec - 1) / kVec)) + (scaled ? 1 : 0)), dim3(256), 0, stream, (const type *)hidden, d.hidden_stride, (int64_t)N, d.D,
+                       (type *)(ws + p.hidden), p.d_pad, targets, row_weight, i64, d.V, status, scale);
     LogitArgs a = {};
     a.targets = targets;
     a.i64 = i64;
@@ -580,7 +592,7 @@ int token_loss_grad(const pollux_loss_dims &d, const LossPlan &p, const char *hi
         a.rows = a.o.m = std::min(p.piece, d.V - a.first);
         const char *from = weight + (int64_t)a.first * d.weight_stride * e;
         if (p.pack_weight) {
-            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr);
+            hipLaunchKernelGGL(pack_rows<type>, dim3(blocks_for(a.rows * ((p.d_pad + kVec - 1) / kVec))), dim3(256), 0, stream, (const type *)from, d.weight_stride, (int64_t)a.rows, d.D, (type *)(ws + p.weight), p.d_pad, (const void *)nullptr, (const float *)nullptr, false, 0, (int32_t *)nullptr, (float *)nullptr);
             from = ws + p.weight;
         }
         a.o.a = from;
