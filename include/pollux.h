@@ -495,8 +495,9 @@ enum {
  *   hidden_grad[n,:] = sum_v q[n,v] weight[v,:],   weight_grad[v,:] = sum_n q[n,v] hidden[n,:].
  * A token without a target, or of row weight 0, adds nothing to weight_grad and has a row of zeros in hidden_grad whatever its
  * hidden row holds.  Either gradient may be NULL.  The logits are formed again, a piece of the vocabulary at a time; q is rounded to
- * the type of the inputs for the matrix units (fp16: scaled, so that weights g of any size keep their precision).  Sums over
- * tokens and entries are in fp32 and in a fixed order: the same call gives the same bits.
+ * the type of the inputs for the matrix units (fp16: scaled, so that weights g of any size keep their precision), but for the target's entry in
+ * hidden_grad, which counts in full.  Sums over tokens and entries are in fp32 and in a fixed order: the same call gives the same bits.
+ * fp32 inputs are multiplied with all of their 24 bits (elements smaller than 2^-109 may count with fewer).
  *
  * Limits: 0 <= N <= 2^20, 1 <= V <= 2^20, 1 <= D <= 2^16, strides below 2^20.  workspace: pollux_loss_workspace_size bytes,
  * 256-byte aligned; pollux_last_status on it reads the status word (PX_ST_BAD_TOKEN).

@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void place_digits(const void *tokens, boo
         }
         if (FIRST) {
             // equal keys go to places in a row, in one of the second pass's workgroups or in two: one lane counts for all that share both
-            // (a frequent token is in a wavefront many times, and adding one by one they would wait for each other: 12 us for 16384 tokens, 7 so)
+            // (a frequent token is in a wavefront many times, and adding one by one they would wait for each other: 16384 tokens 12 us, 10 so)
             const int high = key >> bits, block = to / per_block;
             for (int b = 0; b < bits; ++b) {
                 const unsigned long long set = __ballot((high >> b) & 1);

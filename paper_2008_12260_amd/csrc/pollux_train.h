@@ -31,7 +31,7 @@ __device__ __forceinline__ int token_at(const void *tokens, int64_t n, bool i64,
 struct LossPlan {
     bool grad;
     bool pack_hidden, pack_weight;      // rows that 16-byte loads cannot take are copied to aligned ones first
-    int tiles;                          // which shape of tile the logits are formed in (loss_tiles_shape)
+    int tiles;                          // which shape of tile the logits are formed in (kShape)
     int grad_tiles;                     // and the gradients
     int piece;                          // vocabulary entries taken at a time, a multiple of 256
     int pieces;
