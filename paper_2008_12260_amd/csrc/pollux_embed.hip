@@ -268,28 +268,44 @@ struct SumArgs {
     float scale;
 };
 
-template <class R, class T>
+// WIDE: rows so wide that a wavefront has one window.  Its keys and places then come in one load each, a batch ahead, lane i's
+// being the i-th, and are read out of the lanes: a batch's rows wait for no other load (16384 rows of 2048 in bfloat16 26 us with a load for each, one
+// behind the other).
+template <class R, class T, bool WIDE>
 __global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *rows, T *table)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    const int w = blockIdx.x * A.groups + threadIdx.x / A.lanes;
+    const int group = threadIdx.x / A.lanes, w = blockIdx.x * A.groups + (WIDE ? __builtin_amdgcn_readfirstlane(group) : group);
     const int c = (blockIdx.y * A.lanes + threadIdx.x % A.lanes) * kVec;
-    if (w >= A.windows || c >= A.D) return;
-    const int first = w * A.window, last = min(A.N, first + A.window), left = A.D - c;
+    if (w >= A.windows || (!WIDE && c >= A.D)) return;        // (WIDE: all lanes stay, those past the row's end with nothing to load or store)
+    const int first = w * A.window, last = min(A.N, first + A.window), left = A.D - c, lane = threadIdx.x & 63;
     f32x8 sum = {};
+    constexpr int kAhead = sizeof(R) == 2 ? 16 : 8;
+    int lane_key = 0, lane_place = 0;
+    auto fetch = [&](int at) {
+        if constexpr (WIDE) {
+            const int p = min(at + lane, A.N - 1);
+            lane_key = A.keys[p];
+            lane_place = A.places[p];
+        }
+    };
+    fetch(first);
     int run = A.keys[first];
     bool cut = first > 0 && A.keys[first - 1] == run;         // by the window's first place
-    constexpr int kAhead = 8;
     for (int at = first; at < last; at += kAhead) {
-        f32x8 x[kAhead];
-        int key[kAhead + 1];
+        typename Eight<R>::type x[kAhead];
+        int key[kAhead + 1], place[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int p = min(at + i, A.N - 1);
-            key[i] = A.keys[p];
-            if (at + i < last && key[i] < A.V) x[i] = load8f(rows + (int64_t)A.places[p] * A.ld_rows + c, left);
+            key[i] = WIDE ? __builtin_amdgcn_readlane(lane_key, i) : A.keys[p];
+            place[i] = WIDE ? __builtin_amdgcn_readlane(lane_place, i) : A.places[p];
         }
-        key[kAhead] = at + kAhead < A.N ? A.keys[at + kAhead] : -1;
+        key[kAhead] = at + kAhead >= A.N ? -1 : WIDE ? __builtin_amdgcn_readlane(lane_key, kAhead) : A.keys[at + kAhead];
+        if (at + kAhead < last) fetch(at + kAhead);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (at + i < last && key[i] < A.V) x[i] = load8(rows + (int64_t)place[i] * A.ld_rows + c, left);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (at + i >= last) break;
@@ -299,7 +315,7 @@ __global__ __launch_bounds__(256) void sum_windows(const SumArgs A, const R *row
                 cut = false;
                 sum = f32x8{};
             }
-            sum += x[i];
+            sum += __builtin_convertvector(x[i], f32x8);
             const bool ends = at + i + 1 >= A.N || key[i + 1] != run, final = at + i + 1 >= last;
             if (!ends && !final) continue;
             if (ends && !cut) {
@@ -404,8 +420,9 @@ int embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *token
     a.add = add;
     a.scale = d.scale;
     const unsigned parts = (unsigned)((d.D + 256 * kVec - 1) / (256 * kVec));
-    if (p.windows > 0)
-        hipLaunchKernelGGL((sum_windows<R, T>), dim3((unsigned)((p.windows + a.groups - 1) / a.groups), parts), dim3(256), 0, stream, a, rows, table);
+    const dim3 grid_sums((unsigned)((p.windows + a.groups - 1) / a.groups), parts);
+    if (p.windows > 0 && a.lanes >= 64) hipLaunchKernelGGL((sum_windows<R, T, true>), grid_sums, dim3(256), 0, stream, a, rows, table);
+    else if (p.windows > 0) hipLaunchKernelGGL((sum_windows<R, T, false>), grid_sums, dim3(256), 0, stream, a, rows, table);
     if (p.windows > 1) hipLaunchKernelGGL(join_runs<T>, dim3((unsigned)(p.windows - 1), (unsigned)((d.D + 64 * kVec - 1) / (64 * kVec))), dim3(256), 0, stream, a, table);
     return status_of(hipGetLastError());
 }

@@ -30,11 +30,13 @@
 namespace px {
 namespace {
 
+#ifdef __HIP_DEVICE_COMPILE__
 __device__ __forceinline__ int target_of(const void *targets, int64_t n, bool i64, int V)
 {
     bool bad;
     return token_at(targets, n, i64, V, bad);
 }
+#endif
 
 constexpr float kLog2e = 1.44269504088896340736f;
 

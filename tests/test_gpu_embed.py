@@ -236,3 +236,17 @@ def test_tables_of_any_place_are_zeroed_to_their_ends_and_no_further():
         named = torch.unique(tokens[tokens >= 0])
         value, bound = gradient(torch.searchsorted(named, tokens.clamp(min=-1)).where(tokens >= 0, -1), rows, len(named), 1.0)
         close(got[named], value, bound)
+
+
+@pytest.mark.parametrize("rows_type,table_type", [("float32", "float32"), ("bfloat16", "bfloat16"), ("float16", "float32")])
+@pytest.mark.parametrize("N,V,D,share", [(1, 5, 300, 0.0), (9, 2, 520, 0.3), (17, 40, 257, 0.0), (1025, 3, 264, 0.1), (8193, 700, 1000, 0.1), (16390, 9000, 513, 0.0), (33000, 50, 300, 0.9),
+                                         (140001, 400, 258, 0.1)])
+def test_gradients_of_wide_rows(N, V, D, share, rows_type, table_type):
+    """Rows of more than 256 elements: a wavefront a window, in windows of 8 to 128 places, runs within and across them, few and most tokens masked."""
+    import torch
+    import paper_2008_12260_amd as px
+    tokens = tokens_of(N, V, N + D, ignored=share)
+    rows = torch.randn((N, D), device="cuda", generator=torch.Generator("cuda").manual_seed(D)).to(getattr(torch, rows_type))
+    rows[tokens < 0] = float("nan")
+    got = px.embed_grad(tokens, rows, V, 1.25, dtype=getattr(torch, table_type))
+    close(got, *gradient(tokens, rows, V, 1.25))
