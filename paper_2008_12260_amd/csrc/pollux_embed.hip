@@ -58,11 +58,12 @@ __global__ __launch_bounds__(256) void embed_rows(const void *tokens, bool i64, 
 }
 
 // ---- sort ----------------------------------------------------------------------------------------------------------
-// Keys are tokens, V for none (sorted last, and dropped).  Up to kFew tokens: one workgroup counts, for every token, those before it.
+// Keys are tokens, V for none (sorted last, and dropped).  Up to kFew tokens: one workgroup counts, for every token, those before it
+// (265 tokens 17 us in all; 642 30 so, in the passes 25).
 // More: two passes, lowest digit first, of ceil(log2(V + 1)) / 2 bits.
 
 // A table's rows from `first` on, `rows` of them, zeroed by the workgroups from `blocks` on, kZeroAhead groups of 16 bytes a thread and turn.
-constexpr int kFew = 1024, kThreads = 1024, kWaves = kThreads / 64, kMaxBits = 10, kZeroAhead = 4;
+constexpr int kFew = 512, kThreads = 1024, kWaves = kThreads / 64, kMaxBits = 10, kZeroAhead = 4;
 struct ZeroArgs {
     char *table;
     int64_t ld;                 // bytes
@@ -110,34 +111,35 @@ __device__ __forceinline__ bool zero_rows(const ZeroArgs &Z)
     return true;
 }
 
-__global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i64, int N, int V, int32_t *status, int *keys, int *places, const ZeroArgs Z)
+// `parts` threads a token (a power of two, at most a wavefront), each of which compares it with as great a share of all; a key and its position in one
+// number, so that one comparison decides (219 tokens: 7 us of comparing with a thread each and two).
+__global__ __launch_bounds__(kThreads) void rank_few(const void *tokens, bool i64, int N, int V, int parts, int32_t *status, int *keys, int *places, const ZeroArgs Z)
 {
     if (zero_rows(Z)) return;
+    static_assert(kFew <= 1 << 10 && kFew <= kThreads, "positions of 10 bits below keys of 20");
     __shared__ int shared[kFew];
     __shared__ int bad_any;
-    const int n = threadIdx.x;
-    if (n == 0) bad_any = 0;
-    if (n < kStatusWords) status[n] = 0;
+    const int tid = threadIdx.x;
+    if (tid == 0) bad_any = 0;
+    if (tid < kStatusWords) status[tid] = 0;
     bool bad = false;
-    int key = 0x7fffffff;
-    if (n < N) {
-        const int v = token_at(tokens, n, i64, V, bad);
-        key = v < 0 ? V : v;
+    if (tid < N) {
+        const int v = token_at(tokens, tid, i64, V, bad);
+        shared[tid] = (v < 0 ? V : v) << 10 | tid;
     }
-    shared[n] = key;
     __syncthreads();
     if (bad) bad_any = 1;
+    const int n = tid / parts, mine = n < N ? shared[n] : 0;
     int before = 0;
-    for (int i = 0; i < N; ++i) {
-        const int k = shared[i];
-        before += k < key || (k == key && i < n) ? 1 : 0;
-    }
-    if (n < N) {
-        keys[before] = key;
+#pragma unroll 8
+    for (int i = tid % parts; i < N; i += parts) before += shared[i] < mine ? 1 : 0;
+    for (int w = 1; w < parts; w <<= 1) before += __shfl_xor(before, w);
+    if (n < N && tid % parts == 0) {
+        keys[before] = mine >> 10;
         places[before] = n;
     }
     __syncthreads();
-    if (n == 0 && bad_any) *status = PX_ST_BAD_TOKEN;
+    if (tid == 0 && bad_any) *status = PX_ST_BAD_TOKEN;
 }
 
 // A workgroup's tokens counted by their lowest digit; the second pass's counts and the status word are cleared.
@@ -393,7 +395,9 @@ int embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *token
     };
     if (p.passes == 0) {
         const ZeroArgs z = zero(0, 16, 1);
-        hipLaunchKernelGGL(rank_few, grid(z), dim3(kThreads), 0, stream, tokens, i64, N, d.V, status, keys[1], places[1], z);
+        int parts = 1;
+        while (parts < 64 && 2 * parts * N <= kThreads) parts *= 2;
+        hipLaunchKernelGGL(rank_few, grid(z), dim3(kThreads), 0, stream, tokens, i64, N, d.V, parts, status, keys[1], places[1], z);
     } else {
         int *counts = (int *)(ws + p.counts), *counts2 = counts + ((size_t)p.blocks << p.bits);
         const ZeroArgs z[3] = {zero(0, 4, p.blocks), zero(4, 11, p.blocks), zero(11, 16, p.blocks)};

@@ -250,3 +250,15 @@ def test_gradients_of_wide_rows(N, V, D, share, rows_type, table_type):
     rows[tokens < 0] = float("nan")
     got = px.embed_grad(tokens, rows, V, 1.25, dtype=getattr(torch, table_type))
     close(got, *gradient(tokens, rows, V, 1.25))
+
+
+def test_every_number_of_few_tokens_is_ranked():
+    """Up to 1024 tokens are ranked by threads in proportion: each count of them has its own share."""
+    import torch
+    import paper_2008_12260_amd as px
+    rows = torch.randn((1025, 24), device="cuda")
+    for N in list(range(1, 40)) + [63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 800, 1023, 1024, 1025]:
+        tokens = tokens_of(N, 37, N, ignored=0.2)
+        close(px.embed_grad(tokens, rows[:N], 37), *gradient(tokens, rows[:N], 37, 1.0))
+    tokens = tokens_of(900, (1 << 20) - 1, 3, skewed=False)
+    close(px.embed_grad(tokens, rows[:900, :8], (1 << 20) - 1), *gradient(tokens, rows[:900, :8], (1 << 20) - 1, 1.0))
