@@ -100,7 +100,7 @@ def test_tokens_outside_the_table_are_reported_and_give_zeros():
             assert px.pollux_last_status(ws) == 0
 
 
-# up to 1024 tokens one workgroup sorts, beyond them several; windows hold 32 places, and 128 beyond 2^16 tokens
+# up to 512 tokens one workgroup ranks, beyond them several sort; windows hold 8 to 32 places, and 128 beyond 2^17 tokens
 CASES = [(1, 1, 1), (1, 100, 64), (7, 3, 5), (33, 1000, 40), (1024, 50, 24), (1025, 50, 24), (1500, 1, 8), (5000, 1023, 100), (5000, 1024, 2500),
          (70001, 30000, 9), (200000, 300, 16), (3000, 1000003, 3)]
 
@@ -253,7 +253,7 @@ def test_gradients_of_wide_rows(N, V, D, share, rows_type, table_type):
 
 
 def test_every_number_of_few_tokens_is_ranked():
-    """Up to 1024 tokens are ranked by threads in proportion: each count of them has its own share."""
+    """Up to 512 tokens are ranked by threads in proportion: each count of them has its own share."""
     import torch
     import paper_2008_12260_amd as px
     rows = torch.randn((1025, 24), device="cuda")
