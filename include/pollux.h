@@ -599,8 +599,11 @@ int pollux_noise_scale(const pollux_noise_dims *dims,    /* host */
  * Orthogonalised update of `batch` gradient matrices G [rows, cols]: X = G / |G|_F (zeros for a gradient of zeros), then `steps` times
  *   X <- a X + (b X X' + c (X X')^2) X        (rows <= cols; for more rows than columns on the transposes)
  * which, with the coefficients of a Newton-Schulz iteration (1.5, -0.5, 0) or of one tuned for few steps, moves every singular
- * value of G towards 1.  update: bfloat16.  The products take X in fp16, scaled to its range, with sums in fp32: the update is
- * within about 2^-9 of its size (2-norm) of the formula's, which is the rounding of the result.
+ * value of G towards 1.  update: bfloat16.  The products take fp16 operands, X scaled to that range, with sums in fp32; the term a X takes X to
+ * within 2^-22 of each element, so that directions G has none of stay empty but for 2^-22 a^steps.  Five steps of the
+ * coefficients (3.4445, -4.7750, 2.0315) are within 2^-8 of the update's size (2-norm) of the formula's whatever G's rank and spectrum are, if the
+ * smaller side is 64 or more (the larger part of that is the rounding of the result); of a few rows or columns, whose errors do not
+ * average, within 2^-5.
  * Limits: batch >= 0, 1 <= rows, cols <= 2^16 with the smaller <= 2^14, batch * rows * cols < 2^40, 0 <= steps <= 64,
  * coefficients finite.  Matrix k begins grads_batch_stride (update_batch_stride) elements after matrix k - 1; rows are
  * grads_stride (update_stride) apart; 0 stands for contiguous.

@@ -93,6 +93,7 @@ struct OrthoPlan {
     double unit;                // X is held times this power of two
     size_t norms;               // double [batch, norm_blocks]
     size_t x[2];                // _Float16 [batch, rows, x_pad]: before and after a step
+    size_t low;                 // _Float16 [batch, rows, x_pad]: what rounding left of X, times 2^11
     size_t gram, poly;          // _Float16 [batch, m, m_pad]: X X', b X X' + c (X X')^2
     size_t total;
 };
