@@ -1,7 +1,8 @@
 // The gradient noise scale of several gradients, and their mean, in one pass over them.
 //
 // Per element, with deviations d_i = g_i - g_0 from the first gradient (exact in fp64 for 16-bit gradients; equal gradients
-// then show no noise at all): sum_i (g_i - mean)^2 = sum d_i^2 - (sum d_i)^2 / B and mean = g_0 + sum d_i / B.  Bound by reading
+// then show no noise at all): sum_i (g_i - mean)^2 = sum d_i^2 - (sum d_i)^2 / B and mean = g_0 + sum d_i / B.  Where g_0 is infinite the
+// deviations are those from 0, g_0's own among them: the mean is then infinite, or NaN, as the formula's is.  Bound by reading
 // the gradients: about five fp64 operations an element hide behind 2 bytes of it.  Workgroups leave fp64 sums in the workspace
 // and a second launch adds them up in their order, so that the result depends on nothing but the gradients.
 
@@ -25,8 +26,15 @@ __global__ __launch_bounds__(kThreads) void noise_sums(const E *grads, int64_t n
     const double over_b = 1.0 / B;
     for (int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kVec; at < n; at += (int64_t)gridDim.x * kThreads * kVec) {
         const int64_t left = n - at;
-        const f32x8 g0 = load8f(grads + at, left);
-        double s1[kVec] = {}, s2[kVec] = {};
+        f32x8 g0 = load8f(grads + at, left);
+        double s1[kVec], s2[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const bool infinite = fabsf(g0[i]) == __builtin_inff();
+            s1[i] = infinite ? (double)g0[i] : 0.0;
+            s2[i] = infinite ? (double)__builtin_inff() : 0.0;
+            g0[i] = infinite ? 0.f : g0[i];
+        }
         for (int b = 1; b < B; b += kAhead) {
             f32x8 g[kAhead];
 #pragma unroll
