@@ -17,6 +17,18 @@ namespace {
 
 constexpr int kThreads = 256;
 
+#ifdef __HIP_DEVICE_COMPILE__
+// A mean in fp32 on its way to 16 bits, where it is rounded: towards 0, the last bit standing for whatever was cut off.  That bit is far below the middle of two
+// neighbours of 16 bits, so that rounding it gives what rounding the mean itself would.
+__device__ __forceinline__ float to_be_rounded(double m)
+{
+    const float f = (float)m;
+    unsigned u = __float_as_uint(f);
+    if ((double)f != m) u = (u - (fabs((double)f) > fabs(m) ? 1u : 0u)) | 1u;
+    return __uint_as_float(u);
+}
+#endif
+
 template <class E, class M>
 __global__ __launch_bounds__(kThreads) void noise_sums(const E *grads, int64_t n, int B, int64_t stride, const float *precondition, M *mean, double2 *sums)
 {
@@ -56,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void noise_sums(const E *grads, int64_t n
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             const double m = (double)g0[i] + s1[i] * over_b;
-            out[i] = (float)m;
+            out[i] = sizeof(M) == 2 ? to_be_rounded(m) : (float)m;
             if (i < left) {
                 const double w = precondition ? (double)p[i] * (double)p[i] : 1.0;
                 const double v = fma(-s1[i] * over_b, s1[i], s2[i]);
