@@ -497,7 +497,7 @@ enum {
  * hidden row holds.  Either gradient may be NULL.  The logits are formed again, a piece of the vocabulary at a time; q is rounded to
  * the type of the inputs for the matrix units (fp16: scaled, so that weights g of any size keep their precision), but for the target's entry in
  * hidden_grad, which counts in full.  Sums over tokens and entries are in fp32 and in a fixed order: the same call gives the same bits.
- * fp32 inputs are multiplied with all of their 24 bits (elements smaller than 2^-109 may count with fewer).
+ * fp32 inputs: a product is off by at most 2^-24 of itself before it is summed (elements smaller than 2^-109 may count with fewer bits).
  *
  * Limits: 0 <= N <= 2^20, 1 <= V <= 2^20, 1 <= D <= 2^16, strides below 2^20.  workspace: pollux_loss_workspace_size bytes,
  * 256-byte aligned; pollux_last_status on it reads the status word (PX_ST_BAD_TOKEN).
