@@ -4,7 +4,8 @@ the scheduler is given.
 
 Arguments are checked and marshalled here; every step runs in the library's kernels.  Results and scratch memory are allocated
 by torch on the stream that the call is enqueued on (`stream`, else the current one); nothing synchronises, so the calls
-can be recorded into a graph.  A caller who hands over results or scratch memory from another stream keeps them in order, as with any
+can be recorded into a graph.  Nor does anything record for autograd: a tensor that requires grad is refused where grad mode is on, because its
+gradient would be lost (inside a torch.autograd.Function grad mode is off, and the calls make its forward and backward).  A caller who hands over results or scratch memory from another stream keeps them in order, as with any
 torch operation.
 """
 from __future__ import annotations
@@ -37,6 +38,16 @@ def _on_device(*tensors):
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor {tuple(t.shape)} is on {t.device}: it has to be on the current GPU, cuda:{here}")
+
+
+def _untracked(torch, *tensors):
+    """No given tensor is one that autograd would follow through the call."""
+    if not torch.is_grad_enabled():
+        return
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise ValueError(f"a tensor {tuple(t.shape)} requires grad, which this call does not record: detach it, or call under torch.no_grad(), "
+                             "and take the gradients from embed_grad and token_loss_grad")
 
 
 def _rows(t, name):
@@ -138,6 +149,7 @@ def token_loss(hidden, weight, targets, workspace=None, stream=None):
     targets [N], int64 or int32; -1 is none (loss 0), anything else outside the vocabulary too, reported by
     pollux_last_status(workspace) where the caller gives the workspace."""
     import torch
+    _untracked(torch, hidden, weight)
     with _on(stream):
         _on_device(hidden, weight, targets)
         hidden, weight, targets, sizes = _loss_call(hidden, weight, targets)
@@ -159,6 +171,7 @@ def token_loss_grad(hidden, weight, targets, lse, row_weight=None, hidden_grad=N
     lse: of token_loss on the same arguments; row_weight [N] fp32, or None for ones.  accumulate: weight_grad is given and
     added to."""
     import torch
+    _untracked(torch, hidden, weight, lse, row_weight, hidden_grad, weight_grad)
     with _on(stream):
         _on_device(hidden, weight, targets, lse, row_weight, hidden_grad, weight_grad)
         hidden, weight, targets, sizes = _loss_call(hidden, weight, targets)
@@ -195,6 +208,7 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
     A token that is neither -1 nor an entry of the table counts as -1 and sets PX_ST_BAD_TOKEN in `status`, an int32 tensor
     of one element that the caller clears."""
     import torch
+    _untracked(torch, table, out)
     with _on(stream):
         _on_device(tokens, table, out, status)
         table_type = _type(table, "table")
@@ -219,6 +233,7 @@ def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, acc
     scale times the sum of the rows whose token is v.  accumulate: table_grad is given and added to; rows that no token names
     are then not touched."""
     import torch
+    _untracked(torch, rows_grad, table_grad)
     with _on(stream):
         _on_device(tokens, rows_grad, table_grad)
         count, D = tokens.numel(), rows_grad.shape[-1]
@@ -246,6 +261,7 @@ def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=T
     fp64 tensor [tr(P Sigma P'), |P g|^2, their quotient phi], P the diagonal `precondition` (fp32, one value an element; None: 1).
     want_mean False: None in the place of the mean."""
     import torch
+    _untracked(torch, grads, precondition)
     with _on(stream):
         _on_device(grads, precondition)
         if grads.dim() < 2:
@@ -276,6 +292,7 @@ def orthogonalize(grads, steps=5, coefficients=(3.4445, -4.7750, 2.0315), out=No
     X <- a X + (b X X' + c (X X')^2) X with (a, b, c) = coefficients, which moves the singular values towards 1 (the default
     coefficients bring those above 1e-3 of the norm to 0.7 .. 1.2 in five steps; (1.5, -0.5, 0) converges to 1)."""
     import torch
+    _untracked(torch, grads, out)
     with _on(stream):
         _on_device(grads, out)
         if grads.dim() < 2:
