@@ -258,7 +258,7 @@ def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, acc
 
 def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=True, stream=None):
     """(mean, scale) of the gradients grads[i], each the mean over `examples` examples: their mean, in `mean_dtype` (None: fp32), and the
-    fp64 tensor [tr(P Sigma P'), |P g|^2, their quotient phi], P the diagonal `precondition` (fp32, one value an element; None: 1).
+    fp64 tensor [tr(P Sigma P'), |P g|^2, their quotient phi], P the diagonal `precondition` (fp32, one value an element, in a gradient's shape or flat; None: 1).
     want_mean False: None in the place of the mean."""
     import torch
     _untracked(torch, grads, precondition)
@@ -272,8 +272,8 @@ def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=T
         if n > 1 and flat.stride(1) != 1 or flat.stride(0) < n or flat.data_ptr() % 16:
             flat = flat.clone(memory_format=_contiguous())
         if precondition is not None:
-            if precondition.dtype != torch.float32 or precondition.numel() != n:
-                raise ValueError(f"precondition is {precondition.dtype} of {precondition.numel()} elements: float32 of {n} is wanted")
+            if precondition.dtype != torch.float32 or precondition.shape != torch.Size(shape) and precondition.shape != (n,):
+                raise ValueError(f"precondition is {precondition.dtype} {tuple(precondition.shape)}: float32 of a gradient's shape {tuple(shape)}, or flat, is wanted")
             precondition = precondition.contiguous()
             if precondition.data_ptr() % 16:
                 precondition = precondition.clone()

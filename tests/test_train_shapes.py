@@ -1,0 +1,35 @@
+"""Tensors of the right number of elements in a wrong shape are refused, on the host: the device is not asked, and the library not called."""
+import pytest
+
+import paper_2008_12260_amd as px
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(autouse=True)
+def on_the_host(monkeypatch):
+    """Tensors of the host pass the question which device they are on; a call that passes all checks stops before the library."""
+    class Reached(Exception):
+        pass
+
+    def planned(*args, **more):
+        raise Reached
+    monkeypatch.setattr(px, "_current_device", lambda: -1)
+    monkeypatch.setattr(px.train, "_planned", planned)
+    return Reached
+
+
+def test_preconditions_have_a_gradients_shape(on_the_host):
+    grads = torch.ones((4, 6, 10))
+    for shape in ((10, 6), (6, 10, 1), (3, 20), (1, 60), (60, 1), (59,), ()):
+        with pytest.raises(ValueError, match="precondition"):
+            px.noise_scale(grads, 1.0, torch.ones(shape))
+    for shape in ((6, 10), (60,)):
+        with pytest.raises(on_the_host):
+            px.noise_scale(grads, 1.0, torch.ones(shape))
+    with pytest.raises(on_the_host):
+        px.noise_scale(grads.view(4, 60), 1.0, torch.ones(60))
+    with pytest.raises(ValueError, match="precondition"):
+        px.noise_scale(grads.view(4, 60), 1.0, torch.ones(6, 10))
+    with pytest.raises(ValueError, match="precondition"):
+        px.noise_scale(torch.ones((3, 1)), 1.0, torch.ones(()))
