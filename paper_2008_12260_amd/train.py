@@ -230,14 +230,14 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
 
 def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, accumulate=False, workspace=None, stream=None):
     """Gradient of a table of V entries from that of its looked-up rows: [V, D] in `dtype` (None: that of rows_grad), row v being
-    scale times the sum of the rows whose token is v.  accumulate: table_grad is given and added to; rows that no token names
+    scale times the sum of the rows whose token is v.  rows_grad [*tokens.shape, D], or [tokens.numel(), D].  accumulate: table_grad is given and added to; rows that no token names
     are then not touched."""
     import torch
     _untracked(torch, rows_grad, table_grad)
     with _on(stream):
         _on_device(tokens, rows_grad, table_grad)
-        count, D = tokens.numel(), rows_grad.shape[-1]
-        if rows_grad.shape[:-1] != tokens.shape and rows_grad.numel() != count * D:
+        count, D = tokens.numel(), rows_grad.shape[-1] if rows_grad.dim() else 0
+        if rows_grad.dim() == 0 or rows_grad.shape[:-1] != tokens.shape and rows_grad.shape != (count, D):
             raise ValueError(f"rows_grad {tuple(rows_grad.shape)} has not a row for each of the tokens {tuple(tokens.shape)}")
         if accumulate and table_grad is None:
             raise ValueError("accumulate needs a table_grad to add to")

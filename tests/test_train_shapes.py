@@ -33,3 +33,15 @@ def test_preconditions_have_a_gradients_shape(on_the_host):
         px.noise_scale(grads.view(4, 60), 1.0, torch.ones(6, 10))
     with pytest.raises(ValueError, match="precondition"):
         px.noise_scale(torch.ones((3, 1)), 1.0, torch.ones(()))
+
+
+def test_rows_have_their_tokens_shape(on_the_host):
+    tokens = torch.zeros((4, 6), dtype=torch.int64)
+    for shape in ((6, 4, 8), (2, 12, 8), (24, 2, 4), (192,), (4, 48), (4, 6), (1, 24, 8), (4, 6, 1, 8), ()):
+        with pytest.raises(ValueError, match="rows_grad"):
+            px.embed_grad(tokens, torch.ones(shape), 10)
+    for shape in ((4, 6, 8), (24, 8), (24, 1)):
+        with pytest.raises(on_the_host):
+            px.embed_grad(tokens, torch.ones(shape), 10)
+    with pytest.raises(on_the_host):
+        px.embed_grad(tokens[0, 0], torch.ones(8), 10)
