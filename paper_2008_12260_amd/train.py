@@ -220,6 +220,8 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
         if out is None:
             rows, rows_stride = torch.empty((*tokens.shape, D), dtype=table.dtype if dtype is None else dtype, device=table.device), D
         else:
+            if out.shape != (*tokens.shape, D) and out.shape != (count, D):
+                raise ValueError(f"out {tuple(out.shape)} has not a row of {D} for each of the tokens {tuple(tokens.shape)}")
             rows, rows_stride = _result(out.view(count, D), "out", (count, D), table.dtype if dtype is None else dtype)
         rows_type = table_type if rows.dtype is table.dtype else _type(rows, "rows")
         dims, _ = _planned(_px.EmbedDims, "pollux_embed_workspace_size", (), count, V, D, table_type, rows_type, flag, float(scale), table_stride, rows_stride)

@@ -45,3 +45,13 @@ def test_rows_have_their_tokens_shape(on_the_host):
             px.embed_grad(tokens, torch.ones(shape), 10)
     with pytest.raises(on_the_host):
         px.embed_grad(tokens[0, 0], torch.ones(8), 10)
+
+
+def test_results_have_their_tokens_shape(on_the_host):
+    tokens, table = torch.zeros((4, 6), dtype=torch.int64), torch.ones((10, 8))
+    for shape in ((6, 4, 8), (2, 12, 8), (8, 24), (192,), (4, 48), (4, 6), (1, 24, 8), ()):
+        with pytest.raises(ValueError, match="out"):
+            px.embed(tokens, table, out=torch.empty(shape))
+    for shape in ((4, 6, 8), (24, 8)):
+        with pytest.raises(on_the_host):
+            px.embed(tokens, table, out=torch.empty(shape))
