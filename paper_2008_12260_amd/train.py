@@ -13,6 +13,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import math
 import os
 
 import paper_2008_12260_amd as _px
@@ -115,9 +116,9 @@ def _scratch(workspace, need, device):
 
 
 # What a call's sizes, types and strides determine: the library's description of them and the scratch memory it asks for.  (Asking each time is 2 to
-# 4 us of a call's host time.)
+# 4 us of a call's host time.)  signs: of the values that may be zeros of either sign, which are equal to each other.
 @functools.lru_cache(maxsize=1024)
-def _planned(cls, query, more, *values):
+def _planned(cls, query, more, signs, *values):
     dims, need = cls(*values), ctypes.c_size_t(0)
     _check(getattr(_px.lib(), query)(ctypes.byref(dims), *more, ctypes.byref(need)), query)
     return ctypes.byref(dims), need.value
@@ -153,7 +154,7 @@ def token_loss(hidden, weight, targets, workspace=None, stream=None):
     with _on(stream):
         _on_device(hidden, weight, targets)
         hidden, weight, targets, sizes = _loss_call(hidden, weight, targets)
-        dims, need = _planned(_px.LossDims, "pollux_loss_workspace_size", (0,), *sizes, 0, 0)
+        dims, need = _planned(_px.LossDims, "pollux_loss_workspace_size", (0,), None, *sizes, 0, 0)
         device = hidden.device
         workspace, size = _scratch(workspace, need, device)
         loss = torch.empty(sizes[0], dtype=torch.float32, device=device)
@@ -194,7 +195,7 @@ def token_loss_grad(hidden, weight, targets, lse, row_weight=None, hidden_grad=N
         N, V, D, type_, flags, *strides = sizes
         if accumulate:
             flags |= _px.PX_FLAG_ACCUMULATE
-        dims, bytes_ = _planned(_px.LossDims, "pollux_loss_workspace_size", (1,), N, V, D, type_, flags, *strides, hidden_stride, weight_stride)
+        dims, bytes_ = _planned(_px.LossDims, "pollux_loss_workspace_size", (1,), None, N, V, D, type_, flags, *strides, hidden_stride, weight_stride)
         workspace, size = _scratch(workspace, bytes_, device)
         _check(_px.lib().pollux_token_loss_grad(dims, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), lse.data_ptr(), _px._ptr(row_weight),
                                                 workspace.data_ptr(), size, _px._ptr(hidden_grad), _px._ptr(weight_grad), _px._stream_handle(stream)),
@@ -224,7 +225,9 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
                 raise ValueError(f"out {tuple(out.shape)} has not a row of {D} for each of the tokens {tuple(tokens.shape)}")
             rows, rows_stride = _result(out.view(count, D), "out", (count, D), table.dtype if dtype is None else dtype)
         rows_type = table_type if rows.dtype is table.dtype else _type(rows, "rows")
-        dims, _ = _planned(_px.EmbedDims, "pollux_embed_workspace_size", (), count, V, D, table_type, rows_type, flag, float(scale), table_stride, rows_stride)
+        scale = float(scale)
+        dims, _ = _planned(_px.EmbedDims, "pollux_embed_workspace_size", (), math.copysign(1.0, scale), count, V, D, table_type, rows_type, flag, scale, table_stride,
+                           rows_stride)
         _check(_px.lib().pollux_embed(dims, flat.data_ptr(), table.data_ptr(), rows.data_ptr(), _px._ptr(status),
                                       _px._stream_handle(stream)), "pollux_embed")
     return rows if out is None else out
@@ -249,8 +252,9 @@ def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, acc
         if table_grad is None:
             table_grad = torch.empty((V, D), dtype=rows.dtype if dtype is None else dtype, device=rows.device)
         table_grad, table_stride = _result(table_grad, "table_grad", (V, D), table_grad.dtype if dtype is None else dtype)
-        dims, need = _planned(_px.EmbedDims, "pollux_embed_workspace_size", (), count, V, D, _type(table_grad, "table_grad"), rows_type,
-                              flag | (_px.PX_FLAG_ACCUMULATE if accumulate else 0), float(scale), table_stride, rows_stride)
+        scale = float(scale)
+        dims, need = _planned(_px.EmbedDims, "pollux_embed_workspace_size", (), math.copysign(1.0, scale), count, V, D, _type(table_grad, "table_grad"), rows_type,
+                              flag | (_px.PX_FLAG_ACCUMULATE if accumulate else 0), scale, table_stride, rows_stride)
         workspace, size = _scratch(workspace, need, rows.device)
         _check(_px.lib().pollux_embed_grad(dims, flat.data_ptr(), rows.data_ptr(), workspace.data_ptr(),
                                            size, table_grad.data_ptr(), _px._stream_handle(stream)),
@@ -281,7 +285,7 @@ def noise_scale(grads, examples, precondition=None, mean_dtype=None, want_mean=T
                 precondition = precondition.clone()
         mean = torch.empty(shape, dtype=torch.float32 if mean_dtype is None else mean_dtype, device=flat.device) if want_mean else None
         scale = torch.empty(3, dtype=torch.float64, device=flat.device)
-        dims, need = _planned(_px.NoiseDims, "pollux_noise_workspace_size", (), n, B, type_, _px.PX_TYPE_F32 if mean is None else _type(mean, "mean"), 0,
+        dims, need = _planned(_px.NoiseDims, "pollux_noise_workspace_size", (), None, n, B, type_, _px.PX_TYPE_F32 if mean is None else _type(mean, "mean"), 0,
                               flat.stride(0), float(examples))
         workspace, size = _scratch(None, need, flat.device)
         _check(_px.lib().pollux_noise_scale(dims, flat.data_ptr(), _px._ptr(precondition), workspace.data_ptr(), size,
@@ -312,7 +316,9 @@ def orthogonalize(grads, steps=5, coefficients=(3.4445, -4.7750, 2.0315), out=No
         elif out.shape != shape or out.dtype != torch.bfloat16 or not out.is_contiguous() or out.data_ptr() % 16:
             raise ValueError(f"out is {out.dtype} {tuple(out.shape)}: contiguous bfloat16 {shape} is wanted")
         ld = flat.stride(1) if rows > 1 else cols
-        dims, need = _planned(_px.OrthoDims, "pollux_ortho_workspace_size", (), batch, rows, cols, type_, steps, 0, *(float(c) for c in coefficients), ld, 0,
+        a, b, c = (float(x) for x in coefficients)
+        signs = math.copysign(1.0, a), math.copysign(1.0, b), math.copysign(1.0, c)
+        dims, need = _planned(_px.OrthoDims, "pollux_ortho_workspace_size", (), signs, batch, rows, cols, type_, steps, 0, a, b, c, ld, 0,
                               flat.stride(0) if batch > 1 else 0, 0)
         workspace, size = _scratch(workspace, need, flat.device)
         _check(_px.lib().pollux_orthogonalize(dims, flat.data_ptr(), workspace.data_ptr(), size,
