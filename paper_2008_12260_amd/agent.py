@@ -40,6 +40,7 @@ class Job:
         self.shapes, self.sizes = ((V, D), (D, D), (V, D)), sizes
         self.gradients = torch.empty((0, sum(sizes)), dtype=torch.bfloat16, device="cuda")
         self.before = None                   # the gradient of the iteration before, while m is the same
+        self.status = torch.zeros(1, dtype=torch.int32, device="cuda")       # what the operators report of the tokens
 
     def parts(self, flat):
         """(table, layer, projection) of a flat vector, as views."""
@@ -62,9 +63,9 @@ class Job:
         table, layer, projection = model
         d_table, d_layer, d_projection = self.parts(gradient)
         x, y = tokens[:, :-1].reshape(-1), tokens[:, 1:].reshape(-1)
-        rows = embed(x, table, self.scale)
+        rows = embed(x, table, self.scale, status=self.status)
         hidden = torch.addmm(rows, rows, layer.t())
-        loss, lse = token_loss(hidden, projection, y)
+        loss, lse = token_loss(hidden, projection, y, status=self.status)
         weight = torch.full_like(loss, 1.0 / loss.numel())
         d_hidden, _ = token_loss_grad(hidden, projection, y, lse, weight, weight_grad=d_projection)
         torch.mm(d_hidden.t(), rows, out=d_layer)
@@ -94,6 +95,9 @@ class Job:
             p.sub_(orthogonalize(g) if k == 1 else g * (self.D ** -0.5 / (g.square().mean().sqrt() + 1e-20)), alpha=self.rate)
         torch.cuda.synchronize()
         seconds = time.perf_counter() - began
+        if int(self.status):
+            self.status.zero_()
+            raise ValueError(f"a token is neither -1 nor one of the {self.V} entries of the vocabulary")
         return float(torch.stack(losses).mean()), None if noise is None else noise.cpu().numpy(), seconds
 
 

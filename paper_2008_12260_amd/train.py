@@ -124,6 +124,19 @@ def _planned(cls, query, more, signs, *values):
     return ctypes.byref(dims), need.value
 
 
+def _status_ok(status):
+    import torch
+    if status is not None and (status.dtype != torch.int32 or status.numel() != 1):
+        raise ValueError("status is one int32")
+
+
+def _report(workspace, status):
+    """The call's status word, which is its workspace's first, added to the caller's."""
+    if status is not None:
+        import torch
+        status.bitwise_or_(workspace.view(-1).view(torch.uint8)[:4].view(torch.int32).view(status.shape))
+
+
 def _check(rc, where):
     if rc != _px.PX_OK:
         raise _px.PolluxError(rc, where)
@@ -144,15 +157,16 @@ def _loss_call(hidden, weight, targets):
     return hidden, weight, targets, (N, V, D, type_, flag, hidden_stride, weight_stride)
 
 
-def token_loss(hidden, weight, targets, workspace=None, stream=None):
+def token_loss(hidden, weight, targets, workspace=None, stream=None, status=None):
     """Cross entropy of each row of `hidden` [N, D] over the vocabulary that `weight` [V, D] projects to: (loss [N], lse [N]), fp32.
 
-    targets [N], int64 or int32; -1 is none (loss 0), anything else outside the vocabulary too, reported by
-    pollux_last_status(workspace) where the caller gives the workspace."""
+    targets [N], int64 or int32; -1 is none (loss 0).  One that is neither -1 nor an entry of the vocabulary counts as -1 and sets
+    PX_ST_BAD_TOKEN in `status`, an int32 tensor of one element that the caller clears."""
     import torch
     _untracked(torch, hidden, weight)
     with _on(stream):
-        _on_device(hidden, weight, targets)
+        _on_device(hidden, weight, targets, status)
+        _status_ok(status)
         hidden, weight, targets, sizes = _loss_call(hidden, weight, targets)
         dims, need = _planned(_px.LossDims, "pollux_loss_workspace_size", (0,), None, *sizes, 0, 0)
         device = hidden.device
@@ -161,20 +175,22 @@ def token_loss(hidden, weight, targets, workspace=None, stream=None):
         lse = torch.empty_like(loss)
         _check(_px.lib().pollux_token_loss(dims, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), workspace.data_ptr(), size, loss.data_ptr(),
                                            lse.data_ptr(), _px._stream_handle(stream)), "pollux_token_loss")
+        _report(workspace, status)
     return loss, lse
 
 
 def token_loss_grad(hidden, weight, targets, lse, row_weight=None, hidden_grad=None, weight_grad=None, accumulate=False, need=(True, True),
-                    workspace=None, stream=None):
+                    workspace=None, stream=None, status=None):
     """Gradients of sum_n row_weight[n] * loss[n] with respect to `hidden` and `weight`, in their type: (hidden_grad [N, D],
     weight_grad [V, D]), None for one that is not needed.
 
     lse: of token_loss on the same arguments; row_weight [N] fp32, or None for ones.  accumulate: weight_grad is given and
-    added to."""
+    added to.  status: as token_loss's."""
     import torch
     _untracked(torch, hidden, weight, lse, row_weight, hidden_grad, weight_grad)
     with _on(stream):
-        _on_device(hidden, weight, targets, lse, row_weight, hidden_grad, weight_grad)
+        _on_device(hidden, weight, targets, lse, row_weight, hidden_grad, weight_grad, status)
+        _status_ok(status)
         hidden, weight, targets, sizes = _loss_call(hidden, weight, targets)
         N, V, D = sizes[:3]
         for name, t in (("lse", lse), ("row_weight", row_weight)):
@@ -200,6 +216,7 @@ def token_loss_grad(hidden, weight, targets, lse, row_weight=None, hidden_grad=N
         _check(_px.lib().pollux_token_loss_grad(dims, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), lse.data_ptr(), _px._ptr(row_weight),
                                                 workspace.data_ptr(), size, _px._ptr(hidden_grad), _px._ptr(weight_grad), _px._stream_handle(stream)),
                "pollux_token_loss_grad")
+        _report(workspace, status)
     return hidden_grad, weight_grad
 
 
@@ -215,8 +232,7 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
         table_type = _type(table, "table")
         table, table_stride = _rows(table, "table")
         count, (V, D) = tokens.numel(), table.shape
-        if status is not None and (status.dtype != torch.int32 or status.numel() != 1):
-            raise ValueError("status is one int32")
+        _status_ok(status)
         flat, flag = _tokens(tokens, "tokens", count)
         if out is None:
             rows, rows_stride = torch.empty((*tokens.shape, D), dtype=table.dtype if dtype is None else dtype, device=table.device), D
@@ -233,14 +249,15 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
     return rows if out is None else out
 
 
-def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, accumulate=False, workspace=None, stream=None):
+def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, accumulate=False, workspace=None, stream=None, status=None):
     """Gradient of a table of V entries from that of its looked-up rows: [V, D] in `dtype` (None: that of rows_grad), row v being
     scale times the sum of the rows whose token is v.  rows_grad [*tokens.shape, D], or [tokens.numel(), D].  accumulate: table_grad is given and added to; rows that no token names
-    are then not touched."""
+    are then not touched.  status: as embed's."""
     import torch
     _untracked(torch, rows_grad, table_grad)
     with _on(stream):
-        _on_device(tokens, rows_grad, table_grad)
+        _on_device(tokens, rows_grad, table_grad, status)
+        _status_ok(status)
         count, D = tokens.numel(), rows_grad.shape[-1] if rows_grad.dim() else 0
         if rows_grad.dim() == 0 or rows_grad.shape[:-1] != tokens.shape and rows_grad.shape != (count, D):
             raise ValueError(f"rows_grad {tuple(rows_grad.shape)} has not a row for each of the tokens {tuple(tokens.shape)}")
@@ -259,6 +276,7 @@ def embed_grad(tokens, rows_grad, V, scale=1.0, dtype=None, table_grad=None, acc
         _check(_px.lib().pollux_embed_grad(dims, flat.data_ptr(), rows.data_ptr(), workspace.data_ptr(),
                                            size, table_grad.data_ptr(), _px._stream_handle(stream)),
                "pollux_embed_grad")
+        _report(workspace, status)
     return table_grad
 
 
