@@ -495,8 +495,9 @@ enum {
  *   hidden_grad[n,:] = sum_v q[n,v] weight[v,:],   weight_grad[v,:] = sum_n q[n,v] hidden[n,:].
  * A token without a target, or of row weight 0, adds nothing to weight_grad and has a row of zeros in hidden_grad whatever its
  * hidden row holds.  Either gradient may be NULL.  The logits are formed again, a piece of the vocabulary at a time; q is rounded to
- * the type of the inputs for the matrix units (fp16: scaled, so that weights g of any size keep their precision), but for the target's entry in
- * hidden_grad, which counts in full.  Sums over tokens and entries are in fp32 and in a fixed order: the same call gives the same bits.
+ * the type of the inputs for the matrix units, but for the target's entry in
+ * hidden_grad, which counts in full.  In fp16 q is scaled by one power of two a call, which the largest |g| sets: weights of any size keep their precision, but no q is held
+ * finer than to 2^-37 of that largest, so that rows whose weights are many powers of two below it keep less.  Sums over tokens and entries are in fp32 and in a fixed order: the same call gives the same bits.
  * fp32 inputs: a product is off by at most 2^-24 of itself before it is summed (elements smaller than 2^-109 may count with fewer bits).
  *
  * Limits: 0 <= N <= 2^20, 1 <= V <= 2^20, 1 <= D <= 2^16, strides below 2^20.  workspace: pollux_loss_workspace_size bytes,
