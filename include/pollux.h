@@ -625,9 +625,11 @@ int pollux_orthogonalize(const pollux_ortho_dims *dims,  /* host */
                          void *update,                   /* [batch,rows,cols] bfloat16 out */
                          void *hip_stream);
 
-/* Copies the status word of the last pollux_fitness (or pollux_fitness_timed) call that used `workspace`
- * to *host_out.  Synchronises `hip_stream`.  pollux_goodput_per_gpu and pollux_sim_tick neither clear nor
- * set the word; they leave the workspace as it is. */
+/* Copies the status word of the last call that used `workspace` to *host_out: of pollux_fitness (or
+ * pollux_fitness_timed), pollux_token_loss, pollux_token_loss_grad or pollux_embed_grad.  Synchronises
+ * `hip_stream`.  pollux_goodput_per_gpu and pollux_sim_tick neither clear nor set the word; they leave the
+ * workspace as it is.  The workspaces of pollux_noise_scale and pollux_orthogonalize hold no status word: after those calls
+ * what would be read is scratch memory. */
 int pollux_last_status(const void *workspace, void *hip_stream, int32_t *host_out /* host */);
 
 /* Text for a PX_* return code (static storage, never NULL). */
