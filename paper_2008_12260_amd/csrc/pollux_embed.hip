@@ -381,7 +381,10 @@ int embed_grad(const pollux_embed_dims &d, const EmbedPlan &p, const void *token
     int32_t *status = (int32_t *)(ws + p.status);
     int *keys[2] = {(int *)(ws + p.keys[0]), (int *)(ws + p.keys[1])}, *places[2] = {(int *)(ws + p.places[0]), (int *)(ws + p.places[1])};
     const bool add = d.flags & PX_FLAG_ACCUMULATE;
-    // rows [V at / 16, V to / 16) of the table zeroed by a launch whose own workgroups are `blocks`; as long as what the sort does in it
+    // rows [V at / 16, V to / 16) of the table zeroed by a launch whose own workgroups are `blocks`.  Each of the sort's three launches takes about a third, the second,
+    // which counts besides, the most: a table that is written for longer than the sort runs keeps all three busy (16384 x 2048 in bfloat16 into 65536 rows 77 us, 91 with all
+    // zeros in the first and 85 in the second; 16384 x 4096 into 131072 245, 266, 260), a small one fits any (5003 x 1000 in fp32 into 20011 37, 39, 36; 10^6 x 256 into
+    // 200000 369, 374, 365).  Shares of 4, 7, 5 and of 5, 6, 5 sixteenths are within 1 %.
     // (A table that the memory-side cache of 256 MiB holds beside the rows stays there: 29114 x 2048 in fp32 40 us, 54 with stores past the
     // caches; a larger one only pushes the rows out: 65536 x 2048 in bfloat16 from 16384 rows 95 us, 81 past them.)
     const bool past = (int64_t)d.V * d.D * (int64_t)sizeof(T) + (int64_t)N * d.D * (int64_t)sizeof(R) > (256ll << 20);
@@ -464,6 +467,9 @@ EmbedPlan embed_plan(const pollux_embed_dims &d)
     }
     p.keys[1] = take(4 * (size_t)N);
     p.places[1] = take(4 * (size_t)N);
+    // Windows: of few tokens short ones, which give many wavefronts work and end soon; of many long ones, whose cut runs' pieces are fewer to write and join.  With 8, 16, 32, 64,
+    // 128 places: 5003 x 1000 in fp32 36, 37, 45, 59, 87 us; 16384 x 2048 in bfloat16 80, 78, 78, 85, 105; 65536 x 1024 92, 79, 72, 72, 84; 131072 x 1024 172, 144, 128, 120,
+    // 121; 10^6 x 1024 1185, 943, 829, 760, 733.
     p.window = N <= 1 << 13 ? 8 : N <= 1 << 15 ? 16 : N <= 1 << 17 ? 32 : 128;
     p.windows = (N + p.window - 1) / p.window;
     p.partial = take(2 * (size_t)p.windows * d.D * 4);
