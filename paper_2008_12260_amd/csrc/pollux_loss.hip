@@ -636,12 +636,12 @@ LossPlan loss_plan(const pollux_loss_dims &d, bool grad)
     const int64_t e = size_of_type(d.type), pad = 16 / e, N = d.N;
     const bool f32 = e == 4;
     auto padded = [&](int64_t x) { return (x + pad - 1) / pad * pad; };
-    p.grad = grad;
     p.d_pad = padded(d.D);
     p.pack_hidden = d.hidden_stride % pad != 0 || d.D % pad != 0;
     p.pack_weight = d.weight_stride % pad != 0 || d.D % pad != 0;
-    // A piece's q is held to 512 MiB, packed weights to 256: pieces that large keep the matrix kernels' ends and the sums' passes over
-    // memory to a few per cent.
+    // A piece's q is held to 512 MiB, packed weights to 256.  Up to some 2^16 tokens pieces are then large enough to keep the matrix kernels' ends and the sums' passes over
+    // memory to a few per cent; of 2^18 in 16 bits a piece has 1024 entries, and reading and writing the hidden rows' sums once a piece takes about as long as the
+    // piece's product, of 2^20 (256 entries) several times as long.  There the scratch memory bounds the speed: such a batch is better given in parts.
     int64_t piece = (d.V + 255) / 256 * 256;
     // Forward, tokens are taken so many at a time that no launch has 2^32 threads, whatever its tiles; the lists of tiles are held to 4 GiB by it too.
     p.tokens = 1 << 15;

@@ -29,7 +29,6 @@ __device__ __forceinline__ int token_at(const void *tokens, int64_t n, bool i64,
 // How a loss call cuts the vocabulary, and the byte offsets of its workspace's sections.  Lengths of rows in the workspace are
 // padded to whole 16-byte groups, the padding holding zeros.
 struct LossPlan {
-    bool grad;
     bool pack_hidden, pack_weight;      // rows that 16-byte loads cannot take are copied to aligned ones first
     int tiles;                          // which shape of tile the logits are formed in (kShape)
     int grad_tiles;                     // and the gradients
