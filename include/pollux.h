@@ -625,11 +625,183 @@ int pollux_orthogonalize(const pollux_ortho_dims *dims,  /* host */
                          void *update,                   /* [batch,rows,cols] bfloat16 out */
                          void *hip_stream);
 
+/*
+ * A residual block of a language-model job
+ * ----------------------------------------
+ * What stands between a job's lookup and its loss, and what of it is remembered for the backward pass in 8 bits: the memory that bounds a job's
+ * per-GPU batch size (PX_M_MEM) is mostly activations.
+ *
+ * Kept rows: N rows of D elements as `values`, a byte each in rows of W = D rounded up to a multiple of 32 (0 beyond D), and `scales`, a byte for each
+ * 32 neighbours of a row ([N, W / 32]).  Element = code * 2^(scale - 127); the code is a whole number from -127 to 127 (PX_KEPT_I8, two's complement)
+ * or an e4m3 (PX_KEPT_E4M3: four bits of exponent, three of fraction, largest 448).  The scale is the least with which the largest of the 32 has a
+ * code, codes are rounded to nearest, ties to even: off by at most 1/127 of the largest of the 32 (I8), or by 2^-4 of the element or 2^-17 of that largest (E4M3).  Groups that hold
+ * an infinity or a NaN have scale 255 and are restored as NaN.  Groups whose largest is below 2^-121 (I8), or 2^-119, have scale 0 and fewer bits.  Buffers are contiguous, values aligned to 16 bytes.
+ * Rows, weights and gates in these calls may begin at any element, but for those of pollux_kept_grad.
+ */
+enum {
+    PX_KEPT_NONE = 0,
+    PX_KEPT_I8 = 1,
+    PX_KEPT_E4M3 = 2
+};
+
+/*
+ * pollux_keep: rows -> values, scales.  pollux_restore: rows of any type from them (in fp16, infinite where an element passes its range).
+ * Limits: 0 <= N <= 2^24, 1 <= D <= 2^20, stride below 2^20 (0: D).  No workspace.
+ */
+typedef struct {
+    int64_t N;                  /* rows                                  */
+    int32_t D;                  /* elements of a row                     */
+    int32_t type;               /* PX_TYPE_* of the rows                 */
+    int32_t form;               /* PX_KEPT_I8 or PX_KEPT_E4M3            */
+    int32_t flags;              /* 0                                     */
+    int64_t rows_stride;
+} pollux_keep_dims;
+
+int pollux_keep(const pollux_keep_dims *dims,            /* host */
+                const void *rows,                        /* [N,D] */
+                uint8_t *values, uint8_t *scales,        /* [N,W], [N,W/32] out */
+                void *hip_stream);
+int pollux_restore(const pollux_keep_dims *dims,         /* host */
+                   const uint8_t *values, const uint8_t *scales,
+                   void *rows,                           /* [N,D] out */
+                   void *hip_stream);
+
+/*
+ * The gradient of a layer's weights from its input kept in 8 bits and the gradient of its result:
+ *   weight_grad[m,k] = weight[k] * (sum_n rows_grad[n,m] * kept[n,k]) + bias[k] * (sum_n rows_grad[n,m])
+ * weight and bias, of type weight_type, NULL for 1 and 0, are those of the norm whose normalised rows are kept (pollux_block_edge): the layer's input
+ * was kept[n,k] * weight[k] + bias[k].  The kept rows are nowhere in memory in more than 8 bits: they are turned into the type of rows_grad, which holds them
+ * exactly (fp16 where they are within its range; elements below 2^-126 may count as 0), on their way to the matrix units.  Sums in fp32, in a fixed order; fp32: a product is off by at most 2^-24 of itself.
+ * With PX_FLAG_ACCUMULATE the result is added to what weight_grad holds.
+ *
+ * Limits: 0 <= N <= 2^24, 1 <= D <= 2^16, 1 <= M <= 2^20, strides below 2^20 (0: the row's length).
+ * workspace: pollux_kept_grad_workspace_size bytes, 256-byte aligned.
+ */
+typedef struct {
+    int64_t N;                  /* rows                                  */
+    int32_t D, M;               /* elements of a kept row, of a row of rows_grad */
+    int32_t type;               /* PX_TYPE_* of rows_grad and weight_grad */
+    int32_t weight_type;        /* PX_TYPE_* of weight and bias          */
+    int32_t form;               /* PX_KEPT_I8 or PX_KEPT_E4M3            */
+    int32_t flags;              /* PX_FLAG_ACCUMULATE                    */
+    int64_t rows_grad_stride, weight_grad_stride;
+} pollux_kept_grad_dims;
+
+int pollux_kept_grad_workspace_size(const pollux_kept_grad_dims *dims, size_t *bytes /* host, out */);
+int pollux_kept_grad(const pollux_kept_grad_dims *dims,  /* host */
+                     const uint8_t *values, const uint8_t *scales,
+                     const void *rows_grad,              /* [N,M] */
+                     const void *weight, const void *bias, /* [D] or NULL */
+                     void *workspace, size_t workspace_bytes,
+                     void *weight_grad,                  /* [M,D] out (in/out with PX_FLAG_ACCUMULATE) */
+                     void *hip_stream);
+
+/*
+ * The edge between two blocks: a norm of the block's result, its gate, the scaled residual, the norm before the next block, in one pass.  With the norm
+ *   n(v) = (v - mean) * r,  r = 1 / sqrt(mean((v - mean)^2) + eps),  mean = 0 without PX_EDGE_CENTRED,
+ *   b    = n(branch) * after_weight + after_bias         (PX_EDGE_AFTER; else b = branch)
+ *   y    = residual * x + scale * gate * b               (without a branch, y = x, which is not written)
+ *   rows = n(y) * before_weight + before_bias            (PX_EDGE_BEFORE; else none)
+ * Weights, biases and the gate may be NULL (1, 0, 1).  A row of the gate serves `span` rows in turn (0: all): a learned vector, one a sequence, or with
+ * 1 one a token; gate [ceil(N / span), D].  y is rounded where it is written; the norm before takes it unrounded.
+ * For the backward pass the call leaves (mean, r) of each norm in y_stats and branch_stats, and, where the form is not PX_KEPT_NONE, the normalised rows n(y) and
+ * n(branch) (branch itself without PX_EDGE_AFTER) kept in 8 bits; pointers of a part that there is none of, or that is not wanted, are NULL (values and scales together).
+ *
+ * pollux_block_edge_grad: from the gradients of y (NULL: zeros) and of rows (with PX_EDGE_BEFORE),
+ *   g = y_grad + N'(rows_grad * before_weight; n(y)),  x_grad = residual * g,
+ *   t = scale * gate * g,  branch_grad = N'(t * after_weight; n(branch))  (t without PX_EDGE_AFTER),   N'(d; n) = r * (d - mean(d) - n * mean(d n)),  mean(d) = 0 if not centred,
+ * and the gradients of the weights, biases and gate, summed over the rows that share them in fp32 and in a fixed order.  n(y) and n(branch) are what is kept, or, without a form,
+ * are formed again from y, branch and the stats.  Any gradient may be NULL.
+ *
+ * Types: x and y and their gradients x_type, branch and rows and theirs `type`; x_type is `type` or fp32.  weights and biases and their gradients weight_type, the gate
+ * and its gradient gate_type.
+ * Limits: 0 <= N <= 2^24, 1 <= D <= 2^14, strides below 2^20 (0: D), 0 <= span, eps >= 0, residual and scale finite; eps, residual and scale the same in both calls.
+ * A row of zeros with eps 0 has r = inf.  Outputs and inputs must not overlap, but y may be x and x_grad may be y_grad, with the same stride.
+ * Forward needs no workspace; backward pollux_block_edge_workspace_size bytes, 256-byte aligned.
+ */
+enum {
+    PX_EDGE_AFTER = 1,          /* a norm of the branch                  */
+    PX_EDGE_BEFORE = 2,         /* a norm of y                           */
+    PX_EDGE_CENTRED = 4         /* norms subtract the mean               */
+};
+
+typedef struct {
+    int64_t N;                  /* rows                                  */
+    int32_t D;                  /* elements of a row                     */
+    int32_t x_type, type, weight_type, gate_type;   /* PX_TYPE_*         */
+    int32_t form;               /* PX_KEPT_*                             */
+    int32_t flags;              /* PX_EDGE_*                             */
+    float eps, residual, scale;
+    int64_t span;               /* rows that share a row of the gate     */
+    int64_t x_stride, branch_stride, y_stride, rows_stride;
+    int64_t x_grad_stride, branch_grad_stride, y_grad_stride, rows_grad_stride;
+} pollux_edge_dims;
+
+int pollux_block_edge(const pollux_edge_dims *dims,      /* host */
+                      const void *x,                     /* [N,D] */
+                      const void *branch,                /* [N,D] or NULL */
+                      const void *gate,                  /* [ceil(N/span),D] or NULL */
+                      const void *after_weight, const void *after_bias, const void *before_weight, const void *before_bias, /* [D] or NULL */
+                      void *y,                           /* [N,D] out (with a branch) */
+                      void *rows,                        /* [N,D] out (PX_EDGE_BEFORE) */
+                      float *y_stats, float *branch_stats,               /* [N,2] out, may be NULL */
+                      uint8_t *y_values, uint8_t *y_scales, uint8_t *branch_values, uint8_t *branch_scales, /* out, may be NULL */
+                      void *hip_stream);
+int pollux_block_edge_workspace_size(const pollux_edge_dims *dims, size_t *bytes /* host, out */);
+int pollux_block_edge_grad(const pollux_edge_dims *dims, /* host */
+                           const void *y_grad,           /* [N,D] or NULL */
+                           const void *rows_grad,        /* [N,D] (PX_EDGE_BEFORE) */
+                           const void *y, const void *y_scales,           /* [N,D], or values and scales (PX_EDGE_BEFORE) */
+                           const void *branch, const void *branch_scales, /* the same (PX_EDGE_AFTER, or with gate_grad; else not read) */
+                           const float *y_stats, const float *branch_stats,
+                           const void *gate, const void *after_weight, const void *after_bias, const void *before_weight,
+                           void *workspace, size_t workspace_bytes,
+                           void *x_grad, void *branch_grad, void *gate_grad,                                  /* out, may be NULL */
+                           void *after_weight_grad, void *after_bias_grad, void *before_weight_grad, void *before_bias_grad,
+                           void *hip_stream);
+
+/*
+ * A gated activation: rows = act(gate) * up (up NULL: act(gate)), and the gradients from that of its rows,
+ *   gate_grad = rows_grad * up * act'(gate),  up_grad = rows_grad * act(gate),
+ * from the inputs or from what is kept of them.  act: silu g / (1 + exp(-g)), gelu g Phi(g), or gelu with 1/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
+ * in Phi's place; each is held to 0 where that factor is.  With a form the forward call keeps gate and up in 8 bits, and the backward call takes values (in the places
+ * of gate and up) and scales.  Backward, `rows` are formed again from what it has, for the gradient of the weights behind them.  Any output of the backward call may be NULL.
+ * Outputs and inputs must not overlap.
+ * Limits: 0 <= N <= 2^24, 1 <= F <= 2^19, strides below 2^20 (0: F).  No workspace.
+ */
+enum {
+    PX_ACT_SILU = 0,
+    PX_ACT_GELU = 1,
+    PX_ACT_GELU_TANH = 2
+};
+
+typedef struct {
+    int64_t N;                  /* rows                                  */
+    int32_t F;                  /* elements of a row                     */
+    int32_t type;               /* PX_TYPE_* of all rows                 */
+    int32_t act;                /* PX_ACT_*                              */
+    int32_t form;               /* PX_KEPT_*                             */
+    int32_t flags;              /* 0                                     */
+    int64_t gate_stride, up_stride, rows_stride, rows_grad_stride, gate_grad_stride, up_grad_stride;
+} pollux_gated_dims;
+
+int pollux_gated(const pollux_gated_dims *dims,          /* host */
+                 const void *gate, const void *up,       /* [N,F]; up may be NULL */
+                 void *rows,                             /* [N,F] out */
+                 uint8_t *gate_values, uint8_t *gate_scales, uint8_t *up_values, uint8_t *up_scales, /* out, with a form */
+                 void *hip_stream);
+int pollux_gated_grad(const pollux_gated_dims *dims,     /* host */
+                      const void *rows_grad,             /* [N,F] */
+                      const void *gate, const void *gate_scales,  /* [N,F], or values and scales */
+                      const void *up, const void *up_scales,      /* the same; NULL: there was none */
+                      void *gate_grad, void *up_grad, void *rows, /* [N,F] out, may be NULL */
+                      void *hip_stream);
+
 /* Copies the status word of the last call that used `workspace` to *host_out: of pollux_fitness (or
  * pollux_fitness_timed), pollux_token_loss, pollux_token_loss_grad or pollux_embed_grad.  Synchronises
  * `hip_stream`.  pollux_goodput_per_gpu and pollux_sim_tick neither clear nor set the word; they leave the
- * workspace as it is.  The workspaces of pollux_noise_scale and pollux_orthogonalize hold no status word: after those calls
- * what would be read is scratch memory. */
+ * workspace as it is.  The workspaces of pollux_noise_scale, pollux_orthogonalize, pollux_kept_grad and
+ * pollux_block_edge_grad hold no status word: after those calls what would be read is scratch memory. */
 int pollux_last_status(const void *workspace, void *hip_stream, int32_t *host_out /* host */);
 
 /* Text for a PX_* return code (static storage, never NULL). */

@@ -23,6 +23,9 @@ PX_GA_INHERIT_ROWS = 2
 PX_ST_BAD_PARAM, PX_ST_ZERO_FAIR, PX_ST_BAD_RESTART, PX_ST_NEG_ALLOC, PX_ST_BAD_TOKEN = 1, 2, 4, 8, 16
 PX_TYPE_F32, PX_TYPE_BF16, PX_TYPE_F16 = 0, 1, 2
 PX_FLAG_TOKENS_I64, PX_FLAG_ACCUMULATE = 1, 2
+PX_KEPT_NONE, PX_KEPT_I8, PX_KEPT_E4M3 = 0, 1, 2
+PX_EDGE_AFTER, PX_EDGE_BEFORE, PX_EDGE_CENTRED = 1, 2, 4
+PX_ACT_SILU, PX_ACT_GELU, PX_ACT_GELU_TANH = 0, 1, 2
 
 EXPORTS = ("pollux_version", "pollux_strerror", "pollux_workspace_size", "pollux_fitness", "pollux_fitness_static",
            "pollux_ga_step",
@@ -30,7 +33,9 @@ EXPORTS = ("pollux_version", "pollux_strerror", "pollux_workspace_size", "pollux
            "pollux_fitness_timed", "pollux_apply_best", "pollux_generation",
            "pollux_loss_workspace_size", "pollux_token_loss", "pollux_token_loss_grad", "pollux_embed", "pollux_embed_workspace_size",
            "pollux_embed_grad", "pollux_noise_workspace_size", "pollux_noise_scale", "pollux_ortho_workspace_size",
-           "pollux_orthogonalize")
+           "pollux_orthogonalize",
+           "pollux_keep", "pollux_restore", "pollux_kept_grad_workspace_size", "pollux_kept_grad", "pollux_block_edge",
+           "pollux_block_edge_workspace_size", "pollux_block_edge_grad", "pollux_gated", "pollux_gated_grad")
 
 
 class PolluxError(RuntimeError):
@@ -67,6 +72,26 @@ class NoiseDims(ctypes.Structure):
 class OrthoDims(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "rows", "cols", "type", "steps", "flags")] + [(n, ctypes.c_double) for n in ("a", "b", "c")]
                 + [(n, ctypes.c_int64) for n in ("grads_stride", "update_stride", "grads_batch_stride", "update_batch_stride")])
+
+
+class KeepDims(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("D", "type", "form", "flags")] + [("rows_stride", ctypes.c_int64)]
+
+
+class KeptGradDims(ctypes.Structure):
+    _fields_ = ([("N", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("D", "M", "type", "weight_type", "form", "flags")]
+                + [(n, ctypes.c_int64) for n in ("rows_grad_stride", "weight_grad_stride")])
+
+
+class EdgeDims(ctypes.Structure):
+    _fields_ = ([("N", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("D", "x_type", "type", "weight_type", "gate_type", "form", "flags")]
+                + [(n, ctypes.c_float) for n in ("eps", "residual", "scale")] + [("span", ctypes.c_int64)]
+                + [(n + "_stride", ctypes.c_int64) for n in ("x", "branch", "y", "rows", "x_grad", "branch_grad", "y_grad", "rows_grad")])
+
+
+class GatedDims(ctypes.Structure):
+    _fields_ = ([("N", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("F", "type", "act", "form", "flags")]
+                + [(n + "_stride", ctypes.c_int64) for n in ("gate", "up", "rows", "rows_grad", "gate_grad", "up_grad")])
 
 
 _lib = None
@@ -129,6 +154,14 @@ def lib() -> ctypes.CDLL:
         L.pollux_ortho_workspace_size.argtypes = [ctypes.POINTER(OrthoDims), ctypes.POINTER(sz)]
         L.pollux_orthogonalize.restype = i
         L.pollux_orthogonalize.argtypes = [ctypes.POINTER(OrthoDims), vp, vp, sz, vp, vp]
+        for name, cls, more in (("pollux_keep", KeepDims, [vp] * 4), ("pollux_restore", KeepDims, [vp] * 4),
+                                ("pollux_kept_grad_workspace_size", KeptGradDims, [ctypes.POINTER(sz)]), ("pollux_kept_grad", KeptGradDims, [vp] * 6 + [sz] + [vp] * 2),
+                                ("pollux_block_edge", EdgeDims, [vp] * 16), ("pollux_block_edge_workspace_size", EdgeDims, [ctypes.POINTER(sz)]),
+                                ("pollux_block_edge_grad", EdgeDims, [vp] * 13 + [sz] + [vp] * 8), ("pollux_gated", GatedDims, [vp] * 8),
+                                ("pollux_gated_grad", GatedDims, [vp] * 9)):
+            call = getattr(L, name)
+            call.restype = i
+            call.argtypes = [ctypes.POINTER(cls)] + more
         _lib = L
     return _lib
 
@@ -382,3 +415,4 @@ class FitnessCall:
 
 
 from .train import embed, embed_grad, noise_scale, orthogonalize, token_loss, token_loss_grad  # noqa: E402,F401  (needs the names above)
+from .blocks import Kept, Norm, block_edge, block_edge_grad, gated, gated_grad, keep, kept_grad, restore  # noqa: E402,F401

@@ -1,0 +1,299 @@
+// The gradient of a layer's weights from its input kept in 8 bits:
+//
+//   dW[m,k] = w[k] sum_n dY[n,m] X[n,k] + b[k] sum_n dY[n,m]
+//
+// A product over the rows n, of which both operands are columns in memory: tiles of dW, k in registers (a lane's four values are neighbours of a row of dW).  X is turned into dY's type on its way to
+// LDS and is nowhere in memory in more than 8 bits.  Scales differ from row to row, which is what the product sums over, so that they cannot wait until after it;
+// a norm's weights w can, and are multiplied in where tiles are stored.  Few tiles: the rows are cut in slices, whose sums are joined in order.
+// Bound by the matrix units.
+
+#include "pollux_host.h"
+#include "pollux_kept.h"
+#include "pollux_rows.h"
+#include "pollux_tiles.h"
+#include "pollux_train.h"
+
+#include <math.h>
+
+#include <algorithm>
+
+namespace px {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct KeptGradArgs {
+    Operands o;
+    int tiles_m, tiles_n;
+    int64_t N, slice;
+    int D, M;
+    const void *weight, *bias;
+    int weight_type;
+    const float *sums;          // [M] of rows_grad over the rows, with a bias
+    void *out;                  // weight_grad, or the slices' sums
+    int64_t ld;
+    int slices;
+    bool add;
+};
+
+#ifdef __HIP_DEVICE_COMPILE__
+__device__ __forceinline__ float parameter(const void *p, int type, int at, float none)
+{
+    if (!p) return none;
+    return type == PX_TYPE_F32 ? ((const float *)p)[at] : type == PX_TYPE_BF16 ? (float)((const __bf16 *)p)[at] : (float)((const _Float16 *)p)[at];
+}
+#endif
+
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void kept_tiles(const KeptGradArgs A)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef typename S::element::type type;
+    extern __shared__ __align__(16) char lds[];
+    const Tile t = tile_of(blockIdx.x, A.tiles_m, A.tiles_n, 8);
+    Operands o = A.o;
+    const int64_t row = blockIdx.y * A.slice;
+    o.a += row * o.lda;
+    o.scales += row * (o.lda / kKeptGroup);
+    o.b += row * o.ldb;
+    o.k = (int)max((int64_t)0, min(A.slice, A.N - row));
+    f32x4 acc[S::FM][S::FN];
+    tile_product<S>(o, t, lds, acc);
+    const Place<S> at(t);
+    constexpr bool kPairs = sizeof(type) == 2 && S::FM % 2 == 0;
+    const Pair pair;
+    const int wave_m = at.first_m - (threadIdx.x >> 4 & 3) * 4;
+    const bool sums = A.slices > 1;
+    const int group = sums || !kPairs ? 3 : 7;
+    const bool whole = sums ? (A.D & 3) == 0 : (A.ld & group) == 0;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+        const int n = at.first_n + j * 16;
+        if (sums) {
+            if (n >= A.M) continue;
+            float *const to = (float *)A.out + ((int64_t)blockIdx.y * A.M + n) * A.D;
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int m = at.first_m + 16 * i;
+                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                put<F32>(to + m, v, A.D - m, whole, false);
+            }
+            continue;
+        }
+        type *const to = (type *)A.out + (int64_t)n * A.ld;
+        const float rows = A.bias && n < A.M ? A.sums[n] : 0.f;
+        auto value = [&](int i, int r) {
+            const int m = min(at.first_m + 16 * i + r, A.D - 1);
+            float v = acc[i][j][r];
+            if (A.weight) v *= parameter(A.weight, A.weight_type, m, 1.f);
+            if (A.bias) v = fmaf(rows, parameter(A.bias, A.weight_type, m, 0.f), v);
+            return v;
+        };
+        if constexpr (kPairs) {
+#pragma unroll
+            for (int i = 0; i < S::FM; i += 2) {
+                const f32x4 first = {value(i, 0), value(i, 1), value(i, 2), value(i, 3)}, second = {value(i + 1, 0), value(i + 1, 1), value(i + 1, 2), value(i + 1, 3)};
+                const int m = wave_m + 16 * (i + pair.tile) + pair.row;
+                float v[8];
+                paired32(first, second, v);                // (all lanes change places, those past the last row too)
+                if (n < A.M) put<typename S::element>(to + m, v, A.D - m, whole, A.add);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i) {
+                const int m = at.first_m + 16 * i;
+                const float v[4] = {value(i, 0), value(i, 1), value(i, 2), value(i, 3)};
+                if (n < A.M) put<typename S::element>(to + m, v, A.D - m, whole, A.add);
+            }
+        }
+    }
+#endif
+}
+
+// The slices' sums, added in their order, weighted and rounded.
+template <class T>
+__global__ __launch_bounds__(kThreads) void join_slices(const KeptGradArgs A, const float *slices)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef typename T::type type;
+    const int groups = (A.D + kVec - 1) / kVec;
+    const int64_t total = (int64_t)A.M * groups, one = (int64_t)A.M * A.D;
+    for (int64_t at = blockIdx.x * (int64_t)kThreads + threadIdx.x; at < total; at += gridDim.x * (int64_t)kThreads) {
+        const int64_t n = at / groups;
+        const int c = (int)(at - n * groups) * kVec, left = A.D - c;
+        const float *from = slices + n * A.D + c;
+        f32x8 v = load8f(from, left);
+#pragma unroll 4
+        for (int s = 1; s < A.slices; ++s) v += load8f(from + s * one, left);
+        if (A.weight || A.bias) {
+            const float rows = A.bias ? A.sums[n] : 0.f;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const int m = min(c + i, A.D - 1);
+                v[i] *= parameter(A.weight, A.weight_type, m, 1.f);
+                if (A.bias) v[i] = fmaf(rows, parameter(A.bias, A.weight_type, m, 0.f), v[i]);
+            }
+        }
+        type *const to = (type *)A.out + n * A.ld + c;
+        if (A.add) v += load8f(to, left);
+        store8f(to, left, v);
+    }
+#endif
+}
+
+// Rows copied to aligned ones, padded with zeros.
+template <class E>
+__global__ __launch_bounds__(kThreads) void pad_rows(const E *from, int64_t ld_from, int64_t rows, int cols, E *to, int64_t ld_to)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    const int groups = (int)((ld_to + kVec - 1) / kVec);
+    const int64_t total = rows * groups;
+    for (int64_t at = blockIdx.x * (int64_t)kThreads + threadIdx.x; at < total; at += gridDim.x * (int64_t)kThreads) {
+        const int64_t n = at / groups;
+        const int c = (int)(at - n * groups) * kVec;
+        store8(to + n * ld_to + c, ld_to - c, load8(from + n * ld_from + c, cols - c));
+    }
+#endif
+}
+
+// Sums of rows_grad over the rows: of a part of them, eight columns a thread, by `down` threads that each take every down-th row; then of the parts in order.
+template <class E>
+__global__ __launch_bounds__(kThreads) void sum_rows(const E *rows, int64_t ld, int64_t N, int M, int across, float *parts)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    __shared__ float shared[kThreads][kVec + 1];
+    const int down = kThreads / across, mine = threadIdx.x % across, from = threadIdx.x / across;
+    const int c = (blockIdx.x * across + mine) * kVec, left = M - c;
+    const int64_t each = (N + gridDim.y - 1) / gridDim.y, first = blockIdx.y * each, last = min(first + each, N);
+    f32x8 v = {};
+#pragma unroll 4
+    for (int64_t n = first + from; n < last; n += down) v += load8f(rows + n * ld + c, left);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) shared[threadIdx.x][i] = v[i];
+    __syncthreads();
+    if (from != 0) return;
+    for (int k = 1; k < down; ++k)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] += shared[k * across + mine][i];
+    store8f(parts + (int64_t)blockIdx.y * M + c, left, v);
+#endif
+}
+__global__ __launch_bounds__(kThreads) void sum_parts(const float *parts, int count, int M, float *sums)
+{
+    const int m = blockIdx.x * kThreads + threadIdx.x;
+    if (m >= M) return;
+    float v = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < count; ++k) v += parts[(int64_t)k * M + m];
+    sums[m] = v;
+}
+
+unsigned blocks_for(int64_t groups) { return (unsigned)std::min<int64_t>((groups + kThreads - 1) / kThreads, 8192); }
+
+template <class T, int FORM>
+void launch_tiles(int shape, KeptGradArgs a, hipStream_t stream)
+{
+    auto launch = [&](auto s) {
+        typedef decltype(s) S;
+        a.tiles_m = (a.D + S::BM - 1) / S::BM;
+        a.tiles_n = (a.M + S::BN - 1) / S::BN;
+        hipLaunchKernelGGL(kept_tiles<S>, dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.slices), dim3(S::kThreads), S::kLds, stream, a);
+    };
+    switch (shape) {
+        case 0:
+            if constexpr (!std::is_same<T, F32>::value) launch(TileShape<T, 256, 256, 2, 4, 2, true, true, FORM>());
+            break;
+        case 1: launch(TileShape<T, 128, 128, 2, 2, 2, true, true, FORM>()); break;
+        default: launch(TileShape<T, 64, 64, 2, 2, 2, true, true, FORM>()); break;
+    }
+}
+
+template <class T>
+int kept_grad(const pollux_kept_grad_dims &d, const KeptGradPlan &p, const uint8_t *values, const uint8_t *scales, const char *rows_grad, const void *weight,
+              const void *bias, char *ws, void *weight_grad, hipStream_t stream)
+{
+    typedef typename T::type type;
+    constexpr int e = sizeof(type);
+    KeptGradArgs a = {};
+    a.N = d.N;
+    a.D = d.D;
+    a.M = d.M;
+    a.weight = weight;
+    a.bias = bias;
+    a.weight_type = d.weight_type;
+    a.sums = (const float *)(ws + p.sums);
+    a.add = d.flags & PX_FLAG_ACCUMULATE;
+    a.slice = p.slice;
+    a.slices = p.slices;
+    a.ld = d.weight_grad_stride;
+    if (bias) {
+        int across = 1;
+        while (across < kThreads && across * kVec < d.M) across *= 2;
+        const int columns = (d.M + across * kVec - 1) / (across * kVec);
+        hipLaunchKernelGGL(sum_rows<type>, dim3((unsigned)columns, (unsigned)p.sum_blocks), dim3(kThreads), 0, stream, (const type *)rows_grad, d.rows_grad_stride, d.N, d.M, across,
+                           (float *)(ws + p.parts));
+        hipLaunchKernelGGL(sum_parts, dim3((unsigned)((d.M + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, (const float *)(ws + p.parts), p.sum_blocks, d.M, (float *)(ws + p.sums));
+    }
+    int64_t ld = d.rows_grad_stride;
+    if (p.pack && d.N > 0) {
+        hipLaunchKernelGGL(pad_rows<type>, dim3(blocks_for(d.N * ((p.m_pad + kVec - 1) / kVec))), dim3(kThreads), 0, stream, (const type *)rows_grad, ld, d.N, d.M, (type *)(ws + p.rows), p.m_pad);
+        rows_grad = ws + p.rows;
+        ld = p.m_pad;
+    }
+    const int64_t width = kept_width(d.D);
+    a.o = {(const char *)values, rows_grad, width, ld * e, d.D, d.M, 0, scales};
+    a.out = p.slices > 1 ? (void *)(ws + p.slices_at) : weight_grad;
+    if (d.form == PX_KEPT_I8) launch_tiles<T, PX_KEPT_I8>(p.tiles, a, stream);
+    else launch_tiles<T, PX_KEPT_E4M3>(p.tiles, a, stream);
+    if (p.slices > 1) {
+        a.out = weight_grad;
+        hipLaunchKernelGGL(join_slices<T>, dim3(blocks_for((int64_t)d.M * ((d.D + kVec - 1) / kVec))), dim3(kThreads), 0, stream, a, (const float *)(ws + p.slices_at));
+    }
+    return status_of(hipGetLastError());
+}
+
+}  // namespace
+
+KeptGradPlan kept_grad_plan(const pollux_kept_grad_dims &d)
+{
+    KeptGradPlan p = {};
+    const int e = size_of_type(d.type), pad = 16 / e, depth = kRowBytes / e;
+    const bool f32 = e == 4;
+    p.m_pad = ((int64_t)d.M + pad - 1) / pad * pad;
+    p.pack = d.rows_grad_stride % pad != 0 || d.M % pad != 0;
+    const int64_t stages = std::max<int64_t>(1, (d.N + depth - 1) / depth);
+    // in as many slices of the rows as takes least, their sums being written and read at some 4 and 3 TB/s
+    double least = 1e300;
+    for (int slices = 1; slices <= 64; slices *= 2) {
+        if (slices > 1 && (stages < 4 * slices || (int64_t)slices * d.M * d.D * 4 > (512ll << 20))) break;
+        for (int s = f32 ? 1 : 0; s < 3; ++s) {
+            double cost = shape_cost(kShape[s], d.D, d.M, (double)d.N / slices, slices, f32);
+            if (slices > 1) cost += 4.0 + 4.0 * slices * d.M * d.D * (1 / 4e6 + 1 / 3e6);
+            if (cost < least) least = cost, p.slices = slices, p.tiles = s;
+        }
+    }
+    p.slice = (stages + p.slices - 1) / p.slices * depth;
+    p.sum_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(64, d.N / 64));
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
+    p.parts = take((size_t)p.sum_blocks * d.M * 4);
+    p.sums = take((size_t)d.M * 4);
+    if (p.pack) p.rows = take((size_t)d.N * p.m_pad * e);
+    if (p.slices > 1) p.slices_at = take((size_t)p.slices * d.M * d.D * 4);
+    p.total = o;
+    return p;
+}
+
+int launch_kept_grad(const pollux_kept_grad_dims &d, const KeptGradPlan &p, const uint8_t *values, const uint8_t *scales, const void *rows_grad, const void *weight,
+                     const void *bias, void *workspace, void *weight_grad, hipStream_t stream)
+{
+    const char *rows = (const char *)rows_grad;
+    char *ws = (char *)workspace;
+    switch (d.type) {
+        case PX_TYPE_F32: return kept_grad<F32>(d, p, values, scales, rows, weight, bias, ws, weight_grad, stream);
+        case PX_TYPE_BF16: return kept_grad<Bf16>(d, p, values, scales, rows, weight, bias, ws, weight_grad, stream);
+        default: return kept_grad<F16>(d, p, values, scales, rows, weight, bias, ws, weight_grad, stream);
+    }
+}
+
+}  // namespace px

@@ -286,25 +286,6 @@ __device__ __forceinline__ void add_rest(V &v, float rest, const E *weight, int6
         v[r] += fabsf(more) < __builtin_inff() ? more : 0.f;
     }
 }
-
-// Neighbouring values into a row of which `left` elements remain, added to what it holds if `add`; whole: such groups are aligned.
-template <class T, int COUNT>
-__device__ __forceinline__ void put(typename T::type *to, const float (&v)[COUNT], int left, bool whole, bool add)
-{
-    typedef typename T::type type;
-    typedef type vec __attribute__((ext_vector_type(COUNT)));
-    if (whole && left >= COUNT) {
-        vec old = {}, t;
-        if (add) old = *(const vec *)to;
-#pragma unroll
-        for (int r = 0; r < COUNT; ++r) t[r] = (type)(add ? v[r] + (float)old[r] : v[r]);
-        *(vec *)to = t;
-    } else {
-#pragma unroll
-        for (int r = 0; r < COUNT; ++r)
-            if (r < left) to[r] = (type)(add ? v[r] + (float)to[r] : v[r]);
-    }
-}
 #endif
 
 template <class S>

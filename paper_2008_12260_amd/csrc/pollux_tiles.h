@@ -23,6 +23,7 @@
 
 #include <type_traits>
 
+#include "pollux_kept.h"
 #include "pollux_train.h"
 
 namespace px {
@@ -55,6 +56,7 @@ struct Operands {
     const char *a, *b;
     int64_t lda, ldb;       // bytes from row to row in memory, multiples of 16, as are the pointers
     int m, n, k;
+    const uint8_t *scales;  // of a, kept in 8 bits as its columns: rows of lda codes, lda / 32 scales
 };
 
 // Workgroup -> tile.  Workgroups go round the eight XCDs, each with a cache of its own: the tiles are cut into eight runs, one
@@ -82,9 +84,10 @@ __device__ __forceinline__ Tile triangle_of(int block, int tiles)
     return {m, at - m * (m + 1) / 2};
 }
 
-template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool COLS_A_ = false, bool COLS_B_ = false>
+template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool COLS_A_ = false, bool COLS_B_ = false, int KEPT_ = PX_KEPT_NONE>
 struct TileShape {
     typedef T element;
+    static constexpr int KEPT = KEPT_;                            // the form that A, its columns in memory, is kept in
     static constexpr bool COLS_A = COLS_A_, COLS_B = COLS_B_;     // the operand lies in memory as its columns
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr int kThreads = WM * WN * 64, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
@@ -326,6 +329,112 @@ struct Side {
     }
 };
 
+// The columns of an operand that is kept in 8 bits: its codes come into registers, up to 16 neighbours of one k a load, a stage ahead of the one that they are written to LDS for as elements, where
+// the other operand's loads would put theirs.  Each code is turned once a workgroup: 32 a thread and stage in tiles of 256 x 256 beside 64 products (2 operations a code of i8, half a one of e4m3, where
+// the hardware scales and turns two at a time).
+template <class T, int B_, int F, int THREADS, int FORM>
+struct KeptSide {
+    typedef Side<T, B_, F, THREADS, true> Columns;
+    typedef typename T::piece piece;
+    static constexpr int kSize = Columns::kSize, kDepth = Columns::kDepth, kLine = Columns::kLine, kReads = Columns::kReads;
+    static constexpr int kCodes = B_ * kDepth / THREADS, kWide = kCodes < 16 ? kCodes : 16, kParts = kCodes / kWide, kAcross = B_ / kWide;
+    static constexpr int kLoads = 2 * kParts;                     // codes, and their scale
+    static_assert(kParts * kWide * THREADS == B_ * kDepth && kWide >= 8 && kAcross * kWide == B_, "whole loads");
+    const char *base;
+    const uint8_t *scale_base;
+    int64_t ld;
+    int k, stages, width;
+    Columns columns;                    // (for its reads)
+    int at[kParts], scale_at[kParts], to[kParts], turn[kParts];
+    uint32_t codes[kParts][kWide / 4], bytes[kParts];
+
+    __device__ __forceinline__ KeptSide(const Operands &o, int first, int mine) : columns(o.a, o.lda, 0, 0, 0, mine)
+    {
+        ld = o.lda;
+        k = o.k;
+        stages = (k + kDepth - 1) / kDepth;
+        base = o.a + first;
+        scale_base = o.scales + first / kKeptGroup;
+        width = min((int)ld - first, B_);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            const int unit = i * THREADS + threadIdx.x, row = unit / kAcross, c = unit % kAcross * kWide;
+            at[i] = c < width ? row * (int)ld + c : (int)0x80000000;
+            scale_at[i] = c < width ? row * (int)(ld / kKeptGroup) + c / kKeptGroup : (int)0x80000000;
+            to[i] = row * kLine;
+            turn[i] = (c * kSize / 16) ^ Columns::f(row);         // (of the first of its pieces; the others' last bits differ)
+        }
+        fetch(0);
+    }
+
+    __device__ __forceinline__ void fetch(int stage)
+    {
+        const int rows = min(k - stage * kDepth, kDepth);
+        const int64_t row = (int64_t)min(stage, max(stages - 1, 0)) * kDepth;
+        const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void *)(base + row * ld), 0, rows > 0 ? (int)((rows - 1) * ld) + width : 0, 0x00027000);
+        const auto scales = __builtin_amdgcn_make_buffer_rsrc((void *)(scale_base + row * (ld / kKeptGroup)), 0, rows > 0 ? (int)((rows - 1) * (ld / kKeptGroup)) + width / kKeptGroup : 0, 0x00027000);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            if constexpr (kWide == 16) {
+                const auto v = __builtin_amdgcn_raw_buffer_load_b128(buffer, at[i], 0, 0);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) codes[i][q] = v[q];
+            } else {
+                const auto v = __builtin_amdgcn_raw_buffer_load_b64(buffer, at[i], 0, 0);
+                codes[i][0] = v[0];
+                codes[i][1] = v[1];
+            }
+            bytes[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(scales, scale_at[i], 0, 0);
+        }
+    }
+
+    // Eight codes as elements of 16 bits, or four as those of 32.
+    static __device__ __forceinline__ piece turned(const uint32_t *words, float scale)
+    {
+        if constexpr (kSize == 4) {
+            const f32x8 v = decode8(FORM, u32x2{words[0], 0u}, scale);
+            return f32x4{v[0], v[1], v[2], v[3]};
+        } else if constexpr (FORM == PX_KEPT_I8) {
+            typedef typename T::type vec __attribute__((ext_vector_type(8)));
+            return __builtin_bit_cast(piece, __builtin_convertvector(decode8(FORM, u32x2{words[0], words[1]}, scale), vec));
+        } else {
+            uint32_t out[4];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if constexpr (std::is_same<T, Bf16>::value) {
+                    out[2 * q] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)words[q], scale, false));
+                    out[2 * q + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)words[q], scale, true));
+                } else {
+                    out[2 * q] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)words[q], scale, false));
+                    out[2 * q + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)words[q], scale, true));
+                }
+            }
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+            return __builtin_bit_cast(piece, u32x4{out[0], out[1], out[2], out[3]});
+        }
+    }
+
+    // What has been fetched, which is the stage's, into LDS; the next stage is fetched.
+    __device__ __forceinline__ void load(int stage, lds_char *into)
+    {
+        typedef __attribute__((address_space(3))) piece lds_piece;
+        constexpr int kWords = kSize == 4 ? 1 : 2, kPieces = kWide / (4 * kWords);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            const bool none = bytes[i] == 255;
+            const float scale = FORM == PX_KEPT_E4M3 && none ? 1.f : kept_scale(bytes[i]);
+            uint32_t words[kWide / 4];
+#pragma unroll
+            for (int q = 0; q < kWide / 4; ++q) words[q] = FORM == PX_KEPT_E4M3 && none ? 0x7f7f7f7fu : codes[i][q];          // (NaN)
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) *(lds_piece *)(into + to[i] + (turn[i] ^ q) * 16) = turned(words + q * kWords, scale);
+        }
+        fetch(stage + 1);
+    }
+
+    __device__ __forceinline__ void read(const lds_char *stage, int half, piece (&into)[F]) const { columns.read(stage, half, into); }
+};
+
 template <class S, bool SPLIT>
 __device__ __forceinline__ void form_tile(const Operands &o, Tile t, char *lds_, f32x4 (&acc)[S::FM][S::FN])
 {
@@ -333,9 +442,14 @@ __device__ __forceinline__ void form_tile(const Operands &o, Tile t, char *lds_,
     typedef typename T::piece piece;
     lds_char *const lds = (lds_char *)lds_;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    typedef Side<T, S::BM, S::FM, S::kThreads, S::COLS_A> SideA;
+    constexpr bool kKept = S::KEPT != PX_KEPT_NONE;
+    static_assert(!kKept || (S::COLS_A && S::kStages == 2), "kept operands are columns, a stage ahead in registers");
+    typedef std::conditional_t<kKept, KeptSide<T, S::BM, S::FM, S::kThreads, kKept ? S::KEPT : PX_KEPT_I8>, Side<T, S::BM, S::FM, S::kThreads, S::COLS_A>> SideA;
     typedef Side<T, S::BN, S::FN, S::kThreads, S::COLS_B> SideB;
-    SideA side_a(o.a, o.lda, t.m * S::BM, o.m, o.k, wave / S::WN * S::TM);
+    SideA side_a = [&] {
+        if constexpr (kKept) return SideA(o, t.m * S::BM, wave / S::WN * S::TM);
+        else return SideA(o.a, o.lda, t.m * S::BM, o.m, o.k, wave / S::WN * S::TM);
+    }();
     SideB side_b(o.b, o.ldb, t.n * S::BN, o.n, o.k, wave % S::WN * S::TN);
     const int stages = side_a.stages;
     constexpr int kBytesA = S::BM * kRowBytes;
@@ -404,6 +518,7 @@ __device__ __forceinline__ void form_tile(const Operands &o, Tile t, char *lds_,
                 constexpr int kOf[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};        // the small ones first
 #pragma unroll
                 for (int k = 0; k < 6; ++k)
+                    if (!kKept || kOf[k][0] == 0)           // (kept elements are bfloat16 numbers: their other parts are 0)
 #pragma unroll
                     for (int j = 0; j < S::FN; ++j) acc[i][j] = multiply(a.p[kOf[k][0]], b[j].p[kOf[k][1]], acc[i][j]);
                 a = next;
@@ -509,6 +624,25 @@ __device__ __forceinline__ void paired32(f32x4 first, f32x4 second, float (&to)[
         const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(first[r]), __float_as_uint(second[r]), false, false);
         to[r] = __uint_as_float(both[0]);
         to[r + 4] = __uint_as_float(both[1]);
+    }
+}
+
+// Neighbouring values into a row of which `left` elements remain, added to what it holds if `add`; whole: such groups are aligned.
+template <class T, int COUNT>
+__device__ __forceinline__ void put(typename T::type *to, const float (&v)[COUNT], int left, bool whole, bool add)
+{
+    typedef typename T::type type;
+    typedef type vec __attribute__((ext_vector_type(COUNT)));
+    if (whole && left >= COUNT) {
+        vec old = {}, t;
+        if (add) old = *(const vec *)to;
+#pragma unroll
+        for (int r = 0; r < COUNT; ++r) t[r] = (type)(add ? v[r] + (float)old[r] : v[r]);
+        *(vec *)to = t;
+    } else {
+#pragma unroll
+        for (int r = 0; r < COUNT; ++r)
+            if (r < left) to[r] = (type)(add ? v[r] + (float)to[r] : v[r]);
     }
 }
 

@@ -99,4 +99,56 @@ struct OrthoPlan {
 OrthoPlan ortho_plan(const pollux_ortho_dims &d);
 int launch_orthogonalize(const pollux_ortho_dims &d, const OrthoPlan &p, const void *grads, void *workspace, void *update, hipStream_t stream);
 
+// ---- residual blocks -----------------------------------------------------------------------------------------------
+
+int launch_keep(const pollux_keep_dims &d, const void *rows, uint8_t *values, uint8_t *scales, hipStream_t stream);
+int launch_restore(const pollux_keep_dims &d, const uint8_t *values, const uint8_t *scales, void *rows, hipStream_t stream);
+int launch_gated(const pollux_gated_dims &d, const void *gate, const void *up, void *rows, uint8_t *gate_values, uint8_t *gate_scales, uint8_t *up_values,
+                 uint8_t *up_scales, hipStream_t stream);
+int launch_gated_grad(const pollux_gated_dims &d, const void *rows_grad, const void *gate, const void *up, const uint8_t *gate_scales, const uint8_t *up_scales,
+                      void *gate_grad, void *up_grad, void *rows, hipStream_t stream);
+
+struct KeptGradPlan {
+    bool pack;                  // rows of rows_grad that 16-byte loads cannot take are copied to aligned ones first
+    int tiles;                  // shape of tile
+    int slices;                 // workgroups that share a tile, each a part of the rows
+    int64_t slice;              // rows of a slice, whole stages
+    int64_t m_pad;              // padded row of rows_grad
+    int sum_blocks;             // bias: parts of the rows whose sums are joined
+    size_t rows;                // packed copy [N, m_pad]
+    size_t parts, sums;         // bias: float [sum_blocks, M], [M]: sums of rows_grad over the rows
+    size_t slices_at;           // float [slices, M, D]
+    size_t total;
+};
+KeptGradPlan kept_grad_plan(const pollux_kept_grad_dims &d);
+int launch_kept_grad(const pollux_kept_grad_dims &d, const KeptGradPlan &p, const uint8_t *values, const uint8_t *scales, const void *rows_grad, const void *weight,
+                     const void *bias, void *workspace, void *weight_grad, hipStream_t stream);
+
+// How an edge's rows are shared out: `team` threads have a row between them, eight elements or twice eight each.
+struct EdgePlan {
+    int vectors;                // of eight elements, a thread
+    int team, teams;            // threads of a row; rows that a workgroup has under way at a time
+    int chunk;                  // backward: neighbouring rows that a team sums over
+    int blocks;                 // backward
+    size_t parts;               // float [4][blocks][D]: sums over a workgroup's rows
+    size_t ends;                // float [blocks * teams][2][D]: the gate's gradient of the spans that a team's first and last row cut
+    size_t total;
+};
+EdgePlan edge_plan(const pollux_edge_dims &d);
+struct EdgeArgs;
+int launch_block_edge(const pollux_edge_dims &d, const EdgePlan &p, const EdgeArgs &a, hipStream_t stream);
+int launch_block_edge_grad(const pollux_edge_dims &d, const EdgePlan &p, const EdgeArgs &a, hipStream_t stream);
+
+// A call's pointers.
+struct EdgeArgs {
+    const void *x, *branch, *gate, *after_weight, *after_bias, *before_weight, *before_bias;
+    void *y, *rows;
+    float *y_stats, *branch_stats;
+    uint8_t *y_values, *y_scales, *branch_values, *branch_scales;
+    // backward
+    const void *y_grad, *rows_grad;
+    void *x_grad, *branch_grad, *gate_grad, *after_weight_grad, *after_bias_grad, *before_weight_grad, *before_bias_grad;
+    char *workspace;
+};
+
 }  // namespace px

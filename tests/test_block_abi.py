@@ -1,0 +1,241 @@
+"""A residual block's entry points refuse what they cannot take on the host, before any device is touched (no GPU needed)."""
+import ctypes
+
+import pytest
+
+import paper_2008_12260_amd as px
+
+torch = pytest.importorskip("torch")
+
+FAKE = ctypes.c_void_p(0x10000)          # never dereferenced: validation, or the device check, fails first
+EIGHT, TWO, ODD = ctypes.c_void_p(0x10008), ctypes.c_void_p(0x10002), ctypes.c_void_p(0x10001)
+NULL = ctypes.c_void_p(0)
+
+
+def refused(call, dims, args, changes, code=px.PX_E_INVALID_ARG):
+    """Each (position, value), or tuple of them, alone makes the call fail with `code`; position -1 replaces the dims."""
+    for change in changes:
+        pairs = [change] if not isinstance(change[0], tuple) else change
+        bad, d = list(args), dims
+        for at, value in pairs:
+            if at < 0:
+                d = value
+            else:
+                bad[at] = value
+        assert call(None if d is None else ctypes.byref(d), *bad) == code, change
+
+
+def of(cls, values):
+    def make(**changes):
+        d = cls(*values)
+        for k, v in changes.items():
+            setattr(d, k, v)
+        return d
+    return make
+
+
+def changed(make, changes):
+    return [(-1, None)] + [(-1, make(**c)) for c in changes]
+
+
+keep_dims = of(px.KeepDims, (10, 100, px.PX_TYPE_BF16, px.PX_KEPT_I8, 0, 0))
+kept_grad_dims = of(px.KeptGradDims, (10, 100, 60, px.PX_TYPE_BF16, px.PX_TYPE_F32, px.PX_KEPT_E4M3, 0, 0, 0))
+edge_dims = of(px.EdgeDims, (10, 100, px.PX_TYPE_F32, px.PX_TYPE_BF16, px.PX_TYPE_F32, px.PX_TYPE_BF16, 0, px.PX_EDGE_AFTER | px.PX_EDGE_BEFORE, 1e-6, 1.0, 1.0, 0))
+gated_dims = of(px.GatedDims, (10, 100, px.PX_TYPE_BF16, px.PX_ACT_SILU, 0, 0))
+
+ROWS = [dict(N=-1), dict(N=(1 << 24) + 1)]
+BAD_KEEP = ROWS + [dict(D=0), dict(D=(1 << 20) + 1), dict(type=3), dict(form=0), dict(form=3), dict(flags=1), dict(rows_stride=99), dict(rows_stride=1 << 20)]
+BAD_KEPT_GRAD = ROWS + [dict(D=0), dict(D=(1 << 16) + 1), dict(M=0), dict(M=(1 << 20) + 1), dict(type=-1), dict(weight_type=3), dict(form=0), dict(form=-1), dict(flags=1), dict(flags=4),
+                        dict(rows_grad_stride=59), dict(weight_grad_stride=99), dict(rows_grad_stride=1 << 20)]
+BAD_EDGE = ROWS + [dict(D=0), dict(D=(1 << 14) + 1), dict(x_type=3), dict(type=3), dict(x_type=px.PX_TYPE_F16), dict(type=px.PX_TYPE_F32, x_type=px.PX_TYPE_BF16), dict(weight_type=-1), dict(gate_type=4),
+                   dict(form=3), dict(form=-1), dict(flags=8), dict(eps=-1e-6), dict(eps=float("nan")), dict(eps=float("inf")), dict(residual=float("inf")), dict(scale=float("nan")), dict(span=-1)]
+BAD_EDGE += [{n + "_stride": s} for n in ("x", "branch", "y", "rows", "x_grad", "branch_grad", "y_grad", "rows_grad") for s in (99, 1 << 20, -1)]
+BAD_GATED = ROWS + [dict(F=0), dict(F=(1 << 19) + 1), dict(type=3), dict(act=3), dict(act=-1), dict(form=3), dict(flags=1)]
+BAD_GATED += [{n + "_stride": 99} for n in ("gate", "up", "rows", "rows_grad", "gate_grad", "up_grad")]
+
+
+def test_keeping_and_restoring():
+    for call in (px.lib().pollux_keep, px.lib().pollux_restore):
+        at = {"rows": 0, "values": 1} if call is px.lib().pollux_keep else {"rows": 2, "values": 0}
+        refused(call, keep_dims(), [FAKE] * 3 + [NULL], changed(keep_dims, BAD_KEEP) + [(0, NULL), (1, NULL), (2, NULL), (at["rows"], ODD), (at["values"], EIGHT)])
+
+
+@pytest.mark.parametrize("size,make,bad", [("pollux_kept_grad_workspace_size", kept_grad_dims, BAD_KEPT_GRAD), ("pollux_block_edge_workspace_size", edge_dims, BAD_EDGE)])
+def test_workspaces(size, make, bad):
+    call, n = getattr(px.lib(), size), ctypes.c_size_t()
+    for N in (0, 1, 10, 1 << 24):
+        assert call(ctypes.byref(make(N=N)), ctypes.byref(n)) == px.PX_OK and n.value > 0
+    assert call(ctypes.byref(make()), None) == px.PX_E_INVALID_ARG
+    refused(call, make(), [ctypes.byref(n)], changed(make, bad))
+
+
+def test_workspaces_stay_small_beside_the_rows():
+    n = ctypes.c_size_t()
+    L = px.lib()
+    # 16384 x 4096: the sums of an edge's gradients, and the slices of a product
+    assert L.pollux_block_edge_workspace_size(ctypes.byref(edge_dims(N=16384, D=4096)), ctypes.byref(n)) == px.PX_OK and n.value < 16384 * 4096 * 2 // 2
+    for N, D, M in ((16384, 4096, 16384), (1 << 24, 64, 64), (4096, 1 << 16, 4096)):
+        assert L.pollux_kept_grad_workspace_size(ctypes.byref(kept_grad_dims(N=N, D=D, M=M)), ctypes.byref(n)) == px.PX_OK and n.value <= (600 << 20)
+
+
+def test_kept_grad():
+    # values, scales, rows_grad, weight, bias, workspace, bytes, weight_grad, stream
+    args = [FAKE, FAKE, FAKE, NULL, NULL, FAKE, 1 << 40, FAKE, NULL]
+    call = px.lib().pollux_kept_grad
+    refused(call, kept_grad_dims(), args, changed(kept_grad_dims, BAD_KEPT_GRAD) + [(0, NULL), (1, NULL), (2, NULL), (7, NULL), (0, EIGHT), (2, EIGHT), (3, TWO), (4, TWO), (7, EIGHT)])
+    refused(call, kept_grad_dims(), args, [(5, NULL), (5, EIGHT), (6, 16)], px.PX_E_WORKSPACE)
+
+
+def test_edges():
+    # x, branch, gate, after_weight, after_bias, before_weight, before_bias, y, rows, y_stats, branch_stats, y_values, y_scales, branch_values, branch_scales, stream
+    call = px.lib().pollux_block_edge
+    args = [FAKE] * 11 + [NULL] * 5
+    refused(call, edge_dims(), args, changed(edge_dims, BAD_EDGE) + [(0, NULL), (1, NULL), (7, NULL), (8, NULL), (0, TWO), (1, ODD), (2, ODD), (3, TWO), (4, TWO), (5, TWO), (6, TWO), (7, TWO), (8, ODD),
+                                                                   (9, ctypes.c_void_p(0x10004)), (10, ctypes.c_void_p(0x10004)), (11, FAKE), ((11, FAKE), (12, FAKE)), (14, FAKE)])
+    kept = args[:11] + [FAKE] * 4 + [NULL]
+    refused(call, edge_dims(form=px.PX_KEPT_I8), kept, [(11, NULL), (12, NULL), (13, NULL), (14, NULL), (11, EIGHT), (13, EIGHT)])
+    # what belongs to a part that there is none of
+    refused(call, edge_dims(flags=px.PX_EDGE_AFTER), args, [((k, FAKE),) + tuple((j, NULL) for j in (5, 6, 8, 9) if j != k) for k in (5, 6, 8, 9)])
+    refused(call, edge_dims(flags=px.PX_EDGE_BEFORE), args, [((k, FAKE),) + tuple((j, NULL) for j in (3, 4, 10) if j != k) for k in (3, 4, 10)])
+    alone = [FAKE] + [NULL] * 4 + [FAKE, FAKE, NULL, FAKE, FAKE] + [NULL] * 6
+    refused(call, edge_dims(flags=px.PX_EDGE_BEFORE), alone, [(2, FAKE), (7, FAKE), (10, FAKE), (-1, edge_dims()), ((-1, edge_dims(flags=0)), (5, NULL), (6, NULL), (8, NULL), (9, NULL))])
+
+
+def test_gradients_of_edges():
+    # y_grad, rows_grad, y, y_scales, branch, branch_scales, y_stats, branch_stats, gate, after_weight, after_bias, before_weight, workspace, bytes,
+    # x_grad, branch_grad, gate_grad, after_weight_grad, after_bias_grad, before_weight_grad, before_bias_grad, stream
+    call = px.lib().pollux_block_edge_grad
+    args = [FAKE, FAKE, FAKE, NULL, FAKE, NULL] + [FAKE] * 7 + [1 << 40] + [FAKE] * 7 + [NULL]
+    refused(call, edge_dims(), args, changed(edge_dims, BAD_EDGE) + [(1, NULL), (2, NULL), (3, FAKE), (4, NULL), (5, FAKE), (6, NULL), (7, NULL), (8, NULL), (0, TWO), (1, ODD), (2, TWO), (4, ODD),
+                                                                   (6, ctypes.c_void_p(0x10004)), (8, ODD), (9, TWO), (10, TWO), (11, TWO), (14, TWO), (15, ODD), (16, ODD), (17, TWO), (18, TWO),
+                                                                   (19, TWO), (20, TWO)])
+    refused(call, edge_dims(), args, [(12, NULL), (12, EIGHT), (13, 16)], px.PX_E_WORKSPACE)
+    refused(call, edge_dims(form=px.PX_KEPT_E4M3), args, [(0, FAKE), ((3, FAKE),), ((3, FAKE), (5, FAKE), (2, EIGHT)), ((3, FAKE), (5, FAKE), (4, EIGHT))])
+    refused(call, edge_dims(flags=px.PX_EDGE_BEFORE), args, [(0, FAKE)])
+    refused(call, edge_dims(flags=px.PX_EDGE_AFTER), args, [(0, FAKE)])
+
+
+def test_gated():
+    # gate, up, rows, gate_values, gate_scales, up_values, up_scales, stream
+    args = [FAKE, FAKE, FAKE] + [NULL] * 5
+    call = px.lib().pollux_gated
+    refused(call, gated_dims(), args, changed(gated_dims, BAD_GATED) + [(0, NULL), (2, NULL), (0, ODD), (1, ODD), (2, ODD)] + [(k, FAKE) for k in (3, 4, 5, 6)])
+    refused(call, gated_dims(form=px.PX_KEPT_I8), [FAKE] * 7 + [NULL], [(3, NULL), (4, NULL), (5, NULL), (6, NULL), (1, NULL), (3, EIGHT), (5, EIGHT)])
+    # rows_grad, gate, gate_scales, up, up_scales, gate_grad, up_grad, rows, stream
+    args = [FAKE, FAKE, NULL, FAKE, NULL, FAKE, FAKE, FAKE, NULL]
+    call = px.lib().pollux_gated_grad
+    refused(call, gated_dims(), args, changed(gated_dims, BAD_GATED) + [(0, NULL), (1, NULL), (2, FAKE), (3, NULL), (4, FAKE), (0, ODD), (1, ODD), (3, ODD), (5, ODD), (6, ODD), (7, ODD)])
+    refused(call, gated_dims(form=px.PX_KEPT_I8), [FAKE] * 8 + [NULL], [(2, NULL), (4, NULL), (1, EIGHT), (3, EIGHT)])
+
+
+# ---- in Python -----------------------------------------------------------------------------------------------------
+
+@pytest.fixture
+def on_the_host(monkeypatch):
+    """Tensors of the host pass the question which device they are on; a call that passes all checks stops before the library."""
+    class Reached(Exception):
+        pass
+
+    def stop(*args, **more):
+        raise Reached
+    monkeypatch.setattr(px, "_current_device", lambda: -1)
+    monkeypatch.setattr(px.blocks, "_planned", stop)
+    monkeypatch.setattr(px.blocks, "_dims", stop)
+    return Reached
+
+
+def new(*shape, dtype=torch.bfloat16):
+    return torch.ones(shape, dtype=dtype)
+
+
+def kept(N=6, D=40, form="i8"):
+    W = -(-D // 32) * 32
+    return px.Kept(torch.zeros((N, W), dtype=torch.uint8), torch.zeros((N, W // 32), dtype=torch.uint8), D, form)
+
+
+def state(N=6, D=40, form=None, branch=True, before=True, after=True):
+    stats = torch.ones((N, 2))
+    return px.blocks.EdgeState(stats if before else None, stats if after else None, kept(N, D, form) if form and before else None, kept(N, D, form) if form and after else None,
+                               torch.bfloat16, torch.bfloat16, branch)
+
+
+N_ = px.Norm
+GOOD = [lambda: px.keep(new(6, 40)), lambda: px.keep(new(2, 3, 40), "e4m3"), lambda: px.restore(kept()), lambda: px.kept_grad(kept(), new(6, 24)), lambda: px.kept_grad(kept(), new(2, 3, 24), new(40)),
+        lambda: px.block_edge(new(6, 40), before=N_()), lambda: px.block_edge(new(6, 40), new(6, 40)), lambda: px.block_edge(new(2, 3, 40), new(2, 3, 40), gate=new(2, 1, 40), after=N_(new(40)), keep="i8"),
+        lambda: px.block_edge(new(6, 40, dtype=torch.float32), new(6, 40), before=N_(new(40))),
+        lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(), y=new(6, 40), branch=new(6, 40), after=N_(), before=N_()),
+        lambda: px.block_edge_grad(None, new(6, 40), state(form="i8"), after=N_(), before=N_()),
+        lambda: px.gated(new(6, 40)), lambda: px.gated(new(6, 40), new(6, 40), "gelu", keep="i8"), lambda: px.gated_grad(new(6, 40), new(6, 40), new(6, 40)), lambda: px.gated_grad(new(6, 40), kept(), kept())]
+BAD = [lambda: px.keep(new(6, 40), "i4"), lambda: px.keep(new(6, 40), None), lambda: px.keep(new(6, 40).double()), lambda: px.keep(torch.ones((), dtype=torch.bfloat16)),
+       lambda: px.restore(kept()._replace(width=70)), lambda: px.restore(kept()._replace(form="x")), lambda: px.restore(kept()._replace(values=new(6, 64))), lambda: px.restore(kept()._replace(form=None)),
+       lambda: px.restore(kept(), torch.float64), lambda: px.restore(kept(), out=new(6, 41)), lambda: px.restore(kept(), out=new(40, 6).t()),
+       lambda: px.restore(kept()._replace(scales=torch.zeros((6, 3), dtype=torch.uint8))),
+       lambda: px.kept_grad(kept(), new(7, 24)), lambda: px.kept_grad(kept(), new(6, 24), new(41)), lambda: px.kept_grad(kept(), new(6, 24), new(40), new(40, dtype=torch.float32)),
+       lambda: px.kept_grad(kept(), new(6, 24), accumulate=True), lambda: px.kept_grad(kept(), new(6, 24), weight_grad=new(40, 24)), lambda: px.kept_grad(kept(), new(6, 24).int()),
+       lambda: px.block_edge(new(6, 40)), lambda: px.block_edge(new(6, 40), gate=new(40), before=N_()), lambda: px.block_edge(new(6, 40), after=N_(), before=N_()),
+       lambda: px.block_edge(new(6, 40), new(5, 40)), lambda: px.block_edge(new(6, 40), new(6, 40), gate=new(4, 40)), lambda: px.block_edge(new(6, 40), new(6, 40), gate=new(39)),
+       lambda: px.block_edge(new(6, 40), new(6, 40), gate=new(0, 40)), lambda: px.block_edge(new(6, 40), new(6, 40), after=N_(new(39))), lambda: px.block_edge(new(6, 40), before=N_(new(40), new(40).float())),
+       lambda: px.block_edge(new(6, 40), new(6, 40), rows_dtype=torch.float32), lambda: px.block_edge(new(6, 40), new(6, 40), keep="i7"), lambda: px.block_edge(new(6, 40).double(), before=N_()),
+       lambda: px.block_edge(new(6, 40), before=N_(new(40).int())),
+       lambda: px.block_edge_grad(None, None, state(before=False), after=N_()), lambda: px.block_edge_grad(new(6, 40), None, state(), after=N_(), before=N_()),
+       lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(), after=N_(), before=N_()), lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(form="i8"), after=N_()),
+       lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(form="i8"), before=N_()), lambda: px.block_edge_grad(new(6, 40), new(5, 40), state(form="i8"), after=N_(), before=N_()),
+       lambda: px.block_edge_grad(new(6, 40).float(), new(6, 40), state(form="i8"), after=N_(), before=N_()), lambda: px.block_edge_grad(new(7, 40), new(7, 40), state(form="i8"), after=N_(), before=N_()),
+       lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(form="i8"), after=N_(), before=N_(), need=("y",)),
+       lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(branch=False, after=False), y=new(6, 40), gate=new(40), before=N_()),
+       lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(), y=new(6, 40), branch=new(6, 39), after=N_(), before=N_()),
+       lambda: px.gated(new(6, 40), act="relu"), lambda: px.gated(new(6, 40), new(6, 41)), lambda: px.gated(new(6, 40), new(6, 40).half()), lambda: px.gated(new(6, 40), keep="x"),
+       lambda: px.gated_grad(new(6, 40), kept(), new(6, 40)), lambda: px.gated_grad(new(6, 40), new(6, 40), kept()), lambda: px.gated_grad(new(6, 40), kept(), kept(form="e4m3")),
+       lambda: px.gated_grad(new(6, 40), kept(N=5)), lambda: px.gated_grad(new(6, 40), new(6, 41)), lambda: px.gated_grad(new(6, 40), new(6, 40), new(6, 40), out=new(6, 79))]
+
+
+def test_what_is_taken(on_the_host):
+    for k, call in enumerate(GOOD):
+        with pytest.raises(on_the_host):
+            call()
+            pytest.fail(str(k))
+
+
+def test_what_is_refused(on_the_host):
+    for k, call in enumerate(BAD):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+            pytest.fail(str(k))
+
+
+def test_what_requires_grad_is_refused():
+    leaf = lambda *shape, dtype=torch.float32: torch.ones(shape, dtype=dtype, requires_grad=True)
+    x = torch.ones((6, 40))
+    for call in (lambda: px.keep(leaf(6, 40)), lambda: px.restore(kept(), out=leaf(6, 40)), lambda: px.kept_grad(kept(), leaf(6, 24)), lambda: px.kept_grad(kept(), x, leaf(40)),
+                 lambda: px.block_edge(leaf(6, 40), before=N_()), lambda: px.block_edge(x, before=N_(leaf(40))), lambda: px.block_edge(x, leaf(6, 40)), lambda: px.block_edge(x, x, gate=leaf(40)),
+                 lambda: px.block_edge_grad(leaf(6, 40), x, state(), after=N_(), before=N_()), lambda: px.gated(leaf(6, 40)), lambda: px.gated(x, leaf(6, 40)),
+                 lambda: px.gated_grad(leaf(6, 40), x), lambda: px.gated_grad(x, kept(), out=leaf(6, 40))):
+        with pytest.raises(ValueError, match="requires grad"):
+            call()
+
+
+def test_tensors_that_are_not_on_a_gpu_are_refused():
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is there")
+    for k, call in enumerate(GOOD):
+        with pytest.raises((RuntimeError, ValueError, AssertionError)):
+            call()
+            pytest.fail(str(k))
+
+
+def test_zeros_of_either_sign_have_descriptions_of_their_own(monkeypatch):
+    seen = []
+    dims = px.blocks._dims
+
+    class Reached(Exception):
+        pass
+
+    def watched(*args):
+        seen.append(dims(*args)._obj)
+        raise Reached
+    monkeypatch.setattr(px, "_current_device", lambda: -1)
+    monkeypatch.setattr(px.blocks, "_dims", watched)
+    for zero in (0.0, -0.0, 0.0):
+        with pytest.raises(Reached):
+            px.block_edge(new(6, 40), new(6, 40), residual=zero, scale=zero)
+        assert str(seen[-1].residual) == str(seen[-1].scale) == str(zero)

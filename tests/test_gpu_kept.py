@@ -1,0 +1,135 @@
+"""Rows kept in 8 bits: every code and scale is the definition's, exactly, and restored rows are what the bytes stand for, rounded once."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from kept import FORMS, LARGEST, decoded, encoded  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+TYPES = (torch.float32, torch.bfloat16, torch.float16)
+
+
+def rows(N, D, dtype, seed):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return (torch.randn((N, D), generator=g, device="cuda") * torch.exp(2 * torch.randn((N, D), generator=g, device="cuda"))).to(dtype)
+
+
+def check(x, form):
+    import paper_2008_12260_amd as px
+    kept = px.keep(x, form)
+    N, D = x.shape
+    codes, scale = encoded(x, form)
+    want = (codes * scale).flatten(1)
+    assert kept.values.shape == (N, -(-D // 32) * 32) and kept.scales.shape == (N, -(-D // 32)) and kept.width == D
+    got = decoded(kept.values, kept.scales, kept.values.shape[1], form)
+    assert torch.equal(got, want)
+    live = (codes != 0).any(2)
+    assert torch.equal(torch.exp2(kept.scales.cpu().double() - 127)[live], scale[:, :, 0][live])
+    for dtype in TYPES:
+        again = px.restore(kept, dtype)
+        assert torch.equal(again.cpu(), want[:, :D].float().to(dtype)) and again.dtype == dtype
+    return kept
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,D", [(1, 1), (3, 7), (2, 31), (5, 32), (4, 33), (7, 257), (300, 1000), (65, 4096)])
+def test_codes_and_scales(N, D, dtype, form):
+    check(rows(N, D, dtype, N + D), form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_the_borders_of_a_scale_and_ties(form):
+    """Groups whose largest element is next to where the scale changes, at many exponents, the smallest and the largest among them; other elements on and beside the middle between
+    two codes."""
+    tops = []
+    for e in (-126, -121, -120, -119, -118, -100, -1, 0, 1, 60, 126, 127):
+        for part in (1.0, 1.5, 1.75, 1.8125, 1.984375, 1.9921875, 1.9921874, 1.9921876, 1.7500001, 1.9999999):
+            tops.append(min(part * 2.0 ** e, 3.4028234e38))
+    tops = torch.tensor(tops, dtype=torch.float64).float()
+    x = torch.zeros((len(tops), 32))
+    x[:, 5] = tops
+    x[1::2, 5] *= -1
+    parts = torch.tensor([0.0, 0.5, 1.5, 2.5, 3.5, 17.5, 18.5, 0.4999, 0.5001, -0.5, -1.5, -62.5]) / 127.5
+    for k in range(12):
+        x[:, 10 + k] = tops * parts[k]
+    # whole and half codes of each row's own scale
+    scale = encoded(x, form)[1][:, 0, 0]
+    for k, q in enumerate((0.5, 1.5, 2.5, 8.5, 62.5, 17.0, 19.0, 21.0, 1.0625)):
+        x[:, 22 + k] = (q * scale).float()
+    check(x.cuda(), form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_zeros_and_tiny_rows(form):
+    x = torch.zeros((4, 64), device="cuda")
+    x[1, :32] = 2.0 ** -149
+    x[2] = 2.0 ** -127
+    x[3, 40] = -2.0 ** -126
+    check(x, form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_what_is_not_finite_takes_its_group_with_it(dtype, form):
+    import paper_2008_12260_amd as px
+    x = rows(6, 100, dtype, 3)
+    x[1, 40], x[2, 99], x[3, 0] = float("nan"), float("inf"), float("-inf")
+    kept = px.keep(x, form)
+    for out in TYPES:
+        got = px.restore(kept, out)
+        bad = torch.zeros((6, 100), dtype=torch.bool, device="cuda")
+        bad[1, 32:64] = bad[2, 96:] = bad[3, :32] = True
+        assert torch.equal(torch.isnan(got), bad)
+    x[1, 40] = x[2, 99] = x[3, 0] = 0.0
+    assert torch.equal(px.restore(px.keep(x, form))[~bad], px.restore(kept)[~bad])
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_strides_shapes_and_alignment(form):
+    import paper_2008_12260_amd as px
+    buffer = rows(20, 200, torch.bfloat16, 4)
+    for x in (buffer[:, 3:130], buffer[::3], buffer.t(), buffer[:, :1], buffer[2:2], buffer[:0], buffer[0, 1:41][None]):
+        check(x, form)
+    kept = px.keep(buffer.view(4, 5, 200), form)
+    flat = px.keep(buffer, form)
+    assert torch.equal(kept.values, flat.values) and torch.equal(kept.scales, flat.scales)
+    out = torch.full((20, 300), 7.0, device="cuda")
+    px.restore(flat, out=out[:, 50:250])
+    assert torch.equal(out[:, 50:250], px.restore(flat, torch.float32))
+    assert bool((out[:, :50] == 7).all()) and bool((out[:, 250:] == 7).all())
+
+
+def test_codes_of_every_byte_are_restored():
+    import paper_2008_12260_amd as px
+    values = torch.arange(256, dtype=torch.uint8, device="cuda").view(1, 256).repeat(256, 1)
+    scales = torch.arange(256, dtype=torch.uint8, device="cuda")[:, None].repeat(1, 8)
+    for form in FORMS:
+        want = decoded(values, scales, 256, form).float()
+        got = px.restore(px.Kept(values, scales, 256, form), torch.float32).cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(0.0, 1e39, -1e39), want.nan_to_num(0.0, 1e39, -1e39))
+        assert float(want[127].nan_to_num(0.0).abs().max()) == (128.0 if form == "i8" else LARGEST[form])
+
+
+def test_other_streams_and_graphs():
+    import paper_2008_12260_amd as px
+    x = rows(500, 300, torch.bfloat16, 5)
+    want = px.keep(x)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = px.keep(x, stream=side)
+    back = px.restore(got, stream=side)
+    side.synchronize()
+    assert torch.equal(got.values, want.values) and torch.equal(back, px.restore(want))
+    live = torch.zeros_like(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = px.keep(live, "e4m3")
+        out = px.restore(kept)
+    for k in range(3):
+        live.copy_(rows(500, 300, torch.bfloat16, 6 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, px.restore(px.keep(live, "e4m3")))
