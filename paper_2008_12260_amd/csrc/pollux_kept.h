@@ -31,7 +31,8 @@ constexpr int kXor1 = 0xB1, kXor2 = 0x4E;             // quad_perm [1,0,3,2] and
 
 __device__ __forceinline__ float kept_scale(uint32_t byte)
 {
-    return __uint_as_float(byte == 255 ? 0x7fc00000u : byte ? byte << 23 : 0x00400000u);
+    // (2^-127 is below the normal numbers; a NaN for 255)
+    return __uint_as_float(max(byte << 23, 0x00400000u) | (byte + 1 & 256u) << 14);
 }
 
 // The scale's byte from the bits of the group's largest size: one more than its exponent says where the fraction is from 127/128 on, or over 3/4 (round(127.5) is 128;
@@ -74,7 +75,7 @@ __device__ __forceinline__ f32x8 decode8(int form, u32x2 codes, float scale)
     f32x8 v;
     if (form == PX_KEPT_I8) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = (float)(int8_t)(codes[i >> 2] >> 8 * (i & 3)) * scale;
+        for (int i = 0; i < kVec; ++i) v[i] = (float)((int)(codes[i >> 2] << (24 - 8 * (i & 3))) >> 24) * scale;
     } else {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {

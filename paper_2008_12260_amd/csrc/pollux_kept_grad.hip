@@ -56,7 +56,7 @@ __global__ __launch_bounds__(S::kThreads) void kept_tiles(const KeptGradArgs A)
     o.a += row * o.lda;
     o.scales += row * (o.lda / kKeptGroup);
     o.b += row * o.ldb;
-    o.k = (int)max((int64_t)0, min(A.slice, A.N - row));
+    o.k = __builtin_amdgcn_readfirstlane((int)max((int64_t)0, min(A.slice, A.N - row)));
     f32x4 acc[S::FM][S::FN];
     tile_product<S>(o, t, lds, acc);
     const Place<S> at(t);

@@ -340,13 +340,18 @@ struct KeptSide {
     static constexpr int kCodes = B_ * kDepth / THREADS, kWide = kCodes < 16 ? kCodes : 16, kParts = kCodes / kWide, kAcross = B_ / kWide;
     static constexpr int kLoads = 2 * kParts;                     // codes, and their scale
     static_assert(kParts * kWide * THREADS == B_ * kDepth && kWide >= 8 && kAcross * kWide == B_, "whole loads");
+    static_assert(kParts == 1 || THREADS / kAcross % 16 == 0, "parts' rows are permuted alike");
+    static constexpr int kDown = THREADS / kAcross;               // rows between a thread's parts
     const char *base;
     const uint8_t *scale_base;
     int64_t ld;
     int k, stages, width;
     Columns columns;                    // (for its reads)
-    int at[kParts], scale_at[kParts], to[kParts], turn[kParts];
-    uint32_t codes[kParts][kWide / 4], bytes[kParts];
+    int at, scale_at, to, turn;         // of the first part: in memory, in LDS; the first of its pieces (the others' last bits differ)
+    struct Codes {
+        uint32_t words[kParts][kWide / 4];
+        uint8_t bytes[kParts];
+    } codes;
 
     __device__ __forceinline__ KeptSide(const Operands &o, int first, int mine) : columns(o.a, o.lda, 0, 0, 0, mine)
     {
@@ -356,35 +361,33 @@ struct KeptSide {
         base = o.a + first;
         scale_base = o.scales + first / kKeptGroup;
         width = min((int)ld - first, B_);
-#pragma unroll
-        for (int i = 0; i < kParts; ++i) {
-            const int unit = i * THREADS + threadIdx.x, row = unit / kAcross, c = unit % kAcross * kWide;
-            at[i] = c < width ? row * (int)ld + c : (int)0x80000000;
-            scale_at[i] = c < width ? row * (int)(ld / kKeptGroup) + c / kKeptGroup : (int)0x80000000;
-            to[i] = row * kLine;
-            turn[i] = (c * kSize / 16) ^ Columns::f(row);         // (of the first of its pieces; the others' last bits differ)
-        }
+        const int row = threadIdx.x / kAcross, c = threadIdx.x % kAcross * kWide;
+        at = c < width ? row * (int)ld + c : (int)0x80000000;
+        scale_at = c < width ? row * (int)(ld / kKeptGroup) + c / kKeptGroup : (int)0x80000000;
+        to = row * kLine;
+        turn = (c * kSize / 16) ^ Columns::f(row);
         fetch(0);
     }
 
     __device__ __forceinline__ void fetch(int stage)
     {
-        const int rows = min(k - stage * kDepth, kDepth);
-        const int64_t row = (int64_t)min(stage, max(stages - 1, 0)) * kDepth;
-        const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void *)(base + row * ld), 0, rows > 0 ? (int)((rows - 1) * ld) + width : 0, 0x00027000);
-        const auto scales = __builtin_amdgcn_make_buffer_rsrc((void *)(scale_base + row * (ld / kKeptGroup)), 0, rows > 0 ? (int)((rows - 1) * (ld / kKeptGroup)) + width / kKeptGroup : 0, 0x00027000);
+        // (of no rows, buffers of no bytes)
+        const int rows = __builtin_amdgcn_readfirstlane(max(min(k - stage * kDepth, kDepth), 0)), ld_scales = (int)(ld / kKeptGroup);
+        const int64_t row = (int64_t)min(stage, stages) * kDepth;
+        const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void *)(base + row * ld), 0, __builtin_amdgcn_readfirstlane(max(rows * (int)ld - ((int)ld - width), 0)), 0x00027000);
+        const auto scales = __builtin_amdgcn_make_buffer_rsrc((void *)(scale_base + row * ld_scales), 0, __builtin_amdgcn_readfirstlane(max(rows * ld_scales - (ld_scales - width / kKeptGroup), 0)), 0x00027000);
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
             if constexpr (kWide == 16) {
-                const auto v = __builtin_amdgcn_raw_buffer_load_b128(buffer, at[i], 0, 0);
+                const auto v = __builtin_amdgcn_raw_buffer_load_b128(buffer, at + i * kDown * (int)ld, 0, 0);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) codes[i][q] = v[q];
+                for (int q = 0; q < 4; ++q) codes.words[i][q] = v[q];
             } else {
-                const auto v = __builtin_amdgcn_raw_buffer_load_b64(buffer, at[i], 0, 0);
-                codes[i][0] = v[0];
-                codes[i][1] = v[1];
+                const auto v = __builtin_amdgcn_raw_buffer_load_b64(buffer, at + i * kDown * (int)ld, 0, 0);
+                codes.words[i][0] = v[0];
+                codes.words[i][1] = v[1];
             }
-            bytes[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(scales, scale_at[i], 0, 0);
+            codes.bytes[i] = __builtin_amdgcn_raw_buffer_load_b8(scales, scale_at + i * kDown * ld_scales, 0, 0);
         }
     }
 
@@ -414,21 +417,27 @@ struct KeptSide {
         }
     }
 
-    // What has been fetched, which is the stage's, into LDS; the next stage is fetched.
-    __device__ __forceinline__ void load(int stage, lds_char *into)
+    // Codes into LDS.
+    __device__ __forceinline__ void put(const Codes &from, lds_char *into) const
     {
         typedef __attribute__((address_space(3))) piece lds_piece;
         constexpr int kWords = kSize == 4 ? 1 : 2, kPieces = kWide / (4 * kWords);
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
-            const bool none = bytes[i] == 255;
-            const float scale = FORM == PX_KEPT_E4M3 && none ? 1.f : kept_scale(bytes[i]);
+            const bool none = FORM == PX_KEPT_E4M3 && from.bytes[i] == 255;
+            const float scale = kept_scale(from.bytes[i]);
             uint32_t words[kWide / 4];
 #pragma unroll
-            for (int q = 0; q < kWide / 4; ++q) words[q] = FORM == PX_KEPT_E4M3 && none ? 0x7f7f7f7fu : codes[i][q];          // (NaN)
+            for (int q = 0; q < kWide / 4; ++q) words[q] = none ? 0x7f7f7f7fu : from.words[i][q];          // (NaN)
 #pragma unroll
-            for (int q = 0; q < kPieces; ++q) *(lds_piece *)(into + to[i] + (turn[i] ^ q) * 16) = turned(words + q * kWords, scale);
+            for (int q = 0; q < kPieces; ++q) *(lds_piece *)(into + to + i * kDown * kLine + (turn ^ q) * 16) = turned(words + q * kWords, scale);
         }
+    }
+
+    // What has been fetched, which is the stage's, into LDS; the next stage is fetched.
+    __device__ __forceinline__ void load(int stage, lds_char *into)
+    {
+        put(codes, into);
         fetch(stage + 1);
     }
 
@@ -491,6 +500,7 @@ __device__ __forceinline__ void form_tile(const Operands &o, Tile t, char *lds_,
     // halves, when the whole stage has been read: the loads of the stage kStages later go where it was.
     constexpr int kReads = SideA::kReads + SideB::kReads, kProducts = S::FM * S::FN * (SideA::kSize == 4 ? 4 : 1);
     constexpr int kPerRead = kProducts / (kReads + 4) > 0 ? kProducts / (kReads + 4) : 1, kPerLoad = kPerRead;
+    constexpr int kTurnPer = 3;
     constexpr int kValu = 0x002, kMatrix = 0x008, kVector = 0x010, kLds = 0x100;         // the scheduler's groups of instructions
     piece a0[S::FM], b0[S::FN], a1[S::FM], b1[S::FN];
     typedef std::integral_constant<int, kAhead> some;
@@ -544,19 +554,34 @@ __device__ __forceinline__ void form_tile(const Operands &o, Tile t, char *lds_,
         }
         __builtin_amdgcn_sched_group_barrier(kMatrix, kProducts, 0);
         wait(some());
-        load(s + S::kStages, at);
-        at = at + 1 == S::kStages ? 0 : at + 1;
-        read(at, 0, a0, b0);
+        if constexpr (kKept) {
+            // (LDS is read before it is written: the codes are turned among the products)
+            lds_char *const to = lds + at * S::kStage;
+            side_b.load(s + S::kStages, to + kBytesA);
+            const auto codes = side_a.codes;
+            side_a.fetch(s + S::kStages + 1);
+            at ^= 1;
+            read(at, 0, a0, b0);
+            side_a.put(codes, to);
+        } else {
+            load(s + S::kStages, at);
+            at = at + 1 == S::kStages ? 0 : at + 1;
+            read(at, 0, a0, b0);
+        }
         multiply_all(a1, b1);
+        // (what turns kept codes, between the products too)
+        constexpr int kTurn = kKept ? kTurnPer : 0;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             __builtin_amdgcn_sched_group_barrier(kVector, 1, 1);
             __builtin_amdgcn_sched_group_barrier(kMatrix, kPerLoad, 1);
+            if constexpr (kKept) __builtin_amdgcn_sched_group_barrier(kValu, kTurn, 1);
         }
 #pragma unroll
         for (int i = 0; i < kReads; ++i) {
             __builtin_amdgcn_sched_group_barrier(kLds, 1, 1);
             __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 1);
+            if constexpr (kKept) __builtin_amdgcn_sched_group_barrier(kValu, kTurn, 1);
         }
         __builtin_amdgcn_sched_group_barrier(kMatrix, kProducts, 1);
     }
