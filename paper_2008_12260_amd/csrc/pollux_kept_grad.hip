@@ -141,33 +141,24 @@ __global__ __launch_bounds__(kThreads) void join_slices(const KeptGradArgs A, co
 #endif
 }
 
-// Rows copied to aligned ones, padded with zeros.
-template <class E>
-__global__ __launch_bounds__(kThreads) void pad_rows(const E *from, int64_t ld_from, int64_t rows, int cols, E *to, int64_t ld_to)
+// Sums of rows_grad over the rows: of a part of them, eight columns a thread, by `down` threads that each take every down-th row; then of the parts in order.  to: the rows are copied there
+// on the way, padded with zeros to ld_to.
+template <class E, bool SUMS>
+__global__ __launch_bounds__(kThreads) void sum_rows(const E *rows, int64_t ld, int64_t N, int M, int across, float *parts, E *to, int64_t ld_to)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    const int groups = (int)((ld_to + kVec - 1) / kVec);
-    const int64_t total = rows * groups;
-    for (int64_t at = blockIdx.x * (int64_t)kThreads + threadIdx.x; at < total; at += gridDim.x * (int64_t)kThreads) {
-        const int64_t n = at / groups;
-        const int c = (int)(at - n * groups) * kVec;
-        store8(to + n * ld_to + c, ld_to - c, load8(from + n * ld_from + c, cols - c));
-    }
-#endif
-}
-
-// Sums of rows_grad over the rows: of a part of them, eight columns a thread, by `down` threads that each take every down-th row; then of the parts in order.
-template <class E>
-__global__ __launch_bounds__(kThreads) void sum_rows(const E *rows, int64_t ld, int64_t N, int M, int across, float *parts)
-{
-#ifdef __HIP_DEVICE_COMPILE__
-    __shared__ float shared[kThreads][kVec + 1];
+    __shared__ float shared[SUMS ? kThreads : 1][kVec + 1];
     const int down = kThreads / across, mine = threadIdx.x % across, from = threadIdx.x / across;
     const int c = (blockIdx.x * across + mine) * kVec, left = M - c;
     const int64_t each = (N + gridDim.y - 1) / gridDim.y, first = blockIdx.y * each, last = min(first + each, N);
     f32x8 v = {};
 #pragma unroll 4
-    for (int64_t n = first + from; n < last; n += down) v += load8f(rows + n * ld + c, left);
+    for (int64_t n = first + from; n < last; n += down) {
+        const auto row = load8(rows + n * ld + c, left);
+        if (to) store8(to + n * ld_to + c, ld_to - c, row);
+        if (SUMS) v += __builtin_convertvector(row, f32x8);
+    }
+    if (!SUMS) return;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) shared[threadIdx.x][i] = v[i];
     __syncthreads();
@@ -183,7 +174,7 @@ __global__ __launch_bounds__(kThreads) void sum_parts(const float *parts, int co
     const int m = blockIdx.x * kThreads + threadIdx.x;
     if (m >= M) return;
     float v = 0.f;
-#pragma unroll 8
+#pragma unroll 16
     for (int k = 0; k < count; ++k) v += parts[(int64_t)k * M + m];
     sums[m] = v;
 }
@@ -226,19 +217,20 @@ int kept_grad(const pollux_kept_grad_dims &d, const KeptGradPlan &p, const uint8
     a.slice = p.slice;
     a.slices = p.slices;
     a.ld = d.weight_grad_stride;
-    if (bias) {
-        int across = 1;
-        while (across < kThreads && across * kVec < d.M) across *= 2;
-        const int columns = (d.M + across * kVec - 1) / (across * kVec);
-        hipLaunchKernelGGL(sum_rows<type>, dim3((unsigned)columns, (unsigned)p.sum_blocks), dim3(kThreads), 0, stream, (const type *)rows_grad, d.rows_grad_stride, d.N, d.M, across,
-                           (float *)(ws + p.parts));
-        hipLaunchKernelGGL(sum_parts, dim3((unsigned)((d.M + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, (const float *)(ws + p.parts), p.sum_blocks, d.M, (float *)(ws + p.sums));
-    }
     int64_t ld = d.rows_grad_stride;
-    if (p.pack && d.N > 0) {
-        hipLaunchKernelGGL(pad_rows<type>, dim3(blocks_for(d.N * ((p.m_pad + kVec - 1) / kVec))), dim3(kThreads), 0, stream, (const type *)rows_grad, ld, d.N, d.M, (type *)(ws + p.rows), p.m_pad);
-        rows_grad = ws + p.rows;
-        ld = p.m_pad;
+    if (bias || (p.pack && d.N > 0)) {
+        // (32 threads across: 512 bytes a row, and eight rows under way a workgroup)
+        int across = 1;
+        while (across < 32 && across * kVec < d.M) across *= 2;
+        const dim3 grid((unsigned)((d.M + across * kVec - 1) / (across * kVec)), (unsigned)p.sum_blocks);
+        type *const to = p.pack ? (type *)(ws + p.rows) : nullptr;
+        auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, (const type *)rows_grad, ld, d.N, d.M, across, (float *)(ws + p.parts), to, p.m_pad); };
+        bias ? launch(sum_rows<type, true>) : launch(sum_rows<type, false>);
+        if (bias) hipLaunchKernelGGL(sum_parts, dim3((unsigned)((d.M + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, (const float *)(ws + p.parts), p.sum_blocks, d.M, (float *)(ws + p.sums));
+        if (to) {
+            rows_grad = ws + p.rows;
+            ld = p.m_pad;
+        }
     }
     const int64_t width = kept_width(d.D);
     a.o = {(const char *)values, rows_grad, width, ld * e, d.D, d.M, 0, scales};
@@ -254,6 +246,10 @@ int kept_grad(const pollux_kept_grad_dims &d, const KeptGradPlan &p, const uint8
 
 }  // namespace
 
+// What shapes of tile take (pollux_tiles.h) where one operand's codes are turned on their way to LDS: i8 in 16-bit products of 300 to 65536 rows x 128 to 4096 x 128 to 4096 and in fp32, within some 15 %:
+// 8192 x 2048 x 2048 in one slice 220, 130, 158 us, in four 88, 117, 162; 65536 x 128 x 128 in 32 slices 67, 43, 33; fp32 4096 x 2048 x 4096 253 and 557.
+constexpr ShapeOf kKeptShape[3] = {{256, 256, 1, 1.64, 1.64, 0.00, 0.00, 8.7}, {128, 128, 2, 0.93, 1.38, 1.27, 1.93, 6.0}, {64, 64, 4, 0.62, 1.20, 0.75, 2.14, 4.5}};
+
 KeptGradPlan kept_grad_plan(const pollux_kept_grad_dims &d)
 {
     KeptGradPlan p = {};
@@ -262,18 +258,18 @@ KeptGradPlan kept_grad_plan(const pollux_kept_grad_dims &d)
     p.m_pad = ((int64_t)d.M + pad - 1) / pad * pad;
     p.pack = d.rows_grad_stride % pad != 0 || d.M % pad != 0;
     const int64_t stages = std::max<int64_t>(1, (d.N + depth - 1) / depth);
-    // in as many slices of the rows as takes least, their sums being written and read at some 4 and 3 TB/s
+    // in as many slices of the rows as takes least, their sums being written and read at some 8 TB/s each, out of the caches
     double least = 1e300;
-    for (int slices = 1; slices <= 64; slices *= 2) {
+    for (int slices = 1; slices <= 128; slices += slices < 8 ? 1 : slices / 4) {
         if (slices > 1 && (stages < 4 * slices || (int64_t)slices * d.M * d.D * 4 > (512ll << 20))) break;
         for (int s = f32 ? 1 : 0; s < 3; ++s) {
-            double cost = shape_cost(kShape[s], d.D, d.M, (double)d.N / slices, slices, f32);
-            if (slices > 1) cost += 4.0 + 4.0 * slices * d.M * d.D * (1 / 4e6 + 1 / 3e6);
+            double cost = shape_cost(kKeptShape[s], d.D, d.M, (double)d.N / slices, slices, f32);
+            if (slices > 1) cost += 4.0 + 4.0 * slices * d.M * d.D / 4.2e6;
             if (cost < least) least = cost, p.slices = slices, p.tiles = s;
         }
     }
     p.slice = (stages + p.slices - 1) / p.slices * depth;
-    p.sum_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(64, d.N / 64));
+    p.sum_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(64, d.N / 32));
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };
     p.parts = take((size_t)p.sum_blocks * d.M * 4);
