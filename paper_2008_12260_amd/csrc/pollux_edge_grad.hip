@@ -20,7 +20,50 @@ namespace {
 
 enum Part { kBeforeWeight, kBeforeBias, kAfterWeight, kAfterBias, kParts };
 
-template <class X, class E, int C, int R, bool BRANCH, bool SPANS>
+#ifdef __HIP_DEVICE_COMPILE__
+// Eight elements as they came from memory: of rows (T), or codes and their scale's byte.
+template <class T>
+struct Loaded {
+    static constexpr int kWords = sizeof(T) * 2;
+    uint32_t words[kWords];
+    __device__ __forceinline__ void rows(const T *from, int left)
+    {
+        typedef uint32_t whole __attribute__((ext_vector_type(kWords)));
+        const whole v = __builtin_bit_cast(whole, load8(from, left));
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) words[i] = v[i];
+    }
+    __device__ __forceinline__ void kept(const uint8_t *values, const uint8_t *scales, int64_t at)
+    {
+        const u32x2 codes = *(const u32x2 *)(values + at);
+        words[0] = codes[0];
+        words[1] = codes[1];
+        words[2] = scales[at / kKeptGroup];
+    }
+    __device__ __forceinline__ f32x8 of_rows() const
+    {
+        typedef uint32_t whole __attribute__((ext_vector_type(kWords)));
+        whole v;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) v[i] = words[i];
+        return __builtin_convertvector(__builtin_bit_cast(typename Eight<T>::type, v), f32x8);
+    }
+    // The normalised rows: kept, or formed again.
+    __device__ __forceinline__ f32x8 normalised(int form, float2 stats) const
+    {
+        return form ? decode8(form, u32x2{words[0], words[1]}, kept_scale(words[2])) : (of_rows() - stats.x) * stats.y;
+    }
+};
+__device__ __forceinline__ f32x8 fma8(f32x8 a, f32x8 b, f32x8 c)
+{
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) c[i] = fmaf(a[i], b[i], c[i]);
+    return c;
+}
+#endif
+
+// PLAIN: sums of gradients themselves are wanted too (for biases), not only of their products with normalised rows.
+template <class X, class E, int C, int R, bool BRANCH, bool SPANS, bool PLAIN>
 __global__ __launch_bounds__(1024) void edge_grads(const EdgeKernelArgs A)
 {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -31,15 +74,19 @@ __global__ __launch_bounds__(1024) void edge_grads(const EdgeKernelArgs A)
     const int64_t width = kept_width(D);
     const float over = 1.f / D;
     int parity = 0, c[C], left[C];
-    f32x8 w_a[C], w_b[C], gate[C], sum_pn[C], sum_p[C], sum_tn[C], sum_t[C], span_gn[C], span_g[C];
+    // by: what g is multiplied with on its way to the branch's norm, 0 beyond the row's end; so is rows_grad, which is what keeps both out of the rows' sums
+    // (read again for every row where they would not fit beside the sums)
+    constexpr bool kReload = C > 1;
+    f32x8 w_b[C], by[C], sum_pn[C], sum_p[C], sum_tn[C], sum_t[C], span_gn[C], span_g[C];
     const f32x8 zeros = {};
+    auto gate_of = [&](int k, int64_t row) { return parameters(A.p.gate, d.gate_type, row * D + c[k], left[k], 1.f) * d.scale; };
+    auto after_weight = [&](int k) { return within(parameters(after ? A.p.after_weight : nullptr, d.weight_type, c[k], left[k], 1.f), left[k]); };
 #pragma unroll
     for (int k = 0; k < C; ++k) {
         c[k] = (k * team + mine) * kVec;
         left[k] = D - c[k];
-        w_a[k] = parameters(after ? A.p.after_weight : nullptr, d.weight_type, c[k], left[k], 1.f);
-        w_b[k] = parameters(A.p.before_weight, d.weight_type, c[k], left[k], 1.f);
-        gate[k] = parameters(SPANS ? nullptr : A.p.gate, d.gate_type, c[k], left[k], 1.f) * d.scale;
+        if (!kReload) w_b[k] = parameters(A.p.before_weight, d.weight_type, c[k], left[k], 1.f);
+        if (!kReload && BRANCH && !SPANS) by[k] = gate_of(k, 0) * after_weight(k);
         sum_pn[k] = sum_p[k] = sum_tn[k] = sum_t[k] = span_gn[k] = span_g[k] = zeros;
     }
     const int N = (int)d.N, chunk = blockIdx.x * teams + first;
@@ -55,116 +102,108 @@ __global__ __launch_bounds__(1024) void edge_grads(const EdgeKernelArgs A)
             if (row0 == begin || at != span) {
                 span = at;
 #pragma unroll
-                for (int k = 0; k < C; ++k) gate[k] = parameters(A.p.gate, d.gate_type, (int64_t)span * D + c[k], left[k], 1.f) * d.scale;
+                for (int k = 0; k < C; ++k)
+                    if (!kReload) by[k] = gate_of(k, span) * after_weight(k);
             }
         }
         int64_t row[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) row[r] = row0 + min(r, count - 1);
-        f32x8 g[R][C], n_y[R][C], p[R][C], n_z[R][C];
+        Loaded<X> dy[R][C], y[R][C];
+        Loaded<E> dh[R][C], z[R][C];
         float2 stats_y[R], stats_z[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+            row[r] = row0 + min(r, count - 1);
             if (before) stats_y[r] = ((const float2 *)A.p.y_stats)[row[r]];
             if (BRANCH && after) stats_z[r] = ((const float2 *)A.p.branch_stats)[row[r]];
+            else stats_z[r] = make_float2(0.f, 1.f);
 #pragma unroll
             for (int k = 0; k < C; ++k) {
-                const int64_t kept = min(row[r] * width + c[k], row[r] * width + width - kVec);
-                g[r][k] = A.p.y_grad ? load8f((const X *)A.p.y_grad + row[r] * d.y_grad_stride + c[k], left[k]) : zeros;
+                const int64_t kept = row[r] * width + min((int64_t)c[k], width - kVec);
                 if (before) {
-                    p[r][k] = load8f((const E *)A.p.rows_grad + row[r] * d.rows_grad_stride + c[k], left[k]);
-                    if (d.form) n_y[r][k] = decode8(d.form, *(const u32x2 *)(A.p.y_values + kept), kept_scale(A.p.y_scales[kept / kKeptGroup]));
-                    else n_y[r][k] = load8f((const X *)A.p.y + row[r] * d.y_stride + c[k], left[k]);
+                    dh[r][k].rows((const E *)A.p.rows_grad + row[r] * d.rows_grad_stride + c[k], left[k]);
+                    if (d.form) y[r][k].kept(A.p.y_values, A.p.y_scales, kept);
+                    else y[r][k].rows((const X *)A.p.y + row[r] * d.y_stride + c[k], left[k]);
                 }
-                if (BRANCH) {
-                    if (!has_z) n_z[r][k] = zeros;
-                    else if (d.form) n_z[r][k] = decode8(d.form, *(const u32x2 *)(A.p.branch_values + kept), kept_scale(A.p.branch_scales[kept / kKeptGroup]));
-                    else n_z[r][k] = load8f((const E *)A.p.branch + row[r] * d.branch_stride + c[k], left[k]);
+                if (A.p.y_grad) dy[r][k].rows((const X *)A.p.y_grad + row[r] * d.y_grad_stride + c[k], left[k]);
+                if (BRANCH && has_z) {
+                    if (d.form) z[r][k].kept(A.p.branch_values, A.p.branch_scales, kept);
+                    else z[r][k].rows((const E *)A.p.branch + row[r] * d.branch_stride + c[k], left[k]);
                 }
             }
         }
-        if (!d.form)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int k = 0; k < C; ++k) {
-                    if (before) n_y[r][k] = (n_y[r][k] - stats_y[r].x) * stats_y[r].y;
-                    if (BRANCH && after) n_z[r][k] = (n_z[r][k] - stats_z[r].x) * stats_z[r].y;
-                }
+        f32x8 g[R][C], n[R][C];
         // v - [mean v] - n mean(v n), times r: the gradient through a norm
-        auto through = [&](f32x8(&v)[R][C], const f32x8(&n)[R][C], const float2(&stats)[R]) {
-            float along[R], mean[R];
+        auto through = [&](const float2(&stats)[R]) {
+            float sums[2 * R];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                along[r] = mean[r] = 0.f;
+                sums[r] = sums[R + r] = 0.f;
 #pragma unroll
                 for (int k = 0; k < C; ++k)
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) {
-                        const bool in = !A.ragged || i < left[k];
-                        along[r] = fmaf(in ? v[r][k][i] : 0.f, in ? n[r][k][i] : 0.f, along[r]);
-                        mean[r] += in ? v[r][k][i] : 0.f;
-                    }
+                    for (int i = 0; i < kVec; ++i) sums[r] = fmaf(g[r][k][i], n[r][k][i], sums[r]);
             }
-            over_team(along, team, shared, parity);
-            if (centred) over_team(mean, team, shared, parity);
+            if (centred) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int k = 0; k < C; ++k) sums[R + r] += sum8(g[r][k]);
+                over_team(sums, team, shared, parity);
+            } else {
+                float along[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) along[r] = sums[r];
+                over_team(along, team, shared, parity);
+#pragma unroll
+                for (int r = 0; r < R; ++r) sums[r] = along[r];
+            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float a = along[r] * over, m = centred ? mean[r] * over : 0.f;
+                const float a = -sums[r] * over, m = sums[R + r] * over;
 #pragma unroll
                 for (int k = 0; k < C; ++k)
 #pragma unroll
-                    for (int i = 0; i < kVec; ++i) v[r][k][i] = (fmaf(-a, n[r][k][i], v[r][k][i]) - m) * stats[r].y;
+                    for (int i = 0; i < kVec; ++i) g[r][k][i] = (fmaf(a, n[r][k][i], g[r][k][i]) - m) * stats[r].y;
             }
         };
         if (before) {
-            if (before_sums)
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-                    if (r < count)
-#pragma unroll
-                        for (int k = 0; k < C; ++k) {
-#pragma unroll
-                            for (int i = 0; i < kVec; ++i) sum_pn[k][i] = fmaf(p[r][k][i], n_y[r][k][i], sum_pn[k][i]);
-                            sum_p[k] += p[r][k];
-                        }
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int k = 0; k < C; ++k) p[r][k] *= w_b[k];
-            through(p, n_y, stats_y);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int k = 0; k < C; ++k) g[r][k] += p[r][k];
-        }
-        if (A.p.x_grad)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (r < count)
-#pragma unroll
-                    for (int k = 0; k < C; ++k) store8f((X *)A.p.x_grad + row[r] * d.x_grad_stride + c[k], left[k], g[r][k] * d.residual);
-        if (!BRANCH) continue;
-        if (after_sums)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (r < count)
-#pragma unroll
-                    for (int k = 0; k < C; ++k) {
-                        f32x8 &to = SPANS ? span_gn[k] : sum_tn[k];
-#pragma unroll
-                        for (int i = 0; i < kVec; ++i) to[i] = fmaf(g[r][k][i], n_z[r][k][i], to[i]);
-                        (SPANS ? span_g[k] : sum_t[k]) += g[r][k];
-                    }
-        if (A.p.branch_grad) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int k = 0; k < C; ++k) {
-                    g[r][k] *= gate[k];
-                    if (after) g[r][k] *= w_a[k];
+                    g[r][k] = dh[r][k].of_rows();
+                    n[r][k] = y[r][k].normalised(d.form, stats_y[r]);
+                    if (before_sums && r < count) {
+                        sum_pn[k] = fma8(g[r][k], n[r][k], sum_pn[k]);
+                        if (PLAIN) sum_p[k] += g[r][k];
+                    }
+                    g[r][k] *= kReload ? parameters(A.p.before_weight, d.weight_type, c[k], left[k], 1.f) : w_b[k];
                 }
-            if (after) through(g, n_z, stats_z);
+            through(stats_y);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                if (!before) g[r][k] = zeros;
+                if (A.p.y_grad) g[r][k] += dy[r][k].of_rows();
+                if (A.p.x_grad && r < count) store8f((X *)A.p.x_grad + row[r] * d.x_grad_stride + c[k], left[k], g[r][k] * d.residual);
+            }
+        if (!BRANCH) continue;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                n[r][k] = has_z ? z[r][k].normalised(d.form, stats_z[r]) : zeros;
+                if (after_sums && r < count) {
+                    f32x8 &to = SPANS ? span_gn[k] : sum_tn[k];
+                    to = fma8(g[r][k], n[r][k], to);
+                    if (PLAIN) (SPANS ? span_g[k] : sum_t[k]) += g[r][k];
+                }
+                g[r][k] *= kReload ? gate_of(k, SPANS ? span : 0) * after_weight(k) : by[k];
+            }
+        if (A.p.branch_grad) {
+            if (after) through(stats_z);
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 if (r < count)
@@ -177,20 +216,15 @@ __global__ __launch_bounds__(1024) void edge_grads(const EdgeKernelArgs A)
 #pragma unroll
             for (int k = 0; k < C; ++k) {
                 if (A.p.gate_grad) {
-                    f32x8 v = span_gn[k];
-                    if (after) {
-                        v *= w_a[k];
-                        if (A.p.after_bias) v += span_g[k] * parameters(A.p.after_bias, d.weight_type, c[k], left[k], 0.f);
-                    }
+                    f32x8 v = span_gn[k] * after_weight(k);
+                    if (PLAIN && A.p.after_bias) v = fma8(span_g[k], parameters(A.p.after_bias, d.weight_type, c[k], left[k], 0.f), v);
                     v *= d.scale;
                     if (from >= begin && min(to, (int64_t)N) <= end) store_parameters(A.p.gate_grad, d.gate_type, (int64_t)span * D + c[k], left[k], v);
                     else store8f(A.ends + ((int64_t)chunk * 2 + (from >= begin ? 1 : 0)) * D + c[k], left[k], v);
                 }
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    sum_tn[k][i] = fmaf(gate[k][i], span_gn[k][i], sum_tn[k][i]);
-                    sum_t[k][i] = fmaf(gate[k][i], span_g[k][i], sum_t[k][i]);
-                }
+                const f32x8 gate = gate_of(k, span);
+                sum_tn[k] = fma8(gate, span_gn[k], sum_tn[k]);
+                if (PLAIN) sum_t[k] = fma8(gate, span_g[k], sum_t[k]);
                 span_gn[k] = span_g[k] = zeros;
             }
         }
@@ -212,10 +246,10 @@ __global__ __launch_bounds__(1024) void edge_grads(const EdgeKernelArgs A)
         for (int k = 0; k < C; ++k) store8f(A.parts + ((int64_t)part * gridDim.x + blockIdx.x) * D + c[k], left[k], v[k]);
     };
     if (before && A.p.before_weight_grad) leave(sum_pn, kBeforeWeight);
-    if (before && A.p.before_bias_grad) leave(sum_p, kBeforeBias);
+    if (PLAIN && before && A.p.before_bias_grad) leave(sum_p, kBeforeBias);
     if (after_sums) {
         leave(sum_tn, kAfterWeight);
-        leave(sum_t, kAfterBias);
+        if (PLAIN) leave(sum_t, kAfterBias);
     }
 #endif
 }
@@ -259,7 +293,8 @@ __global__ __launch_bounds__(kJoinColumns *kJoinParts) void edge_join(const Edge
         return;
     }
     const bool shared_gate = d.span == 0;
-    const float tn = total(kAfterWeight), t = total(kAfterBias), by = shared_gate ? d.scale * one(A.p.gate, d.gate_type, 1.f) : 1.f;
+    const bool plain = A.p.after_bias || A.p.after_bias_grad;
+    const float tn = total(kAfterWeight), t = plain ? total(kAfterBias) : 0.f, by = shared_gate ? d.scale * one(A.p.gate, d.gate_type, 1.f) : 1.f;
     if (A.p.after_weight_grad) put(A.p.after_weight_grad, d.weight_type, tn * by);
     if (A.p.after_bias_grad) put(A.p.after_bias_grad, d.weight_type, t * by);
     if (shared_gate && A.p.gate_grad) {
@@ -292,20 +327,22 @@ __global__ __launch_bounds__(256) void gate_join(const EdgeKernelArgs A)
 #endif
 }
 
-template <class X, class E, int C, int R>
+template <class X, class E, int C, bool PLAIN>
 void launch_grads(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stream)
 {
     const dim3 grid(p.blocks), threads(p.team * p.teams);
-    if (!a.p.branch && !a.p.branch_values && !a.p.branch_grad) hipLaunchKernelGGL((edge_grads<X, E, C, R, false, false>), grid, threads, 0, stream, a);
-    else if (a.d.span == 0) hipLaunchKernelGGL((edge_grads<X, E, C, R, true, false>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((edge_grads<X, E, C, R, true, true>), grid, threads, 0, stream, a);
+    constexpr int R = C == 1 && sizeof(X) == 2 ? 2 : 1;
+    if (!a.p.branch && !a.p.branch_values && !a.p.branch_grad) hipLaunchKernelGGL((edge_grads<X, E, C, R, false, false, PLAIN>), grid, threads, 0, stream, a);
+    else if (a.d.span == 0) hipLaunchKernelGGL((edge_grads<X, E, C, 1, true, false, PLAIN>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((edge_grads<X, E, C, 1, true, true, PLAIN>), grid, threads, 0, stream, a);
 }
 
 template <class X, class E>
 void launch_grads(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stream)
 {
-    if (p.vectors == 2) launch_grads<X, E, 2, 1>(p, a, stream);
-    else launch_grads<X, E, 1, 1>(p, a, stream);
+    const bool plain = a.p.before_bias_grad || a.p.after_bias || a.p.after_bias_grad;
+    if (p.vectors == 2) plain ? launch_grads<X, E, 2, true>(p, a, stream) : launch_grads<X, E, 2, false>(p, a, stream);
+    else plain ? launch_grads<X, E, 1, true>(p, a, stream) : launch_grads<X, E, 1, false>(p, a, stream);
 }
 
 }  // namespace
