@@ -84,6 +84,46 @@ __device__ __forceinline__ void store_parameters(void *p, int type, int64_t at, 
     else store8f((_Float16 *)p + at, left, v);
 }
 
+// Eight elements as they came from memory: of rows (T), or codes and their scale's byte.
+template <class T>
+struct Loaded {
+    static constexpr int kWords = sizeof(T) * 2;
+    uint32_t words[kWords];
+    __device__ __forceinline__ void rows(const T *from, int left)
+    {
+        typedef uint32_t whole __attribute__((ext_vector_type(kWords)));
+        const whole v = __builtin_bit_cast(whole, load8(from, left));
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) words[i] = v[i];
+    }
+    __device__ __forceinline__ void kept(const uint8_t *values, const uint8_t *scales, int64_t at)
+    {
+        const u32x2 codes = *(const u32x2 *)(values + at);
+        words[0] = codes[0];
+        words[1] = codes[1];
+        words[2] = scales[at / kKeptGroup];
+    }
+    __device__ __forceinline__ f32x8 of_rows() const
+    {
+        typedef uint32_t whole __attribute__((ext_vector_type(kWords)));
+        whole v;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) v[i] = words[i];
+        return __builtin_convertvector(__builtin_bit_cast(typename Eight<T>::type, v), f32x8);
+    }
+    // The normalised rows: kept, or formed again.
+    __device__ __forceinline__ f32x8 normalised(int form, float2 stats) const
+    {
+        return form ? decode8(form, u32x2{words[0], words[1]}, kept_scale(words[2])) : (of_rows() - stats.x) * stats.y;
+    }
+};
+__device__ __forceinline__ f32x8 fma8(f32x8 a, f32x8 b, f32x8 c)
+{
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) c[i] = fmaf(a[i], b[i], c[i]);
+    return c;
+}
+
 // Sum of eight, and of their squares; what is beyond the row's end counts for nothing.
 __device__ __forceinline__ float sum8(f32x8 v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 __device__ __forceinline__ float squares8(f32x8 v)

@@ -14,7 +14,8 @@
 namespace px {
 namespace {
 
-template <class X, class E, int C, int R, bool BRANCH>
+// BIASED: a norm has biases.
+template <class X, class E, int C, bool BRANCH, bool BIASED>
 __global__ __launch_bounds__(1024) void edge_rows(const EdgeKernelArgs A)
 {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -25,129 +26,124 @@ __global__ __launch_bounds__(1024) void edge_rows(const EdgeKernelArgs A)
     const int64_t width = kept_width(D);
     const float over = 1.f / D;
     int parity = 0, c[C], left[C];
-    f32x8 w_a[C], w_b[C], gate[C];
+    f32x8 w_a[C], w_b[C], b_a[C], b_b[C], gate[C];
+    auto gate_of = [&](int k, int64_t row) { return parameters(A.p.gate, d.gate_type, row * D + c[k], left[k], 1.f) * d.scale; };
 #pragma unroll
     for (int k = 0; k < C; ++k) {
         c[k] = (k * team + mine) * kVec;
         left[k] = D - c[k];
         w_a[k] = parameters(after ? A.p.after_weight : nullptr, d.weight_type, c[k], left[k], 1.f);
         w_b[k] = parameters(A.p.before_weight, d.weight_type, c[k], left[k], 1.f);
-        gate[k] = parameters(d.span ? nullptr : A.p.gate, d.gate_type, c[k], left[k], 1.f) * d.scale;
+        if (BIASED) {
+            b_a[k] = parameters(after ? A.p.after_bias : nullptr, d.weight_type, c[k], left[k], 0.f);
+            b_b[k] = parameters(A.p.before_bias, d.weight_type, c[k], left[k], 0.f);
+        }
+        if (!d.span) gate[k] = gate_of(k, 0);
     }
-    const int N = (int)d.N, step = gridDim.x * teams * R;
+    const int N = (int)d.N, step = gridDim.x * teams;
+    // a row as it comes from memory; the next one's loads are under way while one is worked on
+    constexpr bool kAhead = C == 1;
+    struct Row {
+        Loaded<X> x[C];
+        Loaded<E> z[C];
+    } next;
+    auto load = [&](int64_t row) {
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            if (BRANCH) next.z[k].rows((const E *)A.p.branch + row * d.branch_stride + c[k], left[k]);
+            next.x[k].rows((const X *)A.p.x + row * d.x_stride + c[k], left[k]);
+        }
+    };
+    int row = blockIdx.x * teams + first;
+    if (kAhead && row < N) load(row);
     // (of several wavefronts a row, one team a workgroup: all threads come to every barrier)
-    for (int row0 = (blockIdx.x * teams + first) * R; row0 < N; row0 += step) {
-        f32x8 y[R][C], z[R][C];
-        int64_t row[R];
+    for (; row < N; row += step) {
+        if (!kAhead) load(row);
+        const Row w = next;
+        if (BRANCH && d.span)
 #pragma unroll
-        for (int r = 0; r < R; ++r) row[r] = min(row0 + r, N - 1);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int k = 0; k < C; ++k) {
-                if (BRANCH) z[r][k] = load8f((const E *)A.p.branch + row[r] * d.branch_stride + c[k], left[k]);
-                y[r][k] = load8f((const X *)A.p.x + row[r] * d.x_stride + c[k], left[k]);
-            }
-        // each row of v becomes n(v); [mean, r] of it
-        auto normalise = [&](f32x8(&v)[R][C], float(&mean)[R], float(&spread)[R]) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) mean[r] = 0.f;
+            for (int k = 0; k < C; ++k) gate[k] = gate_of(k, (uint32_t)row / (uint32_t)d.span);
+        if (kAhead && row + step < N) load(row + step);
+        // v becomes n(v), its (mean, r) is left
+        auto normalise = [&](f32x8(&v)[C], float *stats) {
+            float mean[1] = {0.f}, spread[1] = {0.f};
             if (centred) {
 #pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int k = 0; k < C; ++k) mean[r] += sum8(v[r][k]);
+                for (int k = 0; k < C; ++k) mean[0] += sum8(v[k]);
                 over_team(mean, team, shared, parity);
+                mean[0] *= over;
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    mean[r] *= over;
-#pragma unroll
-                    for (int k = 0; k < C; ++k) {
-                        v[r][k] -= mean[r];
-                        if (A.ragged) v[r][k] = within(v[r][k], left[k]);
-                    }
+                for (int k = 0; k < C; ++k) {
+                    v[k] -= mean[0];
+                    if (A.ragged) v[k] = within(v[k], left[k]);
                 }
             }
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                spread[r] = 0.f;
-#pragma unroll
-                for (int k = 0; k < C; ++k) spread[r] += squares8(v[r][k]);
-            }
+            for (int k = 0; k < C; ++k) spread[0] += squares8(v[k]);
             over_team(spread, team, shared, parity);
+            const float r = 1.f / sqrtf(fmaf(spread[0], over, d.eps));
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                spread[r] = 1.f / sqrtf(fmaf(spread[r], over, d.eps));
-#pragma unroll
-                for (int k = 0; k < C; ++k) v[r][k] *= spread[r];
-            }
+            for (int k = 0; k < C; ++k) v[k] *= r;
+            if (stats && mine == 0) ((float2 *)stats)[row] = make_float2(mean[0], r);
         };
-        auto leave = [&](const f32x8(&v)[R][C], uint8_t *values, uint8_t *scales) {
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int k = 0; k < C; ++k) {
-                    const int64_t to = row[r] * width + c[k];
-                    keep8(d.form, v[r][k], values + to, scales + to / kKeptGroup, row0 + r < N && c[k] < width);
-                }
-        };
-        float mean[R], spread[R];
-        if (BRANCH) {
-            if (after) {
-                normalise(z, mean, spread);
-                if (A.p.branch_stats && mine == 0)
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-                        if (row0 + r < N) ((float2 *)A.p.branch_stats)[row[r]] = make_float2(mean[r], spread[r]);
-            }
-            if (A.p.branch_values) leave(z, A.p.branch_values, A.p.branch_scales);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int k = 0; k < C; ++k) {
-                    f32x8 b = z[r][k], g = gate[k];
-                    if (d.span) g = parameters(A.p.gate, d.gate_type, (int64_t)((uint32_t)row[r] / (uint32_t)d.span) * D + c[k], left[k], 1.f) * d.scale;
-                    if (after) {
-                        b *= w_a[k];
-                        if (A.p.after_bias) b += parameters(A.p.after_bias, d.weight_type, c[k], left[k], 0.f);
-                    }
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) y[r][k][i] = fmaf(g[i], b[i], d.residual * y[r][k][i]);
-                    if (row0 + r < N) store8f((X *)A.p.y + row[r] * d.y_stride + c[k], left[k], y[r][k]);
-                }
-        }
-        if (!before) continue;
-        normalise(y, mean, spread);
-        if (A.p.y_stats && mine == 0)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (row0 + r < N) ((float2 *)A.p.y_stats)[row[r]] = make_float2(mean[r], spread[r]);
-        if (A.p.y_values) leave(y, A.p.y_values, A.p.y_scales);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
+        auto leave = [&](const f32x8(&v)[C], uint8_t *values, uint8_t *scales) {
 #pragma unroll
             for (int k = 0; k < C; ++k) {
-                f32x8 h = y[r][k] * w_b[k];
-                if (A.p.before_bias) h += parameters(A.p.before_bias, d.weight_type, c[k], left[k], 0.f);
-                if (row0 + r < N) store8f((E *)A.p.rows + row[r] * d.rows_stride + c[k], left[k], h);
+                const int64_t to = row * width + c[k];
+                keep8(d.form, v[k], values + to, scales + to / kKeptGroup, c[k] < width);
             }
+        };
+        f32x8 y[C], z[C];
+        if (BRANCH) {
+#pragma unroll
+            for (int k = 0; k < C; ++k) z[k] = w.z[k].of_rows();
+            if (after) normalise(z, A.p.branch_stats);
+            if (A.p.branch_values) leave(z, A.p.branch_values, A.p.branch_scales);
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                if (after) {
+                    z[k] *= w_a[k];
+                    if (BIASED) z[k] += b_a[k];
+                }
+                y[k] = fma8(gate[k], z[k], w.x[k].of_rows() * d.residual);
+                store8f((X *)A.p.y + row * d.y_stride + c[k], left[k], y[k]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < C; ++k) y[k] = w.x[k].of_rows();
+        }
+        if (!before) continue;
+        normalise(y, A.p.y_stats);
+        if (A.p.y_values) leave(y, A.p.y_values, A.p.y_scales);
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            f32x8 h = y[k] * w_b[k];
+            if (BIASED) h += b_b[k];
+            store8f((E *)A.p.rows + row * d.rows_stride + c[k], left[k], h);
+        }
     }
 #endif
+}
+
+template <class X, class E, int C>
+void launch_rows_of(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stream)
+{
+    const int threads = p.team * p.teams;
+    auto launch = [&](auto kernel) {
+        // two rounds of what a compute unit holds, 16 wavefronts: more would each load the parameters again
+        const int64_t rows = (a.d.N + p.teams - 1) / p.teams, most = 512 * std::max(1, 1024 / threads);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(rows, most)), dim3(threads), 0, stream, a);
+    };
+    const bool biased = a.p.after_bias || a.p.before_bias;
+    if (a.p.branch) biased ? launch(edge_rows<X, E, C, true, true>) : launch(edge_rows<X, E, C, true, false>);
+    else biased ? launch(edge_rows<X, E, C, false, true>) : launch(edge_rows<X, E, C, false, false>);
 }
 
 template <class X, class E>
 void launch_rows(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stream)
 {
-    const dim3 threads(p.team * p.teams);
-    auto launch = [&](auto kernel, int rows) {
-        // four workgroups a compute unit of 256 threads and up to 16 wavefronts in all: more would each load the parameters again
-        const int64_t batches = (a.d.N + (int64_t)rows * p.teams - 1) / ((int64_t)rows * p.teams), most = 256 * std::max(1, 1024 / (p.team * p.teams)) * 2;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(batches, most)), threads, 0, stream, a);
-    };
-    const bool branch = a.p.branch;
-    if (p.vectors == 2) branch ? launch(edge_rows<X, E, 2, 1, true>, 1) : launch(edge_rows<X, E, 2, 1, false>, 1);
-    else if (a.d.N <= 1024) branch ? launch(edge_rows<X, E, 1, 1, true>, 1) : launch(edge_rows<X, E, 1, 1, false>, 1);
-    else branch ? launch(edge_rows<X, E, 1, 2, true>, 2) : launch(edge_rows<X, E, 1, 2, false>, 2);
+    if (p.vectors == 2) launch_rows_of<X, E, 2>(p, a, stream);
+    else launch_rows_of<X, E, 1>(p, a, stream);
 }
 
 }  // namespace
@@ -166,9 +162,8 @@ EdgePlan edge_plan(const pollux_edge_dims &d)
         p.teams = 1;
     }
     // Backward: 16 wavefronts a compute unit, but rows enough a team that what it writes of sums, 8 to 16 bytes a column, is little beside the rows.
-    const int64_t teams = 4096 * 64 / p.team, least = p.team > 64 ? 8 : 4;
+    const int64_t teams = 4096 * 64 / p.team, least = 4;
     p.chunk = (int)std::max<int64_t>(least, (d.N + teams - 1) / teams);
-    p.chunk = (p.chunk + 1) / 2 * 2;
     p.blocks = (int)((d.N + (int64_t)p.chunk * p.teams - 1) / ((int64_t)p.chunk * p.teams));
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o = up256(o + bytes); return at; };

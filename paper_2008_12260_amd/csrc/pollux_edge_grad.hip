@@ -20,51 +20,10 @@ namespace {
 
 enum Part { kBeforeWeight, kBeforeBias, kAfterWeight, kAfterBias, kParts };
 
-#ifdef __HIP_DEVICE_COMPILE__
-// Eight elements as they came from memory: of rows (T), or codes and their scale's byte.
-template <class T>
-struct Loaded {
-    static constexpr int kWords = sizeof(T) * 2;
-    uint32_t words[kWords];
-    __device__ __forceinline__ void rows(const T *from, int left)
-    {
-        typedef uint32_t whole __attribute__((ext_vector_type(kWords)));
-        const whole v = __builtin_bit_cast(whole, load8(from, left));
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) words[i] = v[i];
-    }
-    __device__ __forceinline__ void kept(const uint8_t *values, const uint8_t *scales, int64_t at)
-    {
-        const u32x2 codes = *(const u32x2 *)(values + at);
-        words[0] = codes[0];
-        words[1] = codes[1];
-        words[2] = scales[at / kKeptGroup];
-    }
-    __device__ __forceinline__ f32x8 of_rows() const
-    {
-        typedef uint32_t whole __attribute__((ext_vector_type(kWords)));
-        whole v;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) v[i] = words[i];
-        return __builtin_convertvector(__builtin_bit_cast(typename Eight<T>::type, v), f32x8);
-    }
-    // The normalised rows: kept, or formed again.
-    __device__ __forceinline__ f32x8 normalised(int form, float2 stats) const
-    {
-        return form ? decode8(form, u32x2{words[0], words[1]}, kept_scale(words[2])) : (of_rows() - stats.x) * stats.y;
-    }
-};
-__device__ __forceinline__ f32x8 fma8(f32x8 a, f32x8 b, f32x8 c)
-{
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) c[i] = fmaf(a[i], b[i], c[i]);
-    return c;
-}
-#endif
-
+// MOST: threads of a workgroup; with spans, whose sums need the most registers, 512 where rows allow it (3003 x 1000 with biases 64 us within the registers of 1024).
 // PLAIN: sums of gradients themselves are wanted too (for biases), not only of their products with normalised rows.
-template <class X, class E, int C, int R, bool BRANCH, bool SPANS, bool PLAIN>
-__global__ __launch_bounds__(1024) void edge_grads(const EdgeKernelArgs A)
+template <class X, class E, int C, bool BRANCH, bool SPANS, bool PLAIN, int MOST>
+__global__ __launch_bounds__(MOST) void edge_grads(const EdgeKernelArgs A)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     __shared__ float shared[2][kMostWaves][8];
@@ -93,124 +52,107 @@ __global__ __launch_bounds__(1024) void edge_grads(const EdgeKernelArgs A)
     const int begin = (int)min((int64_t)chunk * A.chunk, (int64_t)N), end = min(begin + A.chunk, N);
     const bool has_z = A.p.branch || A.p.branch_values;
     const bool after_sums = BRANCH && (A.p.after_weight_grad || A.p.after_bias_grad || A.p.gate_grad), before_sums = before && (A.p.before_weight_grad || A.p.before_bias_grad);
-    int span = 0, count;
-    for (int row0 = begin; row0 < end; row0 += count) {
-        count = min(R, end - row0);
+    // a row as it comes from memory; the next one's loads are under way while one is worked on, where registers hold both: 8192 x 8192 from i8 146 us (164 without), 16384 x 16384 twice the time
+    constexpr bool kAhead = C == 1 && !SPANS && sizeof(X) == 2;
+    struct Row {
+        Loaded<X> dy[C], y[C];
+        Loaded<E> dh[C], z[C];
+        float2 stats_y, stats_z;
+    };
+    auto load = [&](Row &w, int at) {
+        const int64_t row = at;
+        if (before) w.stats_y = ((const float2 *)A.p.y_stats)[row];
+        w.stats_z = BRANCH && after ? ((const float2 *)A.p.branch_stats)[row] : make_float2(0.f, 1.f);
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            const int64_t kept = row * width + min((int64_t)c[k], width - kVec);
+            if (before) {
+                w.dh[k].rows((const E *)A.p.rows_grad + row * d.rows_grad_stride + c[k], left[k]);
+                if (d.form) w.y[k].kept(A.p.y_values, A.p.y_scales, kept);
+                else w.y[k].rows((const X *)A.p.y + row * d.y_stride + c[k], left[k]);
+            }
+            if (A.p.y_grad) w.dy[k].rows((const X *)A.p.y_grad + row * d.y_grad_stride + c[k], left[k]);
+            if (BRANCH && has_z) {
+                if (d.form) w.z[k].kept(A.p.branch_values, A.p.branch_scales, kept);
+                else w.z[k].rows((const E *)A.p.branch + row * d.branch_stride + c[k], left[k]);
+            }
+        }
+    };
+    int span = 0;
+    Row next;
+    if (kAhead && begin < end) load(next, begin);
+    for (int row = begin; row < end; ++row) {
+        if (!kAhead) load(next, row);
+        const Row w = next;
+        if (kAhead && row + 1 < end) load(next, row + 1);
         if (SPANS) {
-            const int at = (uint32_t)row0 / (uint32_t)d.span;
-            count = (int)min((int64_t)count, (at + 1) * d.span - row0);
-            if (row0 == begin || at != span) {
+            const int at = (uint32_t)row / (uint32_t)d.span;
+            if (row == begin || at != span) {
                 span = at;
 #pragma unroll
                 for (int k = 0; k < C; ++k)
                     if (!kReload) by[k] = gate_of(k, span) * after_weight(k);
             }
         }
-        int64_t row[R];
-        Loaded<X> dy[R][C], y[R][C];
-        Loaded<E> dh[R][C], z[R][C];
-        float2 stats_y[R], stats_z[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            row[r] = row0 + min(r, count - 1);
-            if (before) stats_y[r] = ((const float2 *)A.p.y_stats)[row[r]];
-            if (BRANCH && after) stats_z[r] = ((const float2 *)A.p.branch_stats)[row[r]];
-            else stats_z[r] = make_float2(0.f, 1.f);
+        f32x8 g[C], n[C];
+        // v - [mean v] - n mean(v n), times r: the gradient through a norm
+        auto through = [&](float2 stats) {
+            float sums[2] = {0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < C; ++k) {
-                const int64_t kept = row[r] * width + min((int64_t)c[k], width - kVec);
-                if (before) {
-                    dh[r][k].rows((const E *)A.p.rows_grad + row[r] * d.rows_grad_stride + c[k], left[k]);
-                    if (d.form) y[r][k].kept(A.p.y_values, A.p.y_scales, kept);
-                    else y[r][k].rows((const X *)A.p.y + row[r] * d.y_stride + c[k], left[k]);
-                }
-                if (A.p.y_grad) dy[r][k].rows((const X *)A.p.y_grad + row[r] * d.y_grad_stride + c[k], left[k]);
-                if (BRANCH && has_z) {
-                    if (d.form) z[r][k].kept(A.p.branch_values, A.p.branch_scales, kept);
-                    else z[r][k].rows((const E *)A.p.branch + row[r] * d.branch_stride + c[k], left[k]);
-                }
-            }
-        }
-        f32x8 g[R][C], n[R][C];
-        // v - [mean v] - n mean(v n), times r: the gradient through a norm
-        auto through = [&](const float2(&stats)[R]) {
-            float sums[2 * R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                sums[r] = sums[R + r] = 0.f;
-#pragma unroll
-                for (int k = 0; k < C; ++k)
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) sums[r] = fmaf(g[r][k][i], n[r][k][i], sums[r]);
+                for (int i = 0; i < kVec; ++i) sums[0] = fmaf(g[k][i], n[k][i], sums[0]);
+                if (centred) sums[1] += sum8(g[k]);
             }
             if (centred) {
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int k = 0; k < C; ++k) sums[R + r] += sum8(g[r][k]);
                 over_team(sums, team, shared, parity);
             } else {
-                float along[R];
-#pragma unroll
-                for (int r = 0; r < R; ++r) along[r] = sums[r];
+                float along[1] = {sums[0]};
                 over_team(along, team, shared, parity);
-#pragma unroll
-                for (int r = 0; r < R; ++r) sums[r] = along[r];
+                sums[0] = along[0];
             }
+            const float a = -sums[0] * over, m = sums[1] * over;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const float a = -sums[r] * over, m = sums[R + r] * over;
+            for (int k = 0; k < C; ++k)
 #pragma unroll
-                for (int k = 0; k < C; ++k)
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) g[r][k][i] = (fmaf(a, n[r][k][i], g[r][k][i]) - m) * stats[r].y;
-            }
+                for (int i = 0; i < kVec; ++i) g[k][i] = (fmaf(a, n[k][i], g[k][i]) - m) * stats.y;
         };
         if (before) {
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int k = 0; k < C; ++k) {
-                    g[r][k] = dh[r][k].of_rows();
-                    n[r][k] = y[r][k].normalised(d.form, stats_y[r]);
-                    if (before_sums && r < count) {
-                        sum_pn[k] = fma8(g[r][k], n[r][k], sum_pn[k]);
-                        if (PLAIN) sum_p[k] += g[r][k];
-                    }
-                    g[r][k] *= kReload ? parameters(A.p.before_weight, d.weight_type, c[k], left[k], 1.f) : w_b[k];
+            for (int k = 0; k < C; ++k) {
+                g[k] = w.dh[k].of_rows();
+                n[k] = w.y[k].normalised(d.form, w.stats_y);
+                if (before_sums) {
+                    sum_pn[k] = fma8(g[k], n[k], sum_pn[k]);
+                    if (PLAIN) sum_p[k] += g[k];
                 }
-            through(stats_y);
+                g[k] *= kReload ? parameters(A.p.before_weight, d.weight_type, c[k], left[k], 1.f) : w_b[k];
+            }
+            through(w.stats_y);
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int k = 0; k < C; ++k) {
-                if (!before) g[r][k] = zeros;
-                if (A.p.y_grad) g[r][k] += dy[r][k].of_rows();
-                if (A.p.x_grad && r < count) store8f((X *)A.p.x_grad + row[r] * d.x_grad_stride + c[k], left[k], g[r][k] * d.residual);
-            }
+        for (int k = 0; k < C; ++k) {
+            if (!before) g[k] = zeros;
+            if (A.p.y_grad) g[k] += w.dy[k].of_rows();
+            if (A.p.x_grad) store8f((X *)A.p.x_grad + row * d.x_grad_stride + c[k], left[k], g[k] * d.residual);
+        }
         if (!BRANCH) continue;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int k = 0; k < C; ++k) {
-                n[r][k] = has_z ? z[r][k].normalised(d.form, stats_z[r]) : zeros;
-                if (after_sums && r < count) {
-                    f32x8 &to = SPANS ? span_gn[k] : sum_tn[k];
-                    to = fma8(g[r][k], n[r][k], to);
-                    if (PLAIN) (SPANS ? span_g[k] : sum_t[k]) += g[r][k];
-                }
-                g[r][k] *= kReload ? gate_of(k, SPANS ? span : 0) * after_weight(k) : by[k];
+        for (int k = 0; k < C; ++k) {
+            n[k] = has_z ? w.z[k].normalised(d.form, w.stats_z) : zeros;
+            if (after_sums) {
+                f32x8 &to = SPANS ? span_gn[k] : sum_tn[k];
+                to = fma8(g[k], n[k], to);
+                if (PLAIN) (SPANS ? span_g[k] : sum_t[k]) += g[k];
             }
-        if (A.p.branch_grad) {
-            if (after) through(stats_z);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (r < count)
-#pragma unroll
-                    for (int k = 0; k < C; ++k) store8f((E *)A.p.branch_grad + row[r] * d.branch_grad_stride + c[k], left[k], g[r][k]);
+            g[k] *= kReload ? gate_of(k, SPANS ? span : 0) * after_weight(k) : by[k];
         }
-        if (SPANS && after_sums && (row0 + count == end || row0 + count == (span + 1) * d.span)) {
+        if (A.p.branch_grad) {
+            if (after) through(w.stats_z);
+#pragma unroll
+            for (int k = 0; k < C; ++k) store8f((E *)A.p.branch_grad + row * d.branch_grad_stride + c[k], left[k], g[k]);
+        }
+        if (SPANS && after_sums && (row + 1 == end || row + 1 == (span + 1) * d.span)) {
             // the span's last row here: its sums go to where they belong
             const int64_t from = span * d.span, to = from + d.span;
 #pragma unroll
@@ -254,21 +196,21 @@ __global__ __launch_bounds__(1024) void edge_grads(const EdgeKernelArgs A)
 #endif
 }
 
-// The workgroups' sums added in their order: 64 columns by 16 parts of the list; blockIdx.y: of the norm before, or of the rest.
+// The workgroups' sums added in their order: 64 columns by 16 parts of a list.  blockIdx.y: of the norm before, of the rest, and from 2 on of the gates of spans that chunks cut, `cuts` of them.
 constexpr int kJoinColumns = 64, kJoinParts = 16;
-__global__ __launch_bounds__(kJoinColumns *kJoinParts) void edge_join(const EdgeKernelArgs A, int blocks)
+__global__ __launch_bounds__(kJoinColumns *kJoinParts) void edge_join(const EdgeKernelArgs A, int blocks, int chunks, bool rest, int cuts)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     __shared__ float shared[kJoinParts][kJoinColumns];
     const pollux_edge_dims &d = A.d;
     const int column = threadIdx.x % kJoinColumns, part = threadIdx.x / kJoinColumns, c = blockIdx.x * kJoinColumns + column;
-    auto total = [&](int which) {
-        const float *from = A.parts + (int64_t)which * blocks * d.D + c;
+    // of `count` rows of D, `step` elements apart
+    auto total = [&](const float *from, int count, int64_t step) {
         float v = 0.f;
-        const int each = (blocks + kJoinParts - 1) / kJoinParts, first = part * each, last = min(first + each, blocks);
+        const int each = (count + kJoinParts - 1) / kJoinParts, first = part * each, last = min(first + each, count);
         if (c < d.D)
 #pragma unroll 8
-            for (int b = first; b < last; ++b) v += from[(int64_t)b * d.D];
+            for (int b = first; b < last; ++b) v += from[b * step + c];
         __syncthreads();
         shared[part][column] = v;
         __syncthreads();
@@ -277,72 +219,64 @@ __global__ __launch_bounds__(kJoinColumns *kJoinParts) void edge_join(const Edge
         for (int k = 0; k < kJoinParts; ++k) v += shared[k][column];
         return v;
     };
-    auto put = [&](void *to, int type, float v) {
+    auto put = [&](void *to, int type, int64_t at, float v) {
         if (part != 0 || c >= d.D) return;
-        if (type == PX_TYPE_F32) ((float *)to)[c] = v;
-        else if (type == PX_TYPE_BF16) ((__bf16 *)to)[c] = (__bf16)v;
-        else ((_Float16 *)to)[c] = (_Float16)v;
+        if (type == PX_TYPE_F32) ((float *)to)[at + c] = v;
+        else if (type == PX_TYPE_BF16) ((__bf16 *)to)[at + c] = (__bf16)v;
+        else ((_Float16 *)to)[at + c] = (_Float16)v;
     };
     auto one = [&](const void *p, int type, float none) {
         if (!p || c >= d.D) return none;
         return type == PX_TYPE_F32 ? ((const float *)p)[c] : type == PX_TYPE_BF16 ? (float)((const __bf16 *)p)[c] : (float)((const _Float16 *)p)[c];
     };
+    auto sum = [&](int which) { return total(A.parts + (int64_t)which * blocks * d.D, blocks, d.D); };
     if (blockIdx.y == 0) {
-        if (A.p.before_weight_grad) put(A.p.before_weight_grad, d.weight_type, total(kBeforeWeight));
-        if (A.p.before_bias_grad) put(A.p.before_bias_grad, d.weight_type, total(kBeforeBias));
+        if (A.p.before_weight_grad) put(A.p.before_weight_grad, d.weight_type, 0, sum(kBeforeWeight));
+        if (A.p.before_bias_grad) put(A.p.before_bias_grad, d.weight_type, 0, sum(kBeforeBias));
         return;
     }
-    const bool shared_gate = d.span == 0;
-    const bool plain = A.p.after_bias || A.p.after_bias_grad;
-    const float tn = total(kAfterWeight), t = plain ? total(kAfterBias) : 0.f, by = shared_gate ? d.scale * one(A.p.gate, d.gate_type, 1.f) : 1.f;
-    if (A.p.after_weight_grad) put(A.p.after_weight_grad, d.weight_type, tn * by);
-    if (A.p.after_bias_grad) put(A.p.after_bias_grad, d.weight_type, t * by);
-    if (shared_gate && A.p.gate_grad) {
-        const bool after = d.flags & PX_EDGE_AFTER;
-        const float w = one(after ? A.p.after_weight : nullptr, d.weight_type, 1.f), b = one(after ? A.p.after_bias : nullptr, d.weight_type, 0.f);
-        put(A.p.gate_grad, d.gate_type, d.scale * fmaf(w, tn, b == 0.f ? 0.f : b * t));
+    if (blockIdx.y == 1) {
+        if (!rest) return;
+        const bool shared_gate = d.span == 0, plain = A.p.after_bias || A.p.after_bias_grad;
+        const float tn = sum(kAfterWeight), t = plain ? sum(kAfterBias) : 0.f, by = shared_gate ? d.scale * one(A.p.gate, d.gate_type, 1.f) : 1.f;
+        if (A.p.after_weight_grad) put(A.p.after_weight_grad, d.weight_type, 0, tn * by);
+        if (A.p.after_bias_grad) put(A.p.after_bias_grad, d.weight_type, 0, t * by);
+        if (shared_gate && A.p.gate_grad) {
+            const bool after = d.flags & PX_EDGE_AFTER;
+            const float w = one(after ? A.p.after_weight : nullptr, d.weight_type, 1.f), b = one(after ? A.p.after_bias : nullptr, d.weight_type, 0.f);
+            put(A.p.gate_grad, d.gate_type, 0, d.scale * fmaf(w, tn, b == 0.f ? 0.f : b * t));
+        }
+        return;
     }
-#endif
-}
-
-// Gates of spans that chunks cut: their parts added in order.  A thread a column, a workgroup 256 columns of a span.
-__global__ __launch_bounds__(256) void gate_join(const EdgeKernelArgs A)
-{
-#ifdef __HIP_DEVICE_COMPILE__
-    const pollux_edge_dims &d = A.d;
+    // one a span, or, of more spans than borders of chunks, one a border: the span that it cuts, if it is the first to
     const int64_t spans = (d.N + d.span - 1) / d.span;
-    const int c = blockIdx.y * 256 + threadIdx.x;
-    if (c >= d.D) return;
-    for (int64_t s = blockIdx.x; s < spans; s += gridDim.x) {
-        const int64_t from = s * d.span, to = min(from + d.span, d.N);
-        const int64_t first = from / A.chunk, last = (to - 1) / A.chunk;
-        if (first == last) continue;
-        float v = A.ends[(first * 2 + 1) * d.D + c];
-#pragma unroll 8
-        for (int64_t k = first + 1; k <= last; ++k) v += A.ends[k * 2 * d.D + c];
-        if (d.gate_type == PX_TYPE_F32) ((float *)A.p.gate_grad)[s * d.D + c] = v;
-        else if (d.gate_type == PX_TYPE_BF16) ((__bf16 *)A.p.gate_grad)[s * d.D + c] = (__bf16)v;
-        else ((_Float16 *)A.p.gate_grad)[s * d.D + c] = (_Float16)v;
+    for (int k = blockIdx.y - 2; k < cuts; k += gridDim.y - 2) {
+        const int64_t s = spans <= chunks - 1 ? k : ((int64_t)(k + 1) * A.chunk - 1) / d.span;
+        const int64_t from = s * d.span, to = min(from + d.span, d.N), first = from / A.chunk, last = (to - 1) / A.chunk;
+        if (first == last || (spans > chunks - 1 && first != k)) continue;
+        // the first chunk's last span, the others' first
+        const float head = c < d.D ? A.ends[(first * 2 + 1) * d.D + c] : 0.f;
+        put(A.p.gate_grad, d.gate_type, s * d.D, head + total(A.ends + (first + 1) * 2 * d.D, (int)(last - first), 2 * d.D));
     }
 #endif
 }
 
-template <class X, class E, int C, bool PLAIN>
-void launch_grads(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stream)
+template <class X, class E, int C>
+void launch_grads_of(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stream)
 {
-    const dim3 grid(p.blocks), threads(p.team * p.teams);
-    constexpr int R = C == 1 && sizeof(X) == 2 ? 2 : 1;
-    if (!a.p.branch && !a.p.branch_values && !a.p.branch_grad) hipLaunchKernelGGL((edge_grads<X, E, C, R, false, false, PLAIN>), grid, threads, 0, stream, a);
-    else if (a.d.span == 0) hipLaunchKernelGGL((edge_grads<X, E, C, 1, true, false, PLAIN>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((edge_grads<X, E, C, 1, true, true, PLAIN>), grid, threads, 0, stream, a);
+    const bool plain = a.p.before_bias_grad || a.p.after_bias || a.p.after_bias_grad, branch = a.p.branch || a.p.branch_values || a.p.branch_grad;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(p.team * p.teams), 0, stream, a); };
+    if (branch && a.d.span && C == 1 && p.team <= 512) plain ? launch(edge_grads<X, E, 1, true, true, true, 512>) : launch(edge_grads<X, E, 1, true, true, false, 512>);
+    else if (branch && a.d.span) plain ? launch(edge_grads<X, E, C, true, true, true, 1024>) : launch(edge_grads<X, E, C, true, true, false, 1024>);
+    else if (branch) plain ? launch(edge_grads<X, E, C, true, false, true, 1024>) : launch(edge_grads<X, E, C, true, false, false, 1024>);
+    else plain ? launch(edge_grads<X, E, C, false, false, true, 1024>) : launch(edge_grads<X, E, C, false, false, false, 1024>);
 }
 
 template <class X, class E>
 void launch_grads(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stream)
 {
-    const bool plain = a.p.before_bias_grad || a.p.after_bias || a.p.after_bias_grad;
-    if (p.vectors == 2) plain ? launch_grads<X, E, 2, true>(p, a, stream) : launch_grads<X, E, 2, false>(p, a, stream);
-    else plain ? launch_grads<X, E, 1, true>(p, a, stream) : launch_grads<X, E, 1, false>(p, a, stream);
+    if (p.vectors == 2) launch_grads_of<X, E, 2>(p, a, stream);
+    else launch_grads_of<X, E, 1>(p, a, stream);
 }
 
 }  // namespace
@@ -364,12 +298,11 @@ int launch_block_edge_grad(const pollux_edge_dims &d, const EdgePlan &p, const E
         default: d.x_type == PX_TYPE_F32 ? launch_grads<float, _Float16>(p, a, stream) : launch_grads<_Float16, _Float16>(p, a, stream); break;
     }
     const bool spans = d.span != 0, before = a.p.before_weight_grad || a.p.before_bias_grad, rest = a.p.after_weight_grad || a.p.after_bias_grad || (!spans && a.p.gate_grad);
-    if (before || rest) {
-        const int columns = (d.D + kJoinColumns - 1) / kJoinColumns;
-        hipLaunchKernelGGL(edge_join, dim3(columns, rest ? 2 : 1), dim3(kJoinColumns * kJoinParts), 0, stream, a, d.N > 0 ? p.blocks : 0);
-    }
-    if (spans && a.p.gate_grad && d.N > 0 && d.span > 1 && (d.N > p.chunk))
-        hipLaunchKernelGGL(gate_join, dim3((unsigned)std::min<int64_t>((d.N + d.span - 1) / d.span, 4096), (d.D + 255) / 256), dim3(256), 0, stream, a);
+    const int chunks = (int)((d.N + p.chunk - 1) / p.chunk);
+    const int cuts = spans && d.span > 1 && a.p.gate_grad && d.N > 0 ? (int)std::min<int64_t>((d.N + d.span - 1) / d.span, chunks - 1) : 0;
+    if (before || rest || cuts > 0)
+        hipLaunchKernelGGL(edge_join, dim3((d.D + kJoinColumns - 1) / kJoinColumns, cuts > 0 ? 2 + std::min(cuts, 4096) : rest ? 2 : 1), dim3(kJoinColumns * kJoinParts), 0, stream, a,
+                           d.N > 0 ? p.blocks : 0, chunks, rest, cuts);
     return status_of(hipGetLastError());
 }
 
