@@ -130,8 +130,8 @@ void launch_rows_of(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stre
 {
     const int threads = p.team * p.teams;
     auto launch = [&](auto kernel) {
-        // two rounds of what a compute unit holds, 16 wavefronts: more would each load the parameters again
-        const int64_t rows = (a.d.N + p.teams - 1) / p.teams, most = 512 * std::max(1, 1024 / threads);
+        // some 16 to 20 wavefronts a compute unit, each of which goes through its rows: 16384 x 4096 in bfloat16 98 us, with twice as many 115, with eight times 102
+        const int64_t rows = (a.d.N + p.teams - 1) / p.teams, most = 256 * std::max(1, 1280 / threads);
         hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(rows, most)), dim3(threads), 0, stream, a);
     };
     const bool biased = a.p.after_bias || a.p.before_bias;
@@ -161,8 +161,10 @@ EdgePlan edge_plan(const pollux_edge_dims &d)
         p.team = ((eights + p.vectors - 1) / p.vectors + 63) / 64 * 64;
         p.teams = 1;
     }
-    // Backward: 16 wavefronts a compute unit, but rows enough a team that what it writes of sums, 8 to 16 bytes a column, is little beside the rows.
-    const int64_t teams = 4096 * 64 / p.team, least = 4;
+    // Backward: 16 wavefronts a compute unit, which is what its registers hold (20 of rows of 4104 to 5120, two workgroups of ten), but rows enough a team that what it writes of sums, 8 to 16 bytes a
+    // column, is little beside the rows.
+    const int threads = p.team * p.teams;
+    const int64_t teams = 256 * (threads > 512 ? std::max(1, 1280 / threads) : 1024 / threads) * p.teams, least = 4;
     p.chunk = (int)std::max<int64_t>(least, (d.N + teams - 1) / teams);
     p.blocks = (int)((d.N + (int64_t)p.chunk * p.teams - 1) / ((int64_t)p.chunk * p.teams));
     size_t o = 0;

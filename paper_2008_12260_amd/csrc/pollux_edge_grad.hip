@@ -48,8 +48,9 @@ __global__ __launch_bounds__(MOST) void edge_grads(const EdgeKernelArgs A)
         if (!kReload && BRANCH && !SPANS) by[k] = gate_of(k, 0) * after_weight(k);
         sum_pn[k] = sum_p[k] = sum_tn[k] = sum_t[k] = span_gn[k] = span_g[k] = zeros;
     }
-    const int N = (int)d.N, chunk = blockIdx.x * teams + first;
-    const int begin = (int)min((int64_t)chunk * A.chunk, (int64_t)N), end = min(begin + A.chunk, N);
+    // with spans a team's rows are neighbours, else as far apart as there are teams: the chip is then at neighbouring rows at any time
+    const int N = (int)d.N, chunk = blockIdx.x * teams + first, step = SPANS ? 1 : gridDim.x * teams;
+    const int begin = SPANS ? (int)min((int64_t)chunk * A.chunk, (int64_t)N) : chunk, end = SPANS ? min(begin + A.chunk, N) : N;
     const bool has_z = A.p.branch || A.p.branch_values;
     const bool after_sums = BRANCH && (A.p.after_weight_grad || A.p.after_bias_grad || A.p.gate_grad), before_sums = before && (A.p.before_weight_grad || A.p.before_bias_grad);
     // a row as it comes from memory; the next one's loads are under way while one is worked on, where registers hold both: 8192 x 8192 from i8 146 us (164 without), 16384 x 16384 twice the time
@@ -81,10 +82,10 @@ __global__ __launch_bounds__(MOST) void edge_grads(const EdgeKernelArgs A)
     int span = 0;
     Row next;
     if (kAhead && begin < end) load(next, begin);
-    for (int row = begin; row < end; ++row) {
+    for (int row = begin; row < end; row += step) {
         if (!kAhead) load(next, row);
         const Row w = next;
-        if (kAhead && row + 1 < end) load(next, row + 1);
+        if (kAhead && row + step < end) load(next, row + step);
         if (SPANS) {
             const int at = (uint32_t)row / (uint32_t)d.span;
             if (row == begin || at != span) {
