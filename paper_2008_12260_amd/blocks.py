@@ -299,8 +299,11 @@ def _stats(t, name, N):
     return t
 
 
-def block_edge_grad(y_grad, rows_grad, state, y=None, branch=None, gate=None, after=None, before=None, residual=1.0, scale=1.0, centred=False,
-                    need=("x", "branch", "gate", "after", "before"), workspace=None, stream=None):
+_ALL = ("x", "branch", "gate", "after", "before")
+
+
+def block_edge_grad(y_grad, rows_grad, state, y=None, branch=None, gate=None, after=None, before=None, residual=1.0, scale=1.0, centred=False, need=_ALL, workspace=None,
+                    stream=None):
     """EdgeGrads of block_edge: the gradients of x, branch, gate and of the norms' weights and biases, from those of y (None: zeros) and of rows.
 
     gate, after, before, residual, scale, centred: as in the call that left `state`.  Where it kept nothing, y and branch are given as that call returned and
@@ -322,24 +325,23 @@ def block_edge_grad(y_grad, rows_grad, state, y=None, branch=None, gate=None, af
         for name, t, dtype in (("y_grad", y_grad, state.x_dtype), ("rows_grad", rows_grad, state.dtype)):
             if t is not None and (t.shape != shape or t.dtype != dtype):
                 raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}: {dtype} {tuple(shape)} is wanted")
-        flat, _ = _matrix(model, "gradients")
-        N, D = flat.shape
-        device = flat.device
-        rows_of = lambda t, name: (None, 0) if t is None else _matrix(t, name)
-        y_grad_rows, y_grad_ld = rows_of(y_grad, "y_grad")
-        rows_grad_rows, rows_grad_ld = rows_of(rows_grad, "rows_grad")
+        y_grad_rows, y_grad_ld = (None, 0) if y_grad is None else _matrix(y_grad, "y_grad")
+        rows_grad_rows, rows_grad_ld = (None, 0) if rows_grad is None else _matrix(rows_grad, "rows_grad")
+        N, D = (rows_grad_rows if y_grad_rows is None else y_grad_rows).shape
+        device = model.device
         gate_rows, span = _gate(gate, N, D)
         weight_dtype, (w_a, b_a, w_b, b_b) = _vectors(D, after_weight=after and after[0], after_bias=after and after[1], before_weight=before and before[0],
                                                       before_bias=before and before[1])
-        wanted = set(need)
-        if wanted - {"x", "branch", "gate", "after", "before"}:
-            raise ValueError(f"need names {sorted(wanted)}")
-        new = lambda t: None if t is None else torch.empty_like(t, memory_format=_contiguous())
-        x_grad = torch.empty(shape, dtype=state.x_dtype, device=device) if "x" in wanted else None
-        branch_grad = torch.empty(shape, dtype=state.dtype, device=device) if state.branched and "branch" in wanted else None
-        gate_grad = new(gate) if "gate" in wanted else None
-        after_grads = [new(t) for t in (w_a, b_a)] if "after" in wanted else [None, None]
-        before_grads = [new(t) for t in (w_b, b_b)] if "before" in wanted else [None, None]
+        if need is not _ALL and set(need) - set(_ALL):
+            raise ValueError(f"need names {sorted(need)}: some of {_ALL} are wanted")
+
+        def like(t, part):
+            return None if t is None or part not in need else torch.empty(t.shape, dtype=t.dtype, device=device)
+        x_grad = torch.empty(shape, dtype=state.x_dtype, device=device) if "x" in need else None
+        branch_grad = torch.empty(shape, dtype=state.dtype, device=device) if state.branched and "branch" in need else None
+        gate_grad = like(gate, "gate")
+        after_grads = like(w_a, "after"), like(b_a, "after")
+        before_grads = like(w_b, "before"), like(b_b, "before")
         # what the norms were of: kept, or as it was
         asked = after is not None or gate_grad is not None
         y_rows = branch_rows = y_scales = branch_scales = None
@@ -347,6 +349,8 @@ def block_edge_grad(y_grad, rows_grad, state, y=None, branch=None, gate=None, af
         form = _px.PX_KEPT_NONE
         if kept is not None:
             form = _form(kept.form)
+            if any(k is not None and k.form != kept.form for k in (state.y_kept, state.branch_kept)) or before is not None and state.y_kept is None or asked and state.branch_kept is None:
+                raise ValueError("state keeps not what is wanted of it, in one form")
             if before is not None:
                 y_rows, y_scales = _kept(state.y_kept, "state.y_kept", N, D)[:2]
             if asked:

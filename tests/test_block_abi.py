@@ -184,6 +184,9 @@ BAD = [lambda: px.keep(new(6, 40), "i4"), lambda: px.keep(new(6, 40), None), lam
        lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(form="i8"), after=N_(), before=N_(), need=("y",)),
        lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(branch=False, after=False), y=new(6, 40), gate=new(40), before=N_()),
        lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(), y=new(6, 40), branch=new(6, 39), after=N_(), before=N_()),
+       lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(form="i8")._replace(branch_kept=kept(form="e4m3")), after=N_(), before=N_()),
+       lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(form="i8", after=False), gate=new(40), before=N_()),
+       lambda: px.block_edge_grad(new(6, 40), new(6, 40), state(form="i8")._replace(y_kept=None), after=N_(), before=N_()),
        lambda: px.gated(new(6, 40), act="relu"), lambda: px.gated(new(6, 40), new(6, 41)), lambda: px.gated(new(6, 40), new(6, 40).half()), lambda: px.gated(new(6, 40), keep="x"),
        lambda: px.gated_grad(new(6, 40), kept(), new(6, 40)), lambda: px.gated_grad(new(6, 40), new(6, 40), kept()), lambda: px.gated_grad(new(6, 40), kept(), kept(form="e4m3")),
        lambda: px.gated_grad(new(6, 40), kept(N=5)), lambda: px.gated_grad(new(6, 40), new(6, 41)), lambda: px.gated_grad(new(6, 40), new(6, 40), new(6, 40), out=new(6, 79))]

@@ -232,6 +232,23 @@ def test_strides_shapes_and_what_is_needed():
             assert t is None or torch.equal(t, getattr(want, name))
 
 
+def test_a_norm_alone_in_another_type():
+    """The first edge of a stack whose residual stream is in fp32: no branch, rows in 16 bits."""
+    import paper_2008_12260_amd as px
+    for dtype in (BF16, F16):
+        for form in (None, "i8"):
+            case = Case(21, 136, F32, dtype, branch=False).forward()
+            y, rows, state = px.block_edge(case.x, before=case.before, rows_dtype=dtype, keep=form)
+            assert y is case.x and rows.dtype == dtype and state.x_dtype == F32 and state.dtype == dtype
+            near(rows, case.h, case.h_size)
+            grads = px.block_edge_grad(case.y_grad, case.rows_grad, state, y=None if form else y, before=case.before)
+            n = decoded(*state.y_kept).cuda() if form else (y.double() - state.y_stats[:, :1].double()) * state.y_stats[:, 1:].double()
+            want = case.backward(n, None, state)
+            assert grads.x.dtype == F32 and grads.branch is None
+            near(grads.x, *want["x"], 2 * E)
+            near(grads.before_weight, *want["before_weight"], E_SUMS)
+
+
 def test_in_place_through_the_library():
     """y over x, and the gradient of x over that of y, by the C ABI."""
     import ctypes
