@@ -764,7 +764,7 @@ int pollux_block_edge_grad(const pollux_edge_dims *dims, /* host */
  * A gated activation: rows = act(gate) * up (up NULL: act(gate)), and the gradients from that of its rows,
  *   gate_grad = rows_grad * up * act'(gate),  up_grad = rows_grad * act(gate),
  * from the inputs or from what is kept of them.  act: silu g / (1 + exp(-g)), gelu g Phi(g), or gelu with 1/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))
- * in Phi's place; each is held to 0 where that factor is.  With a form the forward call keeps gate and up in 8 bits, and the backward call takes values (in the places
+ * in Phi's place; each is 0 where that factor is, and the factor may count as 0 where it is below 2^-126.  With a form the forward call keeps gate and up in 8 bits, and the backward call takes values (in the places
  * of gate and up) and scales.  Backward, `rows` are formed again from what it has, for the gradient of the weights behind them.  Any output of the backward call may be NULL.
  * Outputs and inputs must not overlap.
  * Limits: 0 <= N <= 2^24, 1 <= F <= 2^19, strides below 2^20 (0: F).  No workspace.

@@ -230,8 +230,15 @@ def run(job, m0=8, m_max=64, Gm=16, Gs=4, rounds=3, iterations=12, on_round=None
 
 
 if __name__ == "__main__":
+    import argparse
+
     def report(state, more):
         m, s, phi, theta = state.choices[-1]
         print(f"loss {np.mean(state.losses[-8:]):.3f}  phi {phi:.0f}  T_grad = {1e3 * theta[0]:.2f} ms + {1e6 * theta[1]:.1f} us m "
               f"(rmsle {more['rmsle']:.3f})  next m = {m}, s = {s}", flush=True)
-    run(Job(), rounds=6, iterations=20, on_round=report)
+    options = argparse.ArgumentParser(description="A small job trained at the batch sizes that the goodput model chooses.")
+    options.add_argument("--blocks", type=int, default=0, help="residual blocks (0: one bare layer)")
+    options.add_argument("--kept", choices=("i8", "e4m3", "none"), default="i8", help="how the blocks remember what their backward pass needs")
+    options.add_argument("--memory", type=int, help="bytes that a micro-batch may remember, which bound the batch size")
+    chosen = options.parse_args()
+    run(Job(blocks=chosen.blocks, kept=None if chosen.kept == "none" else chosen.kept), rounds=6, iterations=20, on_round=report, memory=chosen.memory)

@@ -4,8 +4,8 @@
 //   a = act(g) u;   dg = da u act'(g),  du = da act(g),  with g and u as they are or as 8 bits hold them
 //
 // Eight neighbouring elements a thread, four threads a group of 32; the threads of a launch walk the rows' groups of eight in order, whatever the
-// rows' length, so that short rows fill wavefronts as long ones do.  All are bound by memory: in bfloat16 16384 x 8192 kept as i8 in 71 to 87 us and restored in 66 (4.7 to 5.7 and 6.2 TB/s), 8192 x 16384
-// of silu with both inputs kept 200 to 217, its gradients and rows from them 254 to 264 (5.0 to 5.4, 5.1 to 5.3 TB/s).
+// rows' length, so that short rows fill wavefronts as long ones do.  All are bound by memory: in bfloat16 16384 x 8192 kept as i8 in 72 to 87 us and restored in 66 (4.7 to 5.7 and 6.2 TB/s), 8192 x 16384
+// of any of the three activations 147 us, with both inputs kept 210 (5.5 and 5.1 TB/s), gradients and rows from what is kept 257 (5.2).
 
 #include "pollux_host.h"
 #include "pollux_kept.h"
@@ -50,8 +50,7 @@ __global__ __launch_bounds__(kThreads) void keep_rows(const E *rows, int64_t ld,
     const int64_t width = kept_width(D);
     for (Walk at(N, (int)(width / kVec)); at.there(); at.next()) {
         const int c = at.group * kVec;
-        const f32x8 v = load8f(rows + at.row * ld + c, D - c);
-        keep8(form, v, values + at.row * width + c, scales + (at.row * width + c) / kKeptGroup, true);
+        keep_loaded(form, load8(rows + at.row * ld + c, D - c), values + at.row * width + c, scales + (at.row * width + c) / kKeptGroup);
     }
 #endif
 }
@@ -70,19 +69,47 @@ __global__ __launch_bounds__(kThreads) void restore_rows(const uint8_t *values, 
 }
 
 #ifdef __HIP_DEVICE_COMPILE__
+// exp(x) and 1 / x.  Of results of 16 bits by the hardware's functions as they are, within 2^-23 of themselves and 2^-24 |x| for x's product with log2 e: vector operations bound these kernels otherwise (8192 x 16384
+// in bfloat16 with both inputs kept, silu 229 us and gelu 262 with the library's, vector units 0.97 busy).
+template <class E>
+__device__ __forceinline__ float exp_of(float x)
+{
+    return sizeof(E) == 2 ? __builtin_amdgcn_exp2f(x * 1.44269504088896340736f) : expf(x);
+}
+template <class E>
+__device__ __forceinline__ float over(float x)
+{
+    return sizeof(E) == 2 ? __builtin_amdgcn_rcpf(x) : 1.f / x;
+}
+
+// a b, 0 where either is 0.
+__device__ __forceinline__ float times(float a, float b)
+{
+    float c;
+    asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(c) : "v"(a), "v"(b));
+    return c;
+}
+
 // An activation and its derivative.  Each is g p with p from 0 to 1; where p, or what is left of 1, is 0, so are the products with it, whatever g is.
 struct Activated {
     float value, slope;
 };
-template <int ACT>
+template <class E, int ACT>
 __device__ __forceinline__ Activated activated(float g)
 {
     Activated a;
     if constexpr (ACT == PX_ACT_GELU) {
-        // p = Phi(g), from the side on which it is small
-        const float p = 0.5f * erfcf(g * -0.70710678118654752440f), density = expf(-0.5f * g * g) * 0.39894228040143267794f;
-        a.value = p == 0.f ? 0.f : g * p;
-        a.slope = density == 0.f ? p : fmaf(g, density, p);
+        // p = Phi(g) from the side on which it is small: erfc(z) = t exp(P(t)) exp(-z^2), t = 1 / (1 + z / 2), P the Chebyshev fit of Numerical Recipes (second edition, 6.2), within 1.2e-7 of itself for
+        // every z >= 0;  z^2 = g^2 / 2 is the density's exponent too
+        constexpr float c[10] = {-1.26551223f, 1.00002368f, 0.37409196f, 0.09678418f, -0.18628806f, 0.27886807f, -1.13520398f, 1.48851587f, -0.82215223f, 0.17087277f};
+        const float z = fabsf(g) * 0.70710678118654752440f, t = over<E>(fmaf(z, 0.5f, 1.f));
+        float fit = c[9];
+#pragma unroll
+        for (int i = 8; i >= 0; --i) fit = fmaf(fit, t, c[i]);
+        const float bell = exp_of<E>(-0.5f * g * g), tail = 0.5f * t * exp_of<E>(fit) * bell, density = bell * 0.39894228040143267794f;
+        const float p = g < 0.f ? tail : 1.f - tail;
+        a.value = times(g, p);
+        a.slope = p + times(g, density);
     } else {
         float inner = g, by = 1.f;
         if constexpr (ACT == PX_ACT_GELU_TANH) {
@@ -92,10 +119,12 @@ __device__ __forceinline__ Activated activated(float g)
             inner = k * g * fmaf(0.044715f, square, 1.f);
             by = k * fmaf(3 * 0.044715f, square, 1.f);
         }
-        const float e = expf(-fabsf(inner)), r = 1.f / (1.f + e), small = e * r;           // both sides of p from what is below 1
-        const float p = inner < 0.f ? small : r, pq = r * small;
-        a.value = p == 0.f ? 0.f : g * p;
-        a.slope = pq == 0.f ? p : fmaf(g * pq, by, p);
+        const float e = exp_of<E>(-fabsf(inner)), r = over<E>(1.f + e), small = e * r;           // both sides of p from what is below 1
+        const float p = inner < 0.f ? small : r;
+        float more = times(g, r * small);
+        if constexpr (ACT == PX_ACT_GELU_TANH) more = times(more, by);
+        a.value = times(g, p);
+        a.slope = p + more;
     }
     return a;
 }
@@ -120,19 +149,21 @@ __global__ __launch_bounds__(kThreads) void gated_rows(const GatedArgs A)
     const int64_t width = kept_width(A.F);
     for (Walk at(A.N, (int)(width / kVec)); at.there(); at.next()) {
         const int c = at.group * kVec, left = A.F - c;
-        const f32x8 g = load8f((const E *)A.gate + at.row * A.gate_stride + c, left);
-        f32x8 u, a;
-        if (A.up) u = load8f((const E *)A.up + at.row * A.up_stride + c, left);
+        const auto gate = load8((const E *)A.gate + at.row * A.gate_stride + c, left);
+        typename Eight<E>::type up = {};
+        if (A.up) up = load8((const E *)A.up + at.row * A.up_stride + c, left);
+        const f32x8 g = __builtin_convertvector(gate, f32x8), u = __builtin_convertvector(up, f32x8);
+        f32x8 a;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const float v = activated<ACT>(g[i]).value;
+            const float v = activated<E, ACT>(g[i]).value;
             a[i] = A.up ? v * u[i] : v;
         }
         store8f((E *)A.rows + at.row * A.rows_stride + c, left, a);
         if (A.form) {
             const int64_t to = at.row * width + c;
-            keep8(A.form, g, A.gate_values + to, A.gate_scales + to / kKeptGroup, true);
-            if (A.up) keep8(A.form, u, A.up_values + to, A.up_scales + to / kKeptGroup, true);
+            keep_loaded(A.form, gate, A.gate_values + to, A.gate_scales + to / kKeptGroup);
+            if (A.up) keep_loaded(A.form, up, A.up_values + to, A.up_scales + to / kKeptGroup);
         }
     }
 #endif
@@ -161,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void gated_grads(const GatedArgs A)
         f32x8 dg, du, a;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const Activated v = activated<ACT>(g[i]);
+            const Activated v = activated<E, ACT>(g[i]);
             dg[i] = d[i] * u[i] * v.slope;
             du[i] = d[i] * v.value;
             a[i] = v.value * u[i];

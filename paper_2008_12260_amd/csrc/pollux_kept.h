@@ -9,6 +9,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/pollux.h"
 #include "pollux_rows.h"
 
@@ -99,14 +101,40 @@ __device__ __forceinline__ uint32_t group_size(f32x8 v)
     return max(m, of_lane<kXor2>(m));
 }
 
-// Four neighbouring lanes keep a group, eight values each: at `codes` the lane's eight, at `scale` the group's byte (by the first of them).
-__device__ __forceinline__ void keep8(int form, f32x8 v, uint8_t *codes, uint8_t *scale, bool there)
+// The same of elements as they came from memory: of 16 bits two at a time, as whole numbers, whose order their sizes' is.
+template <class V>
+__device__ __forceinline__ uint32_t loaded_size(V v)
 {
-    const uint32_t byte = kept_byte(form, group_size(v));
+    if constexpr (sizeof(V) == 32) {
+        return group_size(__builtin_convertvector(v, f32x8));
+    } else {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        const u32x4 w = __builtin_bit_cast(u32x4, v) & 0x7fff7fffu;
+        auto larger = [](uint32_t a, uint32_t b) { return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b))); };
+        uint32_t m = larger(larger(w[0], w[1]), larger(w[2], w[3]));
+        m = larger(m, of_lane<kXor1>(m));
+        m = larger(m, of_lane<kXor2>(m));
+        const uint16_t bits = (uint16_t)max(m & 0xffffu, m >> 16);
+        if constexpr (std::is_same<V, typename Eight<__bf16>::type>::value) return (uint32_t)bits << 16;
+        else return __float_as_uint((float)__builtin_bit_cast(_Float16, bits));
+    }
+}
+
+// Four neighbouring lanes keep a group, eight values each: at `codes` the lane's eight, at `scale` the group's byte (by the first of them).
+__device__ __forceinline__ void keep8_of(int form, f32x8 v, uint32_t size, uint8_t *codes, uint8_t *scale, bool there)
+{
+    const uint32_t byte = kept_byte(form, size);
     const u32x2 out = encode8(form, v, byte);
     if (!there) return;
     *(u32x2 *)codes = out;
     if ((threadIdx.x & 3) == 0) *scale = (uint8_t)byte;
+}
+__device__ __forceinline__ void keep8(int form, f32x8 v, uint8_t *codes, uint8_t *scale, bool there) { keep8_of(form, v, group_size(v), codes, scale, there); }
+template <class V>
+__device__ __forceinline__ void keep_loaded(int form, V v, uint8_t *codes, uint8_t *scale)
+{
+    keep8_of(form, __builtin_convertvector(v, f32x8), loaded_size(v), codes, scale, true);
 }
 
 #endif
