@@ -124,10 +124,18 @@ def _kept(k, name, rows=None, width=None):
     return Kept(values, scales, D, form)
 
 
-def _new_kept(N, D, form, device):
+def _new_kept(rows, D, form):
+    """Of rows on the same device."""
     import torch
-    W = -(-D // _GROUP) * _GROUP
-    return Kept(torch.empty((N, W), dtype=torch.uint8, device=device), torch.empty((N, W // _GROUP), dtype=torch.uint8, device=device), D, form)
+    N, W = rows.shape[0], -(-D // _GROUP) * _GROUP
+    return Kept(rows.new_empty((N, W), dtype=torch.uint8), rows.new_empty((N, W // _GROUP), dtype=torch.uint8), D, form)
+
+
+# New tensors are asked of one that is there: a microsecond less than torch.empty with the same attributes.
+def _like(t):
+    """Contiguous, of t's shape and type."""
+    import torch
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _vectors(D, **named):
@@ -156,7 +164,7 @@ def keep(rows, form="i8", stream=None):
             raise ValueError("form is None: 'i8' or 'e4m3' is wanted")
         rows, ld = _matrix(rows, "rows")
         N, D = rows.shape
-        kept = _new_kept(N, D, form, rows.device)
+        kept = _new_kept(rows, D, form)
         _check(_px.lib().pollux_keep(_dims(_px.KeepDims, None, N, D, type_, code, 0, ld), rows.data_ptr(), kept.values.data_ptr(), kept.scales.data_ptr(),
                                      _px._stream_handle(stream)), "pollux_keep")
     return kept
@@ -171,7 +179,7 @@ def restore(kept, dtype=None, out=None, stream=None):
         kept = _kept(kept, "kept")
         N, D = kept.values.shape[0], kept.width
         if out is None:
-            out = torch.empty((N, D), dtype=torch.bfloat16 if dtype is None else dtype, device=kept.values.device)
+            out = kept.values.new_empty((N, D), dtype=torch.bfloat16 if dtype is None else dtype)
         rows, ld = _written(out, "out", (N, D), out.dtype if dtype is None else dtype)
         _check(_px.lib().pollux_restore(_dims(_px.KeepDims, None, N, D, _type(rows, "rows"), _form(kept.form), 0, ld), kept.values.data_ptr(), kept.scales.data_ptr(),
                                         rows.data_ptr(), _px._stream_handle(stream)), "pollux_restore")
@@ -207,7 +215,7 @@ def kept_grad(kept, rows_grad, weight=None, bias=None, weight_grad=None, accumul
         if accumulate and weight_grad is None:
             raise ValueError("accumulate needs a weight_grad to add to")
         if weight_grad is None:
-            weight_grad = torch.empty((M, D), dtype=rows.dtype, device=rows.device)
+            weight_grad = rows.new_empty((M, D))
         out, out_ld = _written(weight_grad, "weight_grad", (M, D), rows.dtype)
         if out.data_ptr() & 15:
             raise ValueError("weight_grad needs a base aligned to 16 bytes")
@@ -225,6 +233,8 @@ def _gate(gate, N, D):
         return None, 0
     if gate.dim() == 0 or gate.shape[-1] != D:
         raise ValueError(f"gate has shape {tuple(gate.shape)}: rows of {D} are wanted")
+    if gate.dim() == 1:
+        return gate.contiguous(), 0
     flat = gate.reshape(-1, D).contiguous()
     G = flat.shape[0]
     if G != 1 and (G == 0 or N % G):
@@ -255,17 +265,16 @@ def block_edge(x, branch=None, gate=None, after=None, before=None, residual=1.0,
         shape, dtype = x.shape, (x.dtype if rows_dtype is None else rows_dtype) if branch is None else branch.dtype
         x_rows, x_ld = _matrix(x, "x")
         N, D = x_rows.shape
-        device = x_rows.device
         branch_rows, branch_ld = (None, 0) if branch is None else _matrix(branch, "branch")
         gate_rows, span = _gate(gate, N, D)
         weight_dtype, (w_a, b_a, w_b, b_b) = _vectors(D, after_weight=after and after[0], after_bias=after and after[1], before_weight=before and before[0],
                                                       before_bias=before and before[1])
-        y = x if branch is None else torch.empty(shape, dtype=x.dtype, device=device)
-        rows = None if before is None else torch.empty(shape, dtype=dtype, device=device)
-        branch_stats = None if after is None else torch.empty((N, 2), dtype=torch.float32, device=device)
-        y_stats = None if before is None else torch.empty((N, 2), dtype=torch.float32, device=device)
-        branch_kept = _new_kept(N, D, keep, device) if form and (after is not None or gate is not None) else None
-        y_kept = _new_kept(N, D, keep, device) if form and before is not None else None
+        y = x if branch is None else _like(x)
+        rows = None if before is None else _like(branch) if branch is not None else x.new_empty(shape, dtype=dtype)
+        branch_stats = None if after is None else x.new_empty((N, 2), dtype=torch.float32)
+        y_stats = None if before is None else x.new_empty((N, 2), dtype=torch.float32)
+        branch_kept = _new_kept(x_rows, D, keep) if form and (after is not None or gate is not None) else None
+        y_kept = _new_kept(x_rows, D, keep) if form and before is not None else None
         flags = (_px.PX_EDGE_AFTER if after is not None else 0) | (_px.PX_EDGE_BEFORE if before is not None else 0) | (_px.PX_EDGE_CENTRED if centred else 0)
         eps, residual, scale = float(eps), float(residual), float(scale)
         dims = _dims(_px.EdgeDims, _zeros(eps, residual, scale), N, D, x_type, _type_of(dtype), _type_of(weight_dtype), _type_of(gate_rows.dtype if gate_rows is not None else None), form, flags,
@@ -336,9 +345,9 @@ def block_edge_grad(y_grad, rows_grad, state, y=None, branch=None, gate=None, af
             raise ValueError(f"need names {sorted(need)}: some of {_ALL} are wanted")
 
         def like(t, part):
-            return None if t is None or part not in need else torch.empty(t.shape, dtype=t.dtype, device=device)
-        x_grad = torch.empty(shape, dtype=state.x_dtype, device=device) if "x" in need else None
-        branch_grad = torch.empty(shape, dtype=state.dtype, device=device) if state.branched and "branch" in need else None
+            return None if t is None or part not in need else _like(t)
+        x_grad = model.new_empty(shape, dtype=state.x_dtype) if "x" in need else None
+        branch_grad = model.new_empty(shape, dtype=state.dtype) if state.branched and "branch" in need else None
         gate_grad = like(gate, "gate")
         after_grads = like(w_a, "after"), like(b_a, "after")
         before_grads = like(w_b, "before"), like(b_b, "before")
@@ -395,10 +404,9 @@ def gated(gate, up=None, act="silu", keep=None, stream=None):
         gate_rows, gate_ld = _matrix(gate, "gate")
         up_rows, up_ld = (None, 0) if up is None else _matrix(up, "up")
         N, F = gate_rows.shape
-        device = gate_rows.device
-        rows = torch.empty(gate.shape, dtype=gate.dtype, device=device)
-        gate_kept = _new_kept(N, F, keep, device) if form else None
-        up_kept = _new_kept(N, F, keep, device) if form and up is not None else None
+        rows = _like(gate)
+        gate_kept = _new_kept(gate_rows, F, keep) if form else None
+        up_kept = _new_kept(gate_rows, F, keep) if form and up is not None else None
         dims = _dims(_px.GatedDims, None, N, F, type_, _ACTS[act], form, 0, gate_ld, up_ld, 0, 0, 0, 0)
         ptr = _px._ptr
         _check(_px.lib().pollux_gated(dims, gate_rows.data_ptr(), ptr(up_rows), rows.data_ptr(), *((None, None) if gate_kept is None else map(ptr, gate_kept[:2])),
@@ -420,7 +428,6 @@ def gated_grad(rows_grad, gate, up=None, act="silu", want_rows=False, out=None, 
         shape, dtype = rows_grad.shape, rows_grad.dtype
         d, d_ld = _matrix(rows_grad, "rows_grad")
         N, F = d.shape
-        device = d.device
         gate_scales = up_scales = None
         gate_ld = up_ld = 0
         form = _px.PX_KEPT_NONE
@@ -440,9 +447,9 @@ def gated_grad(rows_grad, gate, up=None, act="silu", want_rows=False, out=None, 
             up_rows, up_ld = (None, 0) if up is None else _matrix(up, "up")
         halves = 1 if up is None else 2
         if out is None:
-            out = torch.empty((*shape[:-1], halves * F), dtype=dtype, device=device)
+            out = d.new_empty((*shape[:-1], halves * F))
         both, ld = _written(out, "out", (*shape[:-1], halves * F), dtype)
-        rows = torch.empty(shape, dtype=dtype, device=device) if want_rows else None
+        rows = _like(rows_grad) if want_rows else None
         dims = _dims(_px.GatedDims, None, N, F, type_, _ACTS[act], form, 0, gate_ld, up_ld, 0, d_ld, ld, ld)
         ptr = _px._ptr
         _check(_px.lib().pollux_gated_grad(dims, d.data_ptr(), gate_rows.data_ptr(), ptr(gate_scales), ptr(up_rows), ptr(up_scales), both.data_ptr(),
