@@ -196,7 +196,9 @@ def choose(job_params, m_grid, Gs):
 def run(job, m0=8, m_max=64, Gm=16, Gs=4, rounds=3, iterations=12, on_round=None, memory=None):
     """`memory`: bytes that a micro-batch may remember; they bound m as m_max does.  `rounds` times: `iterations` iterations at (m, s), and one at a few others so that the throughput model sees more than one point;
     then the noise scale averaged over the round, theta_sys fitted to all records, and the next (m, s).  Returns the AgentState."""
-    if memory is not None and job.blocks:
+    if memory is not None:
+        if not job.blocks:
+            raise ValueError("memory bounds what residual blocks remember: the job has none")
         m_max = min(m_max, memory // job.bytes_per_example())
         if m_max < m0:
             raise ValueError(f"{memory} bytes hold {m_max} examples: m0 = {m0} are wanted at least")

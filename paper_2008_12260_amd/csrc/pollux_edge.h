@@ -24,7 +24,6 @@ struct EdgeKernelArgs {
 
 constexpr int kMostWaves = 16;
 
-
 // v summed over the `team` lanes that a lane belongs to: 4 to 64.
 __device__ __forceinline__ float over_lanes(float v, int team)
 {

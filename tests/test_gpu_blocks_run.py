@@ -63,6 +63,8 @@ def test_memory_bounds_the_batch():
         chosen = []
         state = run(jobs[kept], m0=8, m_max=32, rounds=1, iterations=4, memory=memory, on_round=lambda s, more: chosen.append(int(more["m_grid"].max())))
         assert chosen == [most] and all(m <= most for m, _, _ in state.records)
+    with pytest.raises(ValueError, match="has none"):
+        run(Job(V=300, D=64, length=16), memory=memory)
     with pytest.raises(ValueError, match="bytes hold"):
         run(jobs[None], m0=8, memory=jobs[None].bytes_per_example() * 7)
 
@@ -143,3 +145,99 @@ def test_a_function_made_of_the_calls_has_the_gradients_autograd_gives():
     net(plain, lambda a, b: torch.nn.functional.gelu(a) * b, *want).backward()
     for a, b in zip(got, want):
         assert float((a.grad.double() - b.grad).abs().max()) <= 2.0 ** -12 * float(b.grad.abs().max())
+
+
+def test_offsets_past_32_bits():
+    """Rows whose elements, and whose bytes in 8 bits, lie beyond 2^32: what is done to the last ones is what is done to them alone."""
+    import paper_2008_12260_amd as px
+    last, D, N = 40, 16384, 300000
+    assert (N - last) * D > 1 << 32
+    g = torch.Generator("cuda").manual_seed(1)
+    few = [torch.randn((last, D), generator=g, device="cuda").bfloat16() for _ in range(4)]
+    many = [torch.zeros((N, D), dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    for big, small in zip(many, few):
+        big[-last:] = small
+    w = 1.0 + 0.1 * torch.randn(D, generator=g, device="cuda")
+    edge = dict(after=px.Norm(w), before=px.Norm(w), gate=w)
+
+    def same(a, b):
+        assert torch.equal(a[-last:], b)
+    y, rows, state = px.block_edge(many[0], many[1], **edge, keep="i8")
+    y_few, rows_few, state_few = px.block_edge(few[0], few[1], **edge, keep="i8")
+    same(y, y_few)
+    same(rows, rows_few)
+    for a, b in ((state.y_kept, state_few.y_kept), (state.branch_kept, state_few.branch_kept)):
+        same(a.values, b.values)
+        same(a.scales, b.scales)
+    same(px.restore(state.y_kept), px.restore(state_few.y_kept))
+    del y, rows
+    a, b = (px.block_edge_grad(t[2], t[3], s, **edge, need=("x", "branch")) for t, s in ((many, state), (few, state_few)))
+    same(a.x, b.x)
+    same(a.branch, b.branch)
+    del a, state
+    a, b = px.gated(many[0], many[1], keep="e4m3"), px.gated(few[0], few[1], keep="e4m3")
+    same(a[0], b[0])
+    same(a[1].values, b[1].values)
+    a, b = px.gated_grad(many[2], *a[1:]), px.gated_grad(few[2], *b[1:])
+    same(a[0], b[0])
+    same(a[1], b[1])
+
+
+def test_a_gradient_over_kept_rows_past_32_bits():
+    """Whole numbers, so that every sum is exact in whatever order."""
+    import paper_2008_12260_amd as px
+    N, D, last = 600000, 8192, 100
+    assert (N - last) * D > 1 << 32
+    g = torch.Generator("cuda").manual_seed(2)
+    values = torch.zeros((N, D), dtype=torch.uint8, device="cuda")
+    values[-last:] = torch.randint(0, 8, (last, D), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.full((N, D // 32), 127, dtype=torch.uint8, device="cuda")
+    d = torch.randint(-3, 4, (N, 64), generator=g, device="cuda").bfloat16()
+    want = d[-last:].double().t() @ values[-last:].double()
+    assert torch.equal(px.kept_grad(px.Kept(values, scales, D, "i8"), d).double(), want.bfloat16().double())
+
+
+def test_many_rows_of_few_elements():
+    """More rows than the chip has under way at once, in every call: as in parts."""
+    import paper_2008_12260_amd as px
+    g = torch.Generator("cuda").manual_seed(3)
+    for N, D in ((400003, 8), (200001, 40)):
+        x, z, d, dh = (torch.randn((N, D), generator=g, device="cuda").bfloat16() for _ in range(4))
+        w = torch.randn(D, generator=g, device="cuda")
+        edge = dict(after=px.Norm(w), before=px.Norm(w, w), gate=w)
+        y, rows, state = px.block_edge(x, z, **edge, keep="i8")
+        grads = px.block_edge_grad(d, dh, state, **edge)
+        a = px.gated(x, z, keep="i8")
+        for at in range(0, N, 70001):
+            to = min(N, at + 70001)
+            y2, rows2, state2 = px.block_edge(x[at:to], z[at:to], **edge, keep="i8")
+            assert torch.equal(y[at:to], y2) and torch.equal(rows[at:to], rows2) and torch.equal(state.y_kept.values[at:to], state2.y_kept.values)
+            grads2 = px.block_edge_grad(d[at:to], dh[at:to], state2, **edge)
+            assert torch.equal(grads.x[at:to], grads2.x) and torch.equal(grads.branch[at:to], grads2.branch)
+            b = px.gated(x[at:to], z[at:to], keep="i8")
+            assert torch.equal(a[0][at:to], b[0]) and torch.equal(a[1].values[at:to], b[1].values) and torch.equal(a[2].scales[at:to], b[2].scales)
+        # sums over all rows: each chain is at most N / 1024 + 100 long
+        n = px.restore(state.y_kept, torch.float32).double()
+        for got, terms in ((grads.before_weight, dh.double() * n), (grads.before_bias, dh.double())):
+            assert bool(((got.double() - terms.sum(0)).abs() <= (N / 1024 + 102) * 2.0 ** -24 * terms.abs().sum(0) + 2.0 ** -24 * terms.sum(0).abs()).all())
+
+
+def test_two_streams_at_once():
+    """The same inputs in calls that overlap, each with scratch memory of its own."""
+    import paper_2008_12260_amd as px
+    g = torch.Generator("cuda").manual_seed(4)
+    x, z, d, dh = (torch.randn((4000, 1000), generator=g, device="cuda").bfloat16() for _ in range(4))
+    w = torch.randn(1000, generator=g, device="cuda")
+    edge = dict(after=px.Norm(w, w), before=px.Norm(w, w), gate=torch.randn((8, 1000), generator=g, device="cuda"), centred=True)
+
+    def all_of(stream=None):
+        y, rows, state = px.block_edge(x, z, **edge, keep="e4m3", stream=stream)
+        return [y, rows, *px.block_edge_grad(d, dh, state, **edge, stream=stream), px.kept_grad(state.y_kept, dh, w, w, stream=stream)]
+    want = all_of()
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    got = [[all_of(s) for s in sides] for _ in range(5)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for one in pair:
+            assert all(torch.equal(a, b) for a, b in zip(one, want))

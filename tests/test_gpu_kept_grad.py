@@ -98,6 +98,19 @@ def test_what_is_not_finite_stays_in_its_columns(dtype, form):
     assert bool(torch.isnan(got[7]).all()) and torch.equal(got[:7], want[:7]) and torch.equal(got[8:], want[8:])
 
 
+@pytest.mark.parametrize("form", FORMS)
+def test_the_smallest_and_the_largest_scales(form):
+    """Elements from 2^-124 to 2^127, and gradients that bring the products back to 1: scales whose byte is 0 (2^-127, no normal number) to the largest, in the types that hold them."""
+    import paper_2008_12260_amd as px
+    g = torch.Generator("cuda").manual_seed(7)
+    for dtype in (torch.float32, torch.bfloat16):
+        for e in (-123, -120, -118, -100, 100, 118, 125):
+            x = (1.0 + torch.rand((200, 96), generator=g, device="cuda")) * 2.0 ** e
+            kept, d = px.keep(x, form), (torch.randn((200, 40), generator=g, device="cuda") * 2.0 ** (-e if abs(e) < 110 else -e // 2)).to(dtype)
+            assert e > -118 or int(kept.scales.min()) <= 3
+            check(px.kept_grad(kept, d), kept, d)
+
+
 def test_no_rows_give_zeros():
     import paper_2008_12260_amd as px
     for dtype in TYPES:
