@@ -8,7 +8,7 @@
 // workgroups' in order.  With one gate for all rows, sums of g n_z and g are all that the last three need.  With a gate for each span of rows, they are taken over a
 // span, weighted with its gate at its end, and are the gate's gradient there, or, where the chunk's first or last row cuts the span, parts of it.  Bound by memory: 4 rows read, 2 written, 10 bytes
 // an element of 16 bits with the normalised rows kept in 8: 16384 x 4096 145 us, 4.6 TB/s (a copy moves 4.6 to 4.8), and 6 for the join; from rows of 16 bits 170.  Rows of more than 8192 have
-// more sums than registers and go by way of scratch memory: 4096 x 16384 361 us.
+// more sums than registers: two of them wait in LDS, and some of the rest goes by way of scratch memory: 4096 x 16384 306 us (364 without LDS), with a gate a sequence 418 (1344).
 
 #include <type_traits>
 
@@ -39,6 +39,17 @@ __global__ __launch_bounds__(MOST) void edge_grads(const EdgeKernelArgs A)
     constexpr bool kReload = C > 1;
     f32x8 w_b[C], by[C], sum_pn[C], sum_p[C], sum_tn[C], sum_t[C], span_gn[C], span_g[C];
     const f32x8 zeros = {};
+    // (and the sums of products wait in LDS: 64 bytes a sum and thread, in and out once a row, beside 160 from memory)
+    constexpr bool kHeld = C > 1;
+    extern __shared__ float4 held[];
+    auto recall = [&](int which, int k) {
+        const float4 a = held[(which * C + k) * 2 * blockDim.x + threadIdx.x], b = held[((which * C + k) * 2 + 1) * blockDim.x + threadIdx.x];
+        return f32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    };
+    auto hold = [&](int which, int k, f32x8 v) {
+        held[(which * C + k) * 2 * blockDim.x + threadIdx.x] = make_float4(v[0], v[1], v[2], v[3]);
+        held[((which * C + k) * 2 + 1) * blockDim.x + threadIdx.x] = make_float4(v[4], v[5], v[6], v[7]);
+    };
     auto gate_of = [&](int k, int64_t row) { return parameters(A.p.gate, d.gate_type, row * D + c[k], left[k], 1.f) * d.scale; };
     auto after_weight = [&](int k) { return within(parameters(after ? A.p.after_weight : nullptr, d.weight_type, c[k], left[k], 1.f), left[k]); };
 #pragma unroll
@@ -48,6 +59,10 @@ __global__ __launch_bounds__(MOST) void edge_grads(const EdgeKernelArgs A)
         if (!kReload) w_b[k] = parameters(A.p.before_weight, d.weight_type, c[k], left[k], 1.f);
         if (!kReload && BRANCH && !SPANS) by[k] = gate_of(k, 0) * after_weight(k);
         sum_pn[k] = sum_p[k] = sum_tn[k] = sum_t[k] = span_gn[k] = span_g[k] = zeros;
+        if (kHeld) {
+            hold(0, k, zeros);
+            hold(1, k, zeros);
+        }
     }
     // with spans a team's rows are neighbours, else as far apart as there are teams: the chip is then at neighbouring rows at any time
     const int N = (int)d.N, chunk = blockIdx.x * teams + first, step = SPANS ? 1 : gridDim.x * teams;
@@ -126,7 +141,8 @@ __global__ __launch_bounds__(MOST) void edge_grads(const EdgeKernelArgs A)
                 g[k] = w.dh[k].of_rows();
                 n[k] = w.y[k].normalised(d.form, w.stats_y);
                 if (before_sums) {
-                    sum_pn[k] = fma8(g[k], n[k], sum_pn[k]);
+                    if (kHeld) hold(0, k, fma8(g[k], n[k], recall(0, k)));
+                    else sum_pn[k] = fma8(g[k], n[k], sum_pn[k]);
                     if (PLAIN) sum_p[k] += g[k];
                 }
                 g[k] *= kReload ? parameters(A.p.before_weight, d.weight_type, c[k], left[k], 1.f) : w_b[k];
@@ -144,8 +160,9 @@ __global__ __launch_bounds__(MOST) void edge_grads(const EdgeKernelArgs A)
         for (int k = 0; k < C; ++k) {
             n[k] = has_z ? w.z[k].normalised(d.form, w.stats_z) : zeros;
             if (after_sums) {
-                f32x8 &to = SPANS ? span_gn[k] : sum_tn[k];
-                to = fma8(g[k], n[k], to);
+                if (SPANS) span_gn[k] = fma8(g[k], n[k], span_gn[k]);
+                else if (kHeld) hold(1, k, fma8(g[k], n[k], recall(1, k)));
+                else sum_tn[k] = fma8(g[k], n[k], sum_tn[k]);
                 if (PLAIN) (SPANS ? span_g[k] : sum_t[k]) += g[k];
             }
             g[k] *= kReload ? gate_of(k, SPANS ? span : 0) * after_weight(k) : by[k];
@@ -168,12 +185,19 @@ __global__ __launch_bounds__(MOST) void edge_grads(const EdgeKernelArgs A)
                     else store8f(A.ends + ((int64_t)chunk * 2 + (from >= begin ? 1 : 0)) * D + c[k], left[k], v);
                 }
                 const f32x8 gate = gate_of(k, span);
-                sum_tn[k] = fma8(gate, span_gn[k], sum_tn[k]);
+                if (kHeld) hold(1, k, fma8(gate, span_gn[k], recall(1, k)));
+                else sum_tn[k] = fma8(gate, span_gn[k], sum_tn[k]);
                 if (PLAIN) sum_t[k] = fma8(gate, span_g[k], sum_t[k]);
                 span_gn[k] = span_g[k] = zeros;
             }
         }
     }
+    if (kHeld)
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            sum_pn[k] = recall(0, k);
+            sum_tn[k] = recall(1, k);
+        }
     // the workgroup's sums: of teams within a wavefront by way of LDS, in their order
     __shared__ float rows[256][kVec + 1];
     auto leave = [&](f32x8(&v)[C], int part) {
@@ -268,7 +292,7 @@ template <class X, class E, int C>
 void launch_grads_of(const EdgePlan &p, const EdgeKernelArgs &a, hipStream_t stream)
 {
     const bool plain = a.p.before_bias_grad || a.p.after_bias || a.p.after_bias_grad, branch = a.p.branch || a.p.branch_values || a.p.branch_grad;
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(p.team * p.teams), 0, stream, a); };
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(p.team * p.teams), C > 1 ? 2 * C * kVec * 4 * p.team : 0, stream, a); };
     if (branch && a.d.span && C == 1 && p.team <= 512) plain ? launch(edge_grads<X, E, 1, true, true, true, 512>) : launch(edge_grads<X, E, 1, true, true, false, 512>);
     else if (branch && a.d.span) plain ? launch(edge_grads<X, E, C, true, true, true, 1024>) : launch(edge_grads<X, E, C, true, true, false, 1024>);
     else if (branch) plain ? launch(edge_grads<X, E, C, true, false, true, 1024>) : launch(edge_grads<X, E, C, true, false, false, 1024>);
