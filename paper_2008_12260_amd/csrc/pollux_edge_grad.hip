@@ -4,9 +4,9 @@
 //   t  = scale gate g,  q = t w_a,   branch_grad = r_z (q - [mean q] - n_z mean(q n_z))
 //   w_b' = sum rows_grad n_y,  b_b' = sum rows_grad,  w_a' = sum t n_z,  b_a' = sum t,  gate' = scale (w_a sum g n_z + b_a sum g) over the rows of its span
 //
-// A team goes through neighbouring rows (a chunk) and holds the sums over them in registers, fp32; a workgroup's go out once, and a second launch adds the
+// A team goes through some of the rows and holds the sums over them in registers, fp32; a workgroup's go out once, and a second launch adds the
 // workgroups' in order.  With one gate for all rows, sums of g n_z and g are all that the last three need.  With a gate for each span of rows, they are taken over a
-// span, weighted with its gate at its end, and are the gate's gradient there, or, where the chunk's first or last row cuts the span, parts of it.  Bound by memory: 4 rows read, 2 written, 10 bytes
+// span, weighted with its gate at its end, and are the gate's gradient there, or, where the team's first or last row cuts the span, parts of it.  Bound by memory: 4 rows read, 2 written, 10 bytes
 // an element of 16 bits with the normalised rows kept in 8: 16384 x 4096 145 us, 4.6 TB/s (a copy moves 4.6 to 4.8), and 6 for the join; from rows of 16 bits 170.  Rows of more than 8192 have
 // more sums than registers: two of them wait in LDS, and some of the rest goes by way of scratch memory: 4096 x 16384 306 us (364 without LDS), with a gate a sequence 418 (1344).
 

@@ -67,6 +67,22 @@ __global__ __launch_bounds__(S::kThreads) void kept_tiles(const KeptGradArgs A)
     const bool sums = A.slices > 1;
     const int group = sums || !kPairs ? 3 : 7;
     const bool whole = sums ? (A.D & 3) == 0 : (A.ld & group) == 0;
+    if (!sums && (A.weight || A.bias)) {
+        // (a lane's columns are its rows' all alike)
+        float rows[S::FN];
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) rows[j] = A.bias && at.first_n + j * 16 < A.M ? A.sums[at.first_n + j * 16] : 0.f;
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int m = min(at.first_m + 16 * i + r, A.D - 1);
+                const float w = parameter(A.weight, A.weight_type, m, 1.f), b = parameter(A.bias, A.weight_type, m, 0.f);
+#pragma unroll
+                for (int j = 0; j < S::FN; ++j) acc[i][j][r] = A.bias ? fmaf(rows[j], b, acc[i][j][r] * w) : acc[i][j][r] * w;
+            }
+    }
+    const bool plain = whole && !sums && !A.add && (t.m + 1) * S::BM <= A.D;
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
         const int n = at.first_n + j * 16;
@@ -82,28 +98,34 @@ __global__ __launch_bounds__(S::kThreads) void kept_tiles(const KeptGradArgs A)
             continue;
         }
         type *const to = (type *)A.out + (int64_t)n * A.ld;
-        const float rows = A.bias && n < A.M ? A.sums[n] : 0.f;
-        auto value = [&](int i, int r) {
-            const int m = min(at.first_m + 16 * i + r, A.D - 1);
-            float v = acc[i][j][r];
-            if (A.weight) v *= parameter(A.weight, A.weight_type, m, 1.f);
-            if (A.bias) v = fmaf(rows, parameter(A.bias, A.weight_type, m, 0.f), v);
-            return v;
-        };
         if constexpr (kPairs) {
 #pragma unroll
             for (int i = 0; i < S::FM; i += 2) {
-                const f32x4 first = {value(i, 0), value(i, 1), value(i, 2), value(i, 3)}, second = {value(i + 1, 0), value(i + 1, 1), value(i + 1, 2), value(i + 1, 3)};
                 const int m = wave_m + 16 * (i + pair.tile) + pair.row;
-                float v[8];
-                paired32(first, second, v);                // (all lanes change places, those past the last row too)
-                if (n < A.M) put<typename S::element>(to + m, v, A.D - m, whole, A.add);
+                // (lanes change places, those past the last row too)
+                if (plain) {
+                    const auto both = paired<typename S::element>(acc[i][j], acc[i + 1][j]);
+                    if (n < A.M) *(typename S::element::piece *)(to + m) = both;
+                } else {
+                    float both[8];
+                    paired32(acc[i][j], acc[i + 1][j], both);
+                    if constexpr (S::BM < 256) {
+                        // (at any alignment: 300 x 4100 x 4200 34 us where single elements take 62; tiles of 256 have no registers left for it)
+                        f32x8 v = {both[0], both[1], both[2], both[3], both[4], both[5], both[6], both[7]};
+                        if (n < A.M && m < A.D) {
+                            if (A.add) v += load8f(to + m, A.D - m);
+                            store8f(to + m, A.D - m, v);
+                        }
+                    } else if (n < A.M) {
+                        put<typename S::element>(to + m, both, A.D - m, whole, A.add);
+                    }
+                }
             }
         } else {
 #pragma unroll
             for (int i = 0; i < S::FM; ++i) {
                 const int m = at.first_m + 16 * i;
-                const float v[4] = {value(i, 0), value(i, 1), value(i, 2), value(i, 3)};
+                const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
                 if (n < A.M) put<typename S::element>(to + m, v, A.D - m, whole, A.add);
             }
         }
@@ -266,6 +288,8 @@ KeptGradPlan kept_grad_plan(const pollux_kept_grad_dims &d)
         for (int s = f32 ? 1 : 0; s < 3; ++s) {
             double cost = shape_cost(kKeptShape[s], d.D, d.M, (double)d.N / slices, slices, f32);
             if (slices > 1) cost += 4.0 + 4.0 * slices * d.M * d.D / 4.2e6;
+            // (tiles of 256 store rows that begin anywhere an element at a time)
+            else if (s == 0 && d.weight_grad_stride % 8 != 0) cost += 25.0 * ceil(ceil(d.D / 256.0) * ceil(d.M / 256.0) / 256);
             if (cost < least) least = cost, p.slices = slices, p.tiles = s;
         }
     }
