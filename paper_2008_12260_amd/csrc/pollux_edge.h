@@ -65,17 +65,7 @@ __device__ __forceinline__ void over_team(float (&v)[K], int team, float (*share
         for (int k = 0; k < K; ++k) v[k] += at[w][k];
 }
 
-// Eight parameters of one of the three types, or `none` where there is no array.
-__device__ __forceinline__ f32x8 parameters(const void *p, int type, int64_t at, int left, float none)
-{
-    f32x8 v;
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) v[i] = none;
-    if (!p) return v;
-    if (type == PX_TYPE_F32) return load8f((const float *)p + at, left);
-    if (type == PX_TYPE_BF16) return load8f((const __bf16 *)p + at, left);
-    return load8f((const _Float16 *)p + at, left);
-}
+// Eight parameters stored as one of the three types.
 __device__ __forceinline__ void store_parameters(void *p, int type, int64_t at, int left, f32x8 v)
 {
     if (type == PX_TYPE_F32) store8f((float *)p + at, left, v);

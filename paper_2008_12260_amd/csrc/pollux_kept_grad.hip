@@ -150,11 +150,11 @@ __global__ __launch_bounds__(kThreads) void join_slices(const KeptGradArgs A, co
         for (int s = 1; s < A.slices; ++s) v += load8f(from + s * one, left);
         if (A.weight || A.bias) {
             const float rows = A.bias ? A.sums[n] : 0.f;
+            v *= parameters(A.weight, A.weight_type, c, left, 1.f);
+            if (A.bias) {
+                const f32x8 b = parameters(A.bias, A.weight_type, c, left, 0.f);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                const int m = min(c + i, A.D - 1);
-                v[i] *= parameter(A.weight, A.weight_type, m, 1.f);
-                if (A.bias) v[i] = fmaf(rows, parameter(A.bias, A.weight_type, m, 0.f), v[i]);
+                for (int i = 0; i < kVec; ++i) v[i] = fmaf(rows, b[i], v[i]);
             }
         }
         type *const to = (type *)A.out + n * A.ld + c;

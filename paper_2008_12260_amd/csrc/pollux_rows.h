@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/pollux.h"
+
 namespace px {
 
 constexpr int kVec = 8;
@@ -69,6 +71,18 @@ template <class E>
 __device__ __forceinline__ void store8f(E *to, int64_t left, f32x8 v)
 {
     store8(to, left, __builtin_convertvector(v, typename Eight<E>::type));
+}
+
+// Eight parameters of one of the three types, or `none` where there is no array.
+__device__ __forceinline__ f32x8 parameters(const void *p, int type, int64_t at, int left, float none)
+{
+    f32x8 v;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = none;
+    if (!p) return v;
+    if (type == PX_TYPE_F32) return load8f((const float *)p + at, left);
+    if (type == PX_TYPE_BF16) return load8f((const __bf16 *)p + at, left);
+    return load8f((const _Float16 *)p + at, left);
 }
 
 #endif
