@@ -275,6 +275,35 @@ def test_in_place_through_the_library():
         assert torch.equal(x, y) and torch.equal(h, rows) and torch.equal(d, grads.x) and torch.equal(dz, grads.branch)
 
 
+def test_a_last_span_that_is_cut_short():
+    """By the C ABI: a gate of ceil(N / span) rows, the last of which serves fewer; as a gate a row, whose gradients are then summed."""
+    import ctypes
+    import paper_2008_12260_amd as px
+    L, p = px.lib(), (lambda t: None if t is None else t.data_ptr())
+    for N, D, span in ((10, 72, 4), (101, 1000, 33), (50, 600, 49), (9, 40, 2)):
+        case = Case(N, D, F32, F32, gates=N)
+        gate = torch.randn((-(-N // span), D), device="cuda")
+        case.gate = case.edge["gate"] = gate.repeat_interleave(span, 0)[:N].contiguous()
+        y, rows, state = px.block_edge(case.x, case.branch, **case.edge)
+        want = px.block_edge_grad(case.y_grad, case.rows_grad, state, y=y, branch=case.branch, **case.edge)
+        dims = px.EdgeDims(N, D, 0, 0, 0, 0, 0, px.PX_EDGE_AFTER | px.PX_EDGE_BEFORE, 1e-6, 1.0, 1.0, span)
+        y2, rows2, gate_grad, dx, dz = torch.empty_like(y), torch.empty_like(rows), torch.full_like(gate, 7.0), torch.empty_like(y), torch.empty_like(y)
+        need = ctypes.c_size_t()
+        assert L.pollux_block_edge_workspace_size(ctypes.byref(dims), ctypes.byref(need)) == px.PX_OK
+        ws = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        assert L.pollux_block_edge(ctypes.byref(dims), p(case.x), p(case.branch), p(gate), p(case.after.weight), None, p(case.before.weight), None, p(y2), p(rows2), None, None, None, None, None, None,
+                                   None) == px.PX_OK
+        assert L.pollux_block_edge_grad(ctypes.byref(dims), p(case.y_grad), p(case.rows_grad), p(y), None, p(case.branch), None, p(state.y_stats), p(state.branch_stats), p(gate), p(case.after.weight), None,
+                                        p(case.before.weight), p(ws), need.value, p(dx), p(dz), p(gate_grad), None, None, None, None, None) == px.PX_OK
+        torch.cuda.synchronize()
+        assert torch.equal(y2, y) and torch.equal(rows2, rows) and torch.equal(dx, want.x) and torch.equal(dz, want.branch)
+        for s in range(gate.shape[0]):
+            terms = want.gate[s * span:(s + 1) * span].double()
+            # (each row's rounded once more there; sums of at most 49)
+            assert bool(((gate_grad[s].double() - terms.sum(0)).abs() <= 64 * 2.0 ** -24 * terms.abs().sum(0) + 2.0 ** -140).all())
+
+
 def test_rows_of_zeros_and_rows_that_are_not_finite():
     import paper_2008_12260_amd as px
     case = Case(40, 300, gates=0)
