@@ -237,9 +237,9 @@ def _gate(gate, N, D):
         return gate.contiguous(), 0
     flat = gate.reshape(-1, D).contiguous()
     G = flat.shape[0]
-    if G != 1 and (G == 0 or N % G):
+    if G != 1 and (N % G if G else N):
         raise ValueError(f"a gate of {G} rows does not divide {N} rows")
-    return flat, 0 if G == 1 else N // G
+    return flat, 0 if G == 1 else N // G if N else 1
 
 
 def _zeros(*values):
@@ -349,6 +349,8 @@ def block_edge_grad(y_grad, rows_grad, state, y=None, branch=None, gate=None, af
         x_grad = model.new_empty(shape, dtype=state.x_dtype) if "x" in need else None
         branch_grad = model.new_empty(shape, dtype=state.dtype) if state.branched and "branch" in need else None
         gate_grad = like(gate, "gate")
+        if gate_grad is not None and N == 0 and span:
+            gate_grad.zero_()                # of no rows the library knows no spans
         after_grads = like(w_a, "after"), like(b_a, "after")
         before_grads = like(w_b, "before"), like(b_b, "before")
         # what the norms were of: kept, or as it was

@@ -330,6 +330,7 @@ int pollux_block_edge_grad(const pollux_edge_dims *dims, const void *y_grad, con
     for (const void *p : {after_weight, after_bias, before_weight, (const void *)after_weight_grad, (const void *)after_bias_grad, (const void *)before_weight_grad, (const void *)before_bias_grad})
         if (!aligned(d.weight_type, p)) return PX_E_INVALID_ARG;
     if (!gate) d.span = 0;
+    if (d.N == 0 && dims->span > 0) gate_grad = nullptr;  // no rows of a gate
     const px::EdgePlan plan = px::edge_plan(d);
     int rc = check_workspace(workspace, workspace_bytes, plan.total);
     if (rc == PX_OK) rc = px::check_device();

@@ -343,6 +343,38 @@ def test_no_rows():
         assert not bool(t.any())
 
 
+@pytest.mark.parametrize("gates", [(0, 50), (3, 50), (2, 3, 50), (1, 50)])
+def test_no_rows_of_gates(gates):
+    import paper_2008_12260_amd as px
+    case = Case(0, 50, gates=1)
+    case.edge["gate"] = torch.ones(gates, device="cuda")
+    y, rows, state = px.block_edge(case.x, case.branch, **case.edge, keep="i8")
+    assert y.shape == rows.shape == (0, 50)
+    used = torch.full((512,), float("nan"), device="cuda")      # (what the gradient is allocated from next, perhaps)
+    del used
+    grads = px.block_edge_grad(case.y_grad, case.rows_grad, state, **case.edge)
+    assert grads.gate.shape == gates and not bool(grads.gate.any()) and not bool(grads.after_weight.any())
+
+
+def test_no_rows_have_no_spans():
+    """By the C ABI a gate of no rows' spans has no rows: nothing is written to its gradient."""
+    import ctypes
+    import paper_2008_12260_amd as px
+    L = px.lib()
+    gate, weight, gate_grad, weight_grad = torch.ones(64, device="cuda"), torch.ones(64, device="cuda"), torch.full((64,), 7.0, device="cuda"), torch.full((64,), 7.0, device="cuda")
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    for span, left in ((3, 7.0), (0, 0.0)):
+        dims = px.EdgeDims(0, 64, 0, 0, 0, 0, 0, px.PX_EDGE_AFTER, 1e-6, 1.0, 1.0, span)
+        need = ctypes.c_size_t()
+        assert L.pollux_block_edge_workspace_size(ctypes.byref(dims), ctypes.byref(need)) == px.PX_OK and need.value <= 256
+        gate_grad.fill_(7.0)
+        torch.cuda.synchronize()
+        assert L.pollux_block_edge_grad(ctypes.byref(dims), None, None, None, None, None, None, None, None, gate.data_ptr(), weight.data_ptr(), None, None, ws.data_ptr(), 256, None, None,
+                                        gate_grad.data_ptr(), weight_grad.data_ptr(), None, None, None, None) == px.PX_OK
+        torch.cuda.synchronize()
+        assert bool((gate_grad == left).all()) and not bool(weight_grad.any())
+
+
 def test_gradients_are_differences():
     """fp32, along random directions, steps h = 2^-6: a difference is within h^2 times a third derivative (some units here, of sums of 24 x 40 terms of size 1: below 2^-12 * 2^7) and 2^-24 * 2^10 / h of
     the derivative."""
