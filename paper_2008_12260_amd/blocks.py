@@ -227,14 +227,19 @@ def kept_grad(kept, rows_grad, weight=None, bias=None, weight_grad=None, accumul
     return weight_grad
 
 
-def _gate(gate, N, D):
-    """(the gate as rows, of how many rows each serves: 0 for one that serves all)"""
+def _gate(gate, shape, N, D):
+    """(the gate as rows, of how many rows of [*shape] each serves: 0 for one that serves all)"""
     if gate is None:
         return None, 0
     if gate.dim() == 0 or gate.shape[-1] != D:
         raise ValueError(f"gate has shape {tuple(gate.shape)}: rows of {D} are wanted")
     if gate.dim() == 1:
         return gate.contiguous(), 0
+    if gate.dim() == len(shape) > 2:
+        # what broadcasts over a dimension before one that it has serves rows that are not neighbours
+        k = next((k for k in range(len(shape) - 1) if gate.shape[k] != shape[k]), len(shape) - 1)
+        if any(size != 1 for size in gate.shape[k:-1]):
+            raise ValueError(f"gate has shape {tuple(gate.shape)} beside {tuple(shape)}: the first dimensions of that, and ones, are wanted")
     flat = gate.reshape(-1, D).contiguous()
     G = flat.shape[0]
     if G != 1 and (N % G if G else N):
@@ -250,7 +255,7 @@ def block_edge(x, branch=None, gate=None, after=None, before=None, residual=1.0,
     """(y, rows, state): y = residual * x + scale * gate * after(branch), rows = before(y); all [..., D], in one pass.
 
     after, before: Norm, or None for no norm (`rows` is then None); centred: norms subtract the mean.  branch None: y is x, and the call is the norm `before`.
-    gate: [D], or [..., D] of G rows, each of which serves N / G rows in turn (one a sequence, one a token).  x may be float32 beside a branch of 16 bits: y has x's type, rows the branch's
+    gate: [D], or [..., D] of G rows, each of which serves N / G rows in turn (one a sequence, [B, 1, D], one a token).  x may be float32 beside a branch of 16 bits: y has x's type, rows the branch's
     (rows_dtype, or x's, without one).  keep "i8" or "e4m3": the normalised rows, which block_edge_grad needs, are left in 8 bits in `state`, and y and branch need not be remembered."""
     import torch
     weights = (*(after or ()), *(before or ()))
@@ -266,7 +271,7 @@ def block_edge(x, branch=None, gate=None, after=None, before=None, residual=1.0,
         x_rows, x_ld = _matrix(x, "x")
         N, D = x_rows.shape
         branch_rows, branch_ld = (None, 0) if branch is None else _matrix(branch, "branch")
-        gate_rows, span = _gate(gate, N, D)
+        gate_rows, span = _gate(gate, shape, N, D)
         weight_dtype, (w_a, b_a, w_b, b_b) = _vectors(D, after_weight=after and after[0], after_bias=after and after[1], before_weight=before and before[0],
                                                       before_bias=before and before[1])
         y = x if branch is None else _like(x)
@@ -338,7 +343,7 @@ def block_edge_grad(y_grad, rows_grad, state, y=None, branch=None, gate=None, af
         rows_grad_rows, rows_grad_ld = (None, 0) if rows_grad is None else _matrix(rows_grad, "rows_grad")
         N, D = (rows_grad_rows if y_grad_rows is None else y_grad_rows).shape
         device = model.device
-        gate_rows, span = _gate(gate, N, D)
+        gate_rows, span = _gate(gate, shape, N, D)
         weight_dtype, (w_a, b_a, w_b, b_b) = _vectors(D, after_weight=after and after[0], after_bias=after and after[1], before_weight=before and before[0],
                                                       before_bias=before and before[1])
         if need is not _ALL and set(need) - set(_ALL):

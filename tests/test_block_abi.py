@@ -192,6 +192,20 @@ BAD = [lambda: px.keep(new(6, 40), "i4"), lambda: px.keep(new(6, 40), None), lam
        lambda: px.gated_grad(new(6, 40), kept(N=5)), lambda: px.gated_grad(new(6, 40), new(6, 41)), lambda: px.gated_grad(new(6, 40), new(6, 40), new(6, 40), out=new(6, 79))]
 
 
+# A gate of as many dimensions as x: one a sequence, one a token, one for all; not one a position, which neighbours do not share.
+SHAPES = [((2, 1, 40), True), ((2, 3, 40), True), ((1, 1, 40), True), ((1, 3, 40), False), ((3, 2, 40), False), ((6, 1, 40), False), ((6, 40), True), ((2, 40), True)]
+
+
+@pytest.mark.parametrize("shape,taken", SHAPES)
+def test_shapes_of_gates(on_the_host, shape, taken):
+    x, rows, gate = new(2, 3, 40), new(2, 3, 40), new(*shape)
+    calls = [lambda: px.block_edge(x, rows, gate=gate, after=N_()),
+             lambda: px.block_edge_grad(x, rows, state(), y=x, branch=rows, gate=gate, after=N_(), before=N_())]
+    for call in calls:
+        with pytest.raises(on_the_host if taken else ValueError):
+            call()
+
+
 def test_what_is_taken(on_the_host):
     for k, call in enumerate(GOOD):
         with pytest.raises(on_the_host):
