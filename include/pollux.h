@@ -700,7 +700,7 @@ int pollux_kept_grad(const pollux_kept_grad_dims *dims,  /* host */
  * The edge between two blocks: a norm of the block's result, its gate, the scaled residual, the norm before the next block, in one pass.  With the norm
  *   n(v) = (v - mean) * r,  r = 1 / sqrt(mean((v - mean)^2) + eps),  mean = 0 without PX_EDGE_CENTRED,
  *   b    = n(branch) * after_weight + after_bias         (PX_EDGE_AFTER; else b = branch)
- *   y    = residual * x + scale * gate * b               (without a branch, y = x, which is not written)
+ *   y    = residual * x + scale * gate * b               (without a branch, y = x, which is not written, and residual is 1: other values are refused)
  *   rows = n(y) * before_weight + before_bias            (PX_EDGE_BEFORE; else none)
  * Weights, biases and the gate may be NULL (1, 0, 1).  A row of the gate serves `span` rows in turn (0: all): a learned vector, one a sequence, or with
  * 1 one a token; gate [ceil(N / span), D].  y is rounded where it is written; the norm before takes it unrounded.

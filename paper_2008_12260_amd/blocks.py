@@ -254,7 +254,8 @@ def _zeros(*values):
 def block_edge(x, branch=None, gate=None, after=None, before=None, residual=1.0, scale=1.0, eps=1e-6, centred=False, keep=None, rows_dtype=None, stream=None):
     """(y, rows, state): y = residual * x + scale * gate * after(branch), rows = before(y); all [..., D], in one pass.
 
-    after, before: Norm, or None for no norm (`rows` is then None); centred: norms subtract the mean.  branch None: y is x, and the call is the norm `before`.
+    after, before: Norm, or None for no norm (`rows` is then None); centred: norms subtract the mean.  branch None: y is x, and the call is the norm `before`
+    (residual and scale then count for nothing, here and in block_edge_grad: a stack may give all its edges the same).
     gate: [D], or [..., D] of G rows, each of which serves N / G rows in turn (one a sequence, [B, 1, D], one a token).  x may be float32 beside a branch of 16 bits: y has x's type, rows the branch's
     (rows_dtype, or x's, without one).  keep "i8" or "e4m3": the normalised rows, which block_edge_grad needs, are left in 8 bits in `state`, and y and branch need not be remembered."""
     import torch
@@ -281,7 +282,7 @@ def block_edge(x, branch=None, gate=None, after=None, before=None, residual=1.0,
         branch_kept = _new_kept(x_rows, D, keep) if form and (after is not None or gate is not None) else None
         y_kept = _new_kept(x_rows, D, keep) if form and before is not None else None
         flags = (_px.PX_EDGE_AFTER if after is not None else 0) | (_px.PX_EDGE_BEFORE if before is not None else 0) | (_px.PX_EDGE_CENTRED if centred else 0)
-        eps, residual, scale = float(eps), float(residual), float(scale)
+        eps, residual, scale = float(eps), 1.0 if branch is None else float(residual), float(scale)
         dims = _dims(_px.EdgeDims, _zeros(eps, residual, scale), N, D, x_type, _type_of(dtype), _type_of(weight_dtype), _type_of(gate_rows.dtype if gate_rows is not None else None), form, flags,
                      eps, residual, scale, span, x_ld, branch_ld, 0, 0, 0, 0, 0, 0)
         ptr = _px._ptr
@@ -384,7 +385,7 @@ def block_edge_grad(y_grad, rows_grad, state, y=None, branch=None, gate=None, af
         if after is not None:
             _stats(state.branch_stats, "branch_stats", N)
         flags = (_px.PX_EDGE_AFTER if after is not None else 0) | (_px.PX_EDGE_BEFORE if before is not None else 0) | (_px.PX_EDGE_CENTRED if centred else 0)
-        residual, scale = float(residual), float(scale)
+        residual, scale = float(residual) if state.branched else 1.0, float(scale)
         dims, bytes_ = _planned(_px.EdgeDims, "pollux_block_edge_workspace_size", (), _zeros(residual, scale), N, D, _type_of(state.x_dtype), _type_of(state.dtype), _type_of(weight_dtype),
                                 _type_of(gate_rows.dtype if gate_rows is not None else None), form, flags, 0.0, residual, scale, span, 0, branch_ld, y_ld, 0, 0, 0,
                                 y_grad_ld, rows_grad_ld)

@@ -268,6 +268,8 @@ int pollux_block_edge(const pollux_edge_dims *dims, const void *x, const void *b
     const bool before = d.flags & PX_EDGE_BEFORE, after = d.flags & PX_EDGE_AFTER;
     // nothing to do without a branch and a norm; what belongs to a part that there is none of is not given
     if (d.N > 0 && !branch && (!before || after || y || gate || branch_stats || branch_values)) return PX_E_INVALID_ARG;
+    // (backward, a branch whose rows are not read looks like none: x's gradient is residual g there, and y is x here)
+    if (d.N > 0 && !branch && d.residual != 1.f) return PX_E_INVALID_ARG;
     if (!after && (after_weight || after_bias || branch_stats)) return PX_E_INVALID_ARG;
     if (!before && (before_weight || before_bias || rows || y_stats || y_values)) return PX_E_INVALID_ARG;
     if (d.N > 0 && (!y_values != !y_scales || !branch_values != !branch_scales || (d.form == PX_KEPT_NONE && (y_values || branch_values)))) return PX_E_INVALID_ARG;

@@ -101,6 +101,15 @@ def test_edges():
     refused(call, edge_dims(flags=px.PX_EDGE_BEFORE), alone, [(2, FAKE), (7, FAKE), (10, FAKE), (-1, edge_dims()), ((-1, edge_dims(flags=0)), (5, NULL), (6, NULL), (8, NULL), (9, NULL))])
 
 
+def test_an_edge_without_a_branch_has_no_residual_scale():
+    """y is x there, and the backward call, which cannot tell a branch that it does not read from none, multiplies with residual."""
+    call = px.lib().pollux_block_edge
+    alone = [FAKE] + [NULL] * 4 + [FAKE, FAKE, NULL, FAKE, FAKE] + [NULL] * 6
+    refused(call, edge_dims(flags=px.PX_EDGE_BEFORE, residual=0.75), alone, [(0, FAKE), (-1, edge_dims(flags=px.PX_EDGE_BEFORE, residual=0.0))])
+    if not torch.cuda.is_available():        # residual 1 passes the checks
+        assert call(ctypes.byref(edge_dims(flags=px.PX_EDGE_BEFORE)), *alone) != px.PX_E_INVALID_ARG
+
+
 def test_gradients_of_edges():
     # y_grad, rows_grad, y, y_scales, branch, branch_scales, y_stats, branch_stats, gate, after_weight, after_bias, before_weight, workspace, bytes,
     # x_grad, branch_grad, gate_grad, after_weight_grad, after_bias_grad, before_weight_grad, before_bias_grad, stream
@@ -204,6 +213,26 @@ def test_shapes_of_gates(on_the_host, shape, taken):
     for call in calls:
         with pytest.raises(on_the_host if taken else ValueError):
             call()
+
+
+def test_without_a_branch_both_calls_leave_the_residual_out(monkeypatch):
+    seen = []
+
+    class Reached(Exception):
+        pass
+
+    def watched(cls, *args):
+        seen.append(cls(*args[1:] if isinstance(args[0], tuple) else args[3:]))
+        raise Reached
+    monkeypatch.setattr(px, "_current_device", lambda: -1)
+    monkeypatch.setattr(px.blocks, "_dims", watched)
+    monkeypatch.setattr(px.blocks, "_planned", watched)
+    x = new(6, 40)
+    for branch, residual in ((None, 1.0), (x, 0.75)):
+        for call in (lambda: px.block_edge(x, branch, before=N_(), residual=0.75), lambda: px.block_edge_grad(x, x, state(branch=branch is not None, after=False), y=x, before=N_(), residual=0.75)):
+            with pytest.raises(Reached):
+                call()
+            assert seen[-1].D == 40 and seen[-1].residual == residual
 
 
 def test_what_is_taken(on_the_host):

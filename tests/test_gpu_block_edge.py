@@ -249,6 +249,28 @@ def test_a_norm_alone_in_another_type():
             near(grads.before_weight, *want["before_weight"], E_SUMS)
 
 
+@pytest.mark.parametrize("form", (None,) + FORMS)
+def test_a_norm_alone_under_a_residual_scale(form):
+    """Without a branch y is x whatever the stack's residual is: the gradients are those of the forward call, differentiated."""
+    import paper_2008_12260_amd as px
+    for N, D, centred in ((12, 40, False), (9, 1000, True), (3, 9000, False)):
+        case = Case(N, D, F32, F32, branch=False, centred=centred, biased=True)
+        want = px.block_edge(case.x, before=case.before, centred=centred, keep=form)
+        want_grads = px.block_edge_grad(case.y_grad, case.rows_grad, want[2], y=None if form else want[0], before=case.before, centred=centred)
+        y, rows, state = px.block_edge(case.x, before=case.before, residual=0.75, centred=centred, keep=form)
+        assert y is case.x and torch.equal(rows, want[1])
+        grads = px.block_edge_grad(case.y_grad, case.rows_grad, state, y=None if form else y, before=case.before, residual=0.75, centred=centred)
+        for a, b in zip(grads, want_grads):
+            assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+        if form is None:
+            x = case.x.double().requires_grad_()
+            v = x - x.mean(1, keepdim=True) if centred else x
+            n = v * (v.square().mean(1, keepdim=True) + 1e-6).rsqrt()
+            (x * case.y_grad + (n * case.before.weight + case.before.bias) * case.rows_grad).sum().backward()
+            case.forward()
+            near(grads.x, x.grad, case.backward(case.n_y, None, state)["x"][1], 2 * E)
+
+
 def test_in_place_through_the_library():
     """y over x, and the gradient of x over that of y, by the C ABI."""
     import ctypes
