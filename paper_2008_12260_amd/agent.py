@@ -104,13 +104,17 @@ class Job:
             both = torch.mm(rows, w_in.t())
             a, *inputs = gated(both[:, :F], both[:, F:], keep=keep)
             between.append(inputs if keep else (both[:, :F], both[:, F:]))
+            del both, inputs                 # what is not remembered goes as soon as it is used
             branch = torch.mm(a, w_out.t())
+            del a
             stream, rows, state = block_edge(stream, branch, **edge, keep=keep)
             remembered.append((state, None, None, None) if keep else (state, stream, branch, rows))
+            del branch
+        del stream, state
         loss, lse = token_loss(rows, projection, y, status=self.status)
         weight = torch.full_like(loss, 1.0 / loss.numel())
         d_rows, _ = token_loss_grad(rows, projection, y, lse, weight, weight_grad=d_projection)
-        del rows, stream
+        del rows
         d_stream = None
         for k in range(self.blocks, -1, -1):
             state, stream, branch, _ = remembered.pop()

@@ -241,3 +241,35 @@ def test_two_streams_at_once():
     for pair in got:
         for one in pair:
             assert all(torch.equal(a, b) for a, b in zip(one, want))
+
+
+@pytest.mark.parametrize("kept", [None, "i8", "e4m3"])
+def test_a_micro_batch_holds_no_more_than_it_remembers(kept):
+    """Allocated when the loss is taken: of each edge what its gradient needs, of each block its activation's inputs, and beside them the tokens and the rows that the loss takes.
+    (Bytes asked for: of what is allocated, the allocator's larger blocks may be up to 1 MiB each more.)"""
+    from paper_2008_12260_amd.agent import Job
+    import paper_2008_12260_amd as px
+    asked = lambda: torch.cuda.memory_stats()["requested_bytes.all.current"]
+    for blocks, D, F in ((1, 256, 512), (2, 256, 512), (3, 136, 1000)):
+        job = Job(V=300, D=D, length=64, seed=6, blocks=blocks, width=F, kept=kept)
+        model, gradient, tokens = job.parts(job.parameters.bfloat16()), torch.empty(job.parameters.numel(), dtype=torch.bfloat16, device="cuda"), job.examples(16)
+        seen, loss = [], px.agent.token_loss
+
+        def watched(rows, *args, **more):
+            torch.cuda.synchronize()
+            seen.append(asked())
+            return loss(rows, *args, **more)
+        px.agent.token_loss = watched
+        try:
+            job.micro_batch(tokens, model, gradient)
+            torch.cuda.synchronize()
+            base = asked()
+            job.micro_batch(tokens, model, gradient)
+        finally:
+            px.agent.token_loss = loss
+        row = (lambda width: 2 * width) if kept is None else (lambda width: 33 * -(-width // 32))
+        # norms' sums; norms before and after; the activations' inputs; without a form the rows of all products but the last too
+        each = 8 * (2 * blocks + 1) + (2 * blocks + 1) * row(D) + 2 * blocks * row(F) + (blocks * row(D) if kept is None else 0)
+        held, rows = seen[-1] - base, 16 * 64
+        around = rows * (2 * 8 + 2 * D) + 64 * 1024
+        assert rows * each <= held <= rows * each + around, (blocks, D, F)
