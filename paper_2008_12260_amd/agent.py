@@ -139,13 +139,17 @@ class Job:
         return loss.mean()
 
     def bytes_per_example(self):
-        """What a micro-batch remembers between its passes, an example: of each block the rows that its norms made, its activation's two inputs and the norms' sums; where they are not in 8 bits,
-        the rows that its products took too."""
+        """What a micro-batch remembers between its passes, an example: of each edge, one more than there are blocks, the rows that its norms made and their sums, of each block its activation's
+        two inputs; where they are not in 8 bits, the rows that the blocks' first products took too."""
+        if not self.blocks:
+            return 0
+        # norms before all blocks and after the last, and norms after each
+        norms = 2 * self.blocks + 1
         if self.kept is None:
-            row = 2 * (3 * self.D + 2 * self.width)
+            row = 2 * ((norms + self.blocks) * self.D + 2 * self.blocks * self.width)
         else:
-            row = 33 * (2 * (-(-self.D // 32)) + 2 * (-(-self.width // 32)))
-        return self.length * self.blocks * (row + 16)
+            row = 33 * (norms * -(-self.D // 32) + 2 * self.blocks * -(-self.width // 32))
+        return self.length * (row + 8 * norms)
 
     def iteration(self, m, s):
         """One iteration of s + 1 micro-batches of m examples: (mean loss, [tr(Sigma), |g|^2, phi] or None where there is a single

@@ -273,3 +273,33 @@ def test_a_micro_batch_holds_no_more_than_it_remembers(kept):
         held, rows = seen[-1] - base, 16 * 64
         around = rows * (2 * 8 + 2 * D) + 64 * 1024
         assert rows * each <= held <= rows * each + around, (blocks, D, F)
+
+
+@pytest.mark.parametrize("kept", [None, "i8", "e4m3"])
+def test_bytes_of_an_example_count_every_edge(kept):
+    """Another example's share of what is asked for until the loss is taken, less its tokens and the rows that the loss takes: to a byte."""
+    from paper_2008_12260_amd.agent import Job
+    import paper_2008_12260_amd as px
+    asked = lambda: torch.cuda.memory_stats()["requested_bytes.all.current"]
+    for blocks, D, F in ((1, 256, 512), (2, 64, 40), (3, 136, 1000)):
+        job = Job(V=300, D=D, length=64, seed=6, blocks=blocks, width=F, kept=kept)
+        model, gradient = job.parts(job.parameters.bfloat16()), torch.empty(job.parameters.numel(), dtype=torch.bfloat16, device="cuda")
+        seen, loss = [], px.agent.token_loss
+
+        def watched(rows, *args, **more):
+            torch.cuda.synchronize()
+            seen.append(asked())
+            return loss(rows, *args, **more)
+        px.agent.token_loss = watched
+        try:
+            job.micro_batch(job.examples(3), model, gradient)
+            for m in (16, 17):
+                tokens = job.examples(m)
+                torch.cuda.synchronize()
+                base = asked()
+                job.micro_batch(tokens, model, gradient)
+                seen[-1] -= base
+        finally:
+            px.agent.token_loss = loss
+        assert seen[-1] - seen[-2] == job.bytes_per_example() + 64 * (2 * 8 + 2 * D), (blocks, D, F)
+    assert Job(V=300, D=64, length=64).bytes_per_example() == 0
