@@ -235,10 +235,12 @@ def _gate(gate, shape, N, D):
         raise ValueError(f"gate has shape {tuple(gate.shape)}: rows of {D} are wanted")
     if gate.dim() == 1:
         return gate.contiguous(), 0
-    if gate.dim() == len(shape) > 2:
-        # what broadcasts over a dimension before one that it has serves rows that are not neighbours
-        k = next((k for k in range(len(shape) - 1) if gate.shape[k] != shape[k]), len(shape) - 1)
-        if any(size != 1 for size in gate.shape[k:-1]):
+    lead = tuple(gate.shape[:-1])
+    if gate.dim() <= len(shape) > 2:
+        # What broadcasts over a dimension before one that it has serves rows that are not neighbours.  Of fewer dimensions it is one of x's first ones, or one that broadcasts to no other rows.
+        at = (1,) * (len(shape) - gate.dim()) + lead
+        k = next((k for k in range(len(shape) - 1) if at[k] != shape[k]), len(shape) - 1)
+        if any(size != 1 for size in at[k:]) and (len(at) == len(lead) or lead != tuple(shape[:len(lead)]) and all(a in (1, b) for a, b in zip(at, shape))):
             raise ValueError(f"gate has shape {tuple(gate.shape)} beside {tuple(shape)}: the first dimensions of that, and ones, are wanted")
     flat = gate.reshape(-1, D).contiguous()
     G = flat.shape[0]
@@ -256,7 +258,8 @@ def block_edge(x, branch=None, gate=None, after=None, before=None, residual=1.0,
 
     after, before: Norm, or None for no norm (`rows` is then None); centred: norms subtract the mean.  branch None: y is x, and the call is the norm `before`
     (residual and scale then count for nothing, here and in block_edge_grad: a stack may give all its edges the same).
-    gate: [D], or [..., D] of G rows, each of which serves N / G rows in turn (one a sequence, [B, 1, D], one a token).  x may be float32 beside a branch of 16 bits: y has x's type, rows the branch's
+    gate: [D], or [..., D] of G rows, each of which serves N / G rows in turn (one a sequence, [B, 1, D] or [B, D], one a token); one that would broadcast over other rows
+    (one a position, [T, D] beside [B, T, D]) is refused.  x may be float32 beside a branch of 16 bits: y has x's type, rows the branch's
     (rows_dtype, or x's, without one).  keep "i8" or "e4m3": the normalised rows, which block_edge_grad needs, are left in 8 bits in `state`, and y and branch need not be remembered."""
     import torch
     weights = (*(after or ()), *(before or ()))

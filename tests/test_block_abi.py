@@ -215,6 +215,24 @@ def test_shapes_of_gates(on_the_host, shape, taken):
             call()
 
 
+# Of fewer dimensions than x: x's first ones, or rows in turn; not what would broadcast over rows that are not neighbours.
+FEWER = [((2, 3, 40), (3, 40), False), ((4, 3, 40), (3, 40), False), ((1, 3, 40), (3, 40), True), ((3, 3, 40), (3, 40), True), ((2, 1, 40), (2, 40), True), ((2, 3, 40), (1, 40), True),
+         ((4, 3, 40), (6, 40), True), ((2, 3, 40), (6, 40), True), ((2, 3, 4, 40), (3, 1, 40), False), ((2, 3, 4, 40), (4, 40), False), ((2, 3, 4, 40), (3, 4, 40), False),
+         ((2, 3, 4, 40), (2, 3, 40), True), ((2, 3, 4, 40), (2, 40), True), ((2, 3, 4, 40), (1, 1, 40), True), ((2, 2, 4, 40), (2, 1, 40), False), ((1, 2, 4, 40), (2, 1, 40), True),
+         ((2, 3, 4, 40), (24, 40), True), ((6, 40), (2, 40), True), ((6, 40), (2, 1, 40), True), ((6, 40), (3, 40), True)]
+
+
+@pytest.mark.parametrize("rows,shape,taken", FEWER)
+def test_shapes_of_gates_of_fewer_dimensions(on_the_host, rows, shape, taken):
+    x, gate = new(*rows), new(*shape)
+    N = x.numel() // 40
+    calls = [lambda: px.block_edge(x, x, gate=gate, after=N_()),
+             lambda: px.block_edge_grad(x, x, state(N), y=x, branch=x, gate=gate, after=N_(), before=N_())]
+    for call in calls:
+        with pytest.raises(on_the_host if taken else ValueError):
+            call()
+
+
 def test_without_a_branch_both_calls_leave_the_residual_out(monkeypatch):
     seen = []
 
