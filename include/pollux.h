@@ -646,7 +646,7 @@ enum {
 
 /*
  * pollux_keep: rows -> values, scales.  pollux_restore: rows of any type from them (in fp16, infinite where an element passes its range).
- * Limits: 0 <= N <= 2^24, 1 <= D <= 2^20, stride below 2^20 (0: D).  No workspace.
+ * Limits: 0 <= N <= 2^24, 1 <= D <= 2^20, stride D (or 0), or between D and 2^20.  No workspace.
  */
 typedef struct {
     int64_t N;                  /* rows                                  */
@@ -674,7 +674,7 @@ int pollux_restore(const pollux_keep_dims *dims,         /* host */
  * exactly (fp16 where they are within its range; elements below 2^-126 may count as 0), on their way to the matrix units.  Sums in fp32, in a fixed order; fp32: a product is off by at most 2^-24 of itself.
  * With PX_FLAG_ACCUMULATE the result is added to what weight_grad holds.
  *
- * Limits: 0 <= N <= 2^24, 1 <= D <= 2^16, 1 <= M <= 2^20, strides below 2^20 (0: the row's length).
+ * Limits: 0 <= N <= 2^24, 1 <= D <= 2^16, 1 <= M <= 2^20, strides the row's length (or 0), or between that and 2^20.
  * workspace: pollux_kept_grad_workspace_size bytes, 256-byte aligned.
  */
 typedef struct {
@@ -767,7 +767,7 @@ int pollux_block_edge_grad(const pollux_edge_dims *dims, /* host */
  * in Phi's place; each is 0 where that factor is, and the factor may count as 0 where it is below 2^-126.  With a form the forward call keeps gate and up in 8 bits, and the backward call takes values (in the places
  * of gate and up) and scales.  Backward, `rows` are formed again from what it has, for the gradient of the weights behind them.  Any output of the backward call may be NULL.
  * Outputs and inputs must not overlap.
- * Limits: 0 <= N <= 2^24, 1 <= F <= 2^19, strides below 2^20 (0: F).  No workspace.
+ * Limits: 0 <= N <= 2^24, 1 <= F <= 2^19, strides up to 2^20 (0: F).  No workspace.
  */
 enum {
     PX_ACT_SILU = 0,

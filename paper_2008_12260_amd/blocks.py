@@ -78,15 +78,15 @@ def _form(form):
     return _FORMS[form]
 
 
-def _matrix(t, name):
-    """(the tensor as rows, their stride): [..., D] as [N, D], as it is where rows are contiguous, else copied."""
+def _matrix(t, name, most=(1 << 20) - 1):
+    """(the tensor as rows, their stride): [..., D] as [N, D], as it is where rows are contiguous, one after the other or at most `most` apart, else copied."""
     if t.dim() == 0:
         raise ValueError(f"{name} has no dimensions: rows are wanted")
     D = t.shape[-1]
     if t.dim() != 2:
         t = t.reshape(-1, D) if D else t.reshape(math.prod(t.shape[:-1]), 0)
     ld, step = t.stride()
-    if D > 1 and step != 1 or t.shape[0] > 1 and not D <= ld < 1 << 20:
+    if D > 1 and step != 1 or t.shape[0] > 1 and ld != D and not D < ld <= most:
         t, ld = t.clone(memory_format=_contiguous()), D
     return t, ld if t.shape[0] > 1 else D
 
@@ -100,7 +100,7 @@ def _written(t, name, shape, dtype):
         rows = t.view(-1, D) if t.dim() != 2 else t
     except RuntimeError:
         rows = None
-    if rows is None or D > 1 and rows.stride(1) != 1 or rows.shape[0] > 1 and not D <= rows.stride(0) < 1 << 20:
+    if rows is None or D > 1 and rows.stride(1) != 1 or rows.shape[0] > 1 and rows.stride(0) != D and not D < rows.stride(0) < 1 << 20:
         raise ValueError(f"{name} needs contiguous rows, one stride apart")
     return rows, rows.stride(0) if rows.shape[0] > 1 else D
 
@@ -412,8 +412,8 @@ def gated(gate, up=None, act="silu", keep=None, stream=None):
             raise ValueError(f"act is {act!r}: one of {', '.join(_ACTS)} is wanted")
         if up is not None and (up.shape != gate.shape or up.dtype != gate.dtype):
             raise ValueError(f"up is {up.dtype} {tuple(up.shape)}: {gate.dtype} {tuple(gate.shape)} is wanted")
-        gate_rows, gate_ld = _matrix(gate, "gate")
-        up_rows, up_ld = (None, 0) if up is None else _matrix(up, "up")
+        gate_rows, gate_ld = _matrix(gate, "gate", 1 << 20)
+        up_rows, up_ld = (None, 0) if up is None else _matrix(up, "up", 1 << 20)
         N, F = gate_rows.shape
         rows = _like(gate)
         gate_kept = _new_kept(gate_rows, F, keep) if form else None
@@ -454,8 +454,8 @@ def gated_grad(rows_grad, gate, up=None, act="silu", want_rows=False, out=None, 
             for name, t in (("gate", gate), ("up", up)):
                 if t is not None and (t.shape != shape or t.dtype != dtype):
                     raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}: {dtype} {tuple(shape)} is wanted")
-            gate_rows, gate_ld = _matrix(gate, "gate")
-            up_rows, up_ld = (None, 0) if up is None else _matrix(up, "up")
+            gate_rows, gate_ld = _matrix(gate, "gate", 1 << 20)
+            up_rows, up_ld = (None, 0) if up is None else _matrix(up, "up", 1 << 20)
         halves = 1 if up is None else 2
         if out is None:
             out = d.new_empty((*shape[:-1], halves * F))

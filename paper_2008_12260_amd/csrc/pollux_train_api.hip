@@ -13,10 +13,11 @@ bool type_ok(int type) { return type == PX_TYPE_F32 || type == PX_TYPE_BF16 || t
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 bool aligned(int type, const void *p) { return ((uintptr_t)p & (uintptr_t)(px::size_of_type(type) - 1)) == 0; }
 bool aligned8(const void *p) { return ((uintptr_t)p & 7u) == 0; }
-bool stride_ok(int64_t *stride, int64_t width)
+// (rows one after the other may be as wide as their width's own limit)
+bool stride_ok(int64_t *stride, int64_t width, int64_t most = (1 << 20) - 1)
 {
     if (*stride == 0) *stride = width;
-    return *stride >= width && *stride < (1 << 20);
+    return *stride == width || (*stride > width && *stride <= most);
 }
 int check_workspace(const void *ws, size_t bytes, size_t need)
 {
@@ -105,7 +106,7 @@ bool gated_dims_ok(const pollux_gated_dims *in, pollux_gated_dims *d)
     if (!rows_ok(d->N) || d->F < 1 || d->F > (1 << 19) || !type_ok(d->type) || !form_ok(d->form, true) || d->flags != 0) return false;
     if (d->act != PX_ACT_SILU && d->act != PX_ACT_GELU && d->act != PX_ACT_GELU_TANH) return false;
     for (int64_t *stride : {&d->gate_stride, &d->up_stride, &d->rows_stride, &d->rows_grad_stride, &d->gate_grad_stride, &d->up_grad_stride})
-        if (!stride_ok(stride, d->F)) return false;
+        if (!stride_ok(stride, d->F, 1 << 20)) return false;             // halves of rows of 2 F
     return true;
 }
 

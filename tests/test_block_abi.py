@@ -78,6 +78,25 @@ def test_workspaces_stay_small_beside_the_rows():
         assert L.pollux_kept_grad_workspace_size(ctypes.byref(kept_grad_dims(N=N, D=D, M=M)), ctypes.byref(n)) == px.PX_OK and n.value <= (600 << 20)
 
 
+def test_the_widest_rows_are_taken():
+    """Widths at their limits, and no further; strides between rows that are not neighbours stay below 2^20, but for gated's, of halves of rows."""
+    n, L, wide = ctypes.c_size_t(), px.lib(), 1 << 20
+    for stride in (0, wide):
+        assert L.pollux_kept_grad_workspace_size(ctypes.byref(kept_grad_dims(M=wide, rows_grad_stride=stride)), ctypes.byref(n)) == px.PX_OK
+    for make in (kept_grad_dims(M=wide + 1, rows_grad_stride=wide + 1), kept_grad_dims(M=wide - 1, rows_grad_stride=wide), kept_grad_dims(weight_grad_stride=wide)):
+        assert L.pollux_kept_grad_workspace_size(ctypes.byref(make), ctypes.byref(n)) == px.PX_E_INVALID_ARG
+    gated = lambda **changes: (L.pollux_gated_grad, gated_dims(F=1 << 19, **changes), [FAKE, FAKE, NULL, FAKE, NULL, FAKE, FAKE, FAKE, NULL])
+    taken = [(call, keep_dims(D=wide, rows_stride=stride), [FAKE] * 3 + [NULL]) for call in (L.pollux_keep, L.pollux_restore) for stride in (0, wide)]
+    taken += [gated(gate_grad_stride=wide, up_grad_stride=wide), gated(gate_stride=wide, up_stride=wide), gated()]
+    beyond = [(L.pollux_keep, keep_dims(D=wide + 1, rows_stride=wide + 1), [FAKE] * 3 + [NULL]), (L.pollux_keep, keep_dims(D=wide - 1, rows_stride=wide), [FAKE] * 3 + [NULL]),
+              gated(gate_grad_stride=wide + 1), gated(rows_stride=(1 << 19) - 1)]
+    for call, dims, args in beyond:
+        assert call(ctypes.byref(dims), *args) == px.PX_E_INVALID_ARG
+    if not torch.cuda.is_available():
+        for call, dims, args in taken:
+            assert call(ctypes.byref(dims), *args) not in (px.PX_OK, px.PX_E_INVALID_ARG)
+
+
 def test_kept_grad():
     # values, scales, rows_grad, weight, bias, workspace, bytes, weight_grad, stream
     args = [FAKE, FAKE, FAKE, NULL, NULL, FAKE, 1 << 40, FAKE, NULL]
@@ -231,6 +250,12 @@ def test_shapes_of_gates_of_fewer_dimensions(on_the_host, rows, shape, taken):
     for call in calls:
         with pytest.raises(on_the_host if taken else ValueError):
             call()
+
+
+def test_gradients_of_the_widest_activation_have_room(on_the_host):
+    gate = torch.zeros((2, 1 << 20), dtype=torch.bfloat16)
+    with pytest.raises(on_the_host):
+        px.gated_grad(gate[:, :1 << 19], gate[:, :1 << 19], gate[:, 1 << 19:])
 
 
 def test_without_a_branch_both_calls_leave_the_residual_out(monkeypatch):

@@ -303,3 +303,37 @@ def test_bytes_of_an_example_count_every_edge(kept):
             px.agent.token_loss = loss
         assert seen[-1] - seen[-2] == job.bytes_per_example() + 64 * (2 * 8 + 2 * D), (blocks, D, F)
     assert Job(V=300, D=64, length=64).bytes_per_example() == 0
+
+
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float32))
+def test_the_widest_rows(dtype):
+    """Rows at the limits of their widths: as their parts, which are whole groups of 32.  The product is against 64 bits: three products of at most 2^-24 of themselves off and three additions, below
+    2^-21 of the sum of their sizes, and a rounding."""
+    import paper_2008_12260_amd as px
+    g = torch.Generator("cuda").manual_seed(7)
+    W, H = 1 << 20, 1 << 19
+    both, d = (torch.randn((3, W), generator=g, device="cuda").to(dtype) for _ in range(2))
+    parts = [slice(at, at + W // 4) for at in range(0, W, W // 4)]
+    for form in ("i8", "e4m3"):
+        kept = px.keep(both, form)
+        back = px.restore(kept, dtype)
+        for part in parts:
+            few = px.keep(both[:, part], form)
+            assert torch.equal(kept.values[:, part], few.values) and torch.equal(back[:, part], px.restore(few, dtype))
+        few = px.keep(both[:, :40], form)
+        got = px.kept_grad(few, d)
+        assert got.shape == (W, 40)
+        x = px.restore(few, torch.float32).double()
+        want, size = d.double().t().contiguous() @ x, d.double().abs().t().contiguous() @ x.abs()
+        half = torch.finfo(dtype).eps / 2
+        assert bool(((got.double() - want).abs() <= half * want.abs() + 2.0 ** -21 * size).all())
+        rows, *kept = px.gated(both[:, :H], both[:, H:], keep=form)
+        for inputs in (kept, (both[:, :H], both[:, H:])):
+            dg, du, again = px.gated_grad(d[:, :H], *inputs, want_rows=True)
+            assert dg.stride() == (W, 1)
+            for part in parts[:2]:
+                up = slice(H + part.start, H + part.stop)
+                few = px.gated(both[:, part], both[:, up], keep=form)
+                assert torch.equal(rows[:, part], few[0])
+                want = px.gated_grad(d[:, part], *(few[1:] if inputs is kept else (both[:, part], both[:, up])), want_rows=True)
+                assert all(torch.equal(a[:, part], b) for a, b in zip((dg, du, again), want))
