@@ -12,7 +12,7 @@ One block, its products a job's own:
 and backward from block_edge_grad(...), through gated_grad(da, *kept), to kept_grad(s.y_kept, ...), the gradient of the weights that rows met.
 
 As in train.py, arguments are checked and marshalled here, results are allocated by torch on the stream that the call is enqueued on, nothing synchronises or
-records for autograd, and a tensor that requires grad is refused where grad mode is on.
+records for autograd, and a tensor that requires grad is refused where grad mode is on, one with a forward-mode tangent anywhere.
 """
 from __future__ import annotations
 
@@ -23,7 +23,7 @@ from typing import NamedTuple, Optional
 
 import paper_2008_12260_amd as _px
 
-from .train import _check, _contiguous, _on, _on_device, _planned, _scratch, _type
+from .train import _check, _contiguous, _no_tangents, _on, _on_device, _planned, _scratch, _type
 
 _FORMS = {None: _px.PX_KEPT_NONE, "i8": _px.PX_KEPT_I8, "e4m3": _px.PX_KEPT_E4M3}
 _ACTS = {"silu": _px.PX_ACT_SILU, "gelu": _px.PX_ACT_GELU, "gelu_tanh": _px.PX_ACT_GELU_TANH}
@@ -188,6 +188,7 @@ def restore(kept, dtype=None, out=None, stream=None):
 
 def _untracked_here(*tensors):
     import torch
+    _no_tangents(torch, tensors)
     if not torch.is_grad_enabled():
         return
     for t in tensors:

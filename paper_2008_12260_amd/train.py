@@ -5,7 +5,7 @@ the scheduler is given.
 Arguments are checked and marshalled here; every step runs in the library's kernels.  Results and scratch memory are allocated
 by torch on the stream that the call is enqueued on (`stream`, else the current one); nothing synchronises, so the calls
 can be recorded into a graph.  Nor does anything record for autograd: a tensor that requires grad is refused where grad mode is on, because its
-gradient would be lost (inside a torch.autograd.Function grad mode is off, and the calls make its forward and backward).  A caller who hands over results or scratch memory from another stream keeps them in order, as with any
+gradient would be lost (inside a torch.autograd.Function grad mode is off, and the calls make its forward and backward); so is one with a forward-mode tangent.  A caller who hands over results or scratch memory from another stream keeps them in order, as with any
 torch operation.
 """
 from __future__ import annotations
@@ -41,8 +41,19 @@ def _on_device(*tensors):
             raise ValueError(f"a tensor {tuple(t.shape)} is on {t.device}: it has to be on the current GPU, cuda:{here}")
 
 
+def _no_tangents(torch, tensors):
+    """No given tensor is a dual number of forward-mode differentiation: its tangent would be lost."""
+    forward = torch.autograd.forward_ad
+    if forward._current_level < 0:           # (the level entered, asked so that calls outside of one pay next to nothing)
+        return
+    for t in tensors:
+        if t is not None and forward.unpack_dual(t).tangent is not None:
+            raise ValueError(f"a tensor {tuple(t.shape)} has a tangent, which this call does not carry on: unpack it (torch.autograd.forward_ad.unpack_dual)")
+
+
 def _untracked(torch, *tensors):
     """No given tensor is one that autograd would follow through the call."""
+    _no_tangents(torch, tensors)
     if not torch.is_grad_enabled():
         return
     for t in tensors:

@@ -303,6 +303,38 @@ def test_what_requires_grad_is_refused():
             call()
 
 
+def test_what_has_a_tangent_is_refused(on_the_host):
+    """Forward mode, whose dual numbers do not require grad, in grad mode and out of it; outside of a level, and in a Function's forward, they are ordinary tensors."""
+    from torch.autograd import forward_ad
+    x = torch.ones((6, 40))
+    dual = lambda *shape: forward_ad.make_dual(torch.ones(shape), torch.ones(shape))
+    calls = (lambda new: px.keep(new(6, 40)), lambda new: px.restore(kept(), out=new(6, 40)), lambda new: px.kept_grad(kept(), new(6, 24)), lambda new: px.kept_grad(kept(), x, new(40)),
+             lambda new: px.block_edge(new(6, 40), before=N_()), lambda new: px.block_edge(x, before=N_(new(40))), lambda new: px.block_edge(x, new(6, 40)), lambda new: px.block_edge(x, x, gate=new(40)),
+             lambda new: px.block_edge_grad(new(6, 40), x, state(), after=N_(), before=N_()), lambda new: px.gated(new(6, 40)), lambda new: px.gated(x, new(6, 40)),
+             lambda new: px.gated_grad(new(6, 40), x), lambda new: px.gated_grad(x, kept(), out=new(6, 40)))
+    with forward_ad.dual_level():
+        for call in calls:
+            with pytest.raises(ValueError, match="tangent"):
+                call(dual)
+            with torch.no_grad(), pytest.raises(ValueError, match="tangent"):
+                call(dual)
+        with pytest.raises(on_the_host):
+            px.gated(x)
+
+        class Gated(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, x):
+                return px.gated(x)[0]
+
+            @staticmethod
+            def jvp(ctx, x):
+                return x
+        with pytest.raises(on_the_host):
+            Gated.apply(dual(6, 40))
+    with pytest.raises(on_the_host):
+        px.gated(x)
+
+
 def test_tensors_that_are_not_on_a_gpu_are_refused():
     if torch.cuda.is_available():
         pytest.skip("a GPU is there")

@@ -38,6 +38,19 @@ def test_what_requires_grad_is_refused():
             pytest.fail(name)
 
 
+def test_what_has_a_tangent_is_refused():
+    from torch.autograd import forward_ad
+    dual = lambda *shape: forward_ad.make_dual(torch.ones(shape), torch.ones(shape))
+    tokens, x = torch.tensor([1, 0, 3]), torch.ones((3, 8))
+    with forward_ad.dual_level():
+        for call in (lambda: px.embed(tokens, dual(4, 8)), lambda: px.embed_grad(tokens, dual(3, 8), 4), lambda: px.token_loss(dual(3, 8), torch.ones((4, 8)), tokens),
+                     lambda: px.token_loss_grad(x, dual(4, 8), tokens, torch.ones(3)), lambda: px.noise_scale(dual(3, 8), 1.0), lambda: px.orthogonalize(dual(3, 8))):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+            with torch.no_grad(), pytest.raises(ValueError, match="tangent"):
+                call()
+
+
 @pytest.mark.gpu
 def test_what_requires_grad_is_taken_where_it_is_not_followed():
     for name, call in calls("cuda"):
