@@ -635,7 +635,8 @@ int pollux_orthogonalize(const pollux_ortho_dims *dims,  /* host */
  * 32 neighbours of a row ([N, W / 32]).  Element = code * 2^(scale - 127); the code is a whole number from -127 to 127 (PX_KEPT_I8, two's complement)
  * or an e4m3 (PX_KEPT_E4M3: four bits of exponent, three of fraction, largest 448).  The scale is the least with which the largest of the 32 has a
  * code, codes are rounded to nearest, ties to even: off by at most 1/127 of the largest of the 32 (I8), or by 2^-4 of the element or 2^-17 of that largest (E4M3).  Groups that hold
- * an infinity or a NaN have scale 255 and are restored as NaN.  Groups whose largest is below 2^-121 (I8), or 2^-119, have scale 0 and fewer bits.  Buffers are contiguous, values aligned to 16 bytes.
+ * an infinity or a NaN have scale 255 and are restored as NaN.  At the ends of the range: an element whose code stands for 2^128 is restored as infinite (I8: in a
+ * group whose largest is 127.5 * 2^121 or more, as the largest finite bfloat16 is, sizes from 127 * 2^121 on; E4M3: from 1.9375 * 2^127 on), so that a mask of bfloat16's or fp32's lowest value comes back as -inf; groups whose largest is below 2^-121 (I8), or 2^-119, have scale 0 and fewer bits.  Buffers are contiguous, values aligned to 16 bytes.
  * Rows, weights and gates in these calls may begin at any element, but for those of pollux_kept_grad.
  */
 enum {

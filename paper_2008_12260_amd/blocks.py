@@ -155,7 +155,7 @@ def _vectors(D, **named):
 
 def keep(rows, form="i8", stream=None):
     """rows [..., D] in 8 bits, as [N, D]: 32 neighbours of a row share a power of two; form "i8" (within 1/127 of the largest of the 32) or "e4m3" (within 2^-4 of
-    the element).  Groups that hold an infinity or a NaN are restored as NaN."""
+    the element).  Groups that hold an infinity or a NaN are restored as NaN; sizes next to 2^128 (from 1.984 * 2^127 on, and 1.9375 * 2^127) round to it and are restored as infinite."""
     _untracked_here(rows)
     with _on(stream):
         _on_device(rows)

@@ -61,6 +61,26 @@ def test_the_borders_of_a_scale_and_ties(form):
     check(x.cuda(), form)
 
 
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_sizes_that_round_to_the_end_of_the_range(dtype):
+    """2^128 is infinite: from where on, and that what lies below stays within the form's bound."""
+    import paper_2008_12260_amd as px
+    lowest = torch.finfo(dtype).min
+    for form, largest, others in (("i8", 127.5 * 2.0 ** 121, ((127.0 * 2.0 ** 121, True), (126.0 * 2.0 ** 121, False))), ("i8", 127.0 * 2.0 ** 121, ((126.0 * 2.0 ** 121, False),)),
+                                  ("e4m3", 1.9375 * 2.0 ** 127, ((1.921875 * 2.0 ** 127, False), (1.0 * 2.0 ** 127, False))), ("e4m3", 1.921875 * 2.0 ** 127, ())):
+        x = torch.zeros((1, 64), dtype=dtype, device="cuda")
+        x[0, 3], x[0, 40] = -largest, lowest
+        for k, (other, _) in enumerate(others):
+            x[0, 10 + k] = other
+        got = px.restore(px.keep(x, form), torch.float32)[0].double()
+        assert got[40] == float("-inf")
+        ends = largest in (127.5 * 2.0 ** 121, 1.9375 * 2.0 ** 127)
+        for at, value, infinite in ((3, -largest, ends),) + tuple((10 + k, other, end) for k, (other, end) in enumerate(others)):
+            assert bool(torch.isinf(got[at])) == infinite, (form, value)
+            if not infinite:
+                assert abs(float(got[at]) - value) <= (largest / 127.0 if form == "i8" else abs(value) * 2.0 ** -4)
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_zeros_and_tiny_rows(form):
     x = torch.zeros((4, 64), device="cuda")
