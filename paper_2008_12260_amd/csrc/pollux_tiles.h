@@ -566,7 +566,8 @@ __device__ __forceinline__ void form_tile(const Operands &o, Tile t, char *lds_,
         wait(all());
         return;
     }
-    // (the codes' loads are the last four before a stage is waited for: the next stage's operand of 16 bits has come, and theirs go on)
+    // (All but two: the second part's codes and scale are fetched in the half before the wait and go on. The first part's are fetched in the half after it, where the compiler may put them before or among the other operand's
+    // loads, which the wait is for: they are waited for too, as nothing says that they are the last.)
     typedef std::integral_constant<int, kHalves ? 2 : kAhead> ready;
     for (int s = 0; s < stages; ++s) {
         read(at, 1, a1, b1);

@@ -128,7 +128,7 @@ int launch_kept_grad(const pollux_kept_grad_dims &d, const KeptGradPlan &p, cons
 struct EdgePlan {
     int vectors;                // of eight elements, a thread
     int team, teams;            // threads of a row; rows that a workgroup has under way at a time
-    int chunk;                  // backward: neighbouring rows that a team sums over
+    int chunk;                  // backward: the most rows that a team sums over; neighbours with a gate for each span of rows, else as far apart as there are teams
     int blocks;                 // backward
     size_t parts;               // float [4][blocks][D]: sums over a workgroup's rows
     size_t ends;                // float [blocks * teams][2][D]: the gate's gradient of the spans that a team's first and last row cut
