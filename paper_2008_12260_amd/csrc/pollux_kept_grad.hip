@@ -5,8 +5,8 @@
 // A product over the rows n, of which both operands are columns in memory: tiles of dW, k in registers (a lane's four values are neighbours of a row of dW).  X is turned into dY's type on its way to
 // LDS and is nowhere in memory in more than 8 bits.  Scales differ from row to row, which is what the product sums over, so that they cannot wait until after it;
 // a norm's weights w can, and are multiplied in where tiles are stored.  Few tiles: the rows are cut in slices, whose sums are joined in order.
-// Bound by the matrix units, and by the power that they and the codes' turning take together: 16384 x 4096 x 16384 in bfloat16 from e4m3 1.21 PFLOP/s, from i8 1.14 (five operations for two codes where e4m3 takes
-// one), on a card where a library product of 16 bits reaches 1.09.
+// Bound by the matrix units, and by the power that they and the codes' turning take together: 16384 x 4096 x 16384 in bfloat16, in turn on one card three times from cold on, from i8
+// 1.14, 1.21 and 1.23 PFLOP/s, from e4m3 1.18 to 1.19 (a code of i8 takes two and a half operations, one of e4m3 half a one), a library product of 16 bits 1.09, 1.18 and 1.19.
 
 #include "pollux_host.h"
 #include "pollux_kept.h"

@@ -519,7 +519,7 @@ __device__ __forceinline__ void form_tile(const Operands &o, Tile t, char *lds_,
     for (int s = 0; s < S::kStages - 1; ++s) load(s, s);
     wait(some());
     // Codes of i8 in two parts (e4m3, of which less is to turn, gains nothing): one is turned in each half of a stage, so that the matrix units wait for neither.  A stage's first part goes into LDS in the half after which its place is free, the
-    // second in the half before the stage is read, and each is fetched when its place in registers is free, a stage ahead.  (16384 x 4096 x 16384 from i8 1925 us, with both in one half 2035.)
+    // second in the half before the stage is read, and each is fetched when its place in registers is free, a stage ahead.  (16384 x 4096 x 16384 from i8 1925 us, with both in one half 2035, in turn on one card.)
     constexpr bool kHalves = [] {
         if constexpr (kKept) return SideA::kParts == 2 && S::KEPT == PX_KEPT_I8 && !SPLIT;
         else return false;
